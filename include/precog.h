@@ -65,8 +65,9 @@ typedef enum precog_a_kind {
 
 /* Device status bits reported by precog_device_status(). */
 #define PRECOG_DEV_BAD_OFFSETS 0x1u  /* offsets not non-decreasing or beyond T_tot */
-#define PRECOG_DEV_BAD_INDEX 0x2u    /* a bank row index outside [-1, bank_entries), or a
-                                        chunk order entry outside [0, n_chunks) */
+#define PRECOG_DEV_BAD_INDEX 0x2u    /* a bank row index outside [-1, bank_entries), a chunk
+                                        order entry outside [0, n_chunks), or a slot, position
+                                        or token outside its table */
 #define PRECOG_DEV_TIMEOUT 0x4u      /* an mbarrier wait hit its iteration limit */
 #define PRECOG_DEV_BAD_A 0x8u        /* a_kind == PRECOG_A_POWER but A is not */
 
@@ -385,6 +386,182 @@ precog_status precog_smc_route(const void *embeddings, int32_t dtype, int64_t n,
 precog_status precog_smc_consolidate(float *semantic, int64_t n_slots, int64_t state_elems,
                                      const void *states, int32_t states_dtype, const int64_t *d_slots,
                                      int64_t n, float alpha, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * A matrix-valued recurrence: the gated delta rule, the norms of its queries and keys,
+ * and the scores of what is answered from its states.
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * Inputs of the gated delta rule for one layer. Value head h reads query/key head
+ * h / (n_v_heads / n_qk_heads) and keeps a state S of dv rows (value channels) by dk
+ * columns (key coordinates). Per token t of a sequence:
+ *   S <- exp(g[t,h]) * S
+ *   S <- S + beta[t,h] * (v[t,h] - S k[t]) k[t]^T
+ *   y[t,h] = scale * S q[t]
+ * (an outer-product state whose stored value for key k is corrected towards v: the
+ * counterpart, with a matrix a head, of the diagonal recurrence of precog_scan_inputs.)
+ *
+ * Layout (row-major):
+ *   q, k : [rows][n_qk_heads][dk], v : [rows][n_v_heads][dv], in `in_dtype` (F32 or BF16);
+ *          consecutive rows are q_stride, k_stride, v_stride ELEMENTS apart, so that slices
+ *          of one fused projection need no copy. Strides must keep rows 16-byte aligned and
+ *          be at least one row long (ignored where there is at most one row).
+ *   g, beta : fp32 [rows][n_v_heads], dense. g is the logarithm of the decay (usually <= 0;
+ *          -infinity forgets the state, and so does anything below -128, which decays by
+ *          less than fp32 can hold).
+ * q may be NULL when no readout is requested. Requirements: dk a multiple of 8 in [8, 128],
+ * dv a multiple of 8 in [8, 4096], n_v_heads a multiple of n_qk_heads.
+ */
+typedef struct precog_delta_inputs {
+    int32_t n_qk_heads;
+    int32_t n_v_heads;
+    int32_t dk;
+    int32_t dv;
+    int32_t in_dtype;          /* precog_dtype: F32 or BF16 */
+    float scale;               /* of the readout, e.g. dk^-0.5 */
+    const void *q;
+    const void *k;
+    const void *v;
+    const float *g;
+    const float *beta;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t v_stride;
+} precog_delta_inputs;
+
+/*
+ * precog_delta_scan -- roll the gated delta rule over a ragged batch of sequences: chunks of
+ * a corpus from the zero state (offline indexing, Sec. 4.2), or queries from injected states
+ * (Eq. 2); as precog_encode_chunks and precog_prefill_from_state do for the diagonal scan.
+ *
+ *   d_offsets   device int64 [n_seqs+1]: sequence c owns rows d_offsets[c] ..
+ *               d_offsets[c+1]-1. A sequence whose offsets decrease or leave [0, T_tot] is
+ *               skipped and flags PRECOG_DEV_BAD_OFFSETS. Lengths of zero are allowed: the
+ *               state is the initial one.
+ *   T_tot       rows of q, k, v, g and beta (below 2^31)
+ *   bank        device [bank_entries][L_total][n_v_heads][dv][dk] in bank_dtype (F32 or
+ *               BF16), or NULL: every sequence begins with the zero state
+ *   d_idx       device int64 [n_seqs]: the bank row injected into each sequence (-1: the
+ *               zero state; outside [-1, bank_entries): the zero state, and flags
+ *               PRECOG_DEV_BAD_INDEX); NULL: sequence c takes row c, and bank_entries must
+ *               be at least n_seqs
+ *   states_out  device [n_seqs][L_total][n_v_heads][dv][dk] in state_dtype (F32 or BF16,
+ *               rounded to nearest even once): layer `layer` of each entry is written and
+ *               nothing else. May be NULL when y_out is given. It may be the bank itself
+ *               only where each sequence's row is its own.
+ *   layer, L_total  the layer's place in the entries of bank and states_out
+ *   y_out       device [T_tot][n_v_heads][dv] in y_dtype (F32 or BF16), or NULL. Rows
+ *               outside every sequence are left untouched.
+ *   workspace   device scratch of at least precog_delta_scan_workspace_size() bytes (0 for
+ *               most shapes; then it may be NULL)
+ * With BF16 inputs, sequences of more than a few tokens run on the tensor cores in chunks of
+ * 64 tokens: state and sums stay fp32 and every intermediate operand is carried as a pair
+ * of bf16 numbers (16 significant bits), so results agree with the recurrence to about 1e-5
+ * of their norm. F32 inputs and very short sequences run token by token in fp32. Calls of the
+ * same shape repeat bit for bit.
+ */
+precog_status precog_delta_scan(const precog_delta_inputs *in, const int64_t *d_offsets, int64_t n_seqs,
+                                int64_t T_tot, const void *bank, int32_t bank_dtype, int64_t bank_entries,
+                                const int64_t *d_idx, void *states_out, int32_t state_dtype, int32_t layer,
+                                int32_t L_total, void *y_out, int32_t y_dtype, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* Bytes of scratch that precog_delta_scan needs for a call of these sizes on the current
+ * device (0 for most). */
+size_t precog_delta_scan_workspace_size(const precog_delta_inputs *in, int64_t n_seqs, int64_t T_tot);
+
+/*
+ * precog_delta_step -- one token of the gated delta rule for each of n sequences, on a table
+ * of fp32 states that is updated in place (decoding: row i of q, k, v, g, beta is the next
+ * token of the sequence whose state is states[d_slots[i]]).
+ *   states      device fp32 [n_slots][L_total][n_v_heads][dv][dk], 16-byte aligned; layer
+ *               `layer` of the named slots is read and written, nothing else
+ *   d_slots     device int64 [n], each slot at most once (not verified: repeated slots race);
+ *               NULL: sequence i has slot i, and n_slots must be at least n. A slot of -1 is
+ *               an idle row of a padded batch: its y row is zeroed and no state is touched.
+ *               Any other slot outside [0, n_slots) does the same and flags
+ *               PRECOG_DEV_BAD_INDEX.
+ *   y_out       device [n][n_v_heads][dv] in y_dtype (F32 or BF16)
+ */
+precog_status precog_delta_step(const precog_delta_inputs *in, int64_t n, float *states, int64_t n_slots,
+                                const int64_t *d_slots, int32_t layer, int32_t L_total, void *y_out,
+                                int32_t y_dtype, void *stream);
+
+typedef enum precog_norm {
+    PRECOG_NORM_NONE = 0,
+    PRECOG_NORM_L2 = 1,   /* x / sqrt(sum x^2 + eps) */
+    PRECOG_NORM_RMS = 2   /* x / sqrt(mean x^2 + eps) */
+} precog_norm;
+
+/*
+ * Arguments of precog_qk_norm_rope. Every head x of `dim` entries of q and k becomes
+ *   x <- norm(x) * weight        (weight: fp32 [dim] for q and k each, or NULL: 1)
+ *   (a, b) <- (a cos - b sin, b cos + a sin) for each of the rot_dim / 2 pairs,
+ * pair i being entries (i, i + rot_dim / 2), or (2i, 2i + 1) when `interleaved`; entries from
+ * rot_dim on are not rotated. cos and sin are row d_positions[t] of fp32 tables
+ * [n_positions][rot_dim / 2], so any frequencies, scalings or offsets are the caller's choice.
+ * Arithmetic is fp32; outputs are rounded once, to `dtype`.
+ *
+ *   q, k          device [T][n_q_heads][dim] and [T][n_k_heads][dim] in `dtype` (F32, BF16 or
+ *                 F16), rows q_stride / k_stride elements apart; either may have no heads
+ *   q_out, k_out  the same with their own strides; may be q and k themselves
+ *   d_positions   device int64 [T]; a position outside [0, n_positions) leaves the token's rows
+ *                 unwritten and flags PRECOG_DEV_BAD_INDEX. NULL: token t has position t.
+ * Requirements: dim a multiple of 8 in [8, 256], rot_dim even in [0, dim]; pointers and row
+ * strides 16-byte aligned; rot_dim > 0 needs cos and sin (whose rows may have any alignment
+ * of 4 bytes).
+ */
+typedef struct precog_qk_norm_args {
+    int32_t n_q_heads;
+    int32_t n_k_heads;
+    int32_t dim;
+    int32_t rot_dim;
+    int32_t dtype;             /* precog_dtype */
+    int32_t norm;              /* precog_norm */
+    int32_t interleaved;       /* 0 or 1 */
+    float eps;
+    const void *q;
+    const void *k;
+    void *q_out;
+    void *k_out;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t q_out_stride;
+    int64_t k_out_stride;
+    const float *q_weight;
+    const float *k_weight;
+    const float *cos;
+    const float *sin;
+    int64_t n_positions;
+    const int64_t *d_positions;
+} precog_qk_norm_args;
+
+/* precog_qk_norm_rope -- norms of query and key heads with the position rotation, one pass
+ * over T tokens. */
+precog_status precog_qk_norm_rope(const precog_qk_norm_args *args, int64_t T, void *stream);
+
+/*
+ * precog_token_logprobs -- how likely given tokens are: for every row x of logits, with
+ * z = x / temperature,
+ *   d_logprob[r] = z[token] - log sum_i exp(z_i)
+ *   d_entropy[r] = - sum_i p_i log p_i,  p = softmax(z)          (may be NULL)
+ *   d_top_idx[r][j], d_top_logprob[r][j]: the k best entries and their log probabilities,
+ *                  best first, ties to the lower index            (k == 0: NULL)
+ *   logits       device [n_rows][vocab] in `dtype` (F32, BF16 or F16), rows row_stride
+ *                elements apart (any stride >= vocab; any alignment of the elements)
+ *   d_tokens     device int64 [n_rows]; -1: nothing to score, d_logprob[r] = 0. Any other
+ *                token outside [0, vocab) gives NaN and flags PRECOG_DEV_BAD_INDEX.
+ *   k            0 .. 32, at most vocab
+ * Entries of -infinity have probability 0 (a given one scores -infinity) and rank behind all
+ * others. A row that is -infinity throughout has no distribution: its d_logprob, d_entropy and
+ * d_top_logprob are NaN. NaN or +infinity anywhere makes the row's values NaN too (NaN entries
+ * are never listed; places that none is left for hold index -1). Sums are fp32.
+ */
+precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,
+                                    int64_t row_stride, const int64_t *d_tokens, float temperature, int32_t k,
+                                    float *d_logprob, float *d_entropy, int64_t *d_top_idx,
+                                    float *d_top_logprob, void *stream);
 
 /*
  * precog_selftest_wait_timeout -- diagnostic; the paper has no counterpart.

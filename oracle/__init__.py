@@ -24,6 +24,9 @@ module compiles it with gcc and marshals numpy arrays into it.
   smc-sub).
 * :func:`smc_consolidate` -- the semantic-state EMA of Sec. 5.3 (Eq. smc-ema).
 * :func:`scan_complex` -- the scan with the complex diagonal A of Eq. 1.
+* :func:`delta_scan` -- the gated delta rule, token after token.
+* :func:`qk_norm_rope` -- norms of heads with the position rotation.
+* :func:`token_logprobs` -- log probabilities, entropy and best entries of rows of logits.
 """
 from __future__ import annotations
 
@@ -324,3 +327,72 @@ def scan_complex(x, dt, A_re, A_im, B, offsets, C=None, h0=None, want_y=False):
         raise ValueError(f"oracle_scan_complex rejected its arguments (rc={rc})")
     return states, y
 
+
+def delta_scan(q, k, v, g, beta, offsets, scale=1.0, S0=None):
+    """The gated delta rule over ragged sequences, as it is defined: per token and value head
+    S <- e^g S; S <- S + beta (v - S k) k^T; y = scale S q (value head h reads q/k head
+    h // (Hv / Hk)). q may be None. Returns ``(S [n, Hv, dv, dk], y [T, Hv, dv] or None)``; rows
+    of y outside every sequence are NaN."""
+    k, v, g, beta = _f64(k), _f64(v), _f64(g), _f64(beta)
+    T, hv, dv = v.shape
+    hk, dk = k.shape[1:]
+    group = np.arange(hv) // (hv // hk)
+    n = len(offsets) - 1
+    S = np.zeros((n, hv, dv, dk)) if S0 is None else _f64(S0).copy()
+    y = None if q is None else np.full((T, hv, dv), np.nan)
+    for c in range(n):
+        for t in range(int(offsets[c]), int(offsets[c + 1])):
+            kt = k[t, group]
+            H = np.exp(g[t])[:, None, None] * S[c]
+            u = beta[t][:, None] * (v[t] - np.einsum("hvk,hk->hv", H, kt))
+            S[c] = H + u[:, :, None] * kt[:, None, :]
+            if q is not None:
+                y[t] = scale * np.einsum("hvk,hk->hv", S[c], _f64(q[t])[group])
+    return S, y
+
+
+def qk_norm_rope(x, norm, eps, weight=None, cos=None, sin=None, positions=None, interleaved=False):
+    """Norm of each head of ``x [T, H, d]`` ("l2", "rms" or "none"), times ``weight [d]``, then the
+    rotation of its first ``2 * cos.shape[1]`` entries by the tables' rows ``positions``."""
+    x = _f64(x)
+    if norm != "none":
+        total = np.sum(x * x, axis=-1, keepdims=True)
+        x = x / np.sqrt((total if norm == "l2" else total / x.shape[-1]) + eps)
+    if weight is not None:
+        x = x * _f64(weight)
+    if cos is None or cos.shape[1] == 0:
+        return x
+    out, half = x.copy(), cos.shape[1]
+    pos = np.arange(x.shape[0]) if positions is None else np.asarray(positions)
+    for i in range(half):
+        ia, ib = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        c, s = _f64(cos)[pos, i][:, None], _f64(sin)[pos, i][:, None]
+        out[..., ia] = x[..., ia] * c - x[..., ib] * s
+        out[..., ib] = x[..., ib] * c + x[..., ia] * s
+    return out
+
+
+def token_logprobs(logits, tokens, temperature=1.0, k=0):
+    """``(logprob [R], entropy [R], top_idx [R, k], top_logprob [R, k])`` of rows of logits: token -1
+    scores 0; ties to the lower index; a row without a distribution (all -inf, or any NaN or
+    +inf) gives NaN, and lists its comparable entries all the same (-1 where none is left)."""
+    x = _f64(logits)
+    R, V = x.shape
+    lp, H = np.zeros(R), np.zeros(R)
+    idx, best = np.full((R, k), -1, dtype=np.int64), np.full((R, k), np.nan)
+    for r in range(R):
+        z = x[r] / temperature
+        m = np.max(z)
+        if np.isfinite(m):
+            logp = z - m - np.log(np.sum(np.exp(z - m)))
+        else:
+            logp = np.full(V, np.nan)
+        if tokens[r] >= 0:
+            lp[r] = logp[tokens[r]]
+        some = np.isfinite(logp)
+        p = np.exp(logp[some])
+        H[r] = -np.sum(p * logp[some]) if np.isfinite(m) else np.nan
+        order = [i for i in np.argsort(-x[r], kind="stable") if not np.isnan(x[r, i])][:k]
+        idx[r, :len(order)] = order
+        best[r, :len(order)] = logp[order]
+    return lp, H, idx, best

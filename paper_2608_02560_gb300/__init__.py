@@ -17,6 +17,10 @@ Functions carry the C names:
 * :func:`precog_retrieve_keys`, :func:`precog_decode_keys` -- row-sharded retrieval
 * :func:`precog_prefill_composed` -- softmax-weighted top-k injection (Sec. 4.4) + prefill
 * :func:`precog_smc_route`, :func:`precog_smc_consolidate` -- SMC (Sec. 5)
+* :func:`precog_delta_scan`, :func:`precog_delta_step` -- the gated delta rule: chunks or queries
+  from injected matrix states, and one token of each sequence on a table of states
+* :func:`precog_qk_norm_rope`     -- norms of query and key heads with the position rotation
+* :func:`precog_token_logprobs`   -- log probabilities of given tokens, entropy, best entries
 * :func:`precog_retrieve_noalloc`  -- top-1 retrieval without a caller workspace
 * :func:`precog_device_status`    -- device-side status word; :func:`precog_status_string`,
   :func:`precog_last_error`, :func:`precog_abi_version`, :func:`precog_launch_count`
@@ -31,6 +35,7 @@ LIB_PATH = os.path.join(_PKG, "libprecog.so")
 
 PRECOG_F32, PRECOG_BF16, PRECOG_F16 = 0, 1, 2
 PRECOG_OK = 0
+PRECOG_NORM_NONE, PRECOG_NORM_L2, PRECOG_NORM_RMS = 0, 1, 2
 PRECOG_A_GENERAL, PRECOG_A_POWER, PRECOG_A_COMPLEX = 0, 1, 2
 PRECOG_DEV_BAD_OFFSETS, PRECOG_DEV_BAD_INDEX, PRECOG_DEV_TIMEOUT, PRECOG_DEV_BAD_A = 0x1, 0x2, 0x4, 0x8
 STATUS_NAMES = {0: "PRECOG_OK", 1: "PRECOG_ERR_INVALID_ARG", 2: "PRECOG_ERR_UNSUPPORTED",
@@ -51,6 +56,27 @@ class ScanInputs(ctypes.Structure):
                 ("x", ctypes.c_void_p), ("dt", ctypes.c_void_p),
                 ("B", ctypes.c_void_p), ("C", ctypes.c_void_p), ("A", ctypes.c_void_p),
                 ("layer_stride_xd", ctypes.c_int64), ("layer_stride_bc", ctypes.c_int64)]
+
+
+class DeltaInputs(ctypes.Structure):
+    """Mirror of ``precog_delta_inputs`` (include/precog.h)."""
+    _fields_ = [("n_qk_heads", ctypes.c_int32), ("n_v_heads", ctypes.c_int32), ("dk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("in_dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("g", ctypes.c_void_p), ("beta", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class QkNormArgs(ctypes.Structure):
+    """Mirror of ``precog_qk_norm_args`` (include/precog.h)."""
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_k_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("q", ctypes.c_void_p),
+                ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64),
+                ("k_out_stride", ctypes.c_int64), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_positions", ctypes.c_int64),
+                ("d_positions", ctypes.c_void_p)]
 
 
 _lib = None
@@ -97,6 +123,17 @@ def load_library(path: str = LIB_PATH):
     lib.precog_prefill_composed.restype = i32
     lib.precog_prefill_composed.argtypes = [ctypes.POINTER(ScanInputs), i32, i32, vp, i32, i64, i32,
                                             i32, i32, vp, vp, ctypes.c_float, vp, i32, vp, i32, vp]
+    lib.precog_delta_scan.restype = i32
+    lib.precog_delta_scan.argtypes = [ctypes.POINTER(DeltaInputs), vp, i64, i64, vp, i32, i64, vp, vp, i32, i32,
+                                      i32, vp, i32, vp, sz, vp]
+    lib.precog_delta_scan_workspace_size.restype = sz
+    lib.precog_delta_scan_workspace_size.argtypes = [ctypes.POINTER(DeltaInputs), i64, i64]
+    lib.precog_delta_step.restype = i32
+    lib.precog_delta_step.argtypes = [ctypes.POINTER(DeltaInputs), i64, vp, i64, vp, i32, i32, vp, i32, vp]
+    lib.precog_qk_norm_rope.restype = i32
+    lib.precog_qk_norm_rope.argtypes = [ctypes.POINTER(QkNormArgs), i64, vp]
+    lib.precog_token_logprobs.restype = i32
+    lib.precog_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, ctypes.c_float, i32, vp, vp, vp, vp, vp]
     lib.precog_selftest_wait_timeout.restype = i32
     lib.precog_selftest_wait_timeout.argtypes = [ctypes.c_uint32, vp]
     lib.precog_device_status.restype = i32
@@ -195,6 +232,49 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     s = ScanInputs(L, D, N, _dtype_code(x), a_kind, 0, _ptr(x), _ptr(dt), _ptr(B), _ptr(C), _ptr(A), T * D, T * N)
     # the struct holds raw device pointers: keep the tensors alive as long as it lives
     s._keepalive = (x, dt, B, C, A)
+    return s
+
+
+def _rows(t, what: str):
+    """(pointer, elements between rows) of a GPU tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("tensors passed to libprecog must live on the GPU")
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != inner:
+            raise ValueError(f"the rows of {what} must be contiguous")
+        inner *= size
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else inner)
+
+
+def _of(t, dtype, shape, what: str):
+    """The pointer of a contiguous GPU tensor of this dtype and shape (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def delta_inputs(q, k, v, g, beta, scale: float | None = None) -> DeltaInputs:
+    """Describe the gated delta rule's q, k ``[T, Hk, dk]``, v ``[T, Hv, dv]`` (rows may be
+    strided: slices of one projection) and the fp32 gates g (log decay), beta ``[T, Hv]``.
+    ``q`` may be None without a readout; ``scale`` (default dk**-0.5) multiplies the readout."""
+    torch = _torch()
+    T, hk, dk = k.shape
+    hv, dv = v.shape[1], v.shape[2]
+    if v.shape[0] != T or (q is not None and q.shape != k.shape):
+        raise ValueError("q/k/v shapes disagree")
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise TypeError("q, k and v must have one dtype")
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    s = DeltaInputs(hk, hv, dk, dv, _dtype_code(k), dk ** -0.5 if scale is None else scale, qp, kp, vp,
+                    _of(g, torch.float32, (T, hv), "g"), _of(beta, torch.float32, (T, hv), "beta"), qs, ks, vs)
+    # the struct holds raw device pointers: keep the tensors alive as long as it lives
+    s._keepalive = (q, k, v, g, beta)
+    s.rows = T
     return s
 
 
@@ -359,6 +439,114 @@ def precog_smc_consolidate(semantic, states, slots, alpha: float, stream=None):
     _check(lib.precog_smc_consolidate(
         _ptr(semantic), n_slots, elems, _ptr(states), _dtype_code(states), _ptr(slots),
         states.shape[0], alpha, _stream(stream)))
+
+
+def precog_delta_scan_workspace_size(inputs: DeltaInputs, n_seqs: int, T_tot: int) -> int:
+    return int(load_library().precog_delta_scan_workspace_size(ctypes.byref(inputs), n_seqs, T_tot))
+
+
+def _delta_states(inputs: DeltaInputs, t, what: str):
+    if t is not None and (t.dim() != 5 or tuple(t.shape[2:]) != (inputs.n_v_heads, inputs.dv, inputs.dk)):
+        raise ValueError(f"{what} must be [entries, layers, Hv, dv, dk], got {tuple(t.shape)}")
+    return t
+
+
+def precog_delta_scan(inputs: DeltaInputs, offsets, T_tot: int, bank=None, idx=None, layer: int = 0,
+                      states_out=None, y_out=None, workspace=None, stream=None):
+    """Roll the gated delta rule over the sequences of int64 ``offsets [n + 1]``, from zero states
+    or from ``bank[idx[c], layer]`` (``[entries, layers, Hv, dv, dk]``; -1: the zero state), into
+    ``states_out[c, layer]`` and/or ``y_out [T_tot, Hv, dv]``. ``workspace`` is allocated with
+    torch when one is needed and none is given."""
+    lib = load_library()
+    torch = _torch()
+    n = offsets.numel() - 1
+    if T_tot > inputs.rows:
+        raise ValueError("T_tot exceeds the inputs' rows")
+    _delta_states(inputs, bank, "bank")
+    _delta_states(inputs, states_out, "states_out")
+    if states_out is not None and states_out.shape[0] != n:
+        raise ValueError("states_out must have one entry per sequence")
+    if bank is not None and states_out is not None and bank.shape[1] != states_out.shape[1]:
+        raise ValueError("bank and states_out must have the same number of layers")
+    if y_out is not None and tuple(y_out.shape) != (T_tot, inputs.n_v_heads, inputs.dv):
+        raise ValueError("y_out must be [T_tot, Hv, dv]")
+    holder = states_out if states_out is not None else bank
+    need = int(lib.precog_delta_scan_workspace_size(ctypes.byref(inputs), n, T_tot))
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=offsets.device)
+    _check(lib.precog_delta_scan(
+        ctypes.byref(inputs), _of(offsets, torch.int64, (n + 1,), "offsets"), n, T_tot, _ptr(bank),
+        _dtype_code(bank) if bank is not None else PRECOG_F32, bank.shape[0] if bank is not None else 0,
+        _of(idx, torch.int64, (n,), "idx"), _ptr(states_out),
+        _dtype_code(states_out) if states_out is not None else PRECOG_F32, layer,
+        holder.shape[1] if holder is not None else 1, _ptr(y_out),
+        _dtype_code(y_out) if y_out is not None else PRECOG_F32, _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream)))
+
+
+def precog_delta_step(inputs: DeltaInputs, states, slots=None, y_out=None, layer: int = 0, stream=None):
+    """One token of the gated delta rule for each row of ``inputs``, on the fp32 table ``states
+    [slots, layers, Hv, dv, dk]`` (updated in place) at the rows' int64 ``slots`` (-1: an idle
+    row), into ``y_out [n, Hv, dv]``."""
+    torch = _torch()
+    n = inputs.rows
+    _delta_states(inputs, states, "states")
+    if states.dtype != torch.float32:
+        raise ValueError("states must be float32")
+    if y_out is None or tuple(y_out.shape) != (n, inputs.n_v_heads, inputs.dv):
+        raise ValueError("y_out must be [n, Hv, dv]")
+    _check(load_library().precog_delta_step(
+        ctypes.byref(inputs), n, _ptr(states), states.shape[0], _of(slots, torch.int64, (n,), "slots"), layer,
+        states.shape[1], _ptr(y_out), _dtype_code(y_out), _stream(stream)))
+
+
+_NORMS = {"none": PRECOG_NORM_NONE, "l2": PRECOG_NORM_L2, "rms": PRECOG_NORM_RMS}
+
+
+def precog_qk_norm_rope(q, k, q_out, k_out, norm: str = "l2", q_weight=None, k_weight=None, eps: float = 1e-6,
+                        cos=None, sin=None, positions=None, interleaved: bool = False, stream=None):
+    """Norm (``"l2"``, ``"rms"`` or ``"none"``) of every head of q ``[T, Hq, d]`` and k ``[T, Hk, d]``
+    (rows may be strided), times fp32 weights ``[d]``, its first ``2 * cos.shape[1]`` entries
+    rotated by row ``positions[t]`` (int64; default t) of the fp32 tables cos and sin, into
+    ``q_out`` and ``k_out`` (which may be q and k)."""
+    torch = _torch()
+    if norm not in _NORMS:
+        raise ValueError(f"norm must be one of {sorted(_NORMS)}")
+    T, hq, d = q.shape
+    hk = k.shape[1]
+    if k.shape != (T, hk, d) or q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("q/k/q_out/k_out shapes disagree")
+    if not (q.dtype == k.dtype == q_out.dtype == k_out.dtype):
+        raise TypeError("q, k and their outputs must have one dtype")
+    if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
+        raise ValueError("cos and sin must be given together, with one shape")
+    (qp, qs), (kp, ks) = _rows(q, "q"), _rows(k, "k")
+    (qo, qos), (ko, kos) = _rows(q_out, "q_out"), _rows(k_out, "k_out")
+    n_pos, half = cos.shape if cos is not None else (0, 0)
+    args = QkNormArgs(hq, hk, d, 2 * half, _dtype_code(q), _NORMS[norm], int(interleaved), eps, qp, kp, qo, ko, qs,
+                      ks, qos, kos, _of(q_weight, torch.float32, (d,), "q_weight"),
+                      _of(k_weight, torch.float32, (d,), "k_weight"), _of(cos, torch.float32, (n_pos, half), "cos"),
+                      _of(sin, torch.float32, (n_pos, half), "sin"), n_pos,
+                      _of(positions, torch.int64, (T,), "positions") if half else None)
+    _check(load_library().precog_qk_norm_rope(ctypes.byref(args), T, _stream(stream)))
+
+
+def precog_token_logprobs(logits, tokens, logprob, entropy=None, top_idx=None, top_logprob=None,
+                          temperature: float = 1.0, stream=None):
+    """Log probabilities of int64 ``tokens [R]`` (-1: none) under ``softmax(logits / temperature)``
+    (``[R, V]``, rows may be strided) into fp32 ``logprob [R]``, with the distribution's
+    ``entropy [R]`` and its k best entries ``top_idx [R, k]`` (int64), ``top_logprob [R, k]``."""
+    torch = _torch()
+    R, V = logits.shape
+    if (top_idx is None) != (top_logprob is None):
+        raise ValueError("top_idx and top_logprob must be given together")
+    k = top_idx.shape[1] if top_idx is not None else 0
+    lp, stride = _rows(logits, "logits")
+    _check(load_library().precog_token_logprobs(
+        lp, _dtype_code(logits), R, V, stride, _of(tokens, torch.int64, (R,), "tokens"), temperature, k,
+        _of(logprob, torch.float32, (R,), "logprob"), _of(entropy, torch.float32, (R,), "entropy"),
+        _of(top_idx, torch.int64, (R, k), "top_idx"), _of(top_logprob, torch.float32, (R, k), "top_logprob"),
+        _stream(stream)))
 
 
 def precog_selftest_wait_timeout(iterations: int = 4096, stream=None):

@@ -95,6 +95,60 @@ precog::ScanParams base_params(const precog_scan_inputs *in, int64_t rows) {
     return p;
 }
 
+// CTAs of one launch.
+constexpr int64_t kMaxItems = 0x7fffffffLL;
+
+// Checks shared by the delta rule's scan and step.
+precog_status check_delta_inputs(const precog_delta_inputs *in, int64_t rows, bool need_q) {
+    if (in == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "delta inputs pointer is NULL");
+    if (in->in_dtype != PRECOG_F32 && in->in_dtype != PRECOG_BF16)
+        return fail(PRECOG_ERR_UNSUPPORTED, "in_dtype must be PRECOG_F32 or PRECOG_BF16");
+    if (in->n_qk_heads < 1 || in->n_v_heads < 1 || in->n_v_heads % in->n_qk_heads != 0)
+        return fail(PRECOG_ERR_INVALID_ARG, "n_v_heads must be a positive multiple of n_qk_heads");
+    if (in->n_v_heads > 65535) return fail(PRECOG_ERR_UNSUPPORTED, "n_v_heads must be below 2^16");
+    if (in->dk < 8 || in->dk > 128 || in->dk % 8 != 0)
+        return fail(PRECOG_ERR_UNSUPPORTED, "dk=%d: a multiple of 8 in [8, 128] is implemented", in->dk);
+    if (in->dv < 8 || in->dv > 4096 || in->dv % 8 != 0)
+        return fail(PRECOG_ERR_UNSUPPORTED, "dv=%d: a multiple of 8 in [8, 4096] is implemented", in->dv);
+    if (rows == 0) return PRECOG_OK;
+    if (in->k == nullptr || in->v == nullptr || in->g == nullptr || in->beta == nullptr)
+        return fail(PRECOG_ERR_INVALID_ARG, "k, v, g and beta must be non-NULL");
+    if (need_q && in->q == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "q is required when y_out is given");
+    if ((in->q && !aligned16(in->q)) || !aligned16(in->k) || !aligned16(in->v) || !aligned16(in->g) ||
+        !aligned16(in->beta))
+        return fail(PRECOG_ERR_INVALID_ARG, "input pointers must be 16-byte aligned");
+    if (rows > 1) {
+        const int sz = dtype_size(in->in_dtype);
+        const int64_t row_k = static_cast<int64_t>(in->n_qk_heads) * in->dk;
+        const int64_t row_v = static_cast<int64_t>(in->n_v_heads) * in->dv;
+        if ((in->q && in->q_stride < row_k) || in->k_stride < row_k || in->v_stride < row_v)
+            return fail(PRECOG_ERR_INVALID_ARG, "row strides smaller than a row");
+        if ((in->q && (in->q_stride * sz) % 16 != 0) || (in->k_stride * sz) % 16 != 0 || (in->v_stride * sz) % 16 != 0)
+            return fail(PRECOG_ERR_INVALID_ARG, "row strides must keep 16-byte alignment");
+    }
+    return PRECOG_OK;
+}
+
+precog::DeltaParams delta_params(const precog_delta_inputs *in) {
+    precog::DeltaParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.q = in->q;
+    p.k = in->k;
+    p.v = in->v;
+    p.g = in->g;
+    p.beta = in->beta;
+    p.q_stride = in->q_stride;
+    p.k_stride = in->k_stride;
+    p.v_stride = in->v_stride;
+    p.hk = in->n_qk_heads;
+    p.hv = in->n_v_heads;
+    p.dk = in->dk;
+    p.dv = in->dv;
+    p.in_dtype = in->in_dtype;
+    p.scale = in->scale;
+    return p;
+}
+
 std::atomic<uint64_t> g_launches{0};
 std::mutex g_attr_mutex;
 // dynamic shared-memory limit already set, per (kernel, device): the attribute is per device
@@ -512,6 +566,208 @@ precog_status precog_smc_consolidate(float *semantic, int64_t n_slots, int64_t s
     return ok();
 }
 
+precog_status precog_delta_scan(const precog_delta_inputs *in, const int64_t *d_offsets, int64_t n_seqs,
+                                int64_t T_tot, const void *bank, int32_t bank_dtype, int64_t bank_entries,
+                                const int64_t *d_idx, void *states_out, int32_t state_dtype, int32_t layer,
+                                int32_t L_total, void *y_out, int32_t y_dtype, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+    if (T_tot < 0) return fail(PRECOG_ERR_INVALID_ARG, "T_tot must be >= 0");
+    if (T_tot >= 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "T_tot must be below 2^31-1");
+    precog_status s = check_delta_inputs(in, T_tot, y_out != nullptr);
+    if (s != PRECOG_OK) return s;
+    if (n_seqs < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_seqs must be >= 0");
+    if (d_offsets == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "d_offsets is NULL");
+    if (states_out == nullptr && y_out == nullptr)
+        return fail(PRECOG_ERR_INVALID_ARG, "states_out and y_out are both NULL: nothing to do");
+    if ((bank || states_out) && (L_total < 1 || layer < 0 || layer >= L_total))
+        return fail(PRECOG_ERR_INVALID_ARG, "layer must be in [0, L_total)");
+    if (bank) {
+        if (!state_dtype_ok(bank_dtype))
+            return fail(PRECOG_ERR_UNSUPPORTED, "bank_dtype must be PRECOG_F32 or PRECOG_BF16");
+        if (!aligned16(bank)) return fail(PRECOG_ERR_INVALID_ARG, "bank not 16-byte aligned");
+        if (bank_entries < 0) return fail(PRECOG_ERR_INVALID_ARG, "bank_entries must be >= 0");
+        if (d_idx == nullptr && bank_entries < n_seqs)
+            return fail(PRECOG_ERR_INVALID_ARG, "d_idx is NULL but bank has fewer rows than sequences");
+    } else if (d_idx) {
+        return fail(PRECOG_ERR_INVALID_ARG, "d_idx is given without a bank");
+    }
+    if (states_out && (!state_dtype_ok(state_dtype) || !aligned16(states_out)))
+        return fail(PRECOG_ERR_INVALID_ARG, "states_out must be 16-byte aligned F32 or BF16");
+    if (y_out && (!state_dtype_ok(y_dtype) || !aligned16(y_out)))
+        return fail(PRECOG_ERR_INVALID_ARG, "y_out must be 16-byte aligned F32 or BF16");
+    if (n_seqs == 0) return ok();
+    if (n_seqs > kMaxItems / in->n_v_heads / ((in->dv + 15) / 16))
+        return fail(PRECOG_ERR_UNSUPPORTED, "too many sequences for one call");
+    precog::DeltaParams p = delta_params(in);
+    p.offsets = d_offsets;
+    p.n_seqs = n_seqs;
+    p.T_tot = T_tot;
+    const size_t need = precog::delta_scan_workspace_size(p);
+    if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned16(workspace))))
+        return fail(PRECOG_ERR_INVALID_ARG, "workspace too small or misaligned (%zu bytes needed)", need);
+    p.bank = bank;
+    p.bank_dtype = bank_dtype;
+    p.bank_entries = bank_entries;
+    p.idx = d_idx;
+    p.states = states_out;
+    p.state_dtype = state_dtype;
+    p.layer = layer;
+    p.L_total = L_total;
+    p.y = y_out;
+    p.y_dtype = y_dtype;
+    p.workspace = workspace;
+    cudaError_t e = precog::launch_delta_scan(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "delta scan launch");
+    return ok();
+}
+
+size_t precog_delta_scan_workspace_size(const precog_delta_inputs *in, int64_t n_seqs, int64_t T_tot) {
+    if (T_tot < 0 || T_tot >= 0x7fffffffLL || n_seqs < 1 || check_delta_inputs(in, 0, false) != PRECOG_OK) return 0;
+    precog::DeltaParams p = delta_params(in);
+    p.n_seqs = n_seqs;
+    p.T_tot = T_tot;
+    return precog::delta_scan_workspace_size(p);
+}
+
+precog_status precog_delta_step(const precog_delta_inputs *in, int64_t n, float *states, int64_t n_slots,
+                                const int64_t *d_slots, int32_t layer, int32_t L_total, void *y_out,
+                                int32_t y_dtype, void *stream) {
+    if (n < 0) return fail(PRECOG_ERR_INVALID_ARG, "n must be >= 0");
+    precog_status s = check_delta_inputs(in, n, true);
+    if (s != PRECOG_OK) return s;
+    if (states == nullptr || !aligned16(states))
+        return fail(PRECOG_ERR_INVALID_ARG, "states must be non-NULL and 16-byte aligned");
+    if (L_total < 1 || layer < 0 || layer >= L_total)
+        return fail(PRECOG_ERR_INVALID_ARG, "layer must be in [0, L_total)");
+    if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (d_slots == nullptr && n_slots < n)
+        return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
+    if (y_out == nullptr || !state_dtype_ok(y_dtype) || !aligned16(y_out))
+        return fail(PRECOG_ERR_INVALID_ARG, "y_out must be 16-byte aligned F32 or BF16");
+    if (n == 0) return ok();
+    if (n > kMaxItems / in->n_v_heads / ((in->dv + 15) / 16))
+        return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    precog::DeltaParams p = delta_params(in);
+    p.n_seqs = n;
+    p.T_tot = n;
+    p.bank_entries = n_slots;
+    p.idx = d_slots;
+    p.states = states;
+    p.state_dtype = PRECOG_F32;
+    p.layer = layer;
+    p.L_total = L_total;
+    p.y = y_out;
+    p.y_dtype = y_dtype;
+    cudaError_t e = precog::launch_delta_step(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "delta step launch");
+    return ok();
+}
+
+precog_status precog_qk_norm_rope(const precog_qk_norm_args *a, int64_t T, void *stream) {
+    if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
+    if (T < 0) return fail(PRECOG_ERR_INVALID_ARG, "T must be >= 0");
+    const int sz = dtype_size(a->dtype);
+    if (sz == 0) return fail(PRECOG_ERR_UNSUPPORTED, "dtype must be F16, BF16 or F32");
+    if (a->n_q_heads < 0 || a->n_k_heads < 0) return fail(PRECOG_ERR_INVALID_ARG, "numbers of heads must be >= 0");
+    if (a->dim < 8 || a->dim > 256 || a->dim % 8 != 0)
+        return fail(PRECOG_ERR_UNSUPPORTED, "dim=%d: a multiple of 8 in [8, 256] is implemented", a->dim);
+    if (a->n_q_heads > 0x7fffffff / a->dim || a->n_k_heads > 0x7fffffff / a->dim)
+        return fail(PRECOG_ERR_UNSUPPORTED, "rows of 2^31 entries or more are not implemented");
+    if (a->rot_dim < 0 || a->rot_dim > a->dim || a->rot_dim % 2 != 0)
+        return fail(PRECOG_ERR_INVALID_ARG, "rot_dim must be even and in [0, dim]");
+    if (a->norm < PRECOG_NORM_NONE || a->norm > PRECOG_NORM_RMS)
+        return fail(PRECOG_ERR_INVALID_ARG, "norm must be PRECOG_NORM_NONE, _L2 or _RMS");
+    if (a->interleaved != 0 && a->interleaved != 1) return fail(PRECOG_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+    if (!(a->eps >= 0.f)) return fail(PRECOG_ERR_INVALID_ARG, "eps must be >= 0");
+    if (a->rot_dim > 0) {
+        if (a->cos == nullptr || a->sin == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "rot_dim > 0 needs cos and sin");
+        if ((reinterpret_cast<uintptr_t>(a->cos) | reinterpret_cast<uintptr_t>(a->sin)) & 3u)
+            return fail(PRECOG_ERR_INVALID_ARG, "cos and sin must be 4-byte aligned");
+        if (a->n_positions < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_positions must be >= 0");
+        if (a->d_positions == nullptr && a->n_positions < T)
+            return fail(PRECOG_ERR_INVALID_ARG, "d_positions is NULL but the tables have fewer rows than tokens");
+    }
+    precog::QkNormParams p;
+    p.in[0] = a->q, p.in[1] = a->k;
+    p.out[0] = a->q_out, p.out[1] = a->k_out;
+    p.in_stride[0] = a->q_stride, p.in_stride[1] = a->k_stride;
+    p.out_stride[0] = a->q_out_stride, p.out_stride[1] = a->k_out_stride;
+    p.weight[0] = a->q_weight, p.weight[1] = a->k_weight;
+    p.heads[0] = a->n_q_heads, p.heads[1] = a->n_k_heads;
+    for (int i = 0; i < 2; ++i) {
+        if (p.heads[i] == 0 || T == 0) continue;
+        if (p.in[i] == nullptr || p.out[i] == nullptr)
+            return fail(PRECOG_ERR_INVALID_ARG, "q, k, q_out and k_out must be non-NULL where there are heads");
+        if (!aligned16(p.in[i]) || !aligned16(p.out[i]) || !aligned16(p.weight[i]))
+            return fail(PRECOG_ERR_INVALID_ARG, "q, k, their outputs and weights must be 16-byte aligned");
+        if (T > 1) {
+            const int64_t row = static_cast<int64_t>(p.heads[i]) * a->dim;
+            if (p.in_stride[i] < row || p.out_stride[i] < row)
+                return fail(PRECOG_ERR_INVALID_ARG, "row strides smaller than a row");
+            if ((p.in_stride[i] * sz) % 16 != 0 || (p.out_stride[i] * sz) % 16 != 0)
+                return fail(PRECOG_ERR_INVALID_ARG, "row strides must keep 16-byte alignment");
+        } else {
+            p.in_stride[i] = p.out_stride[i] = 0;
+        }
+    }
+    if (T == 0 || p.heads[0] + static_cast<int64_t>(p.heads[1]) == 0) return ok();
+    if (T > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "T must be below 2^31");
+    p.dim = a->dim;
+    p.rot = a->rot_dim;
+    p.dtype = a->dtype;
+    p.norm = a->norm;
+    p.interleaved = a->interleaved;
+    p.eps = a->eps;
+    p.cos = a->cos;
+    p.sin = a->sin;
+    p.n_positions = a->n_positions;
+    p.positions = a->d_positions;
+    p.T = T;
+    cudaError_t e = precog::launch_qk_norm(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "qk norm launch");
+    return ok();
+}
+
+precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,
+                                    int64_t row_stride, const int64_t *d_tokens, float temperature, int32_t k,
+                                    float *d_logprob, float *d_entropy, int64_t *d_top_idx,
+                                    float *d_top_logprob, void *stream) {
+    const int sz = dtype_size(dtype);
+    if (sz == 0) return fail(PRECOG_ERR_UNSUPPORTED, "dtype must be F16, BF16 or F32");
+    if (n_rows < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_rows must be >= 0");
+    if (vocab < 1) return fail(PRECOG_ERR_INVALID_ARG, "vocab must be >= 1");
+    if (vocab > 0x3fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "vocab must be below 2^30");
+    if (row_stride < vocab && n_rows > 1) return fail(PRECOG_ERR_INVALID_ARG, "row_stride must be >= vocab");
+    if (!(temperature > 0.f) || !(1.f / temperature > 0.f) || 1.f / temperature > 3.4e38f)
+        return fail(PRECOG_ERR_INVALID_ARG, "temperature must be positive and finite");
+    if (k < 0 || k > 32) return fail(PRECOG_ERR_UNSUPPORTED, "k must be in [0, 32]");
+    if (k > vocab) return fail(PRECOG_ERR_INVALID_ARG, "k must be at most vocab");
+    if (n_rows == 0) return ok();
+    if (logits == nullptr || d_tokens == nullptr || d_logprob == nullptr)
+        return fail(PRECOG_ERR_INVALID_ARG, "logits, d_tokens and d_logprob must be non-NULL");
+    if (k > 0 && (d_top_idx == nullptr || d_top_logprob == nullptr))
+        return fail(PRECOG_ERR_INVALID_ARG, "k > 0 needs d_top_idx and d_top_logprob");
+    if ((reinterpret_cast<uintptr_t>(logits) & static_cast<uintptr_t>(sz - 1)) != 0)
+        return fail(PRECOG_ERR_INVALID_ARG, "logits must be aligned to their elements");
+    if (n_rows > 0x7fffffffLL / 16) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    precog::LogprobParams p;
+    p.logits = logits;
+    p.dtype = dtype;
+    p.rows = n_rows;
+    p.vocab = vocab;
+    p.stride = row_stride;
+    p.tokens = d_tokens;
+    p.inv_temp = 1.f / temperature;
+    p.k = k;
+    p.logprob = d_logprob;
+    p.entropy = d_entropy;
+    p.top_idx = d_top_idx;
+    p.top_logprob = d_top_logprob;
+    cudaError_t e = precog::launch_logprobs(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "logprobs launch");
+    return ok();
+}
+
 precog_status precog_selftest_wait_timeout(uint32_t iterations, void *stream) {
     if (iterations < 1 || iterations > (1u << 20))
         return fail(PRECOG_ERR_INVALID_ARG, "iterations must be in [1, 2^20]");
@@ -541,11 +797,18 @@ precog_status precog_device_status(void *stream, uint32_t *bits_out) {
     uint32_t l = 0;
     e = precog::scan_latency_status_word_read_clear(&l);
     if (e != cudaSuccess) return cuda_fail(e, "read latency scan status");
-    *bits_out = a | b | c | z | w | l;
+    uint32_t d = 0, n = 0, t = 0;
+    e = precog::delta_status_word_read_clear(&d);
+    if (e != cudaSuccess) return cuda_fail(e, "read delta status");
+    e = precog::qk_norm_status_word_read_clear(&n);
+    if (e != cudaSuccess) return cuda_fail(e, "read qk norm status");
+    e = precog::logprobs_status_word_read_clear(&t);
+    if (e != cudaSuccess) return cuda_fail(e, "read logprobs status");
+    *bits_out = a | b | c | z | w | l | d | n | t;
     if (*bits_out == 0) return ok();
     if (*bits_out & PRECOG_DEV_TIMEOUT)
         return fail(PRECOG_ERR_TIMEOUT, "a device-side wait gave up (bits 0x%x)", *bits_out);
-    return fail(PRECOG_ERR_DEVICE, "device flagged invalid offsets, bank rows or A (bits 0x%x)", *bits_out);
+    return fail(PRECOG_ERR_DEVICE, "device flagged invalid offsets, bank rows, indices or A (bits 0x%x)", *bits_out);
 }
 
 const char *precog_status_string(int32_t status) {

@@ -154,4 +154,63 @@ cudaError_t launch_smc_consolidate(float *sem, int64_t n_slots, int64_t elems, c
                                    cudaStream_t stream);
 cudaError_t smc_status_word_read_clear(uint32_t *bits);
 
+// One layer of the gated delta rule (delta.cu: token by token; delta_chunk.cu: tensor cores).
+struct DeltaParams {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    int64_t q_stride, k_stride, v_stride;   // elements between rows
+    int32_t hk, hv, dk, dv;
+    int32_t in_dtype;                       // precog_dtype
+    float scale;
+    const int64_t *offsets;                 // scan: [n_seqs + 1]
+    int64_t n_seqs;                         // step: rows
+    int64_t T_tot;
+    const void *bank;                       // nullptr: zero states
+    int32_t bank_dtype;
+    int64_t bank_entries;                   // step: slots of the table
+    const int64_t *idx;                     // step: slots
+    void *states;                           // step: the fp32 table
+    int32_t state_dtype;
+    int32_t layer, L_total;
+    void *y;
+    int32_t y_dtype;
+    void *workspace;
+};
+cudaError_t launch_delta_scan(const DeltaParams &p, cudaStream_t stream);
+cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream);
+size_t delta_scan_workspace_size(const DeltaParams &p);
+cudaError_t delta_status_word_read_clear(uint32_t *bits);
+
+// Norms of query and key heads with the rotation (qk_norm.cu).
+struct QkNormParams {
+    const void *in[2];                      // q, k
+    void *out[2];
+    int64_t in_stride[2], out_stride[2];
+    const float *weight[2];
+    int32_t heads[2];
+    int32_t dim, rot, dtype, norm, interleaved;
+    float eps;
+    const float *cos, *sin;
+    int64_t n_positions;
+    const int64_t *positions;
+    int64_t T;
+};
+cudaError_t launch_qk_norm(const QkNormParams &p, cudaStream_t stream);
+cudaError_t qk_norm_status_word_read_clear(uint32_t *bits);
+
+// Log probabilities of given tokens (logprobs.cu).
+struct LogprobParams {
+    const void *logits;
+    int32_t dtype;
+    int64_t rows, vocab, stride;
+    const int64_t *tokens;
+    float inv_temp;
+    int32_t k;
+    float *logprob, *entropy;
+    int64_t *top_idx;
+    float *top_logprob;
+};
+cudaError_t launch_logprobs(const LogprobParams &p, cudaStream_t stream);
+cudaError_t logprobs_status_word_read_clear(uint32_t *bits);
+
 }  // namespace precog
