@@ -10,6 +10,7 @@
 // the two dot products ends in three shuffles. The readout uses S q = e^g (S_old q) + u (k.q),
 // whose shuffles run beside those of S_old k, in place of a second pass over the new state.
 #include "../../include/precog.h"
+#include "delta.h"
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -310,13 +311,17 @@ cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream) {
 size_t delta_scan_workspace_size(const DeltaParams &p) { return 0; }
 
 cudaError_t launch_delta_scan(const DeltaParams &p, cudaStream_t stream) {
+    if (p.in_dtype == PRECOG_BF16 && p.T_tot >= 8 * p.n_seqs) return launch_delta_chunk(p, stream);
     return p.in_dtype == PRECOG_F32 ? scan_cols<float>(p, stream) : scan_cols<__nv_bfloat16>(p, stream);
 }
 
 cudaError_t delta_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_delta_status, sizeof(uint32_t));
+    uint32_t zero = 0, chunk = 0;
+    cudaError_t e = delta_chunk_status_word_read_clear(&chunk);
     if (e != cudaSuccess) return e;
+    e = cudaMemcpyFromSymbol(bits, g_delta_status, sizeof(uint32_t));
+    if (e != cudaSuccess) return e;
+    *bits |= chunk;
     return cudaMemcpyToSymbol(g_delta_status, &zero, sizeof(uint32_t));
 }
 
