@@ -95,7 +95,6 @@ struct Smem {
     uint64_t ready[2];
     uint64_t done_prep, done_ks, done_qs, done_u, done_s, done_o;
     uint32_t tmem_base;
-    uint32_t abort_flag;
 };
 
 __device__ __forceinline__ uint64_t desc_base(const void *tile) {
@@ -113,21 +112,22 @@ __host__ __device__ constexpr uint32_t idesc(int n, bool mn) {
            (static_cast<uint32_t>(kM >> 4) << 24);
 }
 
-// Bounded wait. Once one has given up, all return at once and the CTA runs to its end on
-// whatever is there: every barrier below is still met by all its threads.
-template <int NA>
-__device__ __forceinline__ void wait_one(uint64_t *bar, uint32_t parity, Smem<NA> &sm) {
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
-        if (mbar_try_wait(bar, parity)) return;
-        if ((i & 255u) == 255u && *reinterpret_cast<volatile uint32_t *>(&sm.abort_flag)) return;
+// Bounded wait. A thread whose wait gives up records it and waits for nothing more than a moment
+// from then on: it runs to the end on whatever is there, so that every barrier below is met.
+__device__ __forceinline__ void wait_one(uint64_t *bar, uint32_t parity, uint32_t &patience) {
+    uint32_t i = 0;
+    bool ok;
+    do {
+        ok = mbar_try_wait(bar, parity);
+    } while (!ok && ++i < patience);
+    if (!ok) {
+        patience = 1;
+        atomicOr(&g_delta_chunk_status, PRECOG_DEV_TIMEOUT);
     }
-    atomicOr(&g_delta_chunk_status, PRECOG_DEV_TIMEOUT);
-    *reinterpret_cast<volatile uint32_t *>(&sm.abort_flag) = 1u;
 }
 // The same by all lanes of a warp, which go on together (tensor-memory accesses are a warp's).
-template <int NA>
-__device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, Smem<NA> &sm) {
-    wait_one(bar, parity, sm);
+__device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, uint32_t &patience) {
+    wait_one(bar, parity, patience);
     __syncwarp();
 }
 
@@ -148,8 +148,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int kKeys = NA * 64;               // key coordinates, padded
     constexpr uint32_t kVOff = NA * 2 * kTile;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    Smem<NA> &sm = *reinterpret_cast<Smem<NA> *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // (an offset, not a rounded address: the compiler would lose that it is shared memory)
+    Smem<NA> &sm = *reinterpret_cast<Smem<NA> *>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    uint32_t patience = kWaitLimit;
 
     int64_t item = blockIdx.x;
     const int slice = static_cast<int>(item % slices);
@@ -177,7 +179,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&sm.done_u, 1);
         mbar_init(&sm.done_s, 1);
         mbar_init(&sm.done_o, 1);
-        sm.abort_flag = 0;
         fence_barrier_init();
     }
     if (warp == 12) {
@@ -193,7 +194,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sm.tmem_base;
+    // all 512 columns: they begin at 0, and addresses are constants below
+    constexpr uint32_t tmem = 0;
 
     if (warp == 12) {
         // ---------------- copies ----------------
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         for (int c = 0; c < kStages && c < chunks && lane == 0; ++c) load(c);
         for (int c = 0; c < chunks; ++c) {
-            wait(&sm.through[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, sm);
+            wait(&sm.through[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
             if (Y) {
                 const int n = len - c * kC < kC ? len - c * kC : kC;
                 for (int t = lane; t < n; t += 32)
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int n = len - c * kC < kC ? len - c * kC : kC;
             uint8_t *st = sm.ring[s];
             const uint32_t col = tmem + kColK + buf * kPlace;
-            wait(&sm.full[s], static_cast<uint32_t>(c / kStages) & 1u, sm);
+            wait(&sm.full[s], static_cast<uint32_t>(c / kStages) & 1u, patience);
             if (n < kC) {   // rows beyond the end, whatever they are
                 for (int e = tid; e < NA * 2 * (kC - n) * 8; e += kPrep)
                     *reinterpret_cast<uint4 *>(st + e / ((kC - n) * 8) * kTile + n * 128 + e % ((kC - n) * 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -260,10 +262,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fence_proxy_async_smem();
             }
             // two chunks ago: through with T, P, the gates and the place in tensor memory
-            if (c >= 2) wait(&sm.through[(c - 2) % kStages], static_cast<uint32_t>((c - 2) / kStages) & 1u, sm);
+            if (c >= 2) wait(&sm.through[(c - 2) % kStages], static_cast<uint32_t>((c - 2) / kStages) & 1u, patience);
             tc_fence_before();
             named_sync(kBarPrep, kPrep);
-            if (tid == 0) {
+            if (pw == 0 && elect_one()) {
                 tc_fence_after();
                 const uint64_t d = desc_base(st);
 #pragma unroll
@@ -309,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             named_sync(kBarPrep, kPrep);
             const Log bi = sm.b[i];
             const float beta = sm.beta[buf][i];
-            wait(&sm.done_prep, static_cast<uint32_t>(c) & 1u, sm);
+            wait(&sm.done_prep, static_cast<uint32_t>(c) & 1u, patience);
             tc_fence_after();
             float *at = reinterpret_cast<float *>(sm.tp[buf][0]);   // A^T[j][i]
             // Columns of 16. Left of the diagonal the decay from j to i goes by the last token of
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // and word to the other warps.
         auto leave = [&](int c) {
             if (Y) {
-                wait(&sm.done_o, static_cast<uint32_t>(c) & 1u, sm);
+                wait(&sm.done_o, static_cast<uint32_t>(c) & 1u, patience);
                 tc_fence_after();
                 const uint32_t place = tm + (c & 1) * kPlace + half * 32;
                 uint32_t r[32], q[32];
@@ -501,55 +503,58 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(&sm.through[c % kStages]);
             __syncwarp();
         };
-        for (int c = 0; c < chunks; ++c) {
+        for (int c = 0; c <= chunks; ++c) {   // the last turn only leaves the last chunk
             const int s = c % kStages, buf = c & 1;
             const uint32_t ph = static_cast<uint32_t>(c) & 1u;
             const uint8_t *st = sm.ring[s];
             const uint32_t col_k = kColK + buf * kPlace, col_q = kColQ + buf * kPlace;
-            wait(&sm.ready[buf], static_cast<uint32_t>(c >> 1) & 1u, sm);
-            wait(&sm.full[s], static_cast<uint32_t>(c / kStages) & 1u, sm);
-            // ---- S as a pair, S decayed ----
-            const float whole = sm.eb[buf][kC - 1];
-            if (Y && c > 0) {   // P U of the chunk before reads U's pair, which lies there
-                wait(&sm.done_o, ph ^ 1u, sm);
-                tc_fence_after();
-            }
+            if (c < chunks) {
+                wait(&sm.ready[buf], static_cast<uint32_t>(c >> 1) & 1u, patience);
+                wait(&sm.full[s], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                // ---- S as a pair, S decayed ----
+                const float whole = sm.eb[buf][kC - 1];
+                if (Y && c > 0) {   // P U of the chunk before reads U's pair, which lies there
+                    wait(&sm.done_o, ph ^ 1u, patience);
+                    tc_fence_after();
+                }
 #pragma unroll 1
-            for (int g = 0; g < kHalf; g += 32) {
-                uint32_t r[32], h[16], l[16];
-                tmem_ld32_async(col_s + g, r);
-                tmem_ld_wait(r);
+                for (int g = 0; g < kHalf; g += 32) {
+                    uint32_t r[32], h[16], l[16];
+                    tmem_ld32_async(col_s + g, r);
+                    tmem_ld_wait(r);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    split(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]), h[e], l[e]);
-                    r[2 * e] = __float_as_uint(whole * __uint_as_float(r[2 * e]));
-                    r[2 * e + 1] = __float_as_uint(whole * __uint_as_float(r[2 * e + 1]));
-                }
-                tmem_st16(tm + kColPair + (half * kHalf + g) / 2, h);
-                tmem_st16(tm + kColPair + kHalf + (half * kHalf + g) / 2, l);
-                tmem_st32(col_s + g, r);
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            named_sync(kBarChain, kChain);
-            if (threadIdx.x == 0) {
-                tc_fence_after();
-                const uint64_t d = desc_base(st);
-#pragma unroll
-                for (int q = 0; q < (Y ? 2 : 1); ++q) {
-#pragma unroll
-                    for (int k = 0; k < kKeys / 8; ++k) {   // hi, then lo
-                        const int kk = k % (kKeys / 16);
-                        tc_mma_f16_ts(tmem + (q ? col_q : col_k), tmem + kColPair + k * 8,
-                                      d + ((kk / 4) * 2 + q) * (kTile / 16) + 2 * (kk % 4), idesc(kC, false), k > 0);
+                    for (int e = 0; e < 16; ++e) {
+                        split(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]), h[e], l[e]);
+                        r[2 * e] = __float_as_uint(whole * __uint_as_float(r[2 * e]));
+                        r[2 * e + 1] = __float_as_uint(whole * __uint_as_float(r[2 * e + 1]));
                     }
-                    tc_commit(q ? &sm.done_qs : &sm.done_ks);
+                    tmem_st16(tm + kColPair + (half * kHalf + g) / 2, h);
+                    tmem_st16(tm + kColPair + kHalf + (half * kHalf + g) / 2, l);
+                    tmem_st32(col_s + g, r);
                 }
+                tmem_st_wait();
+                tc_fence_before();
+                named_sync(kBarChain, kChain);
+                if (warp == 0 && elect_one()) {
+                    tc_fence_after();
+                    const uint64_t d = desc_base(st);
+#pragma unroll
+                    for (int q = 0; q < (Y ? 2 : 1); ++q) {
+#pragma unroll
+                        for (int k = 0; k < kKeys / 8; ++k) {   // hi, then lo
+                            const int kk = k % (kKeys / 16);
+                            tc_mma_f16_ts(tmem + (q ? col_q : col_k), tmem + kColPair + k * 8,
+                                          d + ((kk / 4) * 2 + q) * (kTile / 16) + 2 * (kk % 4), idesc(kC, false), k > 0);
+                        }
+                        tc_commit(q ? &sm.done_qs : &sm.done_ks);
+                    }
+                }
+                __syncwarp();
             }
-            __syncwarp();
             if (c > 0) leave(c - 1);
+            if (c == chunks) break;
             // ---- X, in the place of S k: hi of this half's 32 tokens, then lo ----
-            wait(&sm.done_ks, ph, sm);
+            wait(&sm.done_ks, ph, patience);
             tc_fence_after();
             {
                 uint32_t r[32], h[16], l[16];
@@ -572,8 +577,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st_wait();
             tc_fence_before();
             named_sync(kBarChain, kChain);
-            if (threadIdx.x == 0) {
-                if (Y) wait_one(&sm.done_qs, ph, sm);   // S's pair has been read: U takes its place
+            if (warp == 0 && elect_one()) {
+                if (Y) wait_one(&sm.done_qs, ph, patience);   // S's pair has been read: U takes its place
                 tc_fence_after();
                 const uint64_t hi = desc_base(sm.tp[buf][0]), lo = desc_base(sm.tp[buf][1]);
 #pragma unroll
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             __syncwarp();
             // ---- U: a pair for P U, and decayed to the chunk's end, in U's place, for the update ----
-            wait(&sm.done_u, ph, sm);
+            wait(&sm.done_u, ph, patience);
             tc_fence_after();
             {
                 uint32_t r[32], h[16], l[16];
@@ -608,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st_wait();
             tc_fence_before();
             named_sync(kBarChain, kChain);
-            if (threadIdx.x == 0) {
+            if (warp == 0 && elect_one()) {
                 tc_fence_after();
                 const uint64_t d = desc_base(st);
 #pragma unroll
@@ -632,10 +637,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             __syncwarp();
-            wait(&sm.done_s, ph, sm);
+            wait(&sm.done_s, ph, patience);
             tc_fence_after();
         }
-        if (chunks > 0) leave(chunks - 1);
         if (p.states) {
             const int64_t at = ((seq * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
 #pragma unroll
