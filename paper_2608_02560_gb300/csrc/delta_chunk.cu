@@ -17,10 +17,12 @@
 // Warps 0-7, the chain: what each chunk needs of the chunk before it, half the columns each
 // group of four. Per chunk: split S, [S k], [S q, V T], split S k, [S k T], split U, [update],
 // [P U]; [..] are MMAs. y of a chunk leaves while the next one's first MMAs run.
-// Warps 8-11, one chunk ahead: A and P with their decays, the inverse T by substitution in fp32
-// (a product form of the inverse would lose its digits where keys repeat).
-// Warp 12: copies in, three chunks deep, the chunks' gates, and y rows out.
-// Warp 13: issues every MMA, so that no working warp waits in the queue of the tensor cores.
+// Warps 8-15, one chunk ahead: A and P with their decays, the inverse T in fp32: blocks of 16 by
+// substitution (a product form would lose its digits where keys repeat), then joined twice,
+// T10 = -(T1 A10) T0, on mma.sync with operands as pairs of tf32 (16 x 16 and 32 x 32: too small
+// for an MMA of 128 rows, and one multiply per shared-memory read was too slow).
+// Warp 16: copies in, three chunks deep, the chunks' gates, and y rows out.
+// Warp 17: issues every MMA, so that no working warp waits in the queue of the tensor cores.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
@@ -45,16 +47,13 @@ namespace {
 constexpr int kC = 64;                 // tokens of a chunk
 constexpr int kM = 128;                // value channels of a CTA
 constexpr int kStages = 3;
-constexpr int kChain = 256, kPrep = 128;   // threads
+constexpr int kChain = 256, kPrep = 256;   // threads
 constexpr int kThreads = kChain + kPrep + 64;
-constexpr int kH = kC / 2;             // T is solved for in halves
-constexpr int kPad = kH + 4;
+constexpr int kCopyWarp = (kChain + kPrep) / 32, kMmaWarp = kCopyWarp + 1;
+constexpr int kH = kC / 2, kB = kC / 4;    // the inverse: blocks of 16, joined to halves, joined
+constexpr int kPitch = kH + 4;             // (rows of an MMA operand in different banks)
 constexpr uint32_t kTile = kC * 128;   // bytes of a [64 tokens][64 keys] bf16 tile
 constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
-
-// A wait naps up to kNap ns at a time (and wakes when the barrier completes): polling at once took
-// issue slots from the warps that work. kPatience naps are some seconds.
-constexpr uint32_t kNap = 2000, kPatience = 1u << 20;
 
 // tensor memory columns
 constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = kColK + 64, kPlace = 128;
@@ -96,11 +95,10 @@ struct Smem {
     // per stage: [K][Q] tiles of key columns 0..63, then of 64..127, then V's two; the chunk's y rows
     // lie there on their way out
     uint8_t ring[kStages][(NA * 2 + 2) * kTile];
-    // T hi, T lo, P hi, P lo; while T is solved for, A^T in fp32 fills the place of T
+    // T hi, T lo, P hi, P lo; A and what becomes of it, by columns in fp32, fill the place of T before
     uint8_t tp[2][4][kTile];
     Gates gates[kStages];
-    alignas(16) float t11[kH][kH];    // [row][column]
-    alignas(16) float t22[kH][kPad];  // [column][row], read and written as float4
+    alignas(16) float mid[kH * kPitch];   // a product on its way, [row][column]
     uint64_t full[kStages], gated[kStages], through[kStages];
     uint64_t ready[2], done_prep[2], done_o[2];
     uint64_t have_s, have_k, have_u;              // the chain's operands are in tensor memory
@@ -129,7 +127,7 @@ __device__ __forceinline__ void wait_one(uint64_t *bar, uint32_t parity, uint32_
     uint32_t i = 0;
     bool ok;
     do {
-        ok = mbar_try_wait_ns(bar, parity, kNap);
+        ok = mbar_try_wait(bar, parity);
     } while (!ok && ++i < patience);
     if (!ok) {
         patience = 1;
@@ -170,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (an offset, not a rounded address: the compiler would lose that it is shared memory)
     Smem<NA> &sm = *reinterpret_cast<Smem<NA> *>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    uint32_t patience = kPatience;
+    uint32_t patience = kWaitLimit;
 
     int64_t item = blockIdx.x;
     const int slice = static_cast<int>(item % slices);
@@ -193,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&sm.through[s], kChain / 32);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sm.ready[i], kPrep);
+            mbar_init(&sm.ready[i], kPrep / 32);
             mbar_init(&sm.done_prep[i], 1);
             mbar_init(&sm.done_o[i], 1);
         }
@@ -206,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&sm.done_s, 1);
         fence_barrier_init();
     }
-    if (warp == 13) {
+    if (warp == kMmaWarp) {
         tmem_alloc(&sm.tmem_base, 512);
         tmem_relinquish();
     }
@@ -222,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // all 512 columns: they begin at 0, and addresses are constants below
     constexpr uint32_t tmem = 0;
 
-    if (warp == 13) {
+    if (warp == kMmaWarp) {
         // ---------------- MMAs ----------------
         if (elect_one()) {
             // [K; Q] K^T of chunk c, for the warps that work ahead
@@ -296,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
         __syncwarp();
-    } else if (warp == 12) {
+    } else if (warp == kCopyWarp) {
         // ---------------- copies and gates ----------------
         const int y_size = p.y_dtype == PRECOG_F32 ? 4 : 2;
         const int channels = p.dv - slice * kM < kM ? p.dv - slice * kM : kM;
@@ -397,15 +395,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else if (warp >= 8) {
         // ---------------- T and P, one chunk ahead of the chain ----------------
-        const int pw = warp - 8;
-        const int half = pw & 1, i = half * kH + lane;   // this thread's row: of A (warps 8, 9) or P
-        const bool is_a = pw < 2;
-        const uint32_t lanes = static_cast<uint32_t>(pw * 32) << 16;
+        const int tid = threadIdx.x - kChain, quarter = warp & 3, group = (warp >> 2) & 1;
+        const int half = quarter & 1, i = half * kH + lane;   // this thread's row: of A (quarters 0, 1) or P
+        const bool is_a = quarter < 2;
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
             const int buf = c & 1;
             const uint32_t col = tmem + kColK + buf * kPlace;
             const Gates &gt = sm.gates[c % kStages];
+            // column j, row i of A and later of T, turned so that the rows or the columns of an MMA's
+            // operand lie in different banks
+            float *at = reinterpret_cast<float *>(sm.tp[buf][0]);
+            auto place = [](int j, int i) { return j * kC + (i ^ ((j & 7) << 3)); };
             wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
             const Log bi = gt.b[i];
             const float mine = is_a ? gt.beta[i] : p.scale;
@@ -413,11 +415,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (c >= 2) wait(&sm.done_o[buf], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
             wait(&sm.done_prep[buf], static_cast<uint32_t>(c >> 1) & 1u, patience);
             tc_fence_after();
-            float *at = reinterpret_cast<float *>(sm.tp[buf][0]);   // A^T[j][i]
-            // Columns of 16. Left of the diagonal the decay from j to i goes by the last token of
-            // the 16, both factors at most 1 where nothing grows; on it each has its exponential.
+            // Columns of 16: the diagonal halves' by one warp each (A's go on to invert them), P21 and A21
+            // by another. Left of the diagonal the decay from j to i
+            // goes by the last token of the 16, both factors at most 1 where nothing grows; on it
+            // each has its exponential.
 #pragma unroll 1
-            for (int j0 = 0; j0 < (half + 1) * kH; j0 += 16) {
+            for (int j0 = half * group * kH, e0 = 0; e0 < (half | (group ^ 1)) * 2; j0 += kB, ++e0) {
                 float v[16];
                 tmem_ld16(col + lanes + j0, v);
                 if (j0 < half * kH) {
@@ -433,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (is_a) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) at[(j0 + e) * kC + i] = v[e];
+                    for (int e = 0; e < 16; ++e) at[(j0 + e) * kC + (i ^ ((e & 7) << 3))] = v[e];
                 } else {
 #pragma unroll
                     for (int o = 0; o < 16; o += 8) {
@@ -447,88 +450,105 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             tc_fence_before();
-            named_sync(kBarPrep, kPrep);
-            // ---- (I + A)^-1 in halves of 32: T11 and T22, then T21 = -T22 (A21 T11) ----
-            f2 t[kH / 2];
-            if (is_a) {
-                // column `lane` of T11 or T22: from I, rows below l lose A[.][l] T[l], l = 0, 1, ..
+            __syncwarp();
+            // ---- (I + A)^-1 of one half a warp: two blocks of 16, a column a lane ----
+            const int g = lane >> 2, t = lane & 3;   // an MMA's row or column, and its pair
+            if (is_a && half == group) {
+                const int lo = half * kH, up = lo + kB, b = lo + (lane & 16), cc = lane & 15;
+                f2 x[kB / 2];
 #pragma unroll
-                for (int e = 0; e < kH / 2; ++e) t[e] = pack2(2 * e == lane ? 1.f : 0.f, 2 * e + 1 == lane ? 1.f : 0.f);
-                const float *a = at + half * (kH * kC + kH);
+                for (int e = 0; e < kB / 2; ++e) x[e] = pack2(2 * e == cc ? 1.f : 0.f, 2 * e + 1 == cc ? 1.f : 0.f);
+                // from I, rows below l lose A[.][l] T[l], l = 0, 1, ..
 #pragma unroll
-                for (int l = 0; l < kH - 1; ++l) {
-                    float lo, hi;
-                    unpack2(t[l / 2], lo, hi);
-                    const float m = -(l % 2 ? hi : lo);
+                for (int l = 0; l < kB - 1; ++l) {
+                    float even, odd;
+                    unpack2(x[l / 2], even, odd);
+                    const float m = -(l % 2 ? odd : even);
                     const f2 mm = pack2(m, m);
 #pragma unroll
-                    for (int e = (l + 1) / 4 * 4; e < kH; e += 4) {
-                        const float4 x = *reinterpret_cast<const float4 *>(a + l * kC + e);
-                        t[e / 2] = fma2(pack2(x.x, x.y), mm, t[e / 2]);
-                        t[e / 2 + 1] = fma2(pack2(x.z, x.w), mm, t[e / 2 + 1]);
+                    for (int e = (l + 1) / 4 * 4; e < kB; e += 4) {
+                        const float4 a = *reinterpret_cast<const float4 *>(at + (b + l) * kC + ((b + e) ^ ((l & 7) << 3)));
+                        x[e / 2] = fma2(pack2(a.x, a.y), mm, x[e / 2]);
+                        x[e / 2 + 1] = fma2(pack2(a.z, a.w), mm, x[e / 2 + 1]);
                     }
                 }
-                if (half == 0) {
+                __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < kH / 2; ++e) unpack2(t[e], sm.t11[2 * e][lane], sm.t11[2 * e + 1][lane]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kH / 4; ++e) {
-                        float4 x;
-                        unpack2(t[2 * e], x.x, x.y);
-                        unpack2(t[2 * e + 1], x.z, x.w);
-                        *reinterpret_cast<float4 *>(&sm.t22[lane][4 * e]) = x;
-                    }
+                for (int e = 0; e < kB; e += 4) {
+                    float4 a;
+                    unpack2(x[e / 2], a.x, a.y);
+                    unpack2(x[e / 2 + 1], a.z, a.w);
+                    *reinterpret_cast<float4 *>(at + (b + cc) * kC + ((b + e) ^ ((cc & 7) << 3))) = a;
                 }
+                __syncwarp();
+                // T1 A10, whose columns 2 t, 2 t + 1 of 8 then count as the A operand's t and t + 4
+                Sums3 h[2], d[2];
+#pragma unroll
+                for (int k = 0; k < kB; k += 8) {
+                    const float a[4] = {at[place(up + k + t, up + g)], at[place(up + k + t, up + g + 8)],
+                                        at[place(up + k + t + 4, up + g)], at[place(up + k + t + 4, up + g + 8)]};
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        mma_3tf32(h[n], a, {at[place(lo + 8 * n + g, up + k + t)], at[place(lo + 8 * n + g, up + k + t + 4)]});
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float a[4] = {h[k][0], h[k][2], h[k][1], h[k][3]};
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        mma_3tf32(d[n], a, {at[place(lo + 8 * n + g, lo + 8 * k + 2 * t)], at[place(lo + 8 * n + g, lo + 8 * k + 2 * t + 1)]});
+                }
+                __syncwarp();   // A10 has been read
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) at[place(lo + 8 * n + 2 * t + (e & 1), up + g + (e & 2) * 4)] = -d[n][e];
             }
             named_sync(kBarPrep, kPrep);
-            // rows 8 pw .. + 7, column `lane`
-            f2 acc[4];
-            auto product = [&](const float *left, int stride, const float *right, int pitch) {
+            // ---- joined: 16 rows and 8 columns of T22 A21, then of T21, a warp ----
+            {
+                const int r = (warp & 1) * 16, n = (warp >> 1 & 3) * 8;
+                Sums3 d;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = pack2(0.f, 0.f);
-#pragma unroll 8
-                for (int l = 0; l < kH; ++l) {
-                    const float4 x = *reinterpret_cast<const float4 *>(left + l * stride), z = *reinterpret_cast<const float4 *>(left + l * stride + 4);
-                    const float m = right[l * pitch + lane];
-                    const f2 mm = pack2(m, m);
-                    acc[0] = fma2(pack2(x.x, x.y), mm, acc[0]);
-                    acc[1] = fma2(pack2(x.z, x.w), mm, acc[1]);
-                    acc[2] = fma2(pack2(z.x, z.y), mm, acc[2]);
-                    acc[3] = fma2(pack2(z.z, z.w), mm, acc[3]);
-                }
-            };
-            product(at + kH + 8 * pw, kC, &sm.t11[0][0], kH);
-            // A21 T11, where A11 was
+                for (int k = 0; k < kH; k += 8)
+                    mma_3tf32(d, {at[place(kH + k + t, kH + r + g)], at[place(kH + k + t, kH + r + g + 8)],
+                                  at[place(kH + k + t + 4, kH + r + g)], at[place(kH + k + t + 4, kH + r + g + 8)]},
+                              {at[place(n + g, kH + k + t)], at[place(n + g, kH + k + t + 4)]});
 #pragma unroll
-            for (int e = 0; e < 4; ++e) unpack2(acc[e], at[(8 * pw + 2 * e) * kC + lane], at[(8 * pw + 2 * e + 1) * kC + lane]);
+                for (int e = 0; e < 4; ++e) sm.mid[(r + g + (e & 2) * 4) * kPitch + n + 2 * t + (e & 1)] = d[e];
+                named_sync(kBarPrep, kPrep);
+                d = Sums3();
+                const float *mid = sm.mid + (r + g) * kPitch + t;
+#pragma unroll
+                for (int k = 0; k < kH; k += 8)
+                    mma_3tf32(d, {mid[k], mid[8 * kPitch + k], mid[k + 4], mid[8 * kPitch + k + 4]},
+                              {at[place(n + g, k + t)], at[place(n + g, k + t + 4)]});
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at[place(n + 2 * t + (e & 1), kH + r + g + (e & 2) * 4)] = -d[e];
+            }
             named_sync(kBarPrep, kPrep);
-            product(&sm.t22[0][8 * pw], kPad, at, kC);
-            named_sync(kBarPrep, kPrep);   // nobody reads there any more: T takes its place
-            auto put = [&](int row, int col_, f2 ab) {   // T[row .. row + 1][col_]
-                uint32_t h, l;
-                split(ab, h, l);
+            // ---- T diag(beta) as a pair: 16 columns of a row a thread ----
+            {
+                const int row = tid & (kC - 1), j0 = (tid / kC) * kB;
+                const bool there = j0 <= row;   // (blocks right of the diagonal are zero)
+                uint32_t h[8], l[8];
+#pragma unroll
+                for (int e = 0; e < kB; e += 2)
+                    split(mul2(pack2(there ? at[(j0 + e) * kC + (row ^ ((e & 7) << 3))] : 0.f, there ? at[(j0 + e + 1) * kC + (row ^ (((e + 1) & 7) << 3))] : 0.f),
+                               load2(gt.beta + j0 + e)),
+                          h[e / 2], l[e / 2]);
+                named_sync(kBarPrep, kPrep);
 #pragma unroll
                 for (int o = 0; o < 2; ++o) {
-                    const int to = (row + o) * 128 + ((col_ / 8) ^ ((row + o) & 7)) * 16 + (col_ % 8) * 2;
-                    *reinterpret_cast<uint16_t *>(sm.tp[buf][0] + to) = static_cast<uint16_t>(o ? h >> 16 : h);
-                    *reinterpret_cast<uint16_t *>(sm.tp[buf][1] + to) = static_cast<uint16_t>(o ? l >> 16 : l);
+                    const int to = row * 128 + ((j0 / 8 + o) ^ (row & 7)) * 16;
+                    *reinterpret_cast<uint4 *>(sm.tp[buf][0] + to) = make_uint4(h[4 * o], h[4 * o + 1], h[4 * o + 2], h[4 * o + 3]);
+                    *reinterpret_cast<uint4 *>(sm.tp[buf][1] + to) = make_uint4(l[4 * o], l[4 * o + 1], l[4 * o + 2], l[4 * o + 3]);
                 }
-            };
-            if (is_a) {
-                const f2 bb = pack2(gt.beta[i], gt.beta[i]);   // of the column half * 32 + lane
-#pragma unroll
-                for (int e = 0; e < kH / 2; ++e) put(half * kH + 2 * e, half * kH + lane, mul2(t[e], bb));
-            } else {   // T12 = 0: rows 0 .. 31, 64 bytes each, of T hi (warp 10) or T lo
-#pragma unroll
-                for (int e = 4; e < 8; ++e)
-                    *reinterpret_cast<uint4 *>(sm.tp[buf][half] + lane * 128 + (e ^ (lane & 7)) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
-            const f2 bb = pack2(-gt.beta[lane], -gt.beta[lane]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) put(kH + 8 * pw + 2 * e, lane, mul2(acc[e], bb));
             fence_proxy_async_smem();
-            mbar_arrive(&sm.ready[buf]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.ready[buf]);
+            __syncwarp();
         }
     } else {
         // ---------------- the chain ----------------
@@ -705,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 13) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
