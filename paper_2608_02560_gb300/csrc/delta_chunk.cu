@@ -46,7 +46,7 @@ namespace {
 
 constexpr int kC = 64;                 // tokens of a chunk
 constexpr int kM = 128;                // value channels of a CTA
-constexpr int kStages = 3;
+constexpr int kStages = 3, kGates = 4;
 constexpr int kChain = 256, kPrep = 256;   // threads
 constexpr int kThreads = kChain + kPrep + 64;
 constexpr int kCopyWarp = (kChain + kPrep) / 32, kMmaWarp = kCopyWarp + 1;
@@ -58,7 +58,7 @@ constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
 // tensor memory columns
 constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = kColK + 64, kPlace = 128;
 
-constexpr int kBarPrep = 1;
+constexpr int kBarPrep = 1, kBarHalf = 2;   // and 3
 
 // A sum of logs as an unevaluated pair: differences of large sums keep their digits.
 struct Log {
@@ -80,7 +80,7 @@ __device__ __forceinline__ Log shfl(Log a, int from) {
 
 // What the gates of a chunk become.
 struct alignas(16) Gates {
-    Log b[kC];            // in units of log2
+    float bh[kC], bl[kC]; // b in units of log2, a pair
     Log last[4];          // b of the last token of each 16
     float to_last[kC];    // e^{last - b_j}
     float beta[kC];
@@ -92,16 +92,17 @@ struct alignas(16) Gates {
 
 template <int NA>
 struct Smem {
-    // per stage: [K][Q] tiles of key columns 0..63, then of 64..127, then V's two; the chunk's y rows
-    // lie there on their way out
-    uint8_t ring[kStages][(NA * 2 + 2) * kTile];
+    // per stage: [K][Q] tiles of key columns 0..63, then of 64..127; V's two tiles, where the chunk's
+    // bf16 y rows lie on their way out
+    uint8_t kq[kStages][NA * 2 * kTile];
+    uint8_t v[kStages][2 * kTile];
     // T hi, T lo, P hi, P lo; A and what becomes of it, by columns in fp32, fill the place of T before
     uint8_t tp[2][4][kTile];
-    Gates gates[kStages];
+    Gates gates[kGates];
     alignas(16) float mid[kH * kPitch];   // a product on its way, [row][column]
-    uint64_t full[kStages], gated[kStages], through[kStages];
+    uint64_t full_kq[kStages], full_v[kStages], free_kq[kStages], through[kStages], gated[kGates], zeroed;
     uint64_t ready[2], done_prep[2], done_o[2];
-    uint64_t have_s, have_k, have_u;              // the chain's operands are in tensor memory
+    uint64_t have_s, have_k, have_d, have_u;      // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
     uint32_t tmem_base;
 };
@@ -163,7 +164,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     delta_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const DeltaParams p, int slices) {
     constexpr int kKeys = NA * 64;               // key coordinates, padded
-    constexpr uint32_t kVOff = NA * 2 * kTile;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // (an offset, not a rounded address: the compiler would lose that it is shared memory)
     Smem<NA> &sm = *reinterpret_cast<Smem<NA> *>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
@@ -186,10 +186,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&sm.full[s], 1);
-            mbar_init(&sm.gated[s], 1);
+            mbar_init(&sm.full_kq[s], 1);
+            mbar_init(&sm.full_v[s], 1);
+            mbar_init(&sm.free_kq[s], 1);
             mbar_init(&sm.through[s], kChain / 32);
         }
+        for (int i = 0; i < kGates; ++i) mbar_init(&sm.gated[i], 1);
+        mbar_init(&sm.zeroed, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.ready[i], kPrep / 32);
             mbar_init(&sm.done_prep[i], 1);
@@ -197,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(&sm.have_s, kChain / 32);
         mbar_init(&sm.have_k, kChain / 32);
+        mbar_init(&sm.have_d, kChain / 32);
         mbar_init(&sm.have_u, kChain / 32);
         mbar_init(&sm.done_ks, 1);
         mbar_init(&sm.done_qs, 1);
@@ -225,10 +229,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (elect_one()) {
             // [K; Q] K^T of chunk c, for the warps that work ahead
             auto products = [&](int c) {
-                wait_one(&sm.full[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                wait_one(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
                 // rows beyond the end are zeroed first
-                if (len - c * kC < kC) wait_one(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                const uint64_t d = desc_base(sm.ring[c % kStages]);
+                if (len - c * kC < kC) wait_one(&sm.zeroed, 0, patience);
+                const uint64_t d = desc_base(sm.kq[c % kStages]);
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k) {
                     const uint64_t dk = d + (k / 4) * (2 * kTile / 16) + 2 * (k % 4);
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < chunks; ++c) {
                 const uint32_t ph = static_cast<uint32_t>(c) & 1u;
                 const uint32_t col_k = tmem + kColK + ph * kPlace, col_q = tmem + kColQ + ph * kPlace;
-                const uint64_t d = desc_base(sm.ring[c % kStages]), dt = desc_base(sm.tp[ph][0]);
+                const uint64_t d = desc_base(sm.kq[c % kStages]), dv = desc_base(sm.v[c % kStages]), dt = desc_base(sm.tp[ph][0]);
                 // (its place: S k's pair of the chunk before, which [S k T] has read)
                 if (c + 1 < chunks) products(c + 1);
                 wait_one(&sm.ready[ph], static_cast<uint32_t>(c >> 1) & 1u, patience);
@@ -257,10 +261,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tc_commit(q ? &sm.done_qs : &sm.done_ks);
                 }
+                wait_one(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
                 wait_one(Y ? &sm.done_qs : &sm.done_ks, ph, patience);   // S's pair has been read: U takes its place
 #pragma unroll
                 for (int k = 0; k < 8; ++k)   // V T hi, V T lo
-                    tc_mma_f16(tmem + kColPair, d + kVOff / 16 + (k % 4) * (2048 / 16), dt + (k / 4) * (kTile / 16) + 2 * (k % 4),
+                    tc_mma_f16(tmem + kColPair, dv + (k % 4) * (2048 / 16), dt + (k / 4) * (kTile / 16) + 2 * (k % 4),
                                idesc(kC, true, false), k > 0);
                 wait_one(&sm.have_k, ph, patience);
                 tc_fence_after();
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                   dt + (part == 2 ? kTile / 16 : 0) + 2 * kk, idesc(kC, false, false), true);
                 }
                 tc_commit(&sm.done_u);
-                wait_one(&sm.have_u, ph, patience);
+                wait_one(&sm.have_d, ph, patience);
                 tc_fence_after();
 #pragma unroll
                 for (int a = 0; a < NA; ++a)
@@ -282,7 +287,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                                       d + a * (2 * kTile / 16) + kk * (2048 / 16), idesc(64, false, true), true);
                     }
                 tc_commit(&sm.done_s);
+                tc_commit(&sm.free_kq[c % kStages]);
                 if (Y) {
+                    wait_one(&sm.have_u, ph, patience);
+                    tc_fence_after();
 #pragma unroll
                     for (int k = 0; k < 12; ++k) {   // U hi P hi, U lo P hi, U hi P lo, onto S q
                         const int part = k / 4, kk = k % 4;
@@ -296,19 +304,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else if (warp == kCopyWarp) {
         // ---------------- copies and gates ----------------
-        const int y_size = p.y_dtype == PRECOG_F32 ? 4 : 2;
         const int channels = p.dv - slice * kM < kM ? p.dv - slice * kM : kM;
-        auto load = [&](int c) {
-            uint8_t *st = sm.ring[c % kStages];
-            uint64_t *full = &sm.full[c % kStages];
-            const int row = static_cast<int>(begin) + c * kC;
-            const int v_tiles = channels > 64 ? 2 : 1;
-            mbar_arrive_expect_tx(full, (NA * (Y ? 2 : 1) + v_tiles) * kTile);
+        auto load_kq = [&](int c) {
+            uint8_t *st = sm.kq[c % kStages];
+            uint64_t *full = &sm.full_kq[c % kStages];
+            mbar_arrive_expect_tx(full, NA * (Y ? 2 : 1) * kTile);
             for (int a = 0; a < NA; ++a) {
-                tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, row, full);
-                if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, row, full);
+                tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, static_cast<int>(begin) + c * kC, full);
+                if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, static_cast<int>(begin) + c * kC, full);
             }
-            for (int a = 0; a < v_tiles; ++a) tma_load_3d(st + kVOff + a * kTile, &map_v, slice * kM + a * 64, head, row, full);
+        };
+        auto load_v = [&](int c) {
+            uint64_t *full = &sm.full_v[c % kStages];
+            const int tiles = channels > 64 ? 2 : 1;
+            mbar_arrive_expect_tx(full, tiles * kTile);
+            for (int a = 0; a < tiles; ++a)
+                tma_load_3d(sm.v[c % kStages] + a * kTile, &map_v, slice * kM + a * 64, head, static_cast<int>(begin) + c * kC, full);
         };
         float g[2], bt[2];   // of tokens 2 lane, 2 lane + 1 of a chunk to come
         auto load_gates = [&](int c) {
@@ -324,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         auto gate = [&](int c) {
             constexpr float kL = 1.44269502f, kLl = 1.92596303e-8f;   // log2 e
-            Gates &to = sm.gates[c % kStages];
+            Gates &to = sm.gates[c % kGates];
             Log x[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -345,7 +356,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Log b = e ? sum : lane ? before + x[0] : x[0];
                 const int t = 2 * lane + e;
                 const float eb = ex2(b.h + b.l);
-                to.b[t] = b;
+                to.bh[t] = b.h;
+                to.bl[t] = b.l;
                 to.to_last[t] = exp_diff(last, b);
                 to.beta[t] = bt[e];
                 to.ek[t] = -eb;
@@ -354,41 +366,61 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if ((lane & 7) == 7) to.last[lane / 8] = sum;
             if (lane == 31) to.whole = ex2(sum.h + sum.l);
-            const int n = len - c * kC;
-            if (n < kC) {   // rows beyond the end, whatever they are
-                wait(&sm.full[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                for (int e = lane; e < (NA * 2 + 2) * (kC - n) * 8; e += 32)
-                    *reinterpret_cast<uint4 *>(sm.ring[c % kStages] + e / ((kC - n) * 8) * kTile + n * 128 + e % ((kC - n) * 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                fence_proxy_async_smem();
-            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.gated[c % kStages]);
+            if (lane == 0) mbar_arrive(&sm.gated[c % kGates]);
             __syncwarp();
         };
-        for (int c = 0; c < kStages && c < chunks && lane == 0; ++c) load(c);
+        // The last chunk's rows beyond the end, whatever they are, once it is in.
+        auto zero_tail = [&](int c) {
+            const int n = len - c * kC;
+            if (c + 1 < chunks || n == kC) return;
+            wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+            wait(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+            for (int e = lane; e < (NA * 2 + 2) * (kC - n) * 8; e += 32) {
+                const int tile = e / ((kC - n) * 8);
+                uint8_t *to = tile < NA * 2 ? sm.kq[c % kStages] + tile * kTile : sm.v[c % kStages] + (tile - NA * 2) * kTile;
+                *reinterpret_cast<uint4 *>(to + n * 128 + e % ((kC - n) * 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.zeroed);
+            __syncwarp();
+        };
+        for (int c = 0; c < kStages && c < chunks && lane == 0; ++c) {
+            load_kq(c);
+            load_v(c);
+        }
         __syncwarp();
         load_gates(0);
-        for (int c = 0; c < kStages && c < chunks; ++c) {
+        for (int c = 0; c < kGates && c < chunks; ++c) {
             gate(c);
             load_gates(c + 1);
+            if (c < kStages) zero_tail(c);
         }
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            wait(&sm.through[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-            if (Y) {
+            const uint32_t phase = static_cast<uint32_t>(c / kStages) & 1u;
+            wait(&sm.free_kq[c % kStages], phase, patience);
+            if (c + kStages < chunks && lane == 0) load_kq(c + kStages);
+            __syncwarp();
+            wait(&sm.through[c % kStages], phase, patience);
+            if (Y && p.y_dtype == PRECOG_BF16) {
                 const int n = len - c * kC < kC ? len - c * kC : kC;
                 for (int t = lane; t < n; t += 32)
-                    bulk_s2g(static_cast<char *>(p.y) + ((begin + c * kC + t) * p.hv * p.dv + static_cast<int64_t>(head) * p.dv + slice * kM) * y_size,
-                             sm.ring[c % kStages] + t * kM * y_size, channels * y_size);
+                    bulk_s2g(static_cast<__nv_bfloat16 *>(p.y) + (begin + c * kC + t) * p.hv * p.dv + static_cast<int64_t>(head) * p.dv + slice * kM,
+                             sm.v[c % kStages] + t * kM * 2, channels * 2);
                 bulk_commit();
                 bulk_wait_read<0>();
                 __syncwarp();
             }
             if (c + kStages < chunks) {
-                if (lane == 0) load(c + kStages);
+                if (lane == 0) load_v(c + kStages);
                 __syncwarp();
-                gate(c + kStages);
-                load_gates(c + kStages + 1);
+                zero_tail(c + kStages);
+            }
+            if (c + kGates < chunks) {
+                gate(c + kGates);
+                load_gates(c + kGates + 1);
             }
         }
         if (Y) bulk_wait_all();
@@ -403,24 +435,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = 0; c < chunks; ++c) {
             const int buf = c & 1;
             const uint32_t col = tmem + kColK + buf * kPlace;
-            const Gates &gt = sm.gates[c % kStages];
+            const Gates &gt = sm.gates[c % kGates];
             // column j, row i of A and later of T, turned so that the rows or the columns of an MMA's
             // operand lie in different banks
             float *at = reinterpret_cast<float *>(sm.tp[buf][0]);
             auto place = [](int j, int i) { return j * kC + (i ^ ((j & 7) << 3)); };
-            wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-            const Log bi = gt.b[i];
+            wait(&sm.gated[c % kGates], static_cast<uint32_t>(c / kGates) & 1u, patience);
+            const Log bi{gt.bh[i], gt.bl[i]};
+            const f2 bih = pack2(bi.h, bi.h), bil = pack2(bi.l, bi.l), minus = pack2(-1.f, -1.f);
             const float mine = is_a ? gt.beta[i] : p.scale;
             // two chunks ago: through with T and P
             if (c >= 2) wait(&sm.done_o[buf], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
             wait(&sm.done_prep[buf], static_cast<uint32_t>(c >> 1) & 1u, patience);
             tc_fence_after();
-            // Columns of 16: the diagonal halves' by one warp each (A's go on to invert them), P21 and A21
-            // by another. Left of the diagonal the decay from j to i
-            // goes by the last token of the 16, both factors at most 1 where nothing grows; on it
-            // each has its exponential.
+            // Columns of 16, by turns. Left of the diagonal half the decay from j to i goes by the last
+            // token of the 16, both factors at most 1 where nothing grows; on it each entry has its
+            // exponential.
 #pragma unroll 1
-            for (int j0 = half * group * kH, e0 = 0; e0 < (half | (group ^ 1)) * 2; j0 += kB, ++e0) {
+            for (int j0 = group * kB; j0 < (half + 1) * kH; j0 += kH) {
                 float v[16];
                 tmem_ld16(col + lanes + j0, v);
                 if (j0 < half * kH) {
@@ -428,10 +460,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] *= f * gt.to_last[j0 + e];
                 } else {
+                    const int lim = i + (is_a ? 0 : 1) - j0;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float f = exp_diff(bi, gt.b[j0 + e]) * mine;
-                        v[e] = j0 + e < i + (is_a ? 0 : 1) ? v[e] * f : 0.f;
+                    for (int e = 0; e < 16; e += 2) {
+                        float a, b;
+                        unpack2(fma2(load2(gt.bl + j0 + e), minus, fma2(fma2(load2(gt.bh + j0 + e), minus, bih), pack2(1.f, 1.f), bil)), a, b);
+                        v[e] = e < lim ? v[e] * (ex2(a) * mine) : 0.f;
+                        v[e + 1] = e + 1 < lim ? v[e + 1] * (ex2(b) * mine) : 0.f;
                     }
                 }
                 if (is_a) {
@@ -450,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             tc_fence_before();
-            __syncwarp();
+            if (is_a) named_sync(kBarHalf + half, 64);   // the two warps of A's rows
             // ---- (I + A)^-1 of one half a warp: two blocks of 16, a column a lane ----
             const int g = lane >> 2, t = lane & 3;   // an MMA's row or column, and its pair
             if (is_a && half == group) {
@@ -594,115 +629,133 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(bar);
             __syncwarp();
         };
+        const int64_t y_row = static_cast<int64_t>(p.hv) * p.dv;
 #pragma unroll 1
         for (int c = 0; c <= chunks; ++c) {   // the last turn only leaves the last chunk
-            const int s = c % kStages, buf = c & 1;
+            const int buf = c & 1;
             const uint32_t ph = static_cast<uint32_t>(c) & 1u;
-            const Gates &gt = sm.gates[s];
+            const Gates &gt = sm.gates[c % kGates];
             const uint32_t col_k = tm + kColK + buf * kPlace + half * 32, col_q = tm + kColQ + buf * kPlace + half * 32;
-            if (c > 0) {   // P U of the chunk before has read U's pair, and its sums are complete
-                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
-                tc_fence_after();
-            }
             if (c < chunks) {
-                // ---- S as a pair, S decayed ----
-                wait(&sm.gated[s], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                const f2 whole = pack2(gt.whole, gt.whole);
+                // ---- S as a pair ----
 #pragma unroll 1
                 for (int g = 0; g < kHalf; g += 32) {
                     uint32_t r[32], h[16], l[16];
                     tmem_ld32_async(col_s + g, r);
                     tmem_ld_wait(r);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const f2 x = pair_of(r, e);
-                        split(x, h[e], l[e]);
-                        float a, b;
-                        unpack2(mul2(x, whole), a, b);
-                        r[2 * e] = __float_as_uint(a);
-                        r[2 * e + 1] = __float_as_uint(b);
+                    for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
+                    if (g == 0 && c > 0) {   // P U of the chunk before has read U's pair, which lies there
+                        wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
+                        tc_fence_after();
                     }
                     tmem_st16(tm + kColPair + (half * kHalf + g) / 2, h);
                     tmem_st16(tm + kColPair + kHalf + (half * kHalf + g) / 2, l);
-                    tmem_st32(col_s + g, r);
                 }
                 hand_over(&sm.have_s);
+                // ---- S decayed, while S k and S q are formed ----
+                wait(&sm.gated[c % kGates], static_cast<uint32_t>(c / kGates) & 1u, patience);
+                const f2 whole = pack2(gt.whole, gt.whole);
+#pragma unroll 1
+                for (int g = 0; g < kHalf; g += 32) {
+                    uint32_t r[32];
+                    tmem_ld32_async(col_s + g, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float a, b;
+                        unpack2(mul2(pair_of(r, e), whole), a, b);
+                        r[2 * e] = __float_as_uint(a);
+                        r[2 * e + 1] = __float_as_uint(b);
+                    }
+                    tmem_st32(col_s + g, r);
+                }
+                // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
+                wait(&sm.done_ks, ph, patience);
+                tc_fence_after();
+                {
+                    uint32_t r[32], h[16], l[16];
+                    tmem_ld32_async(col_k, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
+                    tmem_st16(col_k, h);
+                    tmem_st16(col_k + 16, l);
+                }
+                hand_over(&sm.have_k);
+                if (Y) {   // scale e^b S q: P U adds to it
+                    wait(&sm.done_qs, ph, patience);
+                    tc_fence_after();
+                    uint32_t r[32];
+                    tmem_ld32_async(col_q, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float a, b;
+                        unpack2(mul2(load2(gt.eq + half * 32 + 2 * e), pair_of(r, e)), a, b);
+                        r[2 * e] = __float_as_uint(a);
+                        r[2 * e + 1] = __float_as_uint(b);
+                    }
+                    tmem_st32(col_q, r);
+                }
+                // ---- U decayed to the chunk's end, as a pair in U's place, for the update; then U's pair ----
+                wait(&sm.done_u, ph, patience);
+                tc_fence_after();
+                {
+                    uint32_t r[32], h[16], l[16];
+                    tmem_ld32_async(tm + kColPair + half * 32, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ec + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
+                    tmem_st16(tm + kColPair + half * 32, h);
+                    tmem_st16(tm + kColPair + half * 32 + 16, l);
+                    hand_over(&sm.have_d);
+                    if (Y) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
+                        tmem_st16(tm + kColPair + 64 + half * 32, h);
+                        tmem_st16(tm + kColPair + 64 + half * 32 + 16, l);
+                        hand_over(&sm.have_u);
+                    }
+                }
+            } else if (c > 0) {
+                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
+                tc_fence_after();
             }
             if (c > 0) {
-                // ---- y of the chunk before, tokens 32 half .. : into its stage, rows of 128 channels ----
+                // ---- y of the chunk before, tokens 32 half .. , while the update runs ----
                 if (Y) {
                     uint32_t r[32];
                     tmem_ld32_async(tm + kColQ + (buf ^ 1) * kPlace + half * 32, r);
                     tmem_ld_wait(r);
-                    uint8_t *to = sm.ring[(c - 1) % kStages];
+                    const int t0 = (c - 1) * kC + half * 32;
                     if (p.y_dtype == PRECOG_F32) {
+                        float *to = static_cast<float *>(p.y) + (begin + t0) * y_row + static_cast<int64_t>(head) * p.dv + ch;
+                        if (live) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) reinterpret_cast<uint32_t *>(to)[(half * 32 + e) * kM + row] = r[e];
-                    } else {
+                            for (int e = 0; e < 32; ++e, to += y_row)
+                                if (t0 + e < len) *to = __uint_as_float(r[e]);
+                        }
+                    } else {   // rows of 128 channels, for the copies
+                        uint16_t *to = reinterpret_cast<uint16_t *>(sm.v[(c - 1) % kStages]) + half * 32 * kM + row;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const uint32_t w = bits2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                            reinterpret_cast<uint16_t *>(to)[(half * 32 + 2 * e) * kM + row] = static_cast<uint16_t>(w);
-                            reinterpret_cast<uint16_t *>(to)[(half * 32 + 2 * e + 1) * kM + row] = static_cast<uint16_t>(w >> 16);
+                            to[2 * e * kM] = static_cast<uint16_t>(w);
+                            to[(2 * e + 1) * kM] = static_cast<uint16_t>(w >> 16);
                         }
+                        fence_proxy_async_smem();
                     }
-                    fence_proxy_async_smem();
                     tc_fence_before();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.through[(c - 1) % kStages]);
                 __syncwarp();
             }
-            if (c == chunks) break;
-            // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
-            wait(&sm.done_ks, ph, patience);
-            tc_fence_after();
-            {
-                uint32_t r[32], h[16], l[16];
-                tmem_ld32_async(col_k, r);
-                tmem_ld_wait(r);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
-                tmem_st16(col_k, h);
-                tmem_st16(col_k + 16, l);
-            }
-            hand_over(&sm.have_k);
-            if (Y) {   // scale e^b S q: P U adds to it
-                wait(&sm.done_qs, ph, patience);
+            if (c < chunks) {
+                wait(&sm.done_s, ph, patience);
                 tc_fence_after();
-                uint32_t r[32];
-                tmem_ld32_async(col_q, r);
-                tmem_ld_wait(r);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float a, b;
-                    unpack2(mul2(load2(gt.eq + half * 32 + 2 * e), pair_of(r, e)), a, b);
-                    r[2 * e] = __float_as_uint(a);
-                    r[2 * e + 1] = __float_as_uint(b);
-                }
-                tmem_st32(col_q, r);
             }
-            // ---- U: a pair for P U, and decayed to the chunk's end, in U's place, for the update ----
-            wait(&sm.done_u, ph, patience);
-            tc_fence_after();
-            {
-                uint32_t r[32], h[16], l[16];
-                tmem_ld32_async(tm + kColPair + half * 32, r);
-                tmem_ld_wait(r);
-                if (Y) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
-                    tmem_st16(tm + kColPair + 64 + half * 32, h);
-                    tmem_st16(tm + kColPair + 64 + half * 32 + 16, l);
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ec + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
-                tmem_st16(tm + kColPair + half * 32, h);
-                tmem_st16(tm + kColPair + half * 32 + 16, l);
-            }
-            hand_over(&sm.have_u);
-            wait(&sm.done_s, ph, patience);
-            tc_fence_after();
         }
         if (p.states) {
             const int64_t at = ((seq * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
