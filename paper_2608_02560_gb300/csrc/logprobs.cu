@@ -4,12 +4,21 @@
 // With z = x / temperature, m = max z, d_i = z_i - m:
 //   S = sum e^{d_i},  W = sum d_i e^{d_i}
 //   log p(token) = d_token - log S,   H = log S - W / S.
-// Every thread keeps (m, S, W) of what it has seen; when its maximum grows by c, S becomes
-// S e^-c and W becomes (W - c S) e^-c, and two threads' sums join the same way. The maximum
-// is tracked on x itself, and d is formed as (x - max x) / temperature: no product overflows
-// where the logits are the type's lowest value, and equal logits differ by exactly 0.
-// Exponentials below 2^-150 of the largest count as zero, -infinity among them.
-#include <climits>
+// Every thread keeps (max, S, W) of what it has seen; when its maximum grows by c, S becomes
+// S e^-c and W becomes (W - c S) e^-c, and two threads' sums join the same way. Exponentials below
+// 2^-150 of the largest count as zero, -infinity among them. d is one FMA, x c - max c; the rounding
+// of max c, the same in every term, is taken out of the result. Where max c itself leaves fp32's
+// range (rows of the type's lowest value) the row is summed again with d = (x - max) c.
+//
+// The best entries: each warp keeps its k best in its lanes, sorted, as keys (value, complement of
+// the index). A warp's first batch gives a bound that at least k entries reach (the k-th of its
+// lanes' maxima), so few entries are ever inserted: about k (1 + ln(n / 512 k)) of a warp's n.
+// Batches whose maximum does not reach the k-th entry cost one comparison.
+//
+// Memory bounds it, at 5 to 8 instructions an entry. A CTA takes a row; with few rows a cluster of
+// up to 8 shares one and joins over distributed shared memory.
+#include <cmath>
+#include <cstddef>
 
 #include "../../include/precog.h"
 #include "internal.h"
@@ -22,6 +31,9 @@ __device__ uint32_t g_logprob_status;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kFly = 4;               // 16-byte vectors of a batch a lane
+constexpr int kMaxParts = 8;          // CTAs of a row
+constexpr float kFar = 1e37f;         // maxima beyond it: max c may leave fp32's range
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kFloor = -150.f;      // exponents below it count as e^d = 0
@@ -70,60 +82,273 @@ __device__ __forceinline__ void insert(u64 &mine, u64 v, int lane) {
     mine = lane < at ? mine : lane == at ? v : up;
 }
 
+// What a CTA has found.
+struct Found {
+    Sums sums;
+    u64 best[32];
+};
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int kN = 4;
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { return __uint_as_float(r[i]); }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int kN = 8;
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
+        return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
+    }
+};
+template <> struct Vec<__half> {
+    static constexpr int kN = 8;
+    static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
+        return __half2float(__ushort_as_half(static_cast<unsigned short>(i % 2 ? r[i / 2] >> 16 : r[i / 2] & 0xffffu)));
+    }
+};
+
+// Descending over the lanes.
+__device__ __forceinline__ float sorted(float v, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int o = size / 2; o > 0; o /= 2) {
+            const float u = __shfl_xor_sync(0xffffffffu, v, o);
+            const bool first = (lane & o) == 0, down = (lane & size) == 0 || size == 32;
+            v = first == down ? fmaxf(u, v) : fminf(u, v);
+        }
+    return v;
+}
+
+// The k best entries of a warp.
+struct Best {
+    u64 mine = 0ull;              // entry `lane`, best first
+    float least = -INFINITY;     // the k-th entry's value once there are k, a bound before
+    bool full = false;
+    __device__ __forceinline__ void add(u64 key, int k, int lane) {
+        insert(mine, key, lane);
+        const u64 last = __shfl_sync(0xffffffffu, mine, k - 1);
+        if (last != 0ull) {
+            full = true;
+            least = value_of(last);
+        }
+    }
+    // Entries come in the order of their indices, so once there are k only larger ones enter.
+    __device__ __forceinline__ bool enters(float x) const { return full ? x > least : x >= least; }
+};
+
+// One entry a lane (`in`: there is one), in the order of the lanes.
+template <bool TOP>
+__device__ __forceinline__ void take_one(float x, uint32_t index, bool in, float c, int k, int lane, Sums &a, Best &b) {
+    if (in) {
+        if (x > a.mx) a = moved(a, x, c);
+        const float d = clamped(fmaf(x, c, -a.mx * c)), e = ex2(d);
+        a.s += e;
+        a.w = fmaf(d, e, a.w);
+    }
+    if constexpr (TOP) {
+        unsigned todo = __ballot_sync(0xffffffffu, in && b.enters(x));
+        while (todo) {
+            const int from = __ffs(static_cast<int>(todo)) - 1;
+            const float v = __shfl_sync(0xffffffffu, x, from);
+            if (b.enters(v)) b.add(key_of(v, __shfl_sync(0xffffffffu, index, from)), k, lane);
+            todo &= todo - 1;
+        }
+    }
+}
+
+// The sums of a row by one warp, d as a difference: for maxima near the ends of fp32's range.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p) {
-    __shared__ Sums warp_sums[kWarps];
-    __shared__ u64 lists[kWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row = blockIdx.x;
-    const T *x = static_cast<const T *>(p.logits) + row * p.stride;
-    const float c = p.inv_temp * kLog2e;
-    const int vocab = static_cast<int>(p.vocab);
+__device__ __noinline__ Sums sums_far(const T *x, int vocab, float c, int lane) {
     Sums a{kLowest, 0.f, 0.f};
-    u64 mine = 0ull, least = 0ull;     // the warp's list and its k-th entry
-    for (int i0 = warp * 32; i0 < vocab; i0 += kThreads) {
-        const int i = i0 + lane;
-        const bool in = i < vocab;
-        const float v = in ? to_f32(x[i]) : -__int_as_float(0x7f800000);
+    for (int i = lane; i < vocab; i += 32) {
+        const float v = to_f32(x[i]);
         if (v > a.mx) a = moved(a, v, c);
         const float d = clamped((v - a.mx) * c), e = ex2(d);
         a.s += e;
         a.w = fmaf(d, e, a.w);
-        if (p.k > 0) {
-            const u64 key = in ? key_of(v, static_cast<uint32_t>(i)) : 0ull;
-            unsigned todo = __ballot_sync(0xffffffffu, key > least);
-            while (todo) {
-                const int from = __ffs(static_cast<int>(todo)) - 1;
-                todo &= todo - 1;
-                const u64 one = __shfl_sync(0xffffffffu, key, from);
-                if (one > least) {
-                    insert(mine, one, lane);
-                    least = __shfl_sync(0xffffffffu, mine, p.k - 1);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        a = joined(a, Sums{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.w, o)}, c);
+    return a;
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p, int parts) {
+    using V = Vec<T>;
+    constexpr int N = V::kN;
+    __shared__ Found found[kWarps + 1];            // of the warps, then the CTA's
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row = blockIdx.x / parts;
+    const int part = static_cast<int>(blockIdx.x % parts);
+    const T *x = static_cast<const T *>(p.logits) + row * p.stride;
+    const float c = p.inv_temp * kLog2e;
+    const int vocab = static_cast<int>(p.vocab), k = p.k;
+    // entries before the row's first 16-byte boundary, whole vectors, entries after the last
+    const int past = static_cast<int>(reinterpret_cast<uintptr_t>(x) & 15u) / static_cast<int>(sizeof(T));
+    const int head = past == 0 ? 0 : N - past < vocab ? N - past : vocab;
+    const int vecs = (vocab - head) / N, tail = vocab - head - vecs * N;
+    const uint4 *xv = reinterpret_cast<const uint4 *>(x + head);
+    const int gw = part * kWarps + warp, warps = parts * kWarps;
+
+    Sums a{-kFar, 0.f, 0.f};
+    float nmc = kFar * c;                          // -max c
+    f2 s2 = pack2(0.f, 0.f), w2 = s2;
+    Best b;
+    if (gw == 0 && head > 0) {
+        take_one<TOP>(lane < head ? to_f32(x[lane < head ? lane : 0]) : 0.f, lane, lane < head, c, k, lane, a, b);
+        nmc = -a.mx * c;
+    }
+    const f2 cc = pack2(c, c);
+    bool first = true;
+#pragma unroll 1
+    for (int v0 = gw * 32; v0 < vecs; v0 += warps * 32 * kFly) {
+        uint32_t r[kFly][4];
+        float top[kFly];
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            const int v = v0 + u * warps * 32 + lane;
+            uint4 q = make_uint4(0u, 0u, 0u, 0u);
+            if (v < vecs) q = __ldcs(xv + v);
+            r[u][0] = q.x, r[u][1] = q.y, r[u][2] = q.z, r[u][3] = q.w;
+        }
+        float most = -__int_as_float(0x7f800000);
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            top[u] = -__int_as_float(0x7f800000);
+            if (v0 + u * warps * 32 + lane < vecs) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) top[u] = fmaxf(top[u], V::get(r[u], i));
+            }
+            most = fmaxf(most, top[u]);
+        }
+        if (most > a.mx) {
+            const float d = clamped((a.mx - most) * c), f = ex2(d);
+            w2 = mul2(fma2(pack2(d, d), s2, w2), pack2(f, f));
+            s2 = mul2(s2, pack2(f, f));
+            const Sums m = moved(a, most, c);
+            a = m;
+            nmc = -most * c;
+        }
+        const f2 nm = pack2(nmc, nmc);
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            if (v0 + u * warps * 32 + lane < vecs) {
+#pragma unroll
+                for (int i = 0; i < N; i += 2) {
+                    float d0, d1;
+                    unpack2(fma2(pack2(V::get(r[u], i), V::get(r[u], i + 1)), cc, nm), d0, d1);
+                    d0 = clamped(d0), d1 = clamped(d1);
+                    const f2 e = pack2(ex2(d0), ex2(d1));
+                    s2 = fma2(e, pack2(1.f, 1.f), s2);
+                    w2 = fma2(pack2(d0, d1), e, w2);
+                }
+            }
+        }
+        if constexpr (TOP) {
+            if (first) {   // k lanes hold an entry as large as the k-th of the lanes' maxima
+                const float bound = __shfl_sync(0xffffffffu, sorted(most, lane), k - 1);
+                if (!b.full && bound > b.least) b.least = bound;
+                first = false;
+            }
+            if (__any_sync(0xffffffffu, b.enters(most))) {
+#pragma unroll
+                for (int u = 0; u < kFly; ++u) {
+                    const int v = v0 + u * warps * 32 + lane;
+                    unsigned left = 0u;      // this lane's entries that may enter
+                    if (v < vecs && b.enters(top[u])) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) left |= b.enters(V::get(r[u], i)) ? 1u << i : 0u;
+                    }
+                    unsigned todo;
+                    while ((todo = __ballot_sync(0xffffffffu, left != 0u)) != 0u) {
+                        const int from = __ffs(static_cast<int>(todo)) - 1;
+                        const int at = __ffs(static_cast<int>(left)) - 1;
+                        float mine = 0.f;
+#pragma unroll
+                        for (int i = 0; i < N; ++i) mine = at == i ? V::get(r[u], i) : mine;
+                        const float value = __shfl_sync(0xffffffffu, mine, from);
+                        const int index = __shfl_sync(0xffffffffu, head + v * N + at, from);
+                        b.add(key_of(value, static_cast<uint32_t>(index)), k, lane);
+                        if (lane == from) left &= left - 1u;
+                        if (b.full && left != 0u) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+                                if (!(V::get(r[u], i) > b.least)) left &= ~(1u << i);
+                        }
+                    }
                 }
             }
         }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Sums b{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o),
-                     __shfl_xor_sync(0xffffffffu, a.w, o)};
-        a = joined(a, b, c);
+    {
+        float lo, hi;
+        unpack2(s2, lo, hi);
+        a.s += lo + hi;
+        unpack2(w2, lo, hi);
+        a.w += lo + hi;
     }
-    if (lane == 0) warp_sums[warp] = a;
-    lists[warp][lane] = mine;
+    if (gw == warps - 1 && tail > 0) {
+        const int i = head + vecs * N + lane;
+        take_one<TOP>(lane < tail ? to_f32(x[lane < tail ? i : 0]) : 0.f, i, lane < tail, c, k, lane, a, b);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        a = joined(a, Sums{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.w, o)}, c);
+    if (lane == 0) found[warp].sums = a;
+    if (TOP) found[warp].best[lane] = b.mine;
     __syncthreads();
-    if (warp != 0) return;
-    a = warp_sums[0];
-    for (int w = 1; w < kWarps; ++w) a = joined(a, warp_sums[w], c);
+    // ---- join the warps, then the row's CTAs ----
+    auto join = [&](const Sums &sums, auto entry) {
+        a = joined(a, sums, c);
+        if constexpr (TOP) {
+            u64 last = __shfl_sync(0xffffffffu, b.mine, k - 1);
+            for (int j = 0; j < k; ++j) {
+                const u64 one = entry(j);
+                if (one <= last) break;                    // sorted: nothing better follows
+                insert(b.mine, one, lane);
+                last = __shfl_sync(0xffffffffu, b.mine, k - 1);
+            }
+        }
+    };
+    if (warp == 0) {
+        for (int w = 1; w < kWarps; ++w) join(found[w].sums, [&](int j) { return found[w].best[j]; });
+        if (lane == 0) found[kWarps].sums = a;
+        if (TOP) found[kWarps].best[lane] = b.mine;
+    }
+    if (parts > 1) {
+        cluster_sync_all();
+        if (warp == 0 && part == 0)
+            for (int o = 1; o < parts; ++o) {
+                const uint32_t other = mapa_shared(&found[kWarps], static_cast<uint32_t>(o));
+                const Sums sums{__uint_as_float(ld_cluster_u32(other)), __uint_as_float(ld_cluster_u32(other + 4)),
+                                __uint_as_float(ld_cluster_u32(other + 8))};
+                // lane j reads entry j: one trip to the other CTA
+                u64 its = 0ull;
+                if constexpr (TOP) {
+                    const uint32_t at = other + static_cast<uint32_t>(offsetof(Found, best)) + 8u * lane;
+                    its = static_cast<u64>(ld_cluster_u32(at)) | static_cast<u64>(ld_cluster_u32(at + 4)) << 32;
+                }
+                join(sums, [&](int j) { return __shfl_sync(0xffffffffu, its, j); });
+            }
+        cluster_sync_all();   // the others' shared memory has been read
+    }
+    if (warp != 0 || part != 0) return;
+    const bool near = fabsf(a.mx) < kFar && fabsf(a.mx * c) < kFar;
+    if (!near) a = sums_far(x, vocab, c, lane);
     const float nan = __int_as_float(0x7fffffff);
     const float log_s = log2f(a.s);                        // NaN where the row holds one
     const bool empty = a.s == 0.f;
+    auto log_p = [&](float v) {
+        // (the sums' d was off by the rounding of max c, the same in each)
+        const float off = near ? fmaf(a.mx, c, -a.mx * c) : 0.f;
+        return empty ? nan : (v - a.mx) * p.inv_temp - (log_s - off) * kLn2;
+    };
     if (lane == 0) {
         const int64_t token = p.tokens[row];
         float lp = 0.f;
         if (token >= 0 && token < p.vocab) {
-            const float v = to_f32(x[token]);
-            lp = empty ? nan : (v - a.mx) * p.inv_temp - log_s * kLn2;
+            lp = log_p(to_f32(x[token]));
         } else if (token != -1) {
             atomicOr(&g_logprob_status, PRECOG_DEV_BAD_INDEX);
             lp = nan;
@@ -131,28 +356,38 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
         p.logprob[row] = lp;
         if (p.entropy) p.entropy[row] = empty ? nan : (log_s - a.w / a.s) * kLn2;
     }
-    if (p.k > 0) {
-        for (int w = 1; w < kWarps; ++w)
-            for (int j = 0; j < p.k; ++j) {
-                const u64 one = lists[w][j];
-                if (one <= least) break;                   // sorted: nothing better follows
-                insert(mine, one, lane);
-                least = __shfl_sync(0xffffffffu, mine, p.k - 1);
-            }
-        if (lane < p.k) {
-            const bool some = mine != 0ull;
-            p.top_idx[row * p.k + lane] = some ? static_cast<int64_t>(0xffffffffu - static_cast<uint32_t>(mine)) : -1;
-            p.top_logprob[row * p.k + lane] = some && !empty ? (value_of(mine) - a.mx) * p.inv_temp - log_s * kLn2 : nan;
-        }
+    if (TOP && lane < k) {
+        const bool some = b.mine != 0ull;
+        p.top_idx[row * k + lane] = some ? static_cast<int64_t>(0xffffffffu - static_cast<uint32_t>(b.mine)) : -1;
+        p.top_logprob[row * k + lane] = some ? log_p(value_of(b.mine)) : nan;
     }
+}
+
+template <typename T, bool TOP>
+cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
+    // One CTA a row, unless that leaves SMs idle and the row is long enough to be shared: parts of
+    // at least 4096 entries.
+    int parts = 1;
+    while (parts < kMaxParts && p.rows * parts * 2 <= device_sm_count() && p.vocab >= 4096LL * parts * 2) parts *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.rows * parts));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP>, p, parts);
+    if (e == cudaSuccess) count_launches(1);
+    return e;
 }
 
 template <typename T>
 cudaError_t launch_typed(const LogprobParams &p, cudaStream_t stream) {
-    logprobs_kernel<T><<<static_cast<unsigned>(p.rows), kThreads, 0, stream>>>(p);
-    cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) count_launches(1);
-    return e;
+    return p.k > 0 ? launch_parts<T, true>(p, stream) : launch_parts<T, false>(p, stream);
 }
 
 }  // namespace

@@ -2,8 +2,13 @@
 //
 //   n = rsqrt(sum x^2 [/ dim] + eps) ;  x <- x n w ;  (a, b) <- (a cos - b sin, b cos + a sin)
 //
-// A vector of `dim` numbers belongs to a group of G lanes; both partners of a rotated pair are
-// read and written by one lane, so outputs may be the inputs.
+// A vector of `dim` numbers belongs to a group of G lanes (the least power of two that leaves a
+// lane at most 8 numbers), its sum of squares to log2(G) shuffles. A lane's 8 numbers are two
+// quads chosen so that both partners of every rotated pair are its own: eight neighbours where
+// pairs are neighbours, else four of the lower half and the same four of the upper one; outputs
+// may therefore be the inputs. A group keeps its token's rotations and the weights in registers
+// and takes kHeads heads, kFly of them in flight. What bounds it is memory: each number is read
+// once and written once.
 #include "../../include/precog.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -14,6 +19,31 @@ namespace {
 __device__ uint32_t g_qk_status;
 
 constexpr int kThreads = 256;
+constexpr int kHeads = 8, kFly = 4;
+
+__device__ __forceinline__ void load_quad(const float *p, float (&v)[4]) {
+    const float4 r = *reinterpret_cast<const float4 *>(p);
+    v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
+}
+__device__ __forceinline__ void load_quad(const __nv_bfloat16 *p, float (&v)[4]) {
+    const uint2 r = *reinterpret_cast<const uint2 *>(p);
+    v[0] = __uint_as_float(r.x << 16), v[1] = __uint_as_float(r.x & 0xffff0000u);
+    v[2] = __uint_as_float(r.y << 16), v[3] = __uint_as_float(r.y & 0xffff0000u);
+}
+__device__ __forceinline__ void load_quad(const __half *p, float (&v)[4]) {
+    const uint2 r = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&r.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&r.y));
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+__device__ __forceinline__ void store_quad(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store_quad(__nv_bfloat16 *p, const float (&v)[4]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+__device__ __forceinline__ void store_quad(__half *p, const float (&v)[4]) {
+    const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -22,9 +52,98 @@ __device__ __forceinline__ void from_f(float *p, float v) { *p = v; }
 __device__ __forceinline__ void from_f(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_f(__half *p, float v) { *p = __float2half_rn(v); }
 
-// One vector a group of G lanes, every entry alone: any rot_dim. Lane l has entries l, l + G, ...
+// `per` heads of a token a group (`parts` groups a token).
+// HALF: pair i is (i, i + rot / 2) with rot / 2 a multiple of 4; else (2 i, 2 i + 1).
+template <typename T, int G, bool HALF, bool WEIGHT>
+__global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p, int parts, int per, int64_t items) {
+    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
+    const int lane = threadIdx.x % G;
+    if (item >= items) return;   // whole groups: the shuffles below stay within one
+    const unsigned mask = G == 32 ? 0xffffffffu : ((1u << G) - 1u) << ((threadIdx.x & 31) / G * G);
+    const int64_t t = item / parts;
+    const int all = p.heads[0] + p.heads[1];
+    const int h0 = static_cast<int>(item % parts) * per, h1 = h0 + per < all ? h0 + per : all;
+    const int64_t pos = p.rot == 0 ? 0 : p.positions ? p.positions[t] : t;
+    if (p.rot != 0 && (pos < 0 || pos >= p.n_positions)) {
+        if (lane == 0) atomicOr(&g_qk_status, PRECOG_DEV_BAD_INDEX);
+        return;
+    }
+    // this lane's quads
+    const int pairs = HALF ? p.rot / 8 : 0;
+    const int e0 = HALF && lane < pairs ? 4 * lane : HALF ? p.rot + 8 * (lane - pairs) : 8 * lane;
+    const int e1 = HALF && lane < pairs ? p.rot / 2 + 4 * lane : e0 + 4;
+    const bool live = 8 * lane < p.dim;
+    float cs[4], sn[4];          // of the lane's four pairs; 1 and 0 where nothing turns
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int pair = HALF ? (lane < pairs ? 4 * lane + i : p.rot) : 4 * lane + i;
+        const bool turn = live && pair < p.rot / 2;
+        cs[i] = turn ? p.cos[pos * (p.rot / 2) + pair] : 1.f;
+        sn[i] = turn ? p.sin[pos * (p.rot / 2) + pair] : 0.f;
+    }
+    float w[WEIGHT ? 2 : 1][8];
+    if constexpr (WEIGHT) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[k][i] = live && p.weight[k] ? p.weight[k][(i < 4 ? e0 : e1 - 4) + i] : 1.f;
+    }
+    const float inv = p.norm == PRECOG_NORM_RMS ? 1.f / static_cast<float>(p.dim) : 1.f;
+#pragma unroll 1
+    for (int h = h0; h < h1; h += kFly) {
+        float x[kFly][8];
+        T *out[kFly];
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) {
+            const int which = h + f >= p.heads[0], head = h + f - (which ? p.heads[0] : 0);
+            const T *in = static_cast<const T *>(p.in[which]) + t * p.in_stride[which] + static_cast<int64_t>(head) * p.dim;
+            out[f] = static_cast<T *>(p.out[which]) + t * p.out_stride[which] + static_cast<int64_t>(head) * p.dim;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[f][i] = 0.f;
+            if (live && h + f < h1) {
+                load_quad(in + e0, *reinterpret_cast<float(*)[4]>(&x[f][0]));
+                load_quad(in + e1, *reinterpret_cast<float(*)[4]>(&x[f][4]));
+            }
+        }
+        float n[kFly];
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) {
+            n[f] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n[f] = fmaf(x[f][i], x[f][i], n[f]);
+        }
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int f = 0; f < kFly; ++f) n[f] += __shfl_xor_sync(mask, n[f], o);
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) {
+            if (!live || h + f >= h1) continue;
+            const float m = p.norm == PRECOG_NORM_NONE ? 1.f : rsqrtf(fmaf(n[f], inv, p.eps));
+            const int which = h + f >= p.heads[0];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[f][i] *= m;
+            if constexpr (WEIGHT) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[f][i] *= which ? w[1][i] : w[0][i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float &a = x[f][HALF ? i : 2 * i], &b = x[f][HALF ? i + 4 : 2 * i + 1];
+                const float a0 = a;
+                a = a0 * cs[i] - b * sn[i];
+                b = b * cs[i] + a0 * sn[i];
+            }
+            store_quad(out[f] + e0, *reinterpret_cast<const float(*)[4]>(&x[f][0]));
+            store_quad(out[f] + e1, *reinterpret_cast<const float(*)[4]>(&x[f][4]));
+        }
+    }
+}
+
+// Every entry alone, for pairs (i, i + rot / 2) with rot / 2 not a multiple of 4: lane l of 16 has the
+// pairs l, l + 16, ...
 template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p, int64_t vectors) {
+__global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const QkNormParams p, int64_t vectors) {
     const int64_t vec = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
     const int lane = threadIdx.x % G;
     const int heads = p.heads[0] + p.heads[1];
@@ -59,13 +178,43 @@ __global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p,
     for (int i = p.rot + lane; i < p.dim; i += G) from_f(out + i, to_f(in[i]) * n * (w ? w[i] : 1.f));
 }
 
+template <typename T, int G, bool HALF, bool WEIGHT>
+cudaError_t launch_lanes(const QkNormParams &p, cudaStream_t stream) {
+    // Eight heads a group reuse its rotations and weights; where that leaves SMs without work (few
+    // tokens), a group takes as many as it has in flight, or one: 1 token of 24 heads 3.9 us in
+    // groups of 8, one each as written below.
+    const int all = p.heads[0] + p.heads[1];
+    int per = kHeads;
+    while (per > 1 && p.T * ((all + per - 1) / per) * G < static_cast<int64_t>(device_sm_count()) * kThreads * 2) per /= 2;
+    const int parts = (all + per - 1) / per;
+    const int64_t items = p.T * parts, blocks = (items * G + kThreads - 1) / kThreads;
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    qk_norm_kernel<T, G, HALF, WEIGHT><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, parts, per, items);
+    return cudaGetLastError();
+}
+
+template <typename T, int G>
+cudaError_t launch_group(const QkNormParams &p, cudaStream_t stream) {
+    const bool weight = p.weight[0] != nullptr || p.weight[1] != nullptr, half = p.rot != 0 && !p.interleaved;
+    if (half) return weight ? launch_lanes<T, G, true, true>(p, stream) : launch_lanes<T, G, true, false>(p, stream);
+    return weight ? launch_lanes<T, G, false, true>(p, stream) : launch_lanes<T, G, false, false>(p, stream);
+}
+
 template <typename T>
 cudaError_t launch_typed(const QkNormParams &p, cudaStream_t stream) {
-    const int64_t vectors = p.T * (static_cast<int64_t>(p.heads[0]) + p.heads[1]);
-    const int64_t blocks = (vectors * 16 + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    qk_norm_kernel<T, 16><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, vectors);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e;
+    if (p.rot != 0 && !p.interleaved && p.rot % 8 != 0) {
+        const int64_t vectors = p.T * (static_cast<int64_t>(p.heads[0]) + p.heads[1]), blocks = (vectors * 16 + kThreads - 1) / kThreads;
+        if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+        qk_norm_any_kernel<T, 16><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, vectors);
+        e = cudaGetLastError();
+    } else if (p.dim <= 64) {
+        e = launch_group<T, 8>(p, stream);
+    } else if (p.dim <= 128) {
+        e = launch_group<T, 16>(p, stream);
+    } else {
+        e = launch_group<T, 32>(p, stream);
+    }
     if (e == cudaSuccess) count_launches(1);
     return e;
 }
