@@ -198,14 +198,20 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is not None:
         return stream.cuda_stream
-    torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None or not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    if _raw_stream is None:
+        torch = _torch()
+        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        if raw is None or device is None or not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _raw_stream = lambda: raw(device())  # noqa: E731
+    return _raw_stream()
 
 
 def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInputs:
@@ -241,19 +247,20 @@ def _rows(t, what: str):
         return None, 0
     if not t.is_cuda:
         raise ValueError("tensors passed to libprecog must live on the GPU")
+    shape, strides = t.shape, t.stride()
     inner = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size > 1 and stride != inner:
+    for i in range(len(shape) - 1, 0, -1):
+        if strides[i] != inner and shape[i] > 1:
             raise ValueError(f"the rows of {what} must be contiguous")
-        inner *= size
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else inner)
+        inner *= shape[i]
+    return t.data_ptr(), (strides[0] if shape[0] > 1 else inner)
 
 
 def _of(t, dtype, shape, what: str):
     """The pointer of a contiguous GPU tensor of this dtype and shape (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     return _ptr(t)
 

@@ -12,8 +12,8 @@
 //
 // The best entries: each warp keeps its k best in its lanes, sorted, as keys (value, complement of
 // the index). A warp's first batch gives a bound that at least k entries reach (the k-th of its
-// lanes' maxima), so few entries are ever inserted: about k (1 + ln(n / 512 k)) of a warp's n.
-// Batches whose maximum does not reach the k-th entry cost one comparison.
+// lanes' maxima), and the CTA's warps share the largest of their k-th values, so few entries are
+// ever inserted. Batches whose maximum does not reach the bound cost one comparison.
 //
 // Memory bounds it, at 5 to 8 instructions an entry. A CTA takes a row; with few rows a cluster of
 // up to 8 shares one and joins over distributed shared memory.
@@ -92,17 +92,31 @@ template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kN = 4;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { return __uint_as_float(r[i]); }
+    // The largest entry; NaN is none.
+    static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
+        return fmaxf(fmaxf(get(r, 0), get(r, 1)), fmaxf(get(r, 2), get(r, 3)));
+    }
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kN = 8;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
     }
+    static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
+        auto two = [&](int i) { return *reinterpret_cast<const __nv_bfloat162 *>(&r[i]); };
+        const __nv_bfloat162 m = __hmax2(__hmax2(two(0), two(1)), __hmax2(two(2), two(3)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
 };
 template <> struct Vec<__half> {
     static constexpr int kN = 8;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __half2float(__ushort_as_half(static_cast<unsigned short>(i % 2 ? r[i / 2] >> 16 : r[i / 2] & 0xffffu)));
+    }
+    static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
+        auto two = [&](int i) { return *reinterpret_cast<const __half2 *>(&r[i]); };
+        const __half2 m = __hmax2(__hmax2(two(0), two(1)), __hmax2(two(2), two(3)));
+        return fmaxf(__low2float(m), __high2float(m));
     }
 };
 
@@ -119,10 +133,23 @@ __device__ __forceinline__ float sorted(float v, int lane) {
     return v;
 }
 
+// The 32 largest of two descending lists, descending; `reversed`: the second, last entry first. (The
+// larger of each pair makes a sequence that falls and rises, which five steps sort.)
+__device__ __forceinline__ u64 merged(u64 v, u64 reversed, int lane) {
+    v = v > reversed ? v : reversed;
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+        const u64 u = __shfl_xor_sync(0xffffffffu, v, o);
+        v = ((lane & o) == 0) == (u > v) ? u : v;
+    }
+    return v;
+}
+
 // The k best entries of a warp.
 struct Best {
-    u64 mine = 0ull;              // entry `lane`, best first
-    float least = -INFINITY;     // the k-th entry's value once there are k, a bound before
+    u64 mine = 0ull;             // entry `lane`, best first
+    float least = -INFINITY;     // the k-th entry's value once there are k
+    float bound = -INFINITY;     // k entries of the row reach it, here or with another warp
     bool full = false;
     __device__ __forceinline__ void add(u64 key, int k, int lane) {
         insert(mine, key, lane);
@@ -133,7 +160,7 @@ struct Best {
         }
     }
     // Entries come in the order of their indices, so once there are k only larger ones enter.
-    __device__ __forceinline__ bool enters(float x) const { return full ? x > least : x >= least; }
+    __device__ __forceinline__ bool enters(float x) const { return x >= bound && (!full || x > least); }
 };
 
 // One entry a lane (`in`: there is one), in the order of the lanes.
@@ -177,7 +204,8 @@ template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p, int parts) {
     using V = Vec<T>;
     constexpr int N = V::kN;
-    __shared__ Found found[kWarps + 1];            // of the warps, then the CTA's
+    __shared__ Found found[kWarps];                // of the warps; the first becomes the CTA's
+    __shared__ uint32_t shared_bound;              // the warps' largest k-th value, as ordered bits
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = blockIdx.x / parts;
     const int part = static_cast<int>(blockIdx.x % parts);
@@ -201,6 +229,10 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
     }
     const f2 cc = pack2(c, c);
     bool first = true;
+    if constexpr (TOP) {
+        if (threadIdx.x == 0) shared_bound = 0u;
+        __syncthreads();
+    }
 #pragma unroll 1
     for (int v0 = gw * 32; v0 < vecs; v0 += warps * 32 * kFly) {
         uint32_t r[kFly][4];
@@ -217,8 +249,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
         for (int u = 0; u < kFly; ++u) {
             top[u] = -__int_as_float(0x7f800000);
             if (v0 + u * warps * 32 + lane < vecs) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) top[u] = fmaxf(top[u], V::get(r[u], i));
+                top[u] = fmaxf(top[u], V::most(r[u]));
             }
             most = fmaxf(most, top[u]);
         }
@@ -246,9 +277,10 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
             }
         }
         if constexpr (TOP) {
+            const uint32_t others = *reinterpret_cast<volatile uint32_t *>(&shared_bound);
+            if (others != 0u) b.bound = fmaxf(b.bound, value_of(static_cast<u64>(others) << 32));
             if (first) {   // k lanes hold an entry as large as the k-th of the lanes' maxima
-                const float bound = __shfl_sync(0xffffffffu, sorted(most, lane), k - 1);
-                if (!b.full && bound > b.least) b.least = bound;
+                b.bound = fmaxf(b.bound, __shfl_sync(0xffffffffu, sorted(most, lane), k - 1));
                 first = false;
             }
             if (__any_sync(0xffffffffu, b.enters(most))) {
@@ -278,6 +310,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
                         }
                     }
                 }
+                if (b.full && lane == 0) atomicMax(&shared_bound, static_cast<uint32_t>(key_of(b.least, 0u) >> 32));
             }
         }
     }
@@ -295,42 +328,43 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         a = joined(a, Sums{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.w, o)}, c);
-    if (lane == 0) found[warp].sums = a;
-    if (TOP) found[warp].best[lane] = b.mine;
-    __syncthreads();
     // ---- join the warps, then the row's CTAs ----
-    auto join = [&](const Sums &sums, auto entry) {
-        a = joined(a, sums, c);
-        if constexpr (TOP) {
-            u64 last = __shfl_sync(0xffffffffu, b.mine, k - 1);
-            for (int j = 0; j < k; ++j) {
-                const u64 one = entry(j);
-                if (one <= last) break;                    // sorted: nothing better follows
-                insert(b.mine, one, lane);
-                last = __shfl_sync(0xffffffffu, b.mine, k - 1);
-            }
-        }
+    auto publish = [&] {
+        if (lane == 0) found[warp].sums = a;
+        if (TOP) found[warp].best[lane] = b.mine;
     };
-    if (warp == 0) {
-        for (int w = 1; w < kWarps; ++w) join(found[w].sums, [&](int j) { return found[w].best[j]; });
-        if (lane == 0) found[kWarps].sums = a;
-        if (TOP) found[kWarps].best[lane] = b.mine;
+    publish();
+    for (int o = kWarps / 2; o > 0; o /= 2) {
+        __syncthreads();
+        if (warp < o) {
+            a = joined(a, found[warp + o].sums, c);
+            if (TOP) b.mine = merged(b.mine, found[warp + o].best[31 - lane], lane);
+            publish();
+        }
     }
     if (parts > 1) {
         cluster_sync_all();
-        if (warp == 0 && part == 0)
-            for (int o = 1; o < parts; ++o) {
-                const uint32_t other = mapa_shared(&found[kWarps], static_cast<uint32_t>(o));
-                const Sums sums{__uint_as_float(ld_cluster_u32(other)), __uint_as_float(ld_cluster_u32(other + 4)),
-                                __uint_as_float(ld_cluster_u32(other + 8))};
-                // lane j reads entry j: one trip to the other CTA
-                u64 its = 0ull;
+        if (warp == 0 && part == 0) {
+            Sums sums[kMaxParts - 1];
+            u64 its[kMaxParts - 1];   // lane j reads the other's entry 31 - j
+#pragma unroll
+            for (int o = 1; o < kMaxParts; ++o) {
+                if (o >= parts) break;
+                const uint32_t other = mapa_shared(&found[0], static_cast<uint32_t>(o));
+                sums[o - 1] = Sums{__uint_as_float(ld_cluster_u32(other)), __uint_as_float(ld_cluster_u32(other + 4)),
+                                   __uint_as_float(ld_cluster_u32(other + 8))};
                 if constexpr (TOP) {
-                    const uint32_t at = other + static_cast<uint32_t>(offsetof(Found, best)) + 8u * lane;
-                    its = static_cast<u64>(ld_cluster_u32(at)) | static_cast<u64>(ld_cluster_u32(at + 4)) << 32;
+                    const uint32_t at = other + static_cast<uint32_t>(offsetof(Found, best)) + 8u * (31 - lane);
+                    its[o - 1] = static_cast<u64>(ld_cluster_u32(at)) | static_cast<u64>(ld_cluster_u32(at + 4)) << 32;
                 }
-                join(sums, [&](int j) { return __shfl_sync(0xffffffffu, its, j); });
             }
+#pragma unroll
+            for (int o = 1; o < kMaxParts; ++o) {
+                if (o >= parts) break;
+                a = joined(a, sums[o - 1], c);
+                if (TOP) b.mine = merged(b.mine, its[o - 1], lane);
+            }
+        }
         cluster_sync_all();   // the others' shared memory has been read
     }
     if (warp != 0 || part != 0) return;
@@ -365,10 +399,10 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
 
 template <typename T, bool TOP>
 cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
-    // One CTA a row, unless that leaves SMs idle and the row is long enough to be shared: parts of
-    // at least 4096 entries.
+    // One CTA a row, unless that leaves SMs with fewer than the four they hold and the row is long
+    // enough to be shared: parts of at least 4096 entries.
     int parts = 1;
-    while (parts < kMaxParts && p.rows * parts * 2 <= device_sm_count() && p.vocab >= 4096LL * parts * 2) parts *= 2;
+    while (parts < kMaxParts && p.rows * parts * 2 <= 4LL * device_sm_count() && p.vocab >= 4096LL * parts * 2) parts *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.rows * parts));
     cfg.blockDim = dim3(kThreads);

@@ -9,6 +9,8 @@
 // may therefore be the inputs. A group keeps its token's rotations and the weights in registers
 // and takes kHeads heads, kFly of them in flight. What bounds it is memory: each number is read
 // once and written once.
+#include <type_traits>
+
 #include "../../include/precog.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -21,30 +23,64 @@ __device__ uint32_t g_qk_status;
 constexpr int kThreads = 256;
 constexpr int kHeads = 8, kFly = 4;
 
-__device__ __forceinline__ void load_quad(const float *p, float (&v)[4]) {
-    const float4 r = *reinterpret_cast<const float4 *>(p);
-    v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
+// Eight numbers as they are stored: two quads, or one 16-byte (fp32: 32-byte) piece if they are
+// neighbours.
+template <typename T> struct Raw { uint2 q[2]; };
+template <> struct Raw<float> { uint4 q[2]; };
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_raw(const T *base, int e0, int e1, Raw<T> &r) {
+    if constexpr (WHOLE && sizeof(T) == 2) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(base + e0);
+        r.q[0] = make_uint2(v.x, v.y), r.q[1] = make_uint2(v.z, v.w);
+    } else {
+        using Q = std::remove_reference_t<decltype(r.q[0])>;
+        r.q[0] = *reinterpret_cast<const Q *>(base + e0), r.q[1] = *reinterpret_cast<const Q *>(base + e1);
+    }
 }
-__device__ __forceinline__ void load_quad(const __nv_bfloat16 *p, float (&v)[4]) {
-    const uint2 r = *reinterpret_cast<const uint2 *>(p);
-    v[0] = __uint_as_float(r.x << 16), v[1] = __uint_as_float(r.x & 0xffff0000u);
-    v[2] = __uint_as_float(r.y << 16), v[3] = __uint_as_float(r.y & 0xffff0000u);
+__device__ __forceinline__ void unpack(const Raw<float> &r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[4 * i] = __uint_as_float(r.q[i].x), v[4 * i + 1] = __uint_as_float(r.q[i].y);
+        v[4 * i + 2] = __uint_as_float(r.q[i].z), v[4 * i + 3] = __uint_as_float(r.q[i].w);
+    }
 }
-__device__ __forceinline__ void load_quad(const __half *p, float (&v)[4]) {
-    const uint2 r = *reinterpret_cast<const uint2 *>(p);
-    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&r.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&r.y));
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16> &r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[4 * i] = __uint_as_float(r.q[i].x << 16), v[4 * i + 1] = __uint_as_float(r.q[i].x & 0xffff0000u);
+        v[4 * i + 2] = __uint_as_float(r.q[i].y << 16), v[4 * i + 3] = __uint_as_float(r.q[i].y & 0xffff0000u);
+    }
 }
-__device__ __forceinline__ void store_quad(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
-__device__ __forceinline__ void store_quad(__nv_bfloat16 *p, const float (&v)[4]) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+__device__ __forceinline__ void unpack(const Raw<__half> &r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&r.q[i].x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&r.q[i].y));
+        v[4 * i] = a.x, v[4 * i + 1] = a.y, v[4 * i + 2] = b.x, v[4 * i + 3] = b.y;
+    }
 }
-__device__ __forceinline__ void store_quad(__half *p, const float (&v)[4]) {
-    const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+__device__ __forceinline__ uint32_t two(const __nv_bfloat16 *, float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
 }
-
+__device__ __forceinline__ uint32_t two(const __half *, float a, float b) {
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void store8(T *base, int e0, int e1, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4 *>(base + e0) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4 *>(base + e1) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        const uint2 a = make_uint2(two(base, v[0], v[1]), two(base, v[2], v[3])), b = make_uint2(two(base, v[4], v[5]), two(base, v[6], v[7]));
+        if constexpr (WHOLE) {
+            *reinterpret_cast<uint4 *>(base + e0) = make_uint4(a.x, a.y, b.x, b.y);
+        } else {
+            *reinterpret_cast<uint2 *>(base + e0) = a;
+            *reinterpret_cast<uint2 *>(base + e1) = b;
+        }
+    }
+}
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
@@ -52,17 +88,19 @@ __device__ __forceinline__ void from_f(float *p, float v) { *p = v; }
 __device__ __forceinline__ void from_f(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void from_f(__half *p, float v) { *p = __float2half_rn(v); }
 
-// `per` heads of a token a group (`parts` groups a token).
+// `per` heads of a token's q or k a group: `qparts` groups a token for q, `parts` in all.
 // HALF: pair i is (i, i + rot / 2) with rot / 2 a multiple of 4; else (2 i, 2 i + 1).
 template <typename T, int G, bool HALF, bool WEIGHT>
-__global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p, int parts, int per, int64_t items) {
+__global__ void __launch_bounds__(kThreads, 3) qk_norm_kernel(const QkNormParams p, int qparts, int parts, int per, int64_t items) {
     const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
     const int lane = threadIdx.x % G;
     if (item >= items) return;   // whole groups: the shuffles below stay within one
     const unsigned mask = G == 32 ? 0xffffffffu : ((1u << G) - 1u) << ((threadIdx.x & 31) / G * G);
     const int64_t t = item / parts;
-    const int all = p.heads[0] + p.heads[1];
-    const int h0 = static_cast<int>(item % parts) * per, h1 = h0 + per < all ? h0 + per : all;
+    int h0 = static_cast<int>(item - t * parts);
+    const int which = h0 >= qparts;
+    h0 = (h0 - (which ? qparts : 0)) * per;
+    const int h1 = h0 + per < p.heads[which] ? h0 + per : p.heads[which];
     const int64_t pos = p.rot == 0 ? 0 : p.positions ? p.positions[t] : t;
     if (p.rot != 0 && (pos < 0 || pos >= p.n_positions)) {
         if (lane == 0) atomicOr(&g_qk_status, PRECOG_DEV_BAD_INDEX);
@@ -70,9 +108,11 @@ __global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p,
     }
     // this lane's quads
     const int pairs = HALF ? p.rot / 8 : 0;
-    const int e0 = HALF && lane < pairs ? 4 * lane : HALF ? p.rot + 8 * (lane - pairs) : 8 * lane;
-    const int e1 = HALF && lane < pairs ? p.rot / 2 + 4 * lane : e0 + 4;
+    const int e0 = HALF && lane < pairs ? 4 * lane : 8 * lane;
+    const int e1 = HALF && lane < pairs ? p.rot / 2 + 4 * lane : 8 * lane + 4;
     const bool live = 8 * lane < p.dim;
+    const T *in = static_cast<const T *>(p.in[which]) + t * p.in_stride[which];
+    T *out = static_cast<T *>(p.out[which]) + t * p.out_stride[which];
     float cs[4], sn[4];          // of the lane's four pairs; 1 and 0 where nothing turns
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -81,36 +121,29 @@ __global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p,
         cs[i] = turn ? p.cos[pos * (p.rot / 2) + pair] : 1.f;
         sn[i] = turn ? p.sin[pos * (p.rot / 2) + pair] : 0.f;
     }
-    float w[WEIGHT ? 2 : 1][8];
+    float w[8];
     if constexpr (WEIGHT) {
+        const float *weight = p.weight[which];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[k][i] = live && p.weight[k] ? p.weight[k][(i < 4 ? e0 : e1 - 4) + i] : 1.f;
+        for (int i = 0; i < 8; ++i) w[i] = live && weight ? weight[(i < 4 ? e0 : e1 - 4) + i] : 1.f;
     }
     const float inv = p.norm == PRECOG_NORM_RMS ? 1.f / static_cast<float>(p.dim) : 1.f;
 #pragma unroll 1
     for (int h = h0; h < h1; h += kFly) {
-        float x[kFly][8];
-        T *out[kFly];
+        Raw<T> raw[kFly];
 #pragma unroll
         for (int f = 0; f < kFly; ++f) {
-            const int which = h + f >= p.heads[0], head = h + f - (which ? p.heads[0] : 0);
-            const T *in = static_cast<const T *>(p.in[which]) + t * p.in_stride[which] + static_cast<int64_t>(head) * p.dim;
-            out[f] = static_cast<T *>(p.out[which]) + t * p.out_stride[which] + static_cast<int64_t>(head) * p.dim;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[f][i] = 0.f;
-            if (live && h + f < h1) {
-                load_quad(in + e0, *reinterpret_cast<float(*)[4]>(&x[f][0]));
-                load_quad(in + e1, *reinterpret_cast<float(*)[4]>(&x[f][4]));
-            }
+            raw[f] = Raw<T>{};
+            if (live && h + f < h1) load_raw<!HALF>(in + static_cast<int64_t>(h + f) * p.dim, e0, e1, raw[f]);
         }
         float n[kFly];
 #pragma unroll
         for (int f = 0; f < kFly; ++f) {
+            float x[8];
+            unpack(raw[f], x);
             n[f] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) n[f] = fmaf(x[f][i], x[f][i], n[f]);
+            for (int i = 0; i < 8; ++i) n[f] = fmaf(x[i], x[i], n[f]);
         }
 #pragma unroll
         for (int o = G / 2; o > 0; o >>= 1)
@@ -120,22 +153,22 @@ __global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormParams p,
         for (int f = 0; f < kFly; ++f) {
             if (!live || h + f >= h1) continue;
             const float m = p.norm == PRECOG_NORM_NONE ? 1.f : rsqrtf(fmaf(n[f], inv, p.eps));
-            const int which = h + f >= p.heads[0];
+            float x[8];
+            unpack(raw[f], x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[f][i] *= m;
+            for (int i = 0; i < 8; ++i) x[i] *= m;
             if constexpr (WEIGHT) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[f][i] *= which ? w[1][i] : w[0][i];
+                for (int i = 0; i < 8; ++i) x[i] *= w[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float &a = x[f][HALF ? i : 2 * i], &b = x[f][HALF ? i + 4 : 2 * i + 1];
+                float &a = x[HALF ? i : 2 * i], &b = x[HALF ? i + 4 : 2 * i + 1];
                 const float a0 = a;
                 a = a0 * cs[i] - b * sn[i];
                 b = b * cs[i] + a0 * sn[i];
             }
-            store_quad(out[f] + e0, *reinterpret_cast<const float(*)[4]>(&x[f][0]));
-            store_quad(out[f] + e1, *reinterpret_cast<const float(*)[4]>(&x[f][4]));
+            store8<!HALF>(out + static_cast<int64_t>(h + f) * p.dim, e0, e1, x);
         }
     }
 }
@@ -180,16 +213,15 @@ __global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const QkNormParam
 
 template <typename T, int G, bool HALF, bool WEIGHT>
 cudaError_t launch_lanes(const QkNormParams &p, cudaStream_t stream) {
-    // Eight heads a group reuse its rotations and weights; where that leaves SMs without work (few
-    // tokens), a group takes as many as it has in flight, or one: 1 token of 24 heads 3.9 us in
-    // groups of 8, one each as written below.
-    const int all = p.heads[0] + p.heads[1];
+    // Eight heads a group reuse its rotations and weights; fewer where that would leave SMs with less
+    // than two CTAs.
     int per = kHeads;
-    while (per > 1 && p.T * ((all + per - 1) / per) * G < static_cast<int64_t>(device_sm_count()) * kThreads * 2) per /= 2;
-    const int parts = (all + per - 1) / per;
+    auto parts_of = [&](int heads) { return (heads + per - 1) / per; };
+    while (per > 1 && p.T * (parts_of(p.heads[0]) + parts_of(p.heads[1])) * G < 2LL * device_sm_count() * kThreads) per /= 2;
+    const int qparts = parts_of(p.heads[0]), parts = qparts + parts_of(p.heads[1]);
     const int64_t items = p.T * parts, blocks = (items * G + kThreads - 1) / kThreads;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    qk_norm_kernel<T, G, HALF, WEIGHT><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, parts, per, items);
+    qk_norm_kernel<T, G, HALF, WEIGHT><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, qparts, parts, per, items);
     return cudaGetLastError();
 }
 
