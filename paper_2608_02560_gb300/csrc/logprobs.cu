@@ -29,8 +29,6 @@ namespace {
 
 __device__ uint32_t g_logprob_status;
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kFly = 4;               // 16-byte vectors of a batch a lane
 constexpr int kMaxParts = 8;          // CTAs of a row
 constexpr float kFar = 1e37f;         // maxima beyond it: max c may leave fp32's range
@@ -88,6 +86,11 @@ struct Found {
     u64 best[32];
 };
 
+__device__ __forceinline__ uint32_t word(const uint32_t (&r)[4], int i) {
+    const uint32_t a = i & 1 ? r[1] : r[0], b = i & 1 ? r[3] : r[2];
+    return i & 2 ? b : a;
+}
+
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kN = 4;
@@ -96,6 +99,14 @@ template <> struct Vec<float> {
     static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
         return fmaxf(fmaxf(get(r, 0), get(r, 1)), fmaxf(get(r, 2), get(r, 3)));
     }
+    // Bit i: entry i is above thr, or (not `strict`) equals it.
+    static __device__ __forceinline__ unsigned reach(const uint32_t (&r)[4], float thr, bool strict) {
+        unsigned m = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m |= get(r, i) > thr || (!strict && get(r, i) == thr) ? 1u << i : 0u;
+        return m;
+    }
+    static __device__ __forceinline__ float at(const uint32_t (&r)[4], int i) { return __uint_as_float(word(r, i)); }
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kN = 8;
@@ -107,6 +118,19 @@ template <> struct Vec<__nv_bfloat16> {
         const __nv_bfloat162 m = __hmax2(__hmax2(two(0), two(1)), __hmax2(two(2), two(3)));
         return fmaxf(__low2float(m), __high2float(m));
     }
+    static __device__ __forceinline__ unsigned reach(const uint32_t (&r)[4], float thr, bool strict) {
+        const __nv_bfloat162 t = __float2bfloat162_rn(thr);   // (an entry's value: exact)
+        unsigned m = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 w = *reinterpret_cast<const __nv_bfloat162 *>(&r[i]);
+            m |= ((strict ? __hgt2_mask(w, t) : __hge2_mask(w, t)) & 0x00020001u) << (2 * i);
+        }
+        return (m | m >> 16) & 0xffu;
+    }
+    static __device__ __forceinline__ float at(const uint32_t (&r)[4], int i) {
+        return __uint_as_float(i % 2 ? word(r, i / 2) & 0xffff0000u : word(r, i / 2) << 16);
+    }
 };
 template <> struct Vec<__half> {
     static constexpr int kN = 8;
@@ -117,6 +141,19 @@ template <> struct Vec<__half> {
         auto two = [&](int i) { return *reinterpret_cast<const __half2 *>(&r[i]); };
         const __half2 m = __hmax2(__hmax2(two(0), two(1)), __hmax2(two(2), two(3)));
         return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ unsigned reach(const uint32_t (&r)[4], float thr, bool strict) {
+        const __half2 t = __float2half2_rn(thr);
+        unsigned m = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 w = *reinterpret_cast<const __half2 *>(&r[i]);
+            m |= ((strict ? __hgt2_mask(w, t) : __hge2_mask(w, t)) & 0x00020001u) << (2 * i);
+        }
+        return (m | m >> 16) & 0xffu;
+    }
+    static __device__ __forceinline__ float at(const uint32_t (&r)[4], int i) {
+        return __half2float(__ushort_as_half(static_cast<unsigned short>(word(r, i / 2) >> (i % 2 * 16))));
     }
 };
 
@@ -145,22 +182,21 @@ __device__ __forceinline__ u64 merged(u64 v, u64 reversed, int lane) {
     return v;
 }
 
-// The k best entries of a warp.
+// The k best entries of a warp. Entries come in the order of their indices: once the warp has k, only
+// ones above the k-th enter; those of a bound that others found may also equal it.
 struct Best {
     u64 mine = 0ull;             // entry `lane`, best first
-    float least = -INFINITY;     // the k-th entry's value once there are k
-    float bound = -INFINITY;     // k entries of the row reach it, here or with another warp
-    bool full = false;
+    float thr = -INFINITY;
+    bool strict = false;
+    __device__ __forceinline__ bool enters(float x) const { return x > thr || (!strict && x == thr); }
+    __device__ __forceinline__ void bound(float v) {
+        if (v > thr) thr = v, strict = false;
+    }
     __device__ __forceinline__ void add(u64 key, int k, int lane) {
         insert(mine, key, lane);
         const u64 last = __shfl_sync(0xffffffffu, mine, k - 1);
-        if (last != 0ull) {
-            full = true;
-            least = value_of(last);
-        }
+        if (last != 0ull && value_of(last) >= thr) thr = value_of(last), strict = true;
     }
-    // Entries come in the order of their indices, so once there are k only larger ones enter.
-    __device__ __forceinline__ bool enters(float x) const { return x >= bound && (!full || x > least); }
 };
 
 // One entry a lane (`in`: there is one), in the order of the lanes.
@@ -200,8 +236,8 @@ __device__ __noinline__ Sums sums_far(const T *x, int vocab, float c, int lane) 
     return a;
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p, int parts) {
+template <typename T, bool TOP, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobParams p, int parts) {
     using V = Vec<T>;
     constexpr int N = V::kN;
     __shared__ Found found[kWarps];                // of the warps; the first becomes the CTA's
@@ -278,39 +314,29 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
         }
         if constexpr (TOP) {
             const uint32_t others = *reinterpret_cast<volatile uint32_t *>(&shared_bound);
-            if (others != 0u) b.bound = fmaxf(b.bound, value_of(static_cast<u64>(others) << 32));
+            if (others != 0u) b.bound(value_of(static_cast<u64>(others) << 32));
             if (first) {   // k lanes hold an entry as large as the k-th of the lanes' maxima
-                b.bound = fmaxf(b.bound, __shfl_sync(0xffffffffu, sorted(most, lane), k - 1));
+                b.bound(__shfl_sync(0xffffffffu, sorted(most, lane), k - 1));
                 first = false;
             }
             if (__any_sync(0xffffffffu, b.enters(most))) {
 #pragma unroll
                 for (int u = 0; u < kFly; ++u) {
                     const int v = v0 + u * warps * 32 + lane;
-                    unsigned left = 0u;      // this lane's entries that may enter
-                    if (v < vecs && b.enters(top[u])) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) left |= b.enters(V::get(r[u], i)) ? 1u << i : 0u;
-                    }
+                    if (!__any_sync(0xffffffffu, b.enters(top[u]))) continue;
+                    unsigned left = v < vecs ? V::reach(r[u], b.thr, b.strict) : 0u;   // this lane's entries that may enter
                     unsigned todo;
                     while ((todo = __ballot_sync(0xffffffffu, left != 0u)) != 0u) {
                         const int from = __ffs(static_cast<int>(todo)) - 1;
                         const int at = __ffs(static_cast<int>(left)) - 1;
-                        float mine = 0.f;
-#pragma unroll
-                        for (int i = 0; i < N; ++i) mine = at == i ? V::get(r[u], i) : mine;
-                        const float value = __shfl_sync(0xffffffffu, mine, from);
+                        const float value = __shfl_sync(0xffffffffu, V::at(r[u], at), from);
                         const int index = __shfl_sync(0xffffffffu, head + v * N + at, from);
                         b.add(key_of(value, static_cast<uint32_t>(index)), k, lane);
                         if (lane == from) left &= left - 1u;
-                        if (b.full && left != 0u) {
-#pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (!(V::get(r[u], i) > b.least)) left &= ~(1u << i);
-                        }
+                        if (b.strict) left &= V::reach(r[u], b.thr, true);
                     }
                 }
-                if (b.full && lane == 0) atomicMax(&shared_bound, static_cast<uint32_t>(key_of(b.least, 0u) >> 32));
+                if (b.strict && lane == 0) atomicMax(&shared_bound, static_cast<uint32_t>(key_of(b.thr, 0u) >> 32));
             }
         }
     }
@@ -397,15 +423,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams 
     }
 }
 
-template <typename T, bool TOP>
-cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
-    // One CTA a row, unless that leaves SMs with fewer than the four they hold and the row is long
-    // enough to be shared: parts of at least 4096 entries.
-    int parts = 1;
-    while (parts < kMaxParts && p.rows * parts * 2 <= 4LL * device_sm_count() && p.vocab >= 4096LL * parts * 2) parts *= 2;
+template <typename T, bool TOP, int kWarps>
+cudaError_t launch_warps(const LogprobParams &p, int parts, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.rows * parts));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(kWarps * 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -414,9 +436,22 @@ cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = parts > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP>, p, parts);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, logprobs_kernel<T, TOP, kWarps>, p, parts);
     if (e == cudaSuccess) count_launches(1);
     return e;
+}
+
+template <typename T, bool TOP>
+cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
+    // Each warp pays for its own first entries, so a row gets only the warps that keep an SM's loads
+    // in flight: two where there are rows for 24 warps an SM, else four or eight. With fewer rows than
+    // fill the SMs and rows long enough to be shared, up to eight CTAs a row: parts of at least 4096.
+    const int64_t sms = device_sm_count();
+    if (p.rows >= 12 * sms) return launch_warps<T, TOP, 2>(p, 1, stream);
+    if (p.rows >= 6 * sms) return launch_warps<T, TOP, 4>(p, 1, stream);
+    int parts = 1;
+    while (parts < kMaxParts && p.rows * parts * 2 <= 4 * sms && p.vocab >= 4096LL * parts * 2) parts *= 2;
+    return launch_warps<T, TOP, 8>(p, parts, stream);
 }
 
 template <typename T>
