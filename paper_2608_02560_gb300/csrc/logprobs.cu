@@ -11,8 +11,8 @@
 // range (rows of the type's lowest value) the row is summed again with d = (x - max) c.
 //
 // The best entries: each warp keeps its k best in its lanes, sorted, as keys (value, complement of
-// the index). A warp's first batch gives a bound that at least k entries reach (the k-th of its
-// lanes' maxima), and the CTA's warps share the largest of their k-th values, so few entries are
+// the index). The CTA's first batches give a bound that at least k entries reach (the k-th of all
+// lanes' maxima), and later the warps share the largest of their k-th values, so few entries are
 // ever inserted. Batches whose maximum does not reach the bound cost one comparison.
 //
 // Memory bounds it, at 5 to 8 instructions an entry. A CTA takes a row; with few rows a cluster of
@@ -182,6 +182,17 @@ __device__ __forceinline__ u64 merged(u64 v, u64 reversed, int lane) {
     return v;
 }
 
+// The same of two lists of plain values.
+__device__ __forceinline__ float merged(float v, float reversed, int lane) {
+    v = fmaxf(v, reversed);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+        const float u = __shfl_xor_sync(0xffffffffu, v, o);
+        v = (lane & o) == 0 ? fmaxf(u, v) : fminf(u, v);
+    }
+    return v;
+}
+
 // The k best entries of a warp. Entries come in the order of their indices: once the warp has k, only
 // ones above the k-th enter; those of a bound that others found may also equal it.
 struct Best {
@@ -241,6 +252,7 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
     using V = Vec<T>;
     constexpr int N = V::kN;
     __shared__ Found found[kWarps];                // of the warps; the first becomes the CTA's
+    __shared__ float tops[kWarps][32];             // the lanes' maxima of the first batches, sorted
     __shared__ uint32_t shared_bound;              // the warps' largest k-th value, as ordered bits
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = blockIdx.x / parts;
@@ -265,12 +277,9 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
     }
     const f2 cc = pack2(c, c);
     bool first = true;
-    if constexpr (TOP) {
-        if (threadIdx.x == 0) shared_bound = 0u;
-        __syncthreads();
-    }
+    if (TOP && threadIdx.x == 0) shared_bound = 0u;
 #pragma unroll 1
-    for (int v0 = gw * 32; v0 < vecs; v0 += warps * 32 * kFly) {
+    for (int v0 = gw * 32; v0 < vecs || (TOP && first); v0 += warps * 32 * kFly) {
         uint32_t r[kFly][4];
         float top[kFly];
 #pragma unroll
@@ -313,11 +322,16 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
             }
         }
         if constexpr (TOP) {
-            const uint32_t others = *reinterpret_cast<volatile uint32_t *>(&shared_bound);
-            if (others != 0u) b.bound(value_of(static_cast<u64>(others) << 32));
-            if (first) {   // k lanes hold an entry as large as the k-th of the lanes' maxima
-                b.bound(__shfl_sync(0xffffffffu, sorted(most, lane), k - 1));
+            if (first) {   // k of the CTA's lanes hold an entry as large as the k-th of their maxima
                 first = false;
+                float v = sorted(most, lane);
+                tops[warp][lane] = v;
+                __syncthreads();   // every warp comes here once
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) v = merged(v, tops[(warp + w) % kWarps][31 - lane], lane);
+                b.bound(__shfl_sync(0xffffffffu, v, k - 1));
+            } else if (const uint32_t others = *reinterpret_cast<volatile uint32_t *>(&shared_bound); others != 0u) {
+                b.bound(value_of(static_cast<u64>(others) << 32));
             }
             if (__any_sync(0xffffffffu, b.enters(most))) {
 #pragma unroll
