@@ -30,6 +30,7 @@ namespace {
 __device__ uint32_t g_logprob_status;
 
 constexpr int kFly = 4;               // 16-byte vectors of a batch a lane
+constexpr int kStages = 3;            // batches of a warp in shared memory
 constexpr int kMaxParts = 8;          // CTAs of a row
 constexpr float kFar = 1e37f;         // maxima beyond it: max c may leave fp32's range
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -94,7 +95,10 @@ __device__ __forceinline__ uint32_t word(const uint32_t (&r)[4], int i) {
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kN = 4;
+    static constexpr bool kRaised = false;   // finite() keeps -infinity out
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { return __uint_as_float(r[i]); }
+    static __device__ __forceinline__ uint32_t lowest(float) { return 0u; }
+    static __device__ __forceinline__ f2 finite(const uint32_t (&r)[4], int i, uint32_t) { return pack2(get(r, i), get(r, i + 1)); }
     // The largest entry; NaN is none.
     static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
         return fmaxf(fmaxf(get(r, 0), get(r, 1)), fmaxf(get(r, 2), get(r, 3)));
@@ -110,8 +114,19 @@ template <> struct Vec<float> {
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kN = 8;
+    static constexpr bool kRaised = true;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
+    }
+    // Entries i, i + 1, not below `low` (two of the same): so that d is finite and d e^d no NaN.
+    static __device__ __forceinline__ f2 finite(const uint32_t (&r)[4], int i, uint32_t low) {
+        const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&r[i / 2]), *reinterpret_cast<const __nv_bfloat162 *>(&low));
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+        return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint32_t lowest(float v) {
+        const __nv_bfloat162 m = __float2bfloat162_rn(v);
+        return *reinterpret_cast<const uint32_t *>(&m);
     }
     static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
         auto two = [&](int i) { return *reinterpret_cast<const __nv_bfloat162 *>(&r[i]); };
@@ -134,8 +149,15 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<__half> {
     static constexpr int kN = 8;
+    static constexpr bool kRaised = false;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __half2float(__ushort_as_half(static_cast<unsigned short>(i % 2 ? r[i / 2] >> 16 : r[i / 2] & 0xffffu)));
+    }
+    // (no entry of fp16 is low enough at every temperature)
+    static __device__ __forceinline__ uint32_t lowest(float) { return 0u; }
+    static __device__ __forceinline__ f2 finite(const uint32_t (&r)[4], int i, uint32_t) {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&r[i / 2]));
+        return pack2(v.x, v.y);
     }
     static __device__ __forceinline__ float most(const uint32_t (&r)[4]) {
         auto two = [&](int i) { return *reinterpret_cast<const __half2 *>(&r[i]); };
@@ -267,8 +289,9 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
     const uint4 *xv = reinterpret_cast<const uint4 *>(x + head);
     const int gw = part * kWarps + warp, warps = parts * kWarps;
 
-    Sums a{-kFar, 0.f, 0.f};
-    float nmc = kFar * c;                          // -max c
+    const float far = kFar * fminf(1.f, 1.f / c);  // a maximum within it: |max c| < kFar
+    Sums a{-far, 0.f, 0.f};
+    float nmc = far * c;                           // -max c
     f2 s2 = pack2(0.f, 0.f), w2 = s2;
     Best b;
     if (gw == 0 && head > 0) {
@@ -276,23 +299,40 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
         nmc = -a.mx * c;
     }
     const f2 cc = pack2(c, c);
+    const uint32_t low = V::lowest(-2.f * far);    // below any maximum, and low c finite
     bool first = true;
+    // A lane copies its own vectors to shared memory, two batches ahead, and reads its own: registers
+    // held too few loads in flight (2048 x 50,257 bf16, 57 us).
+    extern __shared__ __align__(16) uint4 ring[];
+    uint4 *mine = ring + static_cast<size_t>(warp) * kStages * kFly * 32 + lane;
+    const int step = warps * 32 * kFly;
+    auto fetch = [&](int v0, int stage) {
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            const int v = v0 + u * warps * 32 + lane;
+            if (v < vecs) cp_async16(mine + (stage * kFly + u) * 32, xv + v);
+        }
+        cp_async_commit();
+    };
+    int stage = 0;
+    for (int i = 0; i < kStages - 1; ++i) fetch(gw * 32 + i * step, i);
     if (TOP && threadIdx.x == 0) shared_bound = 0u;
 #pragma unroll 1
-    for (int v0 = gw * 32; v0 < vecs || (TOP && first); v0 += warps * 32 * kFly) {
+    for (int v0 = gw * 32; v0 < vecs || (TOP && first); v0 += step) {
+        cp_async_wait<kStages - 2>();
+        fetch(v0 + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
         uint32_t r[kFly][4];
         float top[kFly];
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            const int v = v0 + u * warps * 32 + lane;
-            uint4 q = make_uint4(0u, 0u, 0u, 0u);
-            if (v < vecs) q = __ldcs(xv + v);
+            const uint4 q = mine[(stage * kFly + u) * 32];   // (past the end: whatever is there, not used)
             r[u][0] = q.x, r[u][1] = q.y, r[u][2] = q.z, r[u][3] = q.w;
         }
-        float most = -__int_as_float(0x7f800000);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            top[u] = -__int_as_float(0x7f800000);
+            top[u] = -INFINITY;
             if (v0 + u * warps * 32 + lane < vecs) {
                 top[u] = fmaxf(top[u], V::most(r[u]));
             }
@@ -313,8 +353,8 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
 #pragma unroll
                 for (int i = 0; i < N; i += 2) {
                     float d0, d1;
-                    unpack2(fma2(pack2(V::get(r[u], i), V::get(r[u], i + 1)), cc, nm), d0, d1);
-                    d0 = clamped(d0), d1 = clamped(d1);
+                    unpack2(fma2(V::finite(r[u], i, low), cc, nm), d0, d1);
+                    if constexpr (!V::kRaised) d0 = clamped(d0), d1 = clamped(d1);
                     const f2 e = pack2(ex2(d0), ex2(d1));
                     s2 = fma2(e, pack2(1.f, 1.f), s2);
                     w2 = fma2(pack2(d0, d1), e, w2);
@@ -408,7 +448,8 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
         cluster_sync_all();   // the others' shared memory has been read
     }
     if (warp != 0 || part != 0) return;
-    const bool near = fabsf(a.mx) < kFar && fabsf(a.mx * c) < kFar;
+    // (nor at temperatures where entries below -far would still count)
+    const bool near = fabsf(a.mx) < far && far * c > 1e3f;
     if (!near) a = sums_far(x, vocab, c, lane);
     const float nan = __int_as_float(0x7fffffff);
     const float log_s = log2f(a.s);                        // NaN where the row holds one
@@ -442,6 +483,9 @@ cudaError_t launch_warps(const LogprobParams &p, int parts, cudaStream_t stream)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.rows * parts));
     cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = static_cast<size_t>(kWarps) * kStages * kFly * 32 * 16;
+    const cudaError_t s = ensure_smem(reinterpret_cast<const void *>(logprobs_kernel<T, TOP, kWarps>), static_cast<int>(cfg.dynamicSmemBytes));
+    if (s != cudaSuccess) return s;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -96,6 +96,29 @@ def test_sorted_rows_and_ties(cuda_device):
     _compare(_run(cuda_device, x, tokens, 1.0, 32), ref, 32)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("temp", [1e-3, 30.0, 1e5, 1e36])
+def test_temperatures(cuda_device, dtype, temp):
+    """Rows with masked entries from nearly greedy to nearly uniform. Log probabilities scale with
+    1 / temperature, and with them the rounding of the logits' differences."""
+    import torch
+    gen = torch.Generator(device=cuda_device).manual_seed(17)
+    x = (2 * torch.randn((3, 3000), device=cuda_device, generator=gen)).to(getattr(torch, dtype))
+    x[:, ::3] = float("-inf")
+    x[1, 5] = torch.finfo(x.dtype).min
+    x[2, 7] = torch.finfo(x.dtype).min / 2
+    tokens = torch.tensor([1, 5, 7], device=cuda_device)
+    lp, H, idx, best = _run(cuda_device, x, tokens, temp, 8)
+    ref = oracle.token_logprobs(to_np(x), tokens.tolist(), temp, 8)
+    assert np.array_equal(idx.cpu().numpy(), ref[2])
+    for g, r in ((lp, ref[0]), (H, ref[1]), (best, ref[3])):
+        g = to_np(g)
+        r32 = np.where(np.abs(r) > 3.5e38, -np.inf, r)            # beyond fp32
+        assert np.array_equal(np.isinf(g), np.isinf(r32))
+        fine = np.isfinite(r32)
+        assert np.all(np.abs(g[fine] - r32[fine]) <= TOL + 4 * 2.0 ** -24 * np.abs(r32[fine]) * max(1.0, 20 / temp))
+
+
 def test_tokens_that_are_none_or_outside(cuda_device):
     import torch
     import paper_2608_02560_gb300 as pg
