@@ -95,7 +95,8 @@ __device__ __forceinline__ uint32_t word(const uint32_t (&r)[4], int i) {
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kN = 4;
-    static constexpr bool kRaised = false;   // finite() keeps -infinity out
+    static constexpr uint32_t kNone = 0xff800000u;   // -infinity
+    static constexpr bool kRaised = false;           // finite() keeps -infinity out
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) { return __uint_as_float(r[i]); }
     static __device__ __forceinline__ uint32_t lowest(float) { return 0u; }
     static __device__ __forceinline__ f2 finite(const uint32_t (&r)[4], int i, uint32_t) { return pack2(get(r, i), get(r, i + 1)); }
@@ -114,6 +115,7 @@ template <> struct Vec<float> {
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kN = 8;
+    static constexpr uint32_t kNone = 0xff80ff80u;
     static constexpr bool kRaised = true;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
@@ -149,6 +151,7 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<__half> {
     static constexpr int kN = 8;
+    static constexpr uint32_t kNone = 0xfc00fc00u;
     static constexpr bool kRaised = false;
     static __device__ __forceinline__ float get(const uint32_t (&r)[4], int i) {
         return __half2float(__ushort_as_half(static_cast<unsigned short>(i % 2 ? r[i / 2] >> 16 : r[i / 2] & 0xffffu)));
@@ -325,17 +328,20 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
         float top[kFly];
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            const uint4 q = mine[(stage * kFly + u) * 32];   // (past the end: whatever is there, not used)
+            const uint4 q = mine[(stage * kFly + u) * 32];
             r[u][0] = q.x, r[u][1] = q.y, r[u][2] = q.z, r[u][3] = q.w;
+        }
+        if (v0 + (kFly - 1) * warps * 32 + 32 > vecs) {   // (one branch a batch: the rest is straight)
+#pragma unroll
+            for (int u = 0; u < kFly; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[u][i] = v0 + u * warps * 32 + lane < vecs ? r[u][i] : V::kNone;
         }
         stage = stage == kStages - 1 ? 0 : stage + 1;
         float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            top[u] = -INFINITY;
-            if (v0 + u * warps * 32 + lane < vecs) {
-                top[u] = fmaxf(top[u], V::most(r[u]));
-            }
+            top[u] = fmaxf(-INFINITY, V::most(r[u]));
             most = fmaxf(most, top[u]);
         }
         if (most > a.mx) {
@@ -348,19 +354,16 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
         }
         const f2 nm = pack2(nmc, nmc);
 #pragma unroll
-        for (int u = 0; u < kFly; ++u) {
-            if (v0 + u * warps * 32 + lane < vecs) {
+        for (int u = 0; u < kFly; ++u)
 #pragma unroll
-                for (int i = 0; i < N; i += 2) {
-                    float d0, d1;
-                    unpack2(fma2(V::finite(r[u], i, low), cc, nm), d0, d1);
-                    if constexpr (!V::kRaised) d0 = clamped(d0), d1 = clamped(d1);
-                    const f2 e = pack2(ex2(d0), ex2(d1));
-                    s2 = fma2(e, pack2(1.f, 1.f), s2);
-                    w2 = fma2(pack2(d0, d1), e, w2);
-                }
+            for (int i = 0; i < N; i += 2) {
+                float d0, d1;
+                unpack2(fma2(V::finite(r[u], i, low), cc, nm), d0, d1);
+                if constexpr (!V::kRaised) d0 = clamped(d0), d1 = clamped(d1);
+                const f2 e = pack2(ex2(d0), ex2(d1));
+                s2 = fma2(e, pack2(1.f, 1.f), s2);
+                w2 = fma2(pack2(d0, d1), e, w2);
             }
-        }
         if constexpr (TOP) {
             if (first) {   // k of the CTA's lanes hold an entry as large as the k-th of their maxima
                 first = false;
