@@ -437,8 +437,9 @@ typedef struct precog_delta_inputs {
  *
  *   d_offsets   device int64 [n_seqs+1]: sequence c owns rows d_offsets[c] ..
  *               d_offsets[c+1]-1. A sequence whose offsets decrease or leave [0, T_tot] is
- *               skipped and flags PRECOG_DEV_BAD_OFFSETS. Lengths of zero are allowed: the
- *               state is the initial one.
+ *               skipped and flags PRECOG_DEV_BAD_OFFSETS (and, where a call with a workspace
+ *               cuts its sequences, so are those behind it). Lengths of zero are allowed:
+ *               the state is the initial one.
  *   T_tot       rows of q, k, v, g and beta (below 2^31)
  *   bank        device [bank_entries][L_total][n_v_heads][dv][dk] in bank_dtype (F32 or
  *               BF16), or NULL: every sequence begins with the zero state
@@ -453,8 +454,9 @@ typedef struct precog_delta_inputs {
  *   layer, L_total  the layer's place in the entries of bank and states_out
  *   y_out       device [T_tot][n_v_heads][dv] in y_dtype (F32 or BF16), or NULL. Rows
  *               outside every sequence are left untouched.
- *   workspace   device scratch of at least precog_delta_scan_workspace_size() bytes (0 for
- *               most shapes; then it may be NULL)
+ *   workspace   device scratch of at least precog_delta_scan_workspace_size() bytes, 16-byte
+ *               aligned; 0 bytes (and then NULL) unless few long sequences are to be cut
+ *               into segments that run at once
  * With BF16 inputs, sequences of more than a few tokens run on the tensor cores in chunks of
  * 64 tokens: state and sums stay fp32 and every intermediate operand is carried as a pair
  * of bf16 numbers (16 significant bits), so results agree with the recurrence to about 1e-5
@@ -468,7 +470,7 @@ precog_status precog_delta_scan(const precog_delta_inputs *in, const int64_t *d_
                                 size_t workspace_bytes, void *stream);
 
 /* Bytes of scratch that precog_delta_scan needs for a call of these sizes on the current
- * device (0 for most). */
+ * device (0 for most, and always where T_tot < 1024). */
 size_t precog_delta_scan_workspace_size(const precog_delta_inputs *in, int64_t n_seqs, int64_t T_tot);
 
 /*

@@ -478,9 +478,9 @@ def precog_delta_scan(inputs: DeltaInputs, offsets, T_tot: int, bank=None, idx=N
     if y_out is not None and tuple(y_out.shape) != (T_tot, inputs.n_v_heads, inputs.dv):
         raise ValueError("y_out must be [T_tot, Hv, dv]")
     holder = states_out if states_out is not None else bank
-    need = int(lib.precog_delta_scan_workspace_size(ctypes.byref(inputs), n, T_tot))
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=offsets.device)
+    if workspace is None and T_tot >= 1024:   # below, none is needed
+        need = int(lib.precog_delta_scan_workspace_size(ctypes.byref(inputs), n, T_tot))
+        workspace = torch.empty(need, dtype=torch.uint8, device=offsets.device) if need else None
     _check(lib.precog_delta_scan(
         ctypes.byref(inputs), _of(offsets, torch.int64, (n + 1,), "offsets"), n, T_tot, _ptr(bank),
         _dtype_code(bank) if bank is not None else PRECOG_F32, bank.shape[0] if bank is not None else 0,

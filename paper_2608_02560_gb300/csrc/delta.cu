@@ -315,10 +315,16 @@ cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream) {
     return p.in_dtype == PRECOG_F32 ? step_cols<float>(p, stream) : step_cols<__nv_bfloat16>(p, stream);
 }
 
-size_t delta_scan_workspace_size(const DeltaParams &p) { return 0; }
+namespace {
+
+bool in_chunks(const DeltaParams &p) { return p.in_dtype == PRECOG_BF16 && p.T_tot >= 8 * p.n_seqs; }
+
+}  // namespace
+
+size_t delta_scan_workspace_size(const DeltaParams &p) { return in_chunks(p) ? delta_chunk_workspace_size(p) : 0; }
 
 cudaError_t launch_delta_scan(const DeltaParams &p, cudaStream_t stream) {
-    if (p.in_dtype == PRECOG_BF16 && p.T_tot >= 8 * p.n_seqs) return launch_delta_chunk(p, stream);
+    if (in_chunks(p)) return launch_delta_chunk(p, stream);
     return p.in_dtype == PRECOG_F32 ? scan_cols<float>(p, stream) : scan_cols<__nv_bfloat16>(p, stream);
 }
 

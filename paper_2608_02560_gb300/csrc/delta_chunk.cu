@@ -28,6 +28,12 @@
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
 // of them enters a sum.
 //
+// Few sequences leave SMs idle, and a chain is as long as its sequence. Then each sequence is cut into
+// segments: a state passes through one as S M + B, M a product of e^g (I - beta k k^T) over its tokens.
+// First B (from the zero state, or for the first segment from the initial one) and M (the rows of the
+// identity, with v = 0) of all segments but the last; then the segments' initial states one after
+// another (delta_join_kernel); then the segments themselves, with their readout.
+//
 // Tensor memory: S [128 columns]; a pair area [128]: S's pair, then U (whose place its decayed pair
 // takes) and U's pair; two places [64 + 64] by the chunk's parity: the next chunk's k.k and q.k,
 // then S k and in its place its pair | S q, then y.
@@ -159,10 +165,21 @@ __device__ __forceinline__ f2 pair_of(const uint32_t (&r)[32], int e) {
 }
 __device__ __forceinline__ f2 load2(const float *p) { return *reinterpret_cast<const f2 *>(p); }
 
-template <int NA, bool Y>
+// Segments of `len` tokens (0: whole sequences). Sequence c's first is slot begin / len + c: no two
+// sequences' slots meet, and there are at most T_tot / len + n_seqs.
+struct Cut {
+    int len, slots;
+    int joined;                // 0: B and M; 1: the segments from their initial states
+    float *states;             // [slots][Hv][dv][dk]: B, then the state after the segment
+    float *moves;              // [slots][Hv][dk][dk]: M
+    float *begins;             // [n_seqs][Hv][dv][dk]: initial states of sequences of several segments
+};
+__device__ __forceinline__ int64_t segments(int64_t tokens, int len) { return tokens <= len ? 1 : (tokens + len - 1) / len; }
+
+template <int NA, bool Y, bool CUT>
 __global__ void __launch_bounds__(kThreads, 1)
     delta_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                       const __grid_constant__ CUtensorMap map_v, const DeltaParams p, int slices) {
+                       const __grid_constant__ CUtensorMap map_v, const DeltaParams p, int slices, const Cut cut) {
     constexpr int kKeys = NA * 64;               // key coordinates, padded
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // (an offset, not a rounded address: the compiler would lose that it is shared memory)
@@ -171,14 +188,49 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t patience = kWaitLimit;
 
     int64_t item = blockIdx.x;
-    const int slice = static_cast<int>(item % slices);
-    item /= slices;
+    const bool kept = CUT && !cut.joined;        // B and M: states go to the workspace
+    const int kinds = slices + (kept ? 1 : 0);
+    const int slice = static_cast<int>(item % kinds);
+    const bool ident = kept && slice == slices;  // M
+    item /= kinds;
     const int head = static_cast<int>(item % p.hv);
-    const int64_t seq = item / p.hv;
-    const int64_t begin = p.offsets[seq], end = p.offsets[seq + 1];
-    if (begin < 0 || end < begin || end > p.T_tot) {
-        if (threadIdx.x == 0) atomicOr(&g_delta_chunk_status, PRECOG_DEV_BAD_OFFSETS);
-        return;
+    int64_t seq = item / p.hv;
+    int64_t slot = seq, begin, end;
+    bool first = true, last = true;
+    if constexpr (CUT) {
+        // the sequence that has this slot: found by the lanes, each warp for itself
+        int64_t found = -1;
+        for (int64_t c0 = 0; c0 < p.n_seqs && found < 0; c0 += 32) {
+            const int64_t c = c0 + lane;
+            bool mine = false, bad = false;
+            if (c < p.n_seqs) {
+                const int64_t b = p.offsets[c], e = p.offsets[c + 1], base = b / cut.len + c;
+                bad = b < 0 || e < b || e > p.T_tot;
+                mine = !bad && slot >= base && slot < base + segments(e - b, cut.len);
+            }
+            const unsigned who = __ballot_sync(0xffffffffu, mine), bads = __ballot_sync(0xffffffffu, bad);
+            if (who && (!bads || __ffs(static_cast<int>(who)) < __ffs(static_cast<int>(bads)))) found = c0 + __ffs(static_cast<int>(who)) - 1;
+            else if (bads) {   // what follows may overlap what came before: skipped
+                if (threadIdx.x == 0) atomicOr(&g_delta_chunk_status, PRECOG_DEV_BAD_OFFSETS);
+                return;
+            }
+        }
+        if (found < 0) return;
+        seq = found;
+        begin = p.offsets[seq], end = p.offsets[seq + 1];
+        const int64_t seg = slot - (begin / cut.len + seq), segs = segments(end - begin, cut.len);
+        first = seg == 0, last = seg + 1 == segs;
+        begin += seg * cut.len;
+        end = last ? end : begin + cut.len;
+        // no segment follows the last, the first begins from its state itself; without a readout the
+        // others are done with
+        if (cut.joined ? !Y && !last : last || (ident && first)) return;
+    } else {
+        begin = p.offsets[seq], end = p.offsets[seq + 1];
+        if (begin < 0 || end < begin || end > p.T_tot) {
+            if (threadIdx.x == 0) atomicOr(&g_delta_chunk_status, PRECOG_DEV_BAD_OFFSETS);
+            return;
+        }
     }
     const int len = static_cast<int>(end - begin);
     const int chunks = (len + kC - 1) / kC;
@@ -261,10 +313,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tc_commit(q ? &sm.done_qs : &sm.done_ks);
                 }
-                wait_one(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
                 wait_one(Y ? &sm.done_qs : &sm.done_ks, ph, patience);   // S's pair has been read: U takes its place
+                if (!ident) wait_one(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)   // V T hi, V T lo
+                for (int k = 0; k < 8 && !ident; ++k)   // V T hi, V T lo
                     tc_mma_f16(tmem + kColPair, dv + (k % 4) * (2048 / 16), dt + (k / 4) * (kTile / 16) + 2 * (k % 4),
                                idesc(kC, true, false), k > 0);
                 wait_one(&sm.have_k, ph, patience);
@@ -273,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int k = 0; k < 12; ++k) {   // (S k) hi T hi, lo T hi, hi T lo
                     const int part = k / 4, kk = k % 4;
                     tc_mma_f16_ts(tmem + kColPair, col_k + (kk / 2) * 32 + (kk % 2) * 8 + (part == 1 ? 16 : 0),
-                                  dt + (part == 2 ? kTile / 16 : 0) + 2 * kk, idesc(kC, false, false), true);
+                                  dt + (part == 2 ? kTile / 16 : 0) + 2 * kk, idesc(kC, false, false), !ident || k > 0);
                 }
                 tc_commit(&sm.done_u);
                 wait_one(&sm.have_d, ph, patience);
@@ -315,6 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         };
         auto load_v = [&](int c) {
+            if (ident) return;
             uint64_t *full = &sm.full_v[c % kStages];
             const int tiles = channels > 64 ? 2 : 1;
             mbar_arrive_expect_tx(full, tiles * kTile);
@@ -375,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int n = len - c * kC;
             if (c + 1 < chunks || n == kC) return;
             wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-            wait(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+            if (!ident) wait(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
             for (int e = lane; e < (NA * 2 + 2) * (kC - n) * 8; e += 32) {
                 const int tile = e / ((kC - n) * 8);
                 uint8_t *to = tile < NA * 2 ? sm.kq[c % kStages] + tile * kTile : sm.v[c % kStages] + (tile - NA * 2) * kTile;
@@ -591,20 +644,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row = quarter * 32 + lane;             // value channel within the slice
         const int ch = slice * kM + row;                 // and within the head
         const uint32_t tm = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-        const bool live = ch < p.dv;
+        const bool live = ident ? row < p.dk : ch < p.dv;
         constexpr int kHalf = kKeys / 2;                 // S's columns of this half of the warps
         const uint32_t col_s = tm + kColS + half * kHalf;
         const int64_t head_elems = static_cast<int64_t>(p.dv) * p.dk;
         {   // initial state
-            int64_t entry = -1;
-            if (p.bank) {
-                entry = p.idx ? p.idx[seq] : seq;
+            const void *from = nullptr;
+            int dtype = PRECOG_F32;
+            int64_t at = 0;
+            if (CUT && first && !last && cut.joined) {   // (the bank may be where the last segment's state goes)
+                from = cut.begins;
+                at = (seq * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+            } else if (first && p.bank && !ident) {
+                int64_t entry = p.idx ? p.idx[seq] : seq;
                 if (entry < -1 || entry >= p.bank_entries) {
                     if (threadIdx.x == 0) atomicOr(&g_delta_chunk_status, PRECOG_DEV_BAD_INDEX);
                     entry = -1;
                 }
+                from = entry >= 0 ? p.bank : nullptr;
+                dtype = p.bank_dtype;
+                at = ((entry * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+            } else if (CUT && !first && cut.joined) {
+                from = cut.states;
+                at = ((slot - 1) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
             }
-            const int64_t at = ((entry * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
 #pragma unroll
             for (int g = 0; g < kHalf; g += 32) {
                 uint32_t r[32];
@@ -612,7 +675,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 32; e += 8) {
                     const int col = half * kHalf + g + e;
                     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    if (entry >= 0 && live && col < p.dk) delta_load8(p.bank, p.bank_dtype, at + col, v);
+                    if (from && live && col < p.dk) delta_load8(from, dtype, at + col, v);
+                    if (ident && row >= col && row < col + 8) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) v[x] = row == col + x ? 1.f : 0.f;
+                    }
+                    if (kept && first && !ident && live && col < p.dk)
+                        delta_store8(cut.begins, PRECOG_F32, (seq * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk + col, v);
 #pragma unroll
                     for (int x = 0; x < 8; ++x) r[e + x] = __float_as_uint(v[x]);
                 }
@@ -757,8 +826,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_fence_after();
             }
         }
-        if (p.states) {
-            const int64_t at = ((seq * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+        if (kept || (last && p.states)) {
+            void *to = kept ? (ident ? cut.moves : cut.states) : p.states;
+            const int dtype = kept ? PRECOG_F32 : p.state_dtype;
+            const int64_t at = ident ? (slot * p.hv + head) * p.dk * p.dk + static_cast<int64_t>(row) * p.dk
+                                     : ((kept ? slot : seq * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
 #pragma unroll
             for (int g = 0; g < kHalf; g += 32) {
                 uint32_t r[32];
@@ -770,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         float v[8];
 #pragma unroll
                         for (int x = 0; x < 8; ++x) v[x] = __uint_as_float(r[e + x]);
-                        delta_store8(p.states, p.state_dtype, at + col, v);
+                        delta_store8(to, dtype, at + col, v);
                     }
                 __syncwarp();
             }
@@ -784,18 +856,143 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-template <int NA, bool Y>
-cudaError_t launch(const DeltaParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, int slices,
-                   cudaStream_t stream) {
-    auto kern = delta_chunk_kernel<NA, Y>;
+// The segments' initial states: state after segment s = state before it * M + B, in the place of B,
+// for 16 value channels a CTA. M comes through shared memory, the next one while this one is used.
+constexpr int kJoinRows = 16, kJoinThreads = 128;
+
+__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaParams p, const Cut cut) {
+    extern __shared__ __align__(16) float join_smem[];
+    const int dk = p.dk, pitch = dk + 4;
+    float *move[2] = {join_smem, join_smem + dk * dk};
+    float *rows = join_smem + 2 * dk * dk;                 // [16][pitch]
+    const int tiles = (p.dv + kJoinRows - 1) / kJoinRows;
+    int64_t item = blockIdx.x;
+    const int r0 = static_cast<int>(item % tiles) * kJoinRows;
+    item /= tiles;
+    const int head = static_cast<int>(item % p.hv);
+    const int64_t seq = item / p.hv;
+    const int64_t begin = p.offsets[seq], end = p.offsets[seq + 1];
+    for (int64_t c = 0; c <= seq; ++c)                     // as the segments' own kernel: up to the first bad one
+        if (p.offsets[c] < 0 || p.offsets[c + 1] < p.offsets[c] || p.offsets[c + 1] > p.T_tot) return;
+    const int64_t base = begin / cut.len + seq, segs = segments(end - begin, cut.len);
+    if (segs < 3) return;                                  // the second begins where the first ended
+    const int quads = dk / 4;
+    auto fetch = [&](int64_t seg) {
+        const float *from = cut.moves + ((base + seg) * p.hv + head) * dk * dk;
+        for (int e = threadIdx.x; e < dk * quads; e += kJoinThreads) cp_async16(move[seg & 1] + 4 * e, from + 4 * e);
+        cp_async_commit();
+    };
+    auto state = [&](int64_t seg, int r) { return cut.states + (((base + seg) * p.hv + head) * p.dv + r0 + r) * dk; };
+    fetch(1);
+    for (int e = threadIdx.x; e < kJoinRows * quads; e += kJoinThreads) {
+        const int r = e / quads, c = e % quads;
+        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+        *reinterpret_cast<float4 *>(rows + r * pitch + 4 * c) = r0 + r < p.dv ? *reinterpret_cast<const float4 *>(state(0, r) + 4 * c) : zero;
+    }
+    // thread: 4 rows of warp `threadIdx.x / 32`, 4 columns
+    const int r = threadIdx.x / 32 * 4, c = threadIdx.x % 32 * 4;
+    for (int64_t seg = 1; seg + 1 < segs; ++seg) {
+        if (seg + 2 < segs) fetch(seg + 1);
+        else cp_async_commit();
+        float4 b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            b[i] = c < dk && r0 + r + i < p.dv ? *reinterpret_cast<const float4 *>(state(seg, r + i) + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        cp_async_wait<1>();
+        __syncthreads();
+        f2 acc[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][0] = pack2(b[i].x, b[i].y), acc[i][1] = pack2(b[i].z, b[i].w);
+        const float *m = move[seg & 1];
+        if (c < dk) {
+#pragma unroll 2
+            for (int k = 0; k < dk; k += 4) {
+                float4 s[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const float4 *>(rows + (r + i) * pitch + k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4 x = *reinterpret_cast<const float4 *>(m + (k + e) * dk + c);
+                    const f2 lo = pack2(x.x, x.y), hi = pack2(x.z, x.w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float v = e == 0 ? s[i].x : e == 1 ? s[i].y : e == 2 ? s[i].z : s[i].w;
+                        acc[i][0] = fma2(pack2(v, v), lo, acc[i][0]);
+                        acc[i][1] = fma2(pack2(v, v), hi, acc[i][1]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (c < dk) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float4 x;
+                unpack2(acc[i][0], x.x, x.y);
+                unpack2(acc[i][1], x.z, x.w);
+                *reinterpret_cast<float4 *>(rows + (r + i) * pitch + c) = x;
+                if (r0 + r + i < p.dv) *reinterpret_cast<float4 *>(state(seg, r + i) + c) = x;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+struct Maps {
+    CUtensorMap q, k, v;
+};
+
+template <int NA, bool Y, bool CUT>
+cudaError_t launch(const DeltaParams &p, const Maps &maps, int slices, const Cut &cut, cudaStream_t stream) {
+    auto kern = delta_chunk_kernel<NA, Y, CUT>;
     const int smem = static_cast<int>(sizeof(Smem<NA>) + 1024);
     static_assert(sizeof(Smem<NA>) + 1024 <= 227 * 1024, "one CTA's shared memory");
     cudaError_t e = ensure_smem(reinterpret_cast<const void *>(kern), smem);
     if (e != cudaSuccess) return e;
-    kern<<<static_cast<unsigned>(p.n_seqs * p.hv * slices), kThreads, smem, stream>>>(mq, mk, mv, p, slices);
+    const int64_t ctas = (CUT ? cut.slots : p.n_seqs) * p.hv * (slices + (CUT && !cut.joined ? 1 : 0));
+    if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    kern<<<static_cast<unsigned>(ctas), kThreads, smem, stream>>>(maps.q, maps.k, maps.v, p, slices, cut);
     e = cudaGetLastError();
     if (e == cudaSuccess) count_launches(1);
     return e;
+}
+
+template <int NA>
+cudaError_t launch_all(const DeltaParams &p, const Maps &maps, int slices, Cut cut, cudaStream_t stream) {
+    cudaError_t e;
+    if (cut.len) {
+        e = launch<NA, false, true>(p, maps, slices, cut, stream);
+        if (e != cudaSuccess) return e;
+        const int smem = (2 * p.dk * p.dk + kJoinRows * (p.dk + 4)) * 4;
+        e = ensure_smem(reinterpret_cast<const void *>(delta_join_kernel), smem);
+        if (e != cudaSuccess) return e;
+        const int64_t ctas = p.n_seqs * p.hv * ((p.dv + kJoinRows - 1) / kJoinRows);
+        delta_join_kernel<<<static_cast<unsigned>(ctas), kJoinThreads, smem, stream>>>(p, cut);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        count_launches(1);
+        cut.joined = 1;
+        return p.y ? launch<NA, true, true>(p, maps, slices, cut, stream) : launch<NA, false, true>(p, maps, slices, cut, stream);
+    }
+    return p.y ? launch<NA, true, false>(p, maps, slices, cut, stream) : launch<NA, false, false>(p, maps, slices, cut, stream);
+}
+
+// The segments' length for these sizes, or 0. In chunks of 64 tokens, of which a CTA takes one after
+// another: whole sequences are as long as their rounds of CTAs; segments go in one pass for B and M,
+// one step of the join each, and one pass for themselves. Cut only where that is a third shorter: the
+// estimate knows the sequences' mean length alone.
+int cut_length(const DeltaParams &p) {
+    const int64_t sms = device_sm_count(), slices = (p.dv + kM - 1) / kM, items = p.n_seqs * p.hv * slices;
+    if (items > sms || p.T_tot / p.n_seqs < 16 * kC) return 0;
+    const int64_t chunks = p.T_tot / kC;
+    auto rounds = [&](int64_t ctas) { return (ctas + sms - 1) / sms; };
+    int64_t best = chunks / p.n_seqs, len = 0;
+    for (int64_t per = 4; per < chunks / p.n_seqs; per += 1 + per / 16) {   // chunks of a segment
+        const int64_t segs = (chunks / p.n_seqs + per - 1) / per;            // of a mean sequence
+        const int64_t cost = per * (rounds((items + p.n_seqs * p.hv) * (segs - 1)) + rounds(items * segs)) + segs;
+        if (cost * 3 < best * 2 || (len && cost < best)) best = cost, len = per;
+    }
+    return static_cast<int>(len * kC);
 }
 
 // [rows][heads][dim] bf16 with `stride` elements between rows, in boxes of 64 columns of 64
@@ -811,16 +1008,29 @@ bool rows_map(CUtensorMap *map, const void *base, int dim, int heads, int64_t ro
 
 }  // namespace
 
+size_t delta_chunk_workspace_size(const DeltaParams &p) {
+    const int64_t len = cut_length(p);
+    if (len == 0) return 0;
+    return (static_cast<size_t>(p.T_tot / len + p.n_seqs) * (p.dv + p.dk) + static_cast<size_t>(p.n_seqs) * p.dv) * p.hv * p.dk * sizeof(float);
+}
+
 cudaError_t launch_delta_chunk(const DeltaParams &p, cudaStream_t stream) {
     const bool want_y = p.y != nullptr;
     const int slices = (p.dv + kM - 1) / kM;
-    CUtensorMap mq, mk, mv;
-    if (!rows_map(&mk, p.k, p.dk, p.hk, p.T_tot, p.k_stride) ||
-        !rows_map(&mq, want_y ? p.q : p.k, p.dk, p.hk, p.T_tot, want_y ? p.q_stride : p.k_stride) ||
-        !rows_map(&mv, p.v, p.dv, p.hv, p.T_tot, p.v_stride))
+    Maps maps;
+    if (!rows_map(&maps.k, p.k, p.dk, p.hk, p.T_tot, p.k_stride) ||
+        !rows_map(&maps.q, want_y ? p.q : p.k, p.dk, p.hk, p.T_tot, want_y ? p.q_stride : p.k_stride) ||
+        !rows_map(&maps.v, p.v, p.dv, p.hv, p.T_tot, p.v_stride))
         return cudaErrorInvalidValue;
-    if (p.dk <= 64) return want_y ? launch<1, true>(p, mq, mk, mv, slices, stream) : launch<1, false>(p, mq, mk, mv, slices, stream);
-    return want_y ? launch<2, true>(p, mq, mk, mv, slices, stream) : launch<2, false>(p, mq, mk, mv, slices, stream);
+    Cut cut = {};
+    cut.len = cut_length(p);
+    if (cut.len) {
+        cut.slots = static_cast<int>(p.T_tot / cut.len + p.n_seqs);
+        cut.states = static_cast<float *>(p.workspace);
+        cut.moves = cut.states + static_cast<int64_t>(cut.slots) * p.hv * p.dv * p.dk;
+        cut.begins = cut.moves + static_cast<int64_t>(cut.slots) * p.hv * p.dk * p.dk;
+    }
+    return p.dk <= 64 ? launch_all<1>(p, maps, slices, cut, stream) : launch_all<2>(p, maps, slices, cut, stream);
 }
 
 cudaError_t delta_chunk_status_word_read_clear(uint32_t *bits) {

@@ -208,6 +208,55 @@ def test_long_sequences(cuda_device, T, heads):
     assert pg.precog_device_status()[0] == 0
 
 
+CUT = [
+    # lens, hv, dk, dv, bank, want_y: few sequences whose mean is long, so that they are cut (the
+    # first one's mean is just too short to be)
+    ([2000, 0, 1, 1100, 3000, 64], 1, 64, 64, True, True),
+    ([2500, 0, 1, 4100, 3000, 64, 2400], 1, 64, 64, True, True),
+    ([1500, 4000], 2, 128, 128, True, False),
+    ([2777], 1, 40, 200, False, True),
+    ([1024, 2048], 1, 128, 136, True, True),
+]
+
+
+@pytest.mark.parametrize("lens,hv,dk,dv,bank,want_y", CUT)
+def test_sequences_cut_into_segments(cuda_device, lens, hv, dk, dv, bank, want_y):
+    """Long sequences of a small batch beside empty and short ones; the bank itself receives the
+    states (each sequence's row is its own), and the workspace held NaN."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    n, T = len(lens), sum(lens)
+    q, k, v, g, beta, off = _tensors(lens, 1, hv, dk, dv, torch.bfloat16, cuda_device, 7 + T, rate=0.02)
+    inputs = pg.delta_inputs(q, k, v, g, beta)
+    need = pg.precog_delta_scan_workspace_size(inputs, n, T)
+    assert (need > 0) == (T // n > 1100)
+    ws = torch.full((need // 4,), float("nan"), device=cuda_device)
+    states = torch.randn((n, 1, hv, dv, dk), device=cuda_device)
+    S0 = to_np(states[:, 0]) if bank else None
+    y = torch.full((T, hv, dv), float("nan"), device=cuda_device) if want_y else None
+    pg.precog_delta_scan(inputs, off, T, bank=states if bank else None, states_out=states, y_out=y, workspace=ws)
+    assert pg.precog_device_status()[0] == 0
+    ref_S, ref_y = _ref(q, k, v, g, beta, off, S0)
+    _check(states[:, 0], ref_S, TOL_PAIR)
+    if want_y:
+        _check(y, ref_y, TOL_PAIR)
+
+
+def test_cut_sequences_behind_bad_offsets_are_skipped(cuda_device):
+    import torch
+    import paper_2608_02560_gb300 as pg
+    q, k, v, g, beta, _ = _tensors([6000], 1, 1, 64, 64, torch.bfloat16, cuda_device, 3)
+    off = torch.tensor([0, 2500, 2400, 6000], dtype=torch.int64, device=cuda_device)
+    inputs = pg.delta_inputs(q, k, v, g, beta)
+    assert pg.precog_delta_scan_workspace_size(inputs, 3, 6000) > 0
+    s = torch.full((3, 1, 1, 64, 64), 7.0, device=cuda_device)
+    pg.precog_delta_scan(inputs, off, 6000, states_out=s)
+    assert pg.precog_device_status() == (5, pg.PRECOG_DEV_BAD_OFFSETS)
+    ref, _ = _ref(q[:2500], k[:2500], v[:2500], g[:2500], beta[:2500], off[:2])
+    _check(s[:1, 0], ref, TOL_PAIR)
+    assert bool((s[1:] == 7.0).all())
+
+
 @pytest.mark.parametrize("n,hk,hv,dk,dv,dtype,y_dtype", [
     (1, 1, 1, 8, 8, "float32", "float32"), (3, 2, 4, 128, 128, "bfloat16", "bfloat16"),
     (70, 1, 2, 72, 200, "bfloat16", "float32"), (5, 3, 3, 40, 24, "float32", "bfloat16")])
