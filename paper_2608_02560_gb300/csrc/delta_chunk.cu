@@ -15,14 +15,16 @@
 // the state itself stay fp32. A single bf16 would put 2^-9 of S into every y.
 //
 // Warps 0-7, the chain: what each chunk needs of the chunk before it, half the columns each
-// group of four. Per chunk: split S, [S k], [S q, V T], split S k, [S k T], split U, [update],
-// [P U]; [..] are MMAs. y of a chunk leaves while the next one's first MMAs run.
-// Warps 8-15, one chunk ahead: A and P with their decays, the inverse T in fp32: blocks of 16 by
-// substitution (a product form would lose its digits where keys repeat), then joined twice,
-// T10 = -(T1 A10) T0, on mma.sync with operands as pairs of tf32 (16 x 16 and 32 x 32: too small
-// for an MMA of 128 rows, and one multiply per shared-memory read was too slow).
-// Warp 16: copies in, three chunks deep, the chunks' gates, and y rows out.
-// Warp 17: issues every MMA, so that no working warp waits in the queue of the tensor cores.
+// group of four. Per chunk: split S, [S k], y of the chunk before leaves, [S q, V T], split S k,
+// [S k T], split U, [update], [P U]; [..] are MMAs.
+// Warps 8-15, two teams that take chunks by turns, one or two ahead of the chain (one team of eight
+// was no faster than this one of four, and the chain waited for it: 7000 cycles a chunk): A and P
+// with their decays, the inverse T in fp32: blocks of 16 by substitution (a product form would lose
+// its digits where keys repeat), then joined twice, T10 = -(T1 A10) T0, on mma.sync with operands as
+// pairs of tf32 (16 x 16 and 32 x 32: too small for an MMA of 128 rows, and one multiply per
+// shared-memory read was too slow).
+// Warp 16: K and Q in, three chunks deep, and the chunks' gates. Warp 17: issues every MMA, so that no
+// working warp waits in the queue of the tensor cores. Warp 18: V in and y rows out.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
@@ -35,8 +37,8 @@
 // another (delta_join_kernel); then the segments themselves, with their readout.
 //
 // Tensor memory: S [128 columns]; a pair area [128]: S's pair, then U (whose place its decayed pair
-// takes) and U's pair; two places [64 + 64] by the chunk's parity: the next chunk's k.k and q.k,
-// then S k and in its place its pair | S q, then y.
+// takes) and U's pair; three places [64] by turns: a chunk's k.k and q.k, then its S k, then that
+// one's pair; and S q [64], then y.
 #include <cuda.h>
 
 #include "../../include/precog.h"
@@ -52,19 +54,19 @@ namespace {
 
 constexpr int kC = 64;                 // tokens of a chunk
 constexpr int kM = 128;                // value channels of a CTA
-constexpr int kStages = 3, kGates = 4;
-constexpr int kChain = 256, kPrep = 256;   // threads
-constexpr int kThreads = kChain + kPrep + 64;
-constexpr int kCopyWarp = (kChain + kPrep) / 32, kMmaWarp = kCopyWarp + 1;
+constexpr int kStages = 3, kVStages = 2;
+constexpr int kChain = 256, kTeam = 128;   // threads
+constexpr int kThreads = kChain + 2 * kTeam + 96;
+constexpr int kCopyWarp = (kChain + 2 * kTeam) / 32, kMmaWarp = kCopyWarp + 1, kValueWarp = kCopyWarp + 2;
 constexpr int kH = kC / 2, kB = kC / 4;    // the inverse: blocks of 16, joined to halves, joined
-constexpr int kPitch = kH + 4;             // (rows of an MMA operand in different banks)
+constexpr int kBlock = kH * kH;            // a quarter of A
 constexpr uint32_t kTile = kC * 128;   // bytes of a [64 tokens][64 keys] bf16 tile
 constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
 
 // tensor memory columns
-constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = kColK + 64, kPlace = 128;
+constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = 448;
 
-constexpr int kBarPrep = 1, kBarHalf = 2;   // and 3
+constexpr int kBarTeam = 1;            // and 2
 
 // A sum of logs as an unevaluated pair: differences of large sums keep their digits.
 struct Log {
@@ -101,12 +103,13 @@ struct Smem {
     // per stage: [K][Q] tiles of key columns 0..63, then of 64..127; V's two tiles, where the chunk's
     // bf16 y rows lie on their way out
     uint8_t kq[kStages][NA * 2 * kTile];
-    uint8_t v[kStages][2 * kTile];
-    // T hi, T lo, P hi, P lo; A and what becomes of it, by columns in fp32, fill the place of T before
-    uint8_t tp[2][4][kTile];
-    Gates gates[kGates];
-    alignas(16) float mid[kH * kPitch];   // a product on its way, [row][column]
-    uint64_t full_kq[kStages], full_v[kStages], free_kq[kStages], through[kStages], gated[kGates], zeroed;
+    uint8_t v[kVStages][2 * kTile];
+    uint8_t tp[2][4][kTile];          // T hi, T lo, P hi, P lo
+    float a[2][3 * kBlock];           // a team's A, by columns in quarters 11, 21, 22, and what becomes of it
+    Gates gates[kStages];
+    uint64_t full_kq[kStages], free_kq[kStages], gated[kStages];
+    uint64_t full_v[kVStages], through[kVStages];
+    uint64_t zeroed_kq, zeroed_v;
     uint64_t ready[2], done_prep[2], done_o[2];
     uint64_t have_s, have_k, have_d, have_u;      // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
@@ -151,6 +154,15 @@ __device__ __forceinline__ uint32_t bits2(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
+// Rows n .. 63 of `tiles` tiles, by a warp; MMAs see it.
+__device__ __forceinline__ void zero_rows(uint8_t *first, int tiles, int n, int lane) {
+    const int pieces = (kC - n) * 8;
+    for (int e = lane; e < tiles * pieces; e += 32)
+        *reinterpret_cast<uint4 *>(first + e / pieces * kTile + n * 128 + e % pieces * 16) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
 // Two numbers as bf16 in h and what that leaves, again in bf16, in l.
 __device__ __forceinline__ void split(f2 ab, uint32_t &h, uint32_t &l) {
     float a, b;
@@ -239,17 +251,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&sm.full_kq[s], 1);
-            mbar_init(&sm.full_v[s], 1);
             mbar_init(&sm.free_kq[s], 1);
-            mbar_init(&sm.through[s], kChain / 32);
+            mbar_init(&sm.gated[s], 1);
         }
-        for (int i = 0; i < kGates; ++i) mbar_init(&sm.gated[i], 1);
-        mbar_init(&sm.zeroed, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sm.ready[i], kPrep / 32);
+            mbar_init(&sm.full_v[i], 1);
+            mbar_init(&sm.through[i], kChain / 32);
+            mbar_init(&sm.ready[i], kTeam / 32);
             mbar_init(&sm.done_prep[i], 1);
             mbar_init(&sm.done_o[i], 1);
         }
+        mbar_init(&sm.zeroed_kq, 1);
+        mbar_init(&sm.zeroed_v, 1);
         mbar_init(&sm.have_s, kChain / 32);
         mbar_init(&sm.have_k, kChain / 32);
         mbar_init(&sm.have_d, kChain / 32);
@@ -264,11 +277,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_alloc(&sm.tmem_base, 512);
         tmem_relinquish();
     }
-    // P's upper 16 x 16 blocks are zero for good
-    for (int e = threadIdx.x; e < 4 * static_cast<int>(kTile) / 16; e += kThreads) {
-        const int buf = e / (2 * kTile / 16);
-        reinterpret_cast<uint4 *>(sm.tp[buf][2])[e % (2 * kTile / 16)] = make_uint4(0u, 0u, 0u, 0u);
-    }
+    // the blocks of T and P right of the diagonal are zero for good
+    for (int e = threadIdx.x; e < 8 * static_cast<int>(kTile) / 16; e += kThreads)
+        reinterpret_cast<uint4 *>(sm.tp[0][0])[e] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
@@ -283,28 +294,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto products = [&](int c) {
                 wait_one(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
                 // rows beyond the end are zeroed first
-                if (len - c * kC < kC) wait_one(&sm.zeroed, 0, patience);
+                if (len - c * kC < kC) wait_one(&sm.zeroed_kq, 0, patience);
                 const uint64_t d = desc_base(sm.kq[c % kStages]);
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k) {
                     const uint64_t dk = d + (k / 4) * (2 * kTile / 16) + 2 * (k % 4);
-                    tc_mma_f16(tmem + kColK + (c & 1) * kPlace, dk, dk, idesc(kC, false, false), k > 0);
+                    tc_mma_f16(tmem + kColK + c % 3 * 64, dk, dk, idesc(kC, false, false), k > 0);
                 }
                 tc_commit(&sm.done_prep[c & 1]);
             };
             if (chunks > 0) products(0);
+            if (chunks > 1) products(1);
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
                 const uint32_t ph = static_cast<uint32_t>(c) & 1u;
-                const uint32_t col_k = tmem + kColK + ph * kPlace, col_q = tmem + kColQ + ph * kPlace;
-                const uint64_t d = desc_base(sm.kq[c % kStages]), dv = desc_base(sm.v[c % kStages]), dt = desc_base(sm.tp[ph][0]);
-                // (its place: S k's pair of the chunk before, which [S k T] has read)
-                if (c + 1 < chunks) products(c + 1);
+                const uint32_t col_k = tmem + kColK + c % 3 * 64, col_q = tmem + kColQ;
+                const uint64_t d = desc_base(sm.kq[c % kStages]), dv = desc_base(sm.v[c % kVStages]), dt = desc_base(sm.tp[ph][0]);
                 wait_one(&sm.ready[ph], static_cast<uint32_t>(c >> 1) & 1u, patience);
                 wait_one(&sm.have_s, ph, patience);
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < (Y ? 2 : 1); ++q) {
+                    if (q && c > 0) {   // y of the chunk before has left
+                        wait_one(&sm.through[(c - 1) % kVStages], static_cast<uint32_t>((c - 1) / kVStages) & 1u, patience);
+                        tc_fence_after();
+                    }
 #pragma unroll
                     for (int k = 0; k < kKeys / 8; ++k) {   // hi, then lo
                         const int kk = k % (kKeys / 16);
@@ -314,7 +328,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc_commit(q ? &sm.done_qs : &sm.done_ks);
                 }
                 wait_one(Y ? &sm.done_qs : &sm.done_ks, ph, patience);   // S's pair has been read: U takes its place
-                if (!ident) wait_one(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                if (!ident) {
+                    wait_one(&sm.full_v[c % kVStages], static_cast<uint32_t>(c / kVStages) & 1u, patience);
+                    if (len - c * kC < kC) wait_one(&sm.zeroed_v, 0, patience);
+                }
 #pragma unroll
                 for (int k = 0; k < 8 && !ident; ++k)   // V T hi, V T lo
                     tc_mma_f16(tmem + kColPair, dv + (k % 4) * (2048 / 16), dt + (k / 4) * (kTile / 16) + 2 * (k % 4),
@@ -328,6 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                                   dt + (part == 2 ? kTile / 16 : 0) + 2 * kk, idesc(kC, false, false), !ident || k > 0);
                 }
                 tc_commit(&sm.done_u);
+                // (its place: the pair of the chunk before, whose MMAs are done)
+                if (c + 2 < chunks) products(c + 2);
                 wait_one(&sm.have_d, ph, patience);
                 tc_fence_after();
 #pragma unroll
@@ -356,7 +375,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else if (warp == kCopyWarp) {
         // ---------------- copies and gates ----------------
-        const int channels = p.dv - slice * kM < kM ? p.dv - slice * kM : kM;
         auto load_kq = [&](int c) {
             uint8_t *st = sm.kq[c % kStages];
             uint64_t *full = &sm.full_kq[c % kStages];
@@ -365,14 +383,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, static_cast<int>(begin) + c * kC, full);
                 if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, static_cast<int>(begin) + c * kC, full);
             }
-        };
-        auto load_v = [&](int c) {
-            if (ident) return;
-            uint64_t *full = &sm.full_v[c % kStages];
-            const int tiles = channels > 64 ? 2 : 1;
-            mbar_arrive_expect_tx(full, tiles * kTile);
-            for (int a = 0; a < tiles; ++a)
-                tma_load_3d(sm.v[c % kStages] + a * kTile, &map_v, slice * kM + a * 64, head, static_cast<int>(begin) + c * kC, full);
         };
         float g[2], bt[2];   // of tokens 2 lane, 2 lane + 1 of a chunk to come
         auto load_gates = [&](int c) {
@@ -388,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         auto gate = [&](int c) {
             constexpr float kL = 1.44269502f, kLl = 1.92596303e-8f;   // log2 e
-            Gates &to = sm.gates[c % kGates];
+            Gates &to = sm.gates[c % kStages];
             Log x[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -420,92 +430,93 @@ __global__ void __launch_bounds__(kThreads, 1)
             if ((lane & 7) == 7) to.last[lane / 8] = sum;
             if (lane == 31) to.whole = ex2(sum.h + sum.l);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.gated[c % kGates]);
+            if (lane == 0) mbar_arrive(&sm.gated[c % kStages]);
             __syncwarp();
         };
-        // The last chunk's rows beyond the end, whatever they are, once it is in.
-        auto zero_tail = [&](int c) {
-            const int n = len - c * kC;
-            if (c + 1 < chunks || n == kC) return;
-            wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-            if (!ident) wait(&sm.full_v[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-            for (int e = lane; e < (NA * 2 + 2) * (kC - n) * 8; e += 32) {
-                const int tile = e / ((kC - n) * 8);
-                uint8_t *to = tile < NA * 2 ? sm.kq[c % kStages] + tile * kTile : sm.v[c % kStages] + (tile - NA * 2) * kTile;
-                *reinterpret_cast<uint4 *>(to + n * 128 + e % ((kC - n) * 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.zeroed);
-            __syncwarp();
-        };
-        for (int c = 0; c < kStages && c < chunks && lane == 0; ++c) {
-            load_kq(c);
-            load_v(c);
-        }
+        for (int c = 0; c < kStages && c < chunks && lane == 0; ++c) load_kq(c);
         __syncwarp();
         load_gates(0);
-        for (int c = 0; c < kGates && c < chunks; ++c) {
-            gate(c);
-            load_gates(c + 1);
-            if (c < kStages) zero_tail(c);
-        }
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            const uint32_t phase = static_cast<uint32_t>(c / kStages) & 1u;
-            wait(&sm.free_kq[c % kStages], phase, patience);
-            if (c + kStages < chunks && lane == 0) load_kq(c + kStages);
+            if (c >= kStages) {   // its stage and its gates' place: the update of three chunks before has read them
+                wait(&sm.free_kq[c % kStages], static_cast<uint32_t>(c / kStages - 1) & 1u, patience);
+                if (lane == 0) load_kq(c);
+                __syncwarp();
+            }
+            gate(c);
+            load_gates(c + 1);
+            if (c + 1 == chunks && len - c * kC < kC) {   // rows beyond the end, whatever they are
+                wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                zero_rows(sm.kq[c % kStages], NA * 2, len - c * kC, lane);
+                if (lane == 0) mbar_arrive(&sm.zeroed_kq);
+            }
+        }
+        // all that was asked for has landed
+        for (int c = chunks > kStages ? chunks - kStages : 0; c < chunks; ++c)
+            wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+    } else if (warp == kValueWarp) {
+        // ---------------- V in, y out ----------------
+        const int channels = p.dv - slice * kM < kM ? p.dv - slice * kM : kM;
+        auto load_v = [&](int c) {
+            if (ident) return;
+            uint64_t *full = &sm.full_v[c % kVStages];
+            const int tiles = channels > 64 ? 2 : 1;
+            mbar_arrive_expect_tx(full, tiles * kTile);
+            for (int a = 0; a < tiles; ++a)
+                tma_load_3d(sm.v[c % kVStages] + a * kTile, &map_v, slice * kM + a * 64, head, static_cast<int>(begin) + c * kC, full);
+        };
+#pragma unroll 1
+        for (int c = 0; c < chunks + kVStages; ++c) {
+            if (const int o = c - kVStages; o >= 0) {
+                // the chunk before in this stage: its y
+                wait(&sm.through[o % kVStages], static_cast<uint32_t>(o / kVStages) & 1u, patience);
+                if (Y && p.y_dtype == PRECOG_BF16) {
+                    const int n = len - o * kC < kC ? len - o * kC : kC;
+                    for (int t = lane; t < n; t += 32)
+                        bulk_s2g(static_cast<__nv_bfloat16 *>(p.y) + (begin + o * kC + t) * p.hv * p.dv + static_cast<int64_t>(head) * p.dv + slice * kM,
+                                 sm.v[o % kVStages] + t * kM * 2, channels * 2);
+                    bulk_commit();
+                    bulk_wait_read<0>();
+                    __syncwarp();
+                }
+            }
+            if (c >= chunks) continue;
+            if (lane == 0) load_v(c);
             __syncwarp();
-            wait(&sm.through[c % kStages], phase, patience);
-            if (Y && p.y_dtype == PRECOG_BF16) {
-                const int n = len - c * kC < kC ? len - c * kC : kC;
-                for (int t = lane; t < n; t += 32)
-                    bulk_s2g(static_cast<__nv_bfloat16 *>(p.y) + (begin + c * kC + t) * p.hv * p.dv + static_cast<int64_t>(head) * p.dv + slice * kM,
-                             sm.v[c % kStages] + t * kM * 2, channels * 2);
-                bulk_commit();
-                bulk_wait_read<0>();
-                __syncwarp();
-            }
-            if (c + kStages < chunks) {
-                if (lane == 0) load_v(c + kStages);
-                __syncwarp();
-                zero_tail(c + kStages);
-            }
-            if (c + kGates < chunks) {
-                gate(c + kGates);
-                load_gates(c + kGates + 1);
+            if (c + 1 == chunks && len - c * kC < kC && !ident) {
+                wait(&sm.full_v[c % kVStages], static_cast<uint32_t>(c / kVStages) & 1u, patience);
+                zero_rows(sm.v[c % kVStages], 2, len - c * kC, lane);
+                if (lane == 0) mbar_arrive(&sm.zeroed_v);
             }
         }
         if (Y) bulk_wait_all();
         __syncwarp();
     } else if (warp >= 8) {
-        // ---------------- T and P, one chunk ahead of the chain ----------------
-        const int tid = threadIdx.x - kChain, quarter = warp & 3, group = (warp >> 2) & 1;
+        // ---------------- T and P, ahead of the chain ----------------
+        const int team = (warp >> 2) & 1, quarter = warp & 3, tid = threadIdx.x & (kTeam - 1);
         const int half = quarter & 1, i = half * kH + lane;   // this thread's row: of A (quarters 0, 1) or P
         const bool is_a = quarter < 2;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        // Column j, row i of a quarter of A and later of T, turned so that the rows or the columns of an
+        // MMA's operand lie in different banks.
+        float *a11 = sm.a[team], *a21 = a11 + kBlock, *a22 = a21 + kBlock;
+        auto place = [](int j, int r) { return j * kH + (r ^ ((j & 3) << 3)); };
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
-            const int buf = c & 1;
-            const uint32_t col = tmem + kColK + buf * kPlace;
-            const Gates &gt = sm.gates[c % kGates];
-            // column j, row i of A and later of T, turned so that the rows or the columns of an MMA's
-            // operand lie in different banks
-            float *at = reinterpret_cast<float *>(sm.tp[buf][0]);
-            auto place = [](int j, int i) { return j * kC + (i ^ ((j & 7) << 3)); };
-            wait(&sm.gated[c % kGates], static_cast<uint32_t>(c / kGates) & 1u, patience);
+        for (int c = team; c < chunks; c += 2) {
+            const uint32_t col = tmem + kColK + c % 3 * 64;
+            const Gates &gt = sm.gates[c % kStages];
+            wait(&sm.done_prep[team], static_cast<uint32_t>(c >> 1) & 1u, patience);
+            wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+            tc_fence_after();
             const Log bi{gt.bh[i], gt.bl[i]};
             const f2 bih = pack2(bi.h, bi.h), bil = pack2(bi.l, bi.l), minus = pack2(-1.f, -1.f);
             const float mine = is_a ? gt.beta[i] : p.scale;
             // two chunks ago: through with T and P
-            if (c >= 2) wait(&sm.done_o[buf], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
-            wait(&sm.done_prep[buf], static_cast<uint32_t>(c >> 1) & 1u, patience);
-            tc_fence_after();
-            // Columns of 16, by turns. Left of the diagonal half the decay from j to i goes by the last
-            // token of the 16, both factors at most 1 where nothing grows; on it each entry has its
-            // exponential.
+            if (!is_a && c >= 2) wait(&sm.done_o[team], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
+            // Columns of 16. Left of the diagonal half the decay from j to i goes by the last token of the
+            // 16, both factors at most 1 where nothing grows; on it each entry has its exponential.
 #pragma unroll 1
-            for (int j0 = group * kB; j0 < (half + 1) * kH; j0 += kH) {
+            for (int j0 = 0; j0 < (half + 1) * kH; j0 += kB) {
                 float v[16];
                 tmem_ld16(col + lanes + j0, v);
                 if (j0 < half * kH) {
@@ -516,15 +527,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int lim = i + (is_a ? 0 : 1) - j0;
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
-                        float a, b;
-                        unpack2(fma2(load2(gt.bl + j0 + e), minus, fma2(fma2(load2(gt.bh + j0 + e), minus, bih), pack2(1.f, 1.f), bil)), a, b);
-                        v[e] = e < lim ? v[e] * (ex2(a) * mine) : 0.f;
-                        v[e + 1] = e + 1 < lim ? v[e + 1] * (ex2(b) * mine) : 0.f;
+                        float x, y;
+                        unpack2(fma2(load2(gt.bl + j0 + e), minus, fma2(fma2(load2(gt.bh + j0 + e), minus, bih), pack2(1.f, 1.f), bil)), x, y);
+                        v[e] = e < lim ? v[e] * (ex2(x) * mine) : 0.f;
+                        v[e + 1] = e + 1 < lim ? v[e + 1] * (ex2(y) * mine) : 0.f;
                     }
                 }
                 if (is_a) {
+                    float *to = (half == 0 ? a11 : j0 < kH ? a21 : a22) + (j0 & (kH - 1)) * kH;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) at[(j0 + e) * kC + (i ^ ((e & 7) << 3))] = v[e];
+                    for (int e = 0; e < 16; ++e) to[e * kH + (lane ^ ((e & 3) << 3))] = v[e];
                 } else {
 #pragma unroll
                     for (int o = 0; o < 16; o += 8) {
@@ -532,17 +544,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) split(v[o + 2 * e], v[o + 2 * e + 1], h[e], l[e]);
                         const int to = i * 128 + (((j0 + o) / 8) ^ (i & 7)) * 16;
-                        *reinterpret_cast<uint4 *>(sm.tp[buf][2] + to) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4 *>(sm.tp[buf][3] + to) = make_uint4(l[0], l[1], l[2], l[3]);
+                        *reinterpret_cast<uint4 *>(sm.tp[team][2] + to) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4 *>(sm.tp[team][3] + to) = make_uint4(l[0], l[1], l[2], l[3]);
                     }
                 }
             }
             tc_fence_before();
-            if (is_a) named_sync(kBarHalf + half, 64);   // the two warps of A's rows
+            __syncwarp();
             // ---- (I + A)^-1 of one half a warp: two blocks of 16, a column a lane ----
             const int g = lane >> 2, t = lane & 3;   // an MMA's row or column, and its pair
-            if (is_a && half == group) {
-                const int lo = half * kH, up = lo + kB, b = lo + (lane & 16), cc = lane & 15;
+            if (is_a) {
+                float *a = half == 0 ? a11 : a22;
+                const int b = lane & 16, cc = lane & 15;
                 f2 x[kB / 2];
 #pragma unroll
                 for (int e = 0; e < kB / 2; ++e) x[e] = pack2(2 * e == cc ? 1.f : 0.f, 2 * e + 1 == cc ? 1.f : 0.f);
@@ -555,88 +568,103 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const f2 mm = pack2(m, m);
 #pragma unroll
                     for (int e = (l + 1) / 4 * 4; e < kB; e += 4) {
-                        const float4 a = *reinterpret_cast<const float4 *>(at + (b + l) * kC + ((b + e) ^ ((l & 7) << 3)));
-                        x[e / 2] = fma2(pack2(a.x, a.y), mm, x[e / 2]);
-                        x[e / 2 + 1] = fma2(pack2(a.z, a.w), mm, x[e / 2 + 1]);
+                        const float4 w = *reinterpret_cast<const float4 *>(a + (b + l) * kH + ((b + e) ^ ((l & 3) << 3)));
+                        x[e / 2] = fma2(pack2(w.x, w.y), mm, x[e / 2]);
+                        x[e / 2 + 1] = fma2(pack2(w.z, w.w), mm, x[e / 2 + 1]);
                     }
                 }
                 __syncwarp();
 #pragma unroll
                 for (int e = 0; e < kB; e += 4) {
-                    float4 a;
-                    unpack2(x[e / 2], a.x, a.y);
-                    unpack2(x[e / 2 + 1], a.z, a.w);
-                    *reinterpret_cast<float4 *>(at + (b + cc) * kC + ((b + e) ^ ((cc & 7) << 3))) = a;
+                    float4 w;
+                    unpack2(x[e / 2], w.x, w.y);
+                    unpack2(x[e / 2 + 1], w.z, w.w);
+                    *reinterpret_cast<float4 *>(a + (b + cc) * kH + ((b + e) ^ ((cc & 3) << 3))) = w;
                 }
                 __syncwarp();
                 // T1 A10, whose columns 2 t, 2 t + 1 of 8 then count as the A operand's t and t + 4
                 Sums3 h[2], d[2];
 #pragma unroll
                 for (int k = 0; k < kB; k += 8) {
-                    const float a[4] = {at[place(up + k + t, up + g)], at[place(up + k + t, up + g + 8)],
-                                        at[place(up + k + t + 4, up + g)], at[place(up + k + t + 4, up + g + 8)]};
+                    const float w[4] = {a[place(kB + k + t, kB + g)], a[place(kB + k + t, kB + g + 8)],
+                                        a[place(kB + k + t + 4, kB + g)], a[place(kB + k + t + 4, kB + g + 8)]};
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
-                        mma_3tf32(h[n], a, {at[place(lo + 8 * n + g, up + k + t)], at[place(lo + 8 * n + g, up + k + t + 4)]});
+                        mma_3tf32(h[n], w, {a[place(8 * n + g, kB + k + t)], a[place(8 * n + g, kB + k + t + 4)]});
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float a[4] = {h[k][0], h[k][2], h[k][1], h[k][3]};
+                    const float w[4] = {h[k][0], h[k][2], h[k][1], h[k][3]};
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
-                        mma_3tf32(d[n], a, {at[place(lo + 8 * n + g, lo + 8 * k + 2 * t)], at[place(lo + 8 * n + g, lo + 8 * k + 2 * t + 1)]});
+                        mma_3tf32(d[n], w, {a[place(8 * n + g, 8 * k + 2 * t)], a[place(8 * n + g, 8 * k + 2 * t + 1)]});
                 }
                 __syncwarp();   // A10 has been read
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) at[place(lo + 8 * n + 2 * t + (e & 1), up + g + (e & 2) * 4)] = -d[n][e];
+                    for (int e = 0; e < 4; ++e) a[place(8 * n + 2 * t + (e & 1), kB + g + (e & 2) * 4)] = -d[n][e];
             }
-            named_sync(kBarPrep, kPrep);
-            // ---- joined: 16 rows and 8 columns of T22 A21, then of T21, a warp ----
+            named_sync(kBarTeam + team, kTeam);
+            // ---- joined: 8 columns a warp, T22 A21 in the place of A21 and then T21 in its place ----
             {
-                const int r = (warp & 1) * 16, n = (warp >> 1 & 3) * 8;
-                Sums3 d;
+                const int n = quarter * 8;
+                Sums3 d[2];
 #pragma unroll
-                for (int k = 0; k < kH; k += 8)
-                    mma_3tf32(d, {at[place(kH + k + t, kH + r + g)], at[place(kH + k + t, kH + r + g + 8)],
-                                  at[place(kH + k + t + 4, kH + r + g)], at[place(kH + k + t + 4, kH + r + g + 8)]},
-                              {at[place(n + g, kH + k + t)], at[place(n + g, kH + k + t + 4)]});
+                for (int k = 0; k < kH; k += 8) {
+                    const float w[2] = {a21[place(n + g, k + t)], a21[place(n + g, k + t + 4)]};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sm.mid[(r + g + (e & 2) * 4) * kPitch + n + 2 * t + (e & 1)] = d[e];
-                named_sync(kBarPrep, kPrep);
-                d = Sums3();
-                const float *mid = sm.mid + (r + g) * kPitch + t;
+                    for (int r = 0; r < 2; ++r)
+                        mma_3tf32(d[r], {a22[place(k + t, 16 * r + g)], a22[place(k + t, 16 * r + g + 8)],
+                                         a22[place(k + t + 4, 16 * r + g)], a22[place(k + t + 4, 16 * r + g + 8)]}, w);
+                }
+                __syncwarp();   // these columns have been read
 #pragma unroll
-                for (int k = 0; k < kH; k += 8)
-                    mma_3tf32(d, {mid[k], mid[8 * kPitch + k], mid[k + 4], mid[8 * kPitch + k + 4]},
-                              {at[place(n + g, k + t)], at[place(n + g, k + t + 4)]});
+                for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) at[place(n + 2 * t + (e & 1), kH + r + g + (e & 2) * 4)] = -d[e];
+                    for (int e = 0; e < 4; ++e) a21[place(n + 2 * t + (e & 1), 16 * r + g + (e & 2) * 4)] = d[r][e];
+                named_sync(kBarTeam + team, kTeam);
+                d[0] = d[1] = Sums3();
+#pragma unroll
+                for (int k = 0; k < kH; k += 8) {
+                    const float w[2] = {a11[place(n + g, k + t)], a11[place(n + g, k + t + 4)]};
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        mma_3tf32(d[r], {a21[place(k + t, 16 * r + g)], a21[place(k + t, 16 * r + g + 8)],
+                                         a21[place(k + t + 4, 16 * r + g)], a21[place(k + t + 4, 16 * r + g + 8)]}, w);
+                }
+                named_sync(kBarTeam + team, kTeam);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a21[place(n + 2 * t + (e & 1), 16 * r + g + (e & 2) * 4)] = -d[r][e];
             }
-            named_sync(kBarPrep, kPrep);
-            // ---- T diag(beta) as a pair: 16 columns of a row a thread ----
-            {
-                const int row = tid & (kC - 1), j0 = (tid / kC) * kB;
-                const bool there = j0 <= row;   // (blocks right of the diagonal are zero)
-                uint32_t h[8], l[8];
+            if (is_a && c >= 2) wait(&sm.done_o[team], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
+            named_sync(kBarTeam + team, kTeam);
+            // ---- T diag(beta) as a pair: a row's 32 columns a thread ----
+            const int row = tid & (kC - 1), j1 = tid / kC * kH;
+            if (j1 <= row) {   // (whole warps)
+                const float *from = row < kH ? a11 : j1 ? a22 : a21;
+#pragma unroll 1
+                for (int j0 = 0; j0 < kH; j0 += kB) {
+                    uint32_t h[8], l[8];
 #pragma unroll
-                for (int e = 0; e < kB; e += 2)
-                    split(mul2(pack2(there ? at[(j0 + e) * kC + (row ^ ((e & 7) << 3))] : 0.f, there ? at[(j0 + e + 1) * kC + (row ^ (((e + 1) & 7) << 3))] : 0.f),
-                               load2(gt.beta + j0 + e)),
-                          h[e / 2], l[e / 2]);
-                named_sync(kBarPrep, kPrep);
+                    for (int e = 0; e < kB; e += 2)
+                        split(mul2(pack2(from[(j0 + e) * kH + (lane ^ ((e & 3) << 3))], from[(j0 + e + 1) * kH + (lane ^ (((e + 1) & 3) << 3))]),
+                                   load2(gt.beta + j1 + j0 + e)),
+                              h[e / 2], l[e / 2]);
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const int to = row * 128 + ((j0 / 8 + o) ^ (row & 7)) * 16;
-                    *reinterpret_cast<uint4 *>(sm.tp[buf][0] + to) = make_uint4(h[4 * o], h[4 * o + 1], h[4 * o + 2], h[4 * o + 3]);
-                    *reinterpret_cast<uint4 *>(sm.tp[buf][1] + to) = make_uint4(l[4 * o], l[4 * o + 1], l[4 * o + 2], l[4 * o + 3]);
+                    for (int o = 0; o < 2; ++o) {
+                        const int to = row * 128 + (((j1 + j0) / 8 + o) ^ (row & 7)) * 16;
+                        *reinterpret_cast<uint4 *>(sm.tp[team][0] + to) = make_uint4(h[4 * o], h[4 * o + 1], h[4 * o + 2], h[4 * o + 3]);
+                        *reinterpret_cast<uint4 *>(sm.tp[team][1] + to) = make_uint4(l[4 * o], l[4 * o + 1], l[4 * o + 2], l[4 * o + 3]);
+                    }
                 }
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.ready[buf]);
-            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.ready[team]);
+            named_sync(kBarTeam + team, kTeam);   // A may be written again
         }
     } else {
         // ---------------- the chain ----------------
@@ -703,8 +731,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = 0; c <= chunks; ++c) {   // the last turn only leaves the last chunk
             const int buf = c & 1;
             const uint32_t ph = static_cast<uint32_t>(c) & 1u;
-            const Gates &gt = sm.gates[c % kGates];
-            const uint32_t col_k = tm + kColK + buf * kPlace + half * 32, col_q = tm + kColQ + buf * kPlace + half * 32;
+            const Gates &gt = sm.gates[c % kStages];
+            const uint32_t col_k = tm + kColK + c % 3 * 64 + half * 32, col_q = tm + kColQ + half * 32;
             if (c < chunks) {
                 // ---- S as a pair ----
 #pragma unroll 1
@@ -722,8 +750,57 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_st16(tm + kColPair + kHalf + (half * kHalf + g) / 2, l);
                 }
                 hand_over(&sm.have_s);
-                // ---- S decayed, while S k and S q are formed ----
-                wait(&sm.gated[c % kGates], static_cast<uint32_t>(c / kGates) & 1u, patience);
+            } else if (c > 0) {
+                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
+                tc_fence_after();
+            }
+            if (c > 0) {
+                // ---- y of the chunk before, tokens 32 half .. , while S k is formed ----
+                if (Y) {
+                    uint32_t r[32];
+                    tmem_ld32_async(col_q, r);
+                    tmem_ld_wait(r);
+                    const int t0 = (c - 1) * kC + half * 32;
+                    if (p.y_dtype == PRECOG_F32) {
+                        float *to = static_cast<float *>(p.y) + (begin + t0) * y_row + static_cast<int64_t>(head) * p.dv + ch;
+                        if (live) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e, to += y_row)
+                                if (t0 + e < len) *to = __uint_as_float(r[e]);
+                        }
+                    } else {   // rows of 128 channels, for the copies
+                        uint16_t *to = reinterpret_cast<uint16_t *>(sm.v[(c - 1) % kVStages]) + half * 32 * kM + row;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const uint32_t w = bits2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
+                            to[2 * e * kM] = static_cast<uint16_t>(w);
+                            to[(2 * e + 1) * kM] = static_cast<uint16_t>(w >> 16);
+                        }
+                        fence_proxy_async_smem();
+                    }
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.through[(c - 1) % kVStages]);
+                __syncwarp();
+            }
+            if (c == chunks) break;
+            {
+                wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
+                wait(&sm.done_ks, ph, patience);
+                tc_fence_after();
+                {
+                    uint32_t r[32], h[16], l[16];
+                    tmem_ld32_async(col_k, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
+                    tmem_st16(col_k, h);
+                    tmem_st16(col_k + 16, l);
+                }
+                hand_over(&sm.have_k);
+                // ---- S decayed, while U is formed ----
                 const f2 whole = pack2(gt.whole, gt.whole);
 #pragma unroll 1
                 for (int g = 0; g < kHalf; g += 32) {
@@ -739,19 +816,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tmem_st32(col_s + g, r);
                 }
-                // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
-                wait(&sm.done_ks, ph, patience);
-                tc_fence_after();
-                {
-                    uint32_t r[32], h[16], l[16];
-                    tmem_ld32_async(col_k, r);
-                    tmem_ld_wait(r);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
-                    tmem_st16(col_k, h);
-                    tmem_st16(col_k + 16, l);
-                }
-                hand_over(&sm.have_k);
                 if (Y) {   // scale e^b S q: P U adds to it
                     wait(&sm.done_qs, ph, patience);
                     tc_fence_after();
@@ -787,41 +851,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         hand_over(&sm.have_u);
                     }
                 }
-            } else if (c > 0) {
-                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
-                tc_fence_after();
             }
-            if (c > 0) {
-                // ---- y of the chunk before, tokens 32 half .. , while the update runs ----
-                if (Y) {
-                    uint32_t r[32];
-                    tmem_ld32_async(tm + kColQ + (buf ^ 1) * kPlace + half * 32, r);
-                    tmem_ld_wait(r);
-                    const int t0 = (c - 1) * kC + half * 32;
-                    if (p.y_dtype == PRECOG_F32) {
-                        float *to = static_cast<float *>(p.y) + (begin + t0) * y_row + static_cast<int64_t>(head) * p.dv + ch;
-                        if (live) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e, to += y_row)
-                                if (t0 + e < len) *to = __uint_as_float(r[e]);
-                        }
-                    } else {   // rows of 128 channels, for the copies
-                        uint16_t *to = reinterpret_cast<uint16_t *>(sm.v[(c - 1) % kStages]) + half * 32 * kM + row;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const uint32_t w = bits2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                            to[2 * e * kM] = static_cast<uint16_t>(w);
-                            to[(2 * e + 1) * kM] = static_cast<uint16_t>(w >> 16);
-                        }
-                        fence_proxy_async_smem();
-                    }
-                    tc_fence_before();
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.through[(c - 1) % kStages]);
-                __syncwarp();
-            }
-            if (c < chunks) {
+            {
                 wait(&sm.done_s, ph, patience);
                 tc_fence_after();
             }
