@@ -126,10 +126,11 @@ __global__ void __launch_bounds__(kThreads) delta_step_kernel(const DeltaParams 
     }
 }
 
-// The scan: the state of R rows a thread stays in registers, tokens pass through shared memory
-// in tiles of kTile. What bounds it is the chain from one token's state to the next's (a dot
-// product over the lane's columns, three shuffles, one update), so CTAs hold few rows and many
-// share an SM.
+// The scan: the state of R rows a thread stays in registers, tokens pass through shared memory in
+// tiles of kTile, the next tile's loads in flight behind this one's tokens. What bounds it is the
+// chain from one token's state to the next's: a dot product over the lane's columns in four parallel
+// sums, three shuffles, one update. Everything else runs beside it: S q shares the shuffles' time,
+// e^g S is formed meanwhile, and the next token's rows are read a token ahead.
 constexpr int kTile = 16;
 
 template <typename T, int J, int R>
@@ -181,70 +182,104 @@ __global__ void __launch_bounds__(kThreads) delta_token_scan_kernel(const DeltaP
     const T *qg = want_y ? static_cast<const T *>(p.q) + static_cast<int64_t>(qk) * p.dk : nullptr;
     const T *vg = static_cast<const T *>(p.v) + static_cast<int64_t>(head) * p.dv + row_base;
     const int groups = p.dk / 4;
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 nk[J], nq[J];          // the next tile, on its way
+    float nv[2 * R], ng = 0.f, nb = 0.f;
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int e = threadIdx.x + j * kThreads, t = e / (kCols / 4), c = e % (kCols / 4);
+            const bool there = t0 + t < end && c < groups;
+            nk[j] = there ? load4(kg + (t0 + t) * p.k_stride + 4 * c) : zero;
+            nq[j] = there && want_y ? load4(qg + (t0 + t) * p.q_stride + 4 * c) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * R; ++i) {
+            const int e = threadIdx.x + i * kThreads, t = e / kRows, c = e % kRows;
+            nv[i] = t0 + t < end && row_base + c < p.dv ? to_f32(vg[(t0 + t) * p.v_stride + c]) : 0.f;
+        }
+        if (threadIdx.x < kTile && t0 + threadIdx.x < end) {
+            ng = p.g[(t0 + threadIdx.x) * p.hv + head];
+            nb = p.beta[(t0 + threadIdx.x) * p.hv + head];
+        }
+    };
+    if (begin < end) fetch(begin);
     for (int64_t t0 = begin; t0 < end; t0 += kTile) {
         const int n = end - t0 < kTile ? static_cast<int>(end - t0) : kTile;
         __syncthreads();
-        for (int e = threadIdx.x; e < n * (kCols / 4); e += kThreads) {
-            const int t = e / (kCols / 4), c = e % (kCols / 4);
-            const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-            sk4[t][c] = c < groups ? load4(kg + (t0 + t) * p.k_stride + 4 * c) : zero;
-            sq4[t][c] = want_y && c < groups ? load4(qg + (t0 + t) * p.q_stride + 4 * c) : zero;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int e = threadIdx.x + j * kThreads;
+            (&sk4[0][0])[e] = nk[j];
+            (&sq4[0][0])[e] = nq[j];
         }
-        for (int e = threadIdx.x; e < n * kRows; e += kThreads) {
-            const int t = e / kRows, c = e % kRows;
-            sv[t][c] = row_base + c < p.dv ? to_f32(vg[(t0 + t) * p.v_stride + c]) : 0.f;
-        }
-        if (threadIdx.x < n) {
-            sg[threadIdx.x] = decay_of(p.g[(t0 + threadIdx.x) * p.hv + head]);
-            sb[threadIdx.x] = p.beta[(t0 + threadIdx.x) * p.hv + head];
+#pragma unroll
+        for (int i = 0; i < 2 * R; ++i) (&sv[0][0])[threadIdx.x + i * kThreads] = nv[i];
+        if (threadIdx.x < kTile) {
+            sg[threadIdx.x] = decay_of(ng);
+            sb[threadIdx.x] = nb;
         }
         __syncthreads();
+        if (t0 + kTile < end) fetch(t0 + kTile);
         if (want_y) {
             // k.q of the tile's tokens: 8 lanes a token
             const int t = threadIdx.x / kLanes;   // kTile == kRowSets
             float kq = 0.f;
-            if (t < n)
 #pragma unroll
-                for (int j = 0; j < J; ++j) kq = dot4(sk4[t][lane8 + kLanes * j], sq4[t][lane8 + kLanes * j], kq);
+            for (int j = 0; j < J; ++j) kq = dot4(sk4[t][lane8 + kLanes * j], sq4[t][lane8 + kLanes * j], kq);
             kq = row_sum(kq);
             if (lane8 == 0) skq[t] = kq;
             __syncthreads();
         }
-#pragma unroll 1
+        float4 k[J], q[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            k[j] = sk4[0][lane8 + kLanes * j];
+            q[j] = sq4[0][lane8 + kLanes * j];
+        }
+#pragma unroll 2
         for (int t = 0; t < n; ++t) {
             const float a = sg[t], b = sb[t];
             float sk[R], sq[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) sk[r] = sq[r] = 0.f;
-            float4 k[J];
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                k[j] = sk4[t][lane8 + kLanes * j];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    s[r][j] = scale4(a, s[r][j]);
-                    sk[r] = dot4(s[r][j], k[j], sk[r]);
-                }
-            }
-            if (want_y)
+            for (int r = 0; r < R; ++r) {
+                float4 x = zero, y = zero;        // four sums each
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const float4 q = sq4[t][lane8 + kLanes * j];
+                    x = make_float4(fmaf(s[r][j].x, k[j].x, x.x), fmaf(s[r][j].y, k[j].y, x.y), fmaf(s[r][j].z, k[j].z, x.z), fmaf(s[r][j].w, k[j].w, x.w));
+                    y = make_float4(fmaf(s[r][j].x, q[j].x, y.x), fmaf(s[r][j].y, q[j].y, y.y), fmaf(s[r][j].z, q[j].z, y.z), fmaf(s[r][j].w, q[j].w, y.w));
+                }
+                sk[r] = (x.x + x.y) + (x.z + x.w);
+                sq[r] = (y.x + y.y) + (y.z + y.w);
+            }
+            const int ahead = t + 1 < kTile ? t + 1 : t;
+            float4 k1[J], q1[J];
 #pragma unroll
-                    for (int r = 0; r < R; ++r) sq[r] = dot4(s[r][j], q, sq[r]);
+            for (int j = 0; j < J; ++j) {
+                k1[j] = sk4[ahead][lane8 + kLanes * j];
+                q1[j] = sq4[ahead][lane8 + kLanes * j];
+            }
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    sk[r] += __shfl_xor_sync(0xffffffffu, sk[r], o);
+                    sq[r] += __shfl_xor_sync(0xffffffffu, sq[r], o);
                 }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int row = row_in + r * kRowSets;
-                const float u = b * (sv[t][row] - row_sum(sk[r]));
+                const float u = b * fmaf(-a, sk[r], sv[t][row]);
 #pragma unroll
-                for (int j = 0; j < J; ++j) s[r][j] = axpy4(u, k[j], s[r][j]);
+                for (int j = 0; j < J; ++j) s[r][j] = axpy4(u, k[j], scale4(a, s[r][j]));
                 if (want_y) {
-                    const float y = p.scale * fmaf(u, skq[t], row_sum(sq[r]));
+                    const float y = p.scale * fmaf(u, skq[t], a * sq[r]);
                     if (lane8 == 0 && row_base + row < p.dv)
                         store_any(p.y, p.y_dtype, ((t0 + t) * p.hv + head) * p.dv + row_base + row, y);
                 }
             }
+#pragma unroll
+            for (int j = 0; j < J; ++j) k[j] = k1[j], q[j] = q1[j];
         }
     }
     if (p.states == nullptr) return;
@@ -269,9 +304,8 @@ cudaError_t step_rows(const DeltaParams &p, cudaStream_t stream) {
     return e;
 }
 
-template <typename T, int J>
+template <typename T, int J, int R>
 cudaError_t scan_rows(const DeltaParams &p, cudaStream_t stream) {
-    constexpr int R = 1;
     const int tiles = (p.dv + kRowSets * R - 1) / (kRowSets * R);
     delta_token_scan_kernel<T, J, R><<<static_cast<unsigned>(p.n_seqs * p.hv * tiles), kThreads, 0, stream>>>(p, tiles);
     cudaError_t e = cudaGetLastError();
@@ -279,7 +313,7 @@ cudaError_t scan_rows(const DeltaParams &p, cudaStream_t stream) {
     return e;
 }
 
-static_assert(kTile == kRowSets, "the tile's k.q take 8 lanes a token");
+static_assert(kTile == kRowSets, "the tile's k.q take 8 lanes a token, and a thread fetches 2 R of v");
 
 // Two rows a thread keep more of the states in flight (256 sequences x 16 heads of 128 x 128: 90 us,
 // one row 98, four rows 93), unless that leaves an SM fewer than eight CTAs: then latency counts.
@@ -299,13 +333,20 @@ cudaError_t step_cols(const DeltaParams &p, cudaStream_t stream) {
     }
 }
 
+// Two rows a thread share what they read of a token, where that leaves the SMs two rounds of CTAs.
+template <typename T, int J>
+cudaError_t scan_tiles(const DeltaParams &p, cudaStream_t stream) {
+    return p.n_seqs * p.hv * ((p.dv + 2 * kRowSets - 1) / (2 * kRowSets)) >= 8LL * device_sm_count() ? scan_rows<T, J, 2>(p, stream)
+                                                                                                    : scan_rows<T, J, 1>(p, stream);
+}
+
 template <typename T>
 cudaError_t scan_cols(const DeltaParams &p, cudaStream_t stream) {
     switch ((p.dk + 31) / 32) {
-        case 1: return scan_rows<T, 1>(p, stream);
-        case 2: return scan_rows<T, 2>(p, stream);
-        case 3: return scan_rows<T, 3>(p, stream);
-        default: return scan_rows<T, 4>(p, stream);
+        case 1: return scan_tiles<T, 1>(p, stream);
+        case 2: return scan_tiles<T, 2>(p, stream);
+        case 3: return scan_tiles<T, 3>(p, stream);
+        default: return scan_tiles<T, 4>(p, stream);
     }
 }
 

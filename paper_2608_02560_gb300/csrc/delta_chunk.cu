@@ -109,7 +109,7 @@ struct Smem {
     Gates gates[kStages];
     uint64_t full_kq[kStages], free_kq[kStages], gated[kStages];
     uint64_t full_v[kVStages], through[kVStages];
-    uint64_t zeroed_kq, zeroed_v;
+    uint64_t zeroed_kq, zeroed_v, taken_y;
     uint64_t ready[2], done_prep[2], done_o[2];
     uint64_t have_s, have_k, have_d, have_u;      // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(&sm.zeroed_kq, 1);
         mbar_init(&sm.zeroed_v, 1);
+        mbar_init(&sm.taken_y, kChain / 32);
         mbar_init(&sm.have_s, kChain / 32);
         mbar_init(&sm.have_k, kChain / 32);
         mbar_init(&sm.have_d, kChain / 32);
@@ -315,8 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < (Y ? 2 : 1); ++q) {
-                    if (q && c > 0) {   // y of the chunk before has left
-                        wait_one(&sm.through[(c - 1) % kVStages], static_cast<uint32_t>((c - 1) / kVStages) & 1u, patience);
+                    if (q && c > 0) {   // y of the chunk before has been read
+                        wait_one(&sm.taken_y, ph ^ 1u, patience);
                         tc_fence_after();
                     }
 #pragma unroll
@@ -327,6 +328,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     tc_commit(q ? &sm.done_qs : &sm.done_ks);
                 }
+                // (its place: the pair of the chunk before, whose MMAs are done)
+                if (c + 2 < chunks) products(c + 2);
                 wait_one(Y ? &sm.done_qs : &sm.done_ks, ph, patience);   // S's pair has been read: U takes its place
                 if (!ident) {
                     wait_one(&sm.full_v[c % kVStages], static_cast<uint32_t>(c / kVStages) & 1u, patience);
@@ -345,8 +348,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                                   dt + (part == 2 ? kTile / 16 : 0) + 2 * kk, idesc(kC, false, false), !ident || k > 0);
                 }
                 tc_commit(&sm.done_u);
-                // (its place: the pair of the chunk before, whose MMAs are done)
-                if (c + 2 < chunks) products(c + 2);
                 wait_one(&sm.have_d, ph, patience);
                 tc_fence_after();
 #pragma unroll
@@ -379,9 +380,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint8_t *st = sm.kq[c % kStages];
             uint64_t *full = &sm.full_kq[c % kStages];
             mbar_arrive_expect_tx(full, NA * (Y ? 2 : 1) * kTile);
+            const int row = static_cast<int>(begin) + c * kC;
             for (int a = 0; a < NA; ++a) {
-                tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, static_cast<int>(begin) + c * kC, full);
-                if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, static_cast<int>(begin) + c * kC, full);
+                tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, row, full);
+                if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, row, full);
+                // three stages alone do not hide DRAM's latency: the next one's load finds its rows in L2
+                if (c + 1 >= kStages && c + 1 < chunks) {
+                    tma_prefetch_3d(&map_k, a * 64, qk, row + kC);
+                    if (Y) tma_prefetch_3d(&map_q, a * 64, qk, row + kC);
+                }
             }
         };
         float g[2], bt[2];   // of tokens 2 lane, 2 lane + 1 of a chunk to come
@@ -464,6 +471,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_arrive_expect_tx(full, tiles * kTile);
             for (int a = 0; a < tiles; ++a)
                 tma_load_3d(sm.v[c % kVStages] + a * kTile, &map_v, slice * kM + a * 64, head, static_cast<int>(begin) + c * kC, full);
+            for (int a = 0; a < tiles && c + 1 >= kVStages && c + 1 < chunks; ++a)
+                tma_prefetch_3d(&map_v, slice * kM + a * 64, head, static_cast<int>(begin) + (c + 1) * kC);
         };
 #pragma unroll 1
         for (int c = 0; c < chunks + kVStages; ++c) {
@@ -727,6 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         };
         const int64_t y_row = static_cast<int64_t>(p.hv) * p.dv;
+        if (chunks > 0) wait(&sm.gated[0], 0, patience);
 #pragma unroll 1
         for (int c = 0; c <= chunks; ++c) {   // the last turn only leaves the last chunk
             const int buf = c & 1;
@@ -760,6 +770,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     uint32_t r[32];
                     tmem_ld32_async(col_q, r);
                     tmem_ld_wait(r);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.taken_y);
                     const int t0 = (c - 1) * kC + half * 32;
                     if (p.y_dtype == PRECOG_F32) {
                         float *to = static_cast<float *>(p.y) + (begin + t0) * y_row + static_cast<int64_t>(head) * p.dv + ch;
@@ -778,84 +791,79 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         fence_proxy_async_smem();
                     }
-                    tc_fence_before();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.through[(c - 1) % kVStages]);
                 __syncwarp();
             }
             if (c == chunks) break;
+            // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
+            wait(&sm.done_ks, ph, patience);
+            tc_fence_after();
             {
-                wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                // ---- -e^b S k as a pair in its own place: hi of this half's 32 tokens, then lo ----
-                wait(&sm.done_ks, ph, patience);
-                tc_fence_after();
-                {
-                    uint32_t r[32], h[16], l[16];
-                    tmem_ld32_async(col_k, r);
-                    tmem_ld_wait(r);
+                uint32_t r[32], h[16], l[16];
+                tmem_ld32_async(col_k, r);
+                tmem_ld_wait(r);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
-                    tmem_st16(col_k, h);
-                    tmem_st16(col_k + 16, l);
-                }
-                hand_over(&sm.have_k);
-                // ---- S decayed, while U is formed ----
-                const f2 whole = pack2(gt.whole, gt.whole);
+                for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ek + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
+                tmem_st16(col_k, h);
+                tmem_st16(col_k + 16, l);
+            }
+            hand_over(&sm.have_k);
+            // ---- S decayed, while U is formed ----
+            const f2 whole = pack2(gt.whole, gt.whole);
 #pragma unroll 1
-                for (int g = 0; g < kHalf; g += 32) {
-                    uint32_t r[32];
-                    tmem_ld32_async(col_s + g, r);
-                    tmem_ld_wait(r);
+            for (int g = 0; g < kHalf; g += 32) {
+                uint32_t r[32];
+                tmem_ld32_async(col_s + g, r);
+                tmem_ld_wait(r);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float a, b;
-                        unpack2(mul2(pair_of(r, e), whole), a, b);
-                        r[2 * e] = __float_as_uint(a);
-                        r[2 * e + 1] = __float_as_uint(b);
-                    }
-                    tmem_st32(col_s + g, r);
+                for (int e = 0; e < 16; ++e) {
+                    float a, b;
+                    unpack2(mul2(pair_of(r, e), whole), a, b);
+                    r[2 * e] = __float_as_uint(a);
+                    r[2 * e + 1] = __float_as_uint(b);
                 }
-                if (Y) {   // scale e^b S q: P U adds to it
-                    wait(&sm.done_qs, ph, patience);
-                    tc_fence_after();
-                    uint32_t r[32];
-                    tmem_ld32_async(col_q, r);
-                    tmem_ld_wait(r);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float a, b;
-                        unpack2(mul2(load2(gt.eq + half * 32 + 2 * e), pair_of(r, e)), a, b);
-                        r[2 * e] = __float_as_uint(a);
-                        r[2 * e + 1] = __float_as_uint(b);
-                    }
-                    tmem_st32(col_q, r);
-                }
-                // ---- U decayed to the chunk's end, as a pair in U's place, for the update; then U's pair ----
-                wait(&sm.done_u, ph, patience);
-                tc_fence_after();
-                {
-                    uint32_t r[32], h[16], l[16];
-                    tmem_ld32_async(tm + kColPair + half * 32, r);
-                    tmem_ld_wait(r);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ec + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
-                    tmem_st16(tm + kColPair + half * 32, h);
-                    tmem_st16(tm + kColPair + half * 32 + 16, l);
-                    hand_over(&sm.have_d);
-                    if (Y) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
-                        tmem_st16(tm + kColPair + 64 + half * 32, h);
-                        tmem_st16(tm + kColPair + 64 + half * 32 + 16, l);
-                        hand_over(&sm.have_u);
-                    }
-                }
+                tmem_st32(col_s + g, r);
             }
+            if (Y) {   // scale e^b S q: P U adds to it
+                wait(&sm.done_qs, ph, patience);
+                tc_fence_after();
+                uint32_t r[32];
+                tmem_ld32_async(col_q, r);
+                tmem_ld_wait(r);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float a, b;
+                    unpack2(mul2(load2(gt.eq + half * 32 + 2 * e), pair_of(r, e)), a, b);
+                    r[2 * e] = __float_as_uint(a);
+                    r[2 * e + 1] = __float_as_uint(b);
+                }
+                tmem_st32(col_q, r);
+            }
+            // ---- U decayed to the chunk's end, as a pair in U's place, for the update; then U's pair ----
+            wait(&sm.done_u, ph, patience);
+            tc_fence_after();
             {
-                wait(&sm.done_s, ph, patience);
-                tc_fence_after();
+                uint32_t r[32], h[16], l[16];
+                tmem_ld32_async(tm + kColPair + half * 32, r);
+                tmem_ld_wait(r);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) split(mul2(load2(gt.ec + half * 32 + 2 * e), pair_of(r, e)), h[e], l[e]);
+                tmem_st16(tm + kColPair + half * 32, h);
+                tmem_st16(tm + kColPair + half * 32 + 16, l);
+                hand_over(&sm.have_d);
+                if (Y) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
+                    tmem_st16(tm + kColPair + 64 + half * 32, h);
+                    tmem_st16(tm + kColPair + 64 + half * 32 + 16, l);
+                    hand_over(&sm.have_u);
+                }
             }
+            if (c + 1 < chunks) wait(&sm.gated[(c + 1) % kStages], static_cast<uint32_t>((c + 1) / kStages) & 1u, patience);
+            wait(&sm.done_s, ph, patience);
+            tc_fence_after();
         }
         if (kept || (last && p.states)) {
             void *to = kept ? (ident ? cut.moves : cut.states) : p.states;

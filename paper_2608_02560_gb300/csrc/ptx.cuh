@@ -120,6 +120,11 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const void *tmap, int32_t
         : "memory");
 }
 
+// The same into L2 alone.
+__device__ __forceinline__ void tma_prefetch_3d(const void *tmap, int32_t c0, int32_t c1, int32_t c2) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(tmap), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
 // 4-D tiled TMA load, as tma_load_2d; coordinates innermost first.
 __device__ __forceinline__ void tma_load_4d(void *dst, const void *tmap, int32_t c0, int32_t c1, int32_t c2,
                                             int32_t c3, uint64_t *bar) {
