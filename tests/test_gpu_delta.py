@@ -208,6 +208,43 @@ def test_long_sequences(cuda_device, T, heads):
     assert pg.precog_device_status()[0] == 0
 
 
+@pytest.mark.parametrize("n,hv,dk,dv,most,y_dtype", [
+    (200, 2, 64, 64, 200, "bfloat16"), (170, 1, 128, 136, 130, "float32"), (400, 1, 40, 24, 70, None),
+    (160, 1, 128, 128, 1, "bfloat16")])
+def test_many_short_sequences(cuda_device, n, hv, dk, dv, most, y_dtype):
+    """More items than SMs, of a few chunks each (empty ones among them): they pass through the CTAs as
+    streams. One item has bad offsets, others rows of the bank that do not exist."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    r = np.random.default_rng(n)
+    lens = [int(x) for x in r.integers(0, most + 1, n)]
+    lens[0] = max(most, 9 * n - sum(lens))            # (long enough on average not to go token by token)
+    q, k, v, g, beta, off = _tensors(lens, 1, hv, dk, dv, torch.bfloat16, cuda_device, n)
+    T = sum(lens)
+    bank = torch.randn((5, 1, hv, dv, dk), device=cuda_device)
+    rows = [int(x) for x in r.integers(-1, 5, n)]
+    idx = torch.tensor(rows, device=cuda_device)
+    S0 = np.stack([to_np(bank[i, 0]) if i >= 0 else np.zeros((hv, dv, dk)) for i in rows])
+    states = torch.full((n, 1, hv, dv, dk), 7.0, device=cuda_device)
+    y = torch.full((T, hv, dv), float("nan"), dtype=getattr(torch, y_dtype), device=cuda_device) if y_dtype else None
+    inputs = pg.delta_inputs(q, k, v, g, beta)
+    pg.precog_delta_scan(inputs, off, T, bank=bank, idx=idx, states_out=states, y_out=y)
+    assert pg.precog_device_status()[0] == 0
+    ref_S, ref_y = _ref(q, k, v, g, beta, off, S0)
+    _check(states[:, 0], ref_S, TOL_PAIR)
+    if y_dtype:
+        _check(y, ref_y, TOL_PAIR)
+    first = states.clone()
+    bad = off.clone()
+    bad[5] = T + 1                                     # sequences 4 and 5
+    idx[7] = 5
+    pg.precog_delta_scan(inputs, bad, T, bank=bank, idx=idx, states_out=states.fill_(7.0), y_out=y)
+    assert pg.precog_device_status() == (5, pg.PRECOG_DEV_BAD_OFFSETS | pg.PRECOG_DEV_BAD_INDEX)
+    keep = torch.ones(n, dtype=torch.bool, device=cuda_device)
+    keep[[4, 5, 7]] = False
+    assert torch.equal(states[keep], first[keep]) and bool((states[4:6] == 7.0).all())
+
+
 CUT = [
     # lens, hv, dk, dv, bank, want_y: few sequences whose mean is long, so that they are cut (the
     # first one's mean is just too short to be)
