@@ -358,7 +358,22 @@ cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream) {
 
 namespace {
 
-bool in_chunks(const DeltaParams &p) { return p.in_dtype == PRECOG_BF16 && p.T_tot >= 8 * p.n_seqs; }
+// Whether the chunk kernel is the faster one, by what both measured (16 heads of 128 x 128 unless said):
+//   1 sequence of 32 / 48 tokens    token 9.9 / 13.7 us   chunk 12.5 / 12.2
+//   4 sequences of 16 / 24          token 10.3 / 14.7     chunk 13.3 / 13.0
+//   16 of 8 / 12                    token 21.8 / 27.3     chunk 26.3 / 26.1
+//   256 of 8 / 16                   token 259 / 406       chunk 352 / 347
+//   64 of 40 / 48, 64 x 64          token 67 / 78         chunk 70 / 72
+// A round of CTAs in chunks takes 12 us however few its tokens are. A token of the other kernel takes
+// 0.25 us by its latency, or 6.2 ns a head of 128 x 128 where the SMs are full. Lengths lie on the
+// device: the rule knows their mean.
+bool in_chunks(const DeltaParams &p) {
+    if (p.in_dtype != PRECOG_BF16 || p.n_seqs <= 0) return false;
+    const double heads = static_cast<double>(p.n_seqs) * p.hv, tokens = static_cast<double>(p.T_tot) / p.n_seqs;
+    const double rounds = ceil(heads * ((p.dv + 127) / 128) / device_sm_count());
+    const double token = fmax(0.25, 0.0062 * heads * p.dk * p.dv / (128 * 128));
+    return 3.5 + tokens * token > 12 * rounds;
+}
 
 }  // namespace
 

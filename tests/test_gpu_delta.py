@@ -212,13 +212,13 @@ def test_long_sequences(cuda_device, T, heads):
     (200, 2, 64, 64, 200, "bfloat16"), (170, 1, 128, 136, 130, "float32"), (400, 1, 40, 24, 70, None),
     (160, 1, 128, 128, 1, "bfloat16")])
 def test_many_short_sequences(cuda_device, n, hv, dk, dv, most, y_dtype):
-    """More items than SMs, of a few chunks each (empty ones among them): they pass through the CTAs as
-    streams. One item has bad offsets, others rows of the bank that do not exist."""
+    """More items than SMs, of a few chunks each (empty ones among them), and two calls of them: in the
+    second one sequence has bad offsets and another a row of the bank that does not exist."""
     import torch
     import paper_2608_02560_gb300 as pg
     r = np.random.default_rng(n)
     lens = [int(x) for x in r.integers(0, most + 1, n)]
-    lens[0] = max(most, 9 * n - sum(lens))            # (long enough on average not to go token by token)
+    lens[0] = max(most, 9 * n - sum(lens))            # (one of them longer than the rest together)
     q, k, v, g, beta, off = _tensors(lens, 1, hv, dk, dv, torch.bfloat16, cuda_device, n)
     T = sum(lens)
     bank = torch.randn((5, 1, hv, dv, dk), device=cuda_device)
