@@ -36,9 +36,9 @@
 // identity, with v = 0) of all segments but the last; then the segments' initial states one after
 // another (delta_join_kernel); then the segments themselves, with their readout.
 //
-// Tensor memory: S [128 columns]; a pair area [128]: S's pair, then U (whose place its decayed pair
-// takes) and U's pair; three places [64] by turns: a chunk's k.k and q.k, then its S k, then that
-// one's pair; and S q [64], then y.
+// Tensor memory: S [128 columns]; a pair area [128]: S's pair, then U, whose place its decayed pair
+// takes; places [64] by turns: a chunk's k.k and q.k, then its S k, then that one's pair, then U's
+// (three; four without a readout); and S q [64], then y.
 #include <cuda.h>
 
 #include "../../include/precog.h"
@@ -54,7 +54,7 @@ namespace {
 
 constexpr int kC = 64;                 // tokens of a chunk
 constexpr int kM = 128;                // value channels of a CTA
-constexpr int kStages = 3, kVStages = 2;
+constexpr int kVStages = 2;
 constexpr int kChain = 256, kTeam = 128;   // threads
 constexpr int kThreads = kChain + 2 * kTeam + 96;
 constexpr int kCopyWarp = (kChain + 2 * kTeam) / 32, kMmaWarp = kCopyWarp + 1, kValueWarp = kCopyWarp + 2;
@@ -98,20 +98,22 @@ struct alignas(16) Gates {
     float whole;          // e^{b_C}
 };
 
-template <int NA>
+template <int NA, bool Y>
 struct Smem {
+    // chunks of K and Q on their way, places for k.k in tensor memory: more where no Q and no S q need theirs
+    static constexpr int kStages = Y ? 3 : 6, kSlots = Y ? 3 : 4, kSides = Y ? 2 : 1;
     // per stage: [K][Q] tiles of key columns 0..63, then of 64..127; V's two tiles, where the chunk's
     // bf16 y rows lie on their way out
-    uint8_t kq[kStages][NA * 2 * kTile];
+    uint8_t kq[kStages][NA * kSides * kTile];
     uint8_t v[kVStages][2 * kTile];
-    uint8_t tp[2][4][kTile];          // T hi, T lo, P hi, P lo
+    uint8_t tp[2][2 * kSides][kTile]; // T hi, T lo, P hi, P lo
     float a[2][3 * kBlock];           // a team's A, by columns in quarters 11, 21, 22, and what becomes of it
     Gates gates[kStages];
     uint64_t full_kq[kStages], free_kq[kStages], gated[kStages];
     uint64_t full_v[kVStages], through[kVStages];
     uint64_t zeroed_kq, zeroed_v, taken_y;
-    uint64_t ready[2], done_prep[2], done_o[2];
-    uint64_t have_s, have_k, have_d, have_u;      // the chain's operands are in tensor memory
+    uint64_t done_prep[kSlots], free_slot[kSlots], ready[2], done_o[2];
+    uint64_t have_s[2], have_k, have_d, have_u;   // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
     uint32_t tmem_base;
 };
@@ -195,7 +197,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int kKeys = NA * 64;               // key coordinates, padded
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // (an offset, not a rounded address: the compiler would lose that it is shared memory)
-    Smem<NA> &sm = *reinterpret_cast<Smem<NA> *>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
+    using S = Smem<NA, Y>;
+    constexpr int kStages = S::kStages, kSlots = S::kSlots, kSides = S::kSides;
+    S &sm = *reinterpret_cast<S *>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     uint32_t patience = kWaitLimit;
 
@@ -254,17 +258,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&sm.free_kq[s], 1);
             mbar_init(&sm.gated[s], 1);
         }
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(&sm.done_prep[s], 1);
+            mbar_init(&sm.free_slot[s], 1);
+        }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.full_v[i], 1);
             mbar_init(&sm.through[i], kChain / 32);
             mbar_init(&sm.ready[i], kTeam / 32);
-            mbar_init(&sm.done_prep[i], 1);
             mbar_init(&sm.done_o[i], 1);
+            mbar_init(&sm.have_s[i], kChain / 32);
         }
         mbar_init(&sm.zeroed_kq, 1);
         mbar_init(&sm.zeroed_v, 1);
         mbar_init(&sm.taken_y, kChain / 32);
-        mbar_init(&sm.have_s, kChain / 32);
         mbar_init(&sm.have_k, kChain / 32);
         mbar_init(&sm.have_d, kChain / 32);
         mbar_init(&sm.have_u, kChain / 32);
@@ -279,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_relinquish();
     }
     // the blocks of T and P right of the diagonal are zero for good
-    for (int e = threadIdx.x; e < 8 * static_cast<int>(kTile) / 16; e += kThreads)
+    for (int e = threadIdx.x; e < 4 * kSides * static_cast<int>(kTile) / 16; e += kThreads)
         reinterpret_cast<uint4 *>(sm.tp[0][0])[e] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     tc_fence_before();
@@ -291,45 +298,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == kMmaWarp) {
         // ---------------- MMAs ----------------
         if (elect_one()) {
-            // [K; Q] K^T of chunk c, for the warps that work ahead
-            auto products = [&](int c) {
-                wait_one(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                // rows beyond the end are zeroed first
-                if (len - c * kC < kC) wait_one(&sm.zeroed_kq, 0, patience);
-                const uint64_t d = desc_base(sm.kq[c % kStages]);
-#pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k) {
-                    const uint64_t dk = d + (k / 4) * (2 * kTile / 16) + 2 * (k % 4);
-                    tc_mma_f16(tmem + kColK + c % 3 * 64, dk, dk, idesc(kC, false, false), k > 0);
-                }
-                tc_commit(&sm.done_prep[c & 1]);
-            };
-            if (chunks > 0) products(0);
-            if (chunks > 1) products(1);
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
                 const uint32_t ph = static_cast<uint32_t>(c) & 1u;
-                const uint32_t col_k = tmem + kColK + c % 3 * 64, col_q = tmem + kColQ;
+                const uint32_t col_k = tmem + kColK + c % kSlots * 64, col_q = tmem + kColQ;
                 const uint64_t d = desc_base(sm.kq[c % kStages]), dv = desc_base(sm.v[c % kVStages]), dt = desc_base(sm.tp[ph][0]);
+                wait_one(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+                if (len - c * kC < kC) wait_one(&sm.zeroed_kq, 0, patience);   // rows beyond the end
                 wait_one(&sm.ready[ph], static_cast<uint32_t>(c >> 1) & 1u, patience);
-                wait_one(&sm.have_s, ph, patience);
-                tc_fence_after();
+                // 16 keys of S, hi and lo, onto S k or S q; the first sets it
+                auto read_out = [&](uint32_t col, int kk, int q, bool onto) {
 #pragma unroll
-                for (int q = 0; q < (Y ? 2 : 1); ++q) {
-                    if (q && c > 0) {   // y of the chunk before has been read
+                    for (int l = 0; l < 2; ++l)
+                        tc_mma_f16_ts(col, tmem + kColPair + l * (kKeys / 2) + kk * 8,
+                                      d + ((kk / 4) * kSides + q) * (kTile / 16) + 2 * (kk % 4), idesc(kC, false, false), onto || l);
+                };
+#pragma unroll
+                for (int part = 0; part < NA; ++part) {   // 32 keys of each half as they come
+                    wait_one(&sm.have_s[part], ph, patience);
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) read_out(col_k, k / 2 * (2 * NA) + part * 2 + k % 2, 0, part + k > 0);
+                }
+                tc_commit(&sm.done_ks);
+                if (Y) {
+                    if (c > 0) {   // y of the chunk before has been read
                         wait_one(&sm.taken_y, ph ^ 1u, patience);
                         tc_fence_after();
                     }
 #pragma unroll
-                    for (int k = 0; k < kKeys / 8; ++k) {   // hi, then lo
-                        const int kk = k % (kKeys / 16);
-                        tc_mma_f16_ts(q ? col_q : col_k, tmem + kColPair + k * 8,
-                                      d + ((kk / 4) * 2 + q) * (kTile / 16) + 2 * (kk % 4), idesc(kC, false, false), k > 0);
-                    }
-                    tc_commit(q ? &sm.done_qs : &sm.done_ks);
+                    for (int k = 0; k < kKeys / 16; ++k) read_out(col_q, k, 1, k > 0);
+                    tc_commit(&sm.done_qs);
                 }
-                // (its place: the pair of the chunk before, whose MMAs are done)
-                if (c + 2 < chunks) products(c + 2);
                 wait_one(Y ? &sm.done_qs : &sm.done_ks, ph, patience);   // S's pair has been read: U takes its place
                 if (!ident) {
                     wait_one(&sm.full_v[c % kVStages], static_cast<uint32_t>(c / kVStages) & 1u, patience);
@@ -350,14 +350,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_commit(&sm.done_u);
                 wait_one(&sm.have_d, ph, patience);
                 tc_fence_after();
+                constexpr uint64_t kPast = static_cast<uint64_t>((kSides - 1) * kTile >> 4) << 16;   // Q lies between K's tiles
 #pragma unroll
-                for (int a = 0; a < NA; ++a)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {   // hi, then lo; 16 tokens = two 8-row groups of K
-                        const int kk = k % 4;
-                        tc_mma_f16_ts(tmem + kColS + a * 64, tmem + kColPair + (kk / 2) * 32 + (kk % 2) * 8 + (k / 4) * 16,
-                                      d + a * (2 * kTile / 16) + kk * (2048 / 16), idesc(64, false, true), true);
-                    }
+                for (int k = 0; k < 8; ++k) {   // hi, then lo; 16 tokens = two 8-row groups of K
+                    const int kk = k % 4;
+                    tc_mma_f16_ts(tmem + kColS, tmem + kColPair + (kk / 2) * 32 + (kk % 2) * 8 + (k / 4) * 16,
+                                  d + kPast + kk * (2048 / 16), idesc(kKeys, false, true), true);
+                }
                 tc_commit(&sm.done_s);
                 tc_commit(&sm.free_kq[c % kStages]);
                 if (Y) {
@@ -366,10 +365,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 12; ++k) {   // U hi P hi, U lo P hi, U hi P lo, onto S q
                         const int part = k / 4, kk = k % 4;
-                        tc_mma_f16_ts(col_q, tmem + kColPair + 64 + (kk / 2) * 32 + (kk % 2) * 8 + (part == 1 ? 16 : 0),
+                        tc_mma_f16_ts(col_q, col_k + (kk / 2) * 32 + (kk % 2) * 8 + (part == 1 ? 16 : 0),
                                       dt + (part == 2 ? 3 : 2) * (kTile / 16) + 2 * kk, idesc(kC, false, false), true);
                     }
                 }
+                tc_commit(&sm.free_slot[c % kSlots]);
                 tc_commit(&sm.done_o[ph]);
             }
         }
@@ -379,12 +379,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto load_kq = [&](int c) {
             uint8_t *st = sm.kq[c % kStages];
             uint64_t *full = &sm.full_kq[c % kStages];
-            mbar_arrive_expect_tx(full, NA * (Y ? 2 : 1) * kTile);
+            mbar_arrive_expect_tx(full, NA * kSides * kTile);
             const int row = static_cast<int>(begin) + c * kC;
             for (int a = 0; a < NA; ++a) {
-                tma_load_3d(st + a * 2 * kTile, &map_k, a * 64, qk, row, full);
-                if (Y) tma_load_3d(st + a * 2 * kTile + kTile, &map_q, a * 64, qk, row, full);
-                // three stages alone do not hide DRAM's latency: the next one's load finds its rows in L2
+                tma_load_3d(st + a * kSides * kTile, &map_k, a * 64, qk, row, full);
+                if (Y) tma_load_3d(st + a * kSides * kTile + kTile, &map_q, a * 64, qk, row, full);
+                // the stages alone do not hide DRAM's latency: the next one's load finds its rows in L2
                 if (c + 1 >= kStages && c + 1 < chunks) {
                     tma_prefetch_3d(&map_k, a * 64, qk, row + kC);
                     if (Y) tma_prefetch_3d(&map_q, a * 64, qk, row + kC);
@@ -445,22 +445,33 @@ __global__ void __launch_bounds__(kThreads, 1)
         load_gates(0);
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            if (c >= kStages) {   // its stage and its gates' place: the update of three chunks before has read them
+            if (c >= kStages) {   // its stage and its gates' place: the update of the chunk there before has read them
                 wait(&sm.free_kq[c % kStages], static_cast<uint32_t>(c / kStages - 1) & 1u, patience);
                 if (lane == 0) load_kq(c);
                 __syncwarp();
             }
             gate(c);
             load_gates(c + 1);
-            if (c + 1 == chunks && len - c * kC < kC) {   // rows beyond the end, whatever they are
-                wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
-                zero_rows(sm.kq[c % kStages], NA * 2, len - c * kC, lane);
-                if (lane == 0) mbar_arrive(&sm.zeroed_kq);
-            }
-        }
-        // all that was asked for has landed
-        for (int c = chunks > kStages ? chunks - kStages : 0; c < chunks; ++c)
             wait(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
+            if (len - c * kC < kC) {   // rows beyond the end, whatever they are
+                zero_rows(sm.kq[c % kStages], NA * kSides, len - c * kC, lane);
+                if (lane == 0) mbar_arrive(&sm.zeroed_kq);
+                __syncwarp();
+            }
+            // [K; Q] K^T, for the warps that work ahead, where the chunk there before has left its place
+            if (c >= kSlots) wait(&sm.free_slot[c % kSlots], static_cast<uint32_t>(c / kSlots - 1) & 1u, patience);
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t d = desc_base(sm.kq[c % kStages]);
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k) {
+                    const uint64_t dk = d + (k / 4) * (kSides * kTile / 16) + 2 * (k % 4);
+                    tc_mma_f16(tmem + kColK + c % kSlots * 64, dk, dk, idesc(kC, false, false), k > 0);
+                }
+                tc_commit(&sm.done_prep[c % kSlots]);
+            }
+            __syncwarp();
+        }
     } else if (warp == kValueWarp) {
         // ---------------- V in, y out ----------------
         const int channels = p.dv - slice * kM < kM ? p.dv - slice * kM : kM;
@@ -512,20 +523,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto place = [](int j, int r) { return j * kH + (r ^ ((j & 3) << 3)); };
 #pragma unroll 1
         for (int c = team; c < chunks; c += 2) {
-            const uint32_t col = tmem + kColK + c % 3 * 64;
+            const uint32_t col = tmem + kColK + c % kSlots * 64;
             const Gates &gt = sm.gates[c % kStages];
-            wait(&sm.done_prep[team], static_cast<uint32_t>(c >> 1) & 1u, patience);
+            wait(&sm.done_prep[c % kSlots], static_cast<uint32_t>(c / kSlots) & 1u, patience);
             wait(&sm.gated[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
             tc_fence_after();
             const Log bi{gt.bh[i], gt.bl[i]};
             const f2 bih = pack2(bi.h, bi.h), bil = pack2(bi.l, bi.l), minus = pack2(-1.f, -1.f);
             const float mine = is_a ? gt.beta[i] : p.scale;
             // two chunks ago: through with T and P
-            if (!is_a && c >= 2) wait(&sm.done_o[team], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
+            if (Y && !is_a && c >= 2) wait(&sm.done_o[team], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
             // Columns of 16. Left of the diagonal half the decay from j to i goes by the last token of the
             // 16, both factors at most 1 where nothing grows; on it each entry has its exponential.
 #pragma unroll 1
-            for (int j0 = 0; j0 < (half + 1) * kH; j0 += kB) {
+            for (int j0 = 0; j0 < (is_a || Y ? (half + 1) * kH : 0); j0 += kB) {
                 float v[16];
                 tmem_ld16(col + lanes + j0, v);
                 if (j0 < half * kH) {
@@ -546,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float *to = (half == 0 ? a11 : j0 < kH ? a21 : a22) + (j0 & (kH - 1)) * kH;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) to[e * kH + (lane ^ ((e & 3) << 3))] = v[e];
-                } else {
+                } else if constexpr (Y) {
 #pragma unroll
                     for (int o = 0; o < 16; o += 8) {
                         uint32_t h[4], l[4];
@@ -742,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int buf = c & 1;
             const uint32_t ph = static_cast<uint32_t>(c) & 1u;
             const Gates &gt = sm.gates[c % kStages];
-            const uint32_t col_k = tm + kColK + c % 3 * 64 + half * 32, col_q = tm + kColQ + half * 32;
+            const uint32_t col_k = tm + kColK + c % kSlots * 64 + half * 32, col_q = tm + kColQ + half * 32;
             if (c < chunks) {
                 // ---- S as a pair ----
 #pragma unroll 1
@@ -752,19 +763,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_ld_wait(r);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
-                    if (g == 0 && c > 0) {   // P U of the chunk before has read U's pair, which lies there
-                        wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
-                        tc_fence_after();
-                    }
                     tmem_st16(tm + kColPair + (half * kHalf + g) / 2, h);
                     tmem_st16(tm + kColPair + kHalf + (half * kHalf + g) / 2, l);
+                    hand_over(&sm.have_s[g / 32]);
                 }
-                hand_over(&sm.have_s);
-            } else if (c > 0) {
-                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
-                tc_fence_after();
             }
             if (c > 0) {
+                wait(&sm.done_o[buf ^ 1], static_cast<uint32_t>((c - 1) >> 1) & 1u, patience);
+                tc_fence_after();
                 // ---- y of the chunk before, tokens 32 half .. , while S k is formed ----
                 if (Y) {
                     uint32_t r[32];
@@ -856,8 +862,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (Y) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) split(pair_of(r, e), h[e], l[e]);
-                    tmem_st16(tm + kColPair + 64 + half * 32, h);
-                    tmem_st16(tm + kColPair + 64 + half * 32 + 16, l);
+                    tmem_st16(col_k, h);
+                    tmem_st16(col_k + 16, l);
                     hand_over(&sm.have_u);
                 }
             }
@@ -984,8 +990,8 @@ struct Maps {
 template <int NA, bool Y, bool CUT>
 cudaError_t launch(const DeltaParams &p, const Maps &maps, int slices, const Cut &cut, cudaStream_t stream) {
     auto kern = delta_chunk_kernel<NA, Y, CUT>;
-    const int smem = static_cast<int>(sizeof(Smem<NA>) + 1024);
-    static_assert(sizeof(Smem<NA>) + 1024 <= 227 * 1024, "one CTA's shared memory");
+    const int smem = static_cast<int>(sizeof(Smem<NA, Y>) + 1024);
+    static_assert(sizeof(Smem<NA, Y>) + 1024 <= 227 * 1024, "one CTA's shared memory");
     cudaError_t e = ensure_smem(reinterpret_cast<const void *>(kern), smem);
     if (e != cudaSuccess) return e;
     const int64_t ctas = (CUT ? cut.slots : p.n_seqs) * p.hv * (slices + (CUT && !cut.joined ? 1 : 0));
