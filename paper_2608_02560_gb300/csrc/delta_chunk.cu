@@ -20,9 +20,8 @@
 // Warps 8-15, two teams that take chunks by turns, one or two ahead of the chain (one team of eight
 // was no faster than this one of four, and the chain waited for it: 7000 cycles a chunk): A and P
 // with their decays, the inverse T in fp32: blocks of 16 by substitution (a product form would lose
-// its digits where keys repeat), then joined twice, T10 = -(T1 A10) T0, on mma.sync with operands as
-// pairs of tf32 (16 x 16 and 32 x 32: too small for an MMA of 128 rows, and one multiply per
-// shared-memory read was too slow).
+// its digits where keys repeat), then joined twice, T10 = -(T1 A10) T0, a thread 4 x 2 entries of each
+// product (16 x 16 and 32 x 32: too small for an MMA of 128 rows).
 // Warp 16: K and Q in, three chunks deep, and the chunks' gates. Warp 17: issues every MMA, so that no
 // working warp waits in the queue of the tensor cores. Warp 18: V in and y rows out.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
@@ -178,6 +177,39 @@ __device__ __forceinline__ f2 pair_of(const uint32_t (&r)[32], int e) {
     return pack2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
 }
 __device__ __forceinline__ f2 load2(const float *p) { return *reinterpret_cast<const f2 *>(p); }
+
+// Column j, row i of a quarter of A and later of T: the rows of four neighbouring columns begin in
+// different banks.
+__device__ __forceinline__ int place(int j, int i) { return j * kH + (i ^ ((j & 3) << 3)); }
+// Rows r .. r + 3 of columns n, n + 1 of a product over K: L's columns from lc on, R's rows from rr on.
+template <int K>
+__device__ __forceinline__ void product(f2 (&sum)[2][2], const float *l, int lc, int r, const float *right, int rr, int n) {
+    sum[0][0] = sum[0][1] = sum[1][0] = sum[1][1] = pack2(0.f, 0.f);
+#pragma unroll 2
+    for (int k = 0; k < K; k += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(right + place(n, rr + k));
+        const float4 y = *reinterpret_cast<const float4 *>(right + place(n + 1, rr + k));
+        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 w = *reinterpret_cast<const float4 *>(l + place(lc + k + e, r));
+            const f2 lo = pack2(w.x, w.y), hi = pack2(w.z, w.w), xx = pack2(xs[e], xs[e]), yy = pack2(ys[e], ys[e]);
+            sum[0][0] = fma2(lo, xx, sum[0][0]);
+            sum[0][1] = fma2(hi, xx, sum[0][1]);
+            sum[1][0] = fma2(lo, yy, sum[1][0]);
+            sum[1][1] = fma2(hi, yy, sum[1][1]);
+        }
+    }
+}
+__device__ __forceinline__ void store_product(const f2 (&sum)[2][2], float sign, float *to, int r, int n) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float4 w;
+        unpack2(mul2(sum[j][0], pack2(sign, sign)), w.x, w.y);
+        unpack2(mul2(sum[j][1], pack2(sign, sign)), w.z, w.w);
+        *reinterpret_cast<float4 *>(to + place(n + j, r)) = w;
+    }
+}
 
 // Segments of `len` tokens (0: whole sequences). Sequence c's first is slot begin / len + c: no two
 // sequences' slots meet, and there are at most T_tot / len + n_seqs.
@@ -517,10 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int half = quarter & 1, i = half * kH + lane;   // this thread's row: of A (quarters 0, 1) or P
         const bool is_a = quarter < 2;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        // Column j, row i of a quarter of A and later of T, turned so that the rows or the columns of an
-        // MMA's operand lie in different banks.
         float *a11 = sm.a[team], *a21 = a11 + kBlock, *a22 = a21 + kBlock;
-        auto place = [](int j, int r) { return j * kH + (r ^ ((j & 3) << 3)); };
 #pragma unroll 1
         for (int c = team; c < chunks; c += 2) {
             const uint32_t col = tmem + kColK + c % kSlots * 64;
@@ -572,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_before();
             __syncwarp();
             // ---- (I + A)^-1 of one half a warp: two blocks of 16, a column a lane ----
-            const int g = lane >> 2, t = lane & 3;   // an MMA's row or column, and its pair
+            f2 sum[2][2];
             if (is_a) {
                 float *a = half == 0 ? a11 : a22;
                 const int b = lane & 16, cc = lane & 15;
@@ -602,62 +631,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                     *reinterpret_cast<float4 *>(a + (b + cc) * kH + ((b + e) ^ ((cc & 3) << 3))) = w;
                 }
                 __syncwarp();
-                // T1 A10, whose columns 2 t, 2 t + 1 of 8 then count as the A operand's t and t + 4
-                Sums3 h[2], d[2];
-#pragma unroll
-                for (int k = 0; k < kB; k += 8) {
-                    const float w[4] = {a[place(kB + k + t, kB + g)], a[place(kB + k + t, kB + g + 8)],
-                                        a[place(kB + k + t + 4, kB + g)], a[place(kB + k + t + 4, kB + g + 8)]};
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-                        mma_3tf32(h[n], w, {a[place(8 * n + g, kB + k + t)], a[place(8 * n + g, kB + k + t + 4)]});
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float w[4] = {h[k][0], h[k][2], h[k][1], h[k][3]};
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-                        mma_3tf32(d[n], w, {a[place(8 * n + g, 8 * k + 2 * t)], a[place(8 * n + g, 8 * k + 2 * t + 1)]});
-                }
+                // -(T1 A10) T0 in the place of A10
+                const int r = kB + (lane & 3) * 4, n = (lane >> 2) * 2;
+                product<kB>(sum, a, kB, r, a, kB, n);
                 __syncwarp();   // A10 has been read
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a[place(8 * n + 2 * t + (e & 1), kB + g + (e & 2) * 4)] = -d[n][e];
+                store_product(sum, 1.f, a, r, n);
+                __syncwarp();
+                product<kB>(sum, a, 0, r, a, 0, n);
+                __syncwarp();
+                store_product(sum, -1.f, a, r, n);
             }
             named_sync(kBarTeam + team, kTeam);
             // ---- joined: 8 columns a warp, T22 A21 in the place of A21 and then T21 in its place ----
             {
-                const int n = quarter * 8;
-                Sums3 d[2];
-#pragma unroll
-                for (int k = 0; k < kH; k += 8) {
-                    const float w[2] = {a21[place(n + g, k + t)], a21[place(n + g, k + t + 4)]};
-#pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        mma_3tf32(d[r], {a22[place(k + t, 16 * r + g)], a22[place(k + t, 16 * r + g + 8)],
-                                         a22[place(k + t + 4, 16 * r + g)], a22[place(k + t + 4, 16 * r + g + 8)]}, w);
-                }
+                const int r = (lane & 7) * 4, n = quarter * 8 + (lane >> 3) * 2;
+                product<kH>(sum, a22, 0, r, a21, 0, n);
                 __syncwarp();   // these columns have been read
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a21[place(n + 2 * t + (e & 1), 16 * r + g + (e & 2) * 4)] = d[r][e];
+                store_product(sum, 1.f, a21, r, n);
                 named_sync(kBarTeam + team, kTeam);
-                d[0] = d[1] = Sums3();
-#pragma unroll
-                for (int k = 0; k < kH; k += 8) {
-                    const float w[2] = {a11[place(n + g, k + t)], a11[place(n + g, k + t + 4)]};
-#pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        mma_3tf32(d[r], {a21[place(k + t, 16 * r + g)], a21[place(k + t, 16 * r + g + 8)],
-                                         a21[place(k + t + 4, 16 * r + g)], a21[place(k + t + 4, 16 * r + g + 8)]}, w);
-                }
+                product<kH>(sum, a21, 0, r, a11, 0, n);
                 named_sync(kBarTeam + team, kTeam);
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a21[place(n + 2 * t + (e & 1), 16 * r + g + (e & 2) * 4)] = -d[r][e];
+                store_product(sum, -1.f, a21, r, n);
             }
             if (is_a && c >= 2) wait(&sm.done_o[team], static_cast<uint32_t>((c - 2) >> 1) & 1u, patience);
             named_sync(kBarTeam + team, kTeam);
