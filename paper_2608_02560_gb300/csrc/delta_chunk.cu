@@ -101,10 +101,10 @@ template <int NA, bool Y>
 struct Smem {
     // chunks of K and Q on their way, places for k.k in tensor memory: more where no Q and no S q need theirs
     static constexpr int kStages = Y ? 3 : 6, kSlots = Y ? 3 : 4, kSides = Y ? 2 : 1;
-    // per stage: [K][Q] tiles of key columns 0..63, then of 64..127; V's two tiles, where the chunk's
-    // bf16 y rows lie on their way out
-    uint8_t kq[kStages][NA * kSides * kTile];
+    // V's two tiles, where the chunk's bf16 y rows lie on their way out; per stage, [K][Q] tiles of key
+    // columns 0..63, then of 64..127, [Q][K] for the second team
     uint8_t v[kVStages][2 * kTile];
+    uint8_t kq[kStages][NA * kSides * kTile];
     uint8_t tp[2][2 * kSides][kTile]; // T hi, T lo, P hi, P lo
     float a[2][3 * kBlock];           // a team's A, by columns in quarters 11, 21, 22, and what becomes of it
     Gates gates[kStages];
@@ -227,6 +227,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     delta_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const DeltaParams p, int slices, const Cut cut) {
     constexpr int kKeys = NA * 64;               // key coordinates, padded
+    // Where K and Q lie in chunk c's stage: the second team has k.k in the tensor memory of its third
+    // and fourth warps, so that the teams' work on A falls to all four schedulers.
+    auto tile_of = [](int c, int side) { return Y ? static_cast<int>(kTile) * ((c & 1) ^ side) : 0; };
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // (an offset, not a rounded address: the compiler would lose that it is shared memory)
     using S = Smem<NA, Y>;
@@ -334,7 +337,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < chunks; ++c) {
                 const uint32_t ph = static_cast<uint32_t>(c) & 1u;
                 const uint32_t col_k = tmem + kColK + c % kSlots * 64, col_q = tmem + kColQ;
-                const uint64_t d = desc_base(sm.kq[c % kStages]), dv = desc_base(sm.v[c % kVStages]), dt = desc_base(sm.tp[ph][0]);
+                const uint64_t d = desc_base(sm.kq[c % kStages] + tile_of(c, 0)), past = desc_base(sm.kq[c % kStages] + tile_of(c, 1)) - d;
+                const uint64_t dv = desc_base(sm.v[c % kVStages]), dt = desc_base(sm.tp[ph][0]);
                 wait_one(&sm.full_kq[c % kStages], static_cast<uint32_t>(c / kStages) & 1u, patience);
                 if (len - c * kC < kC) wait_one(&sm.zeroed_kq, 0, patience);   // rows beyond the end
                 wait_one(&sm.ready[ph], static_cast<uint32_t>(c >> 1) & 1u, patience);
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int l = 0; l < 2; ++l)
                         tc_mma_f16_ts(col, tmem + kColPair + l * (kKeys / 2) + kk * 8,
-                                      d + ((kk / 4) * kSides + q) * (kTile / 16) + 2 * (kk % 4), idesc(kC, false, false), onto || l);
+                                      d + q * past + (kk / 4) * (kSides * kTile / 16) + 2 * (kk % 4), idesc(kC, false, false), onto || l);
                 };
 #pragma unroll
                 for (int part = 0; part < NA; ++part) {   // 32 keys of each half as they come
@@ -414,8 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_arrive_expect_tx(full, NA * kSides * kTile);
             const int row = static_cast<int>(begin) + c * kC;
             for (int a = 0; a < NA; ++a) {
-                tma_load_3d(st + a * kSides * kTile, &map_k, a * 64, qk, row, full);
-                if (Y) tma_load_3d(st + a * kSides * kTile + kTile, &map_q, a * 64, qk, row, full);
+                tma_load_3d(st + a * kSides * kTile + tile_of(c, 0), &map_k, a * 64, qk, row, full);
+                if (Y) tma_load_3d(st + a * kSides * kTile + tile_of(c, 1), &map_q, a * 64, qk, row, full);
                 // the stages alone do not hide DRAM's latency: the next one's load finds its rows in L2
                 if (c + 1 >= kStages && c + 1 < chunks) {
                     tma_prefetch_3d(&map_k, a * 64, qk, row + kC);
@@ -490,15 +494,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive(&sm.zeroed_kq);
                 __syncwarp();
             }
-            // [K; Q] K^T, for the warps that work ahead, where the chunk there before has left its place
+            // [K; Q] K^T or [Q; K] K^T, for the warps that work ahead, where the chunk there before has left
+            // its place. (Where there is no Q, those 64 rows are of whatever lies before or behind K.)
             if (c >= kSlots) wait(&sm.free_slot[c % kSlots], static_cast<uint32_t>(c / kSlots - 1) & 1u, patience);
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t d = desc_base(sm.kq[c % kStages]);
+                const uint64_t d = desc_base(sm.kq[c % kStages] + tile_of(c, 0)), up = (c & 1) * (kTile / 16);
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k) {
                     const uint64_t dk = d + (k / 4) * (kSides * kTile / 16) + 2 * (k % 4);
-                    tc_mma_f16(tmem + kColK + c % kSlots * 64, dk, dk, idesc(kC, false, false), k > 0);
+                    tc_mma_f16(tmem + kColK + c % kSlots * 64, dk - up, dk, idesc(kC, false, false), k > 0);
                 }
                 tc_commit(&sm.done_prep[c % kSlots]);
             }
@@ -546,8 +551,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp >= 8) {
         // ---------------- T and P, ahead of the chain ----------------
         const int team = (warp >> 2) & 1, quarter = warp & 3, tid = threadIdx.x & (kTeam - 1);
-        const int half = quarter & 1, i = half * kH + lane;   // this thread's row: of A (quarters 0, 1) or P
-        const bool is_a = quarter < 2;
+        const int half = quarter & 1, i = half * kH + lane;   // this thread's row: of A or P
+        const bool is_a = quarter / 2 == team;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
         float *a11 = sm.a[team], *a21 = a11 + kBlock, *a22 = a21 + kBlock;
 #pragma unroll 1
