@@ -4,6 +4,11 @@
 //
 //   S <- e^g S ;  u = beta (v - S k) ;  S <- S + u k^T ;  y = scale S q
 //
+// A step is bound by memory, each state read and written once: 256 rows x 16 heads of 128 x 128 in
+// 89 us, 6.07 TB/s, 0.89 of the measured copy rate; a single row by its launch. A scan is bound by the
+// latency of its tokens, 0.17 us each (8 sequences of 129 to 256 tokens, 4 heads of 64 x 64, fp32:
+// 43 us).
+//
 // Rows of S (value channels) are independent given k, q and the gates, so a row belongs to 8
 // lanes of a warp and to nobody else: lane l of the 8 holds the four-number groups
 // l, l + 8, l + 16, ... of its columns, so a group's loads are whole 128-byte lines, and each of
@@ -315,7 +320,7 @@ cudaError_t scan_rows(const DeltaParams &p, cudaStream_t stream) {
 
 static_assert(kTile == kRowSets, "the tile's k.q take 8 lanes a token, and a thread fetches 2 R of v");
 
-// Two rows a thread keep more of the states in flight (256 sequences x 16 heads of 128 x 128: 90 us,
+// Two rows a thread keep more of the states in flight (256 sequences x 16 heads of 128 x 128: 89 us,
 // one row 98, four rows 93), unless that leaves an SM fewer than eight CTAs: then latency counts.
 template <typename T, int J>
 cudaError_t step_tiles(const DeltaParams &p, cudaStream_t stream) {
@@ -333,7 +338,9 @@ cudaError_t step_cols(const DeltaParams &p, cudaStream_t stream) {
     }
 }
 
-// Two rows a thread share what they read of a token, where that leaves the SMs two rounds of CTAs.
+// Two rows a thread share what they read of a token, where that leaves an SM eight CTAs (16 heads of
+// 128 x 128, 64 tokens: 256 sequences 1407 us, one row a thread 1617; 32 sequences 188 and 208; 8
+// sequences 72 and 57, one sequence 27 and 17).
 template <typename T, int J>
 cudaError_t scan_tiles(const DeltaParams &p, cudaStream_t stream) {
     return p.n_seqs * p.hv * ((p.dv + 2 * kRowSets - 1) / (2 * kRowSets)) >= 8LL * device_sm_count() ? scan_rows<T, J, 2>(p, stream)
@@ -359,12 +366,12 @@ cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream) {
 namespace {
 
 // Whether the chunk kernel is the faster one, by what both measured (16 heads of 128 x 128 unless said):
-//   1 sequence of 32 / 48 tokens    token 9.9 / 13.7 us   chunk 12.5 / 12.2
-//   4 sequences of 16 / 24          token 10.3 / 14.7     chunk 13.3 / 13.0
-//   16 of 8 / 12                    token 21.8 / 27.3     chunk 26.3 / 26.1
-//   256 of 8 / 16                   token 259 / 406       chunk 352 / 347
-//   64 of 40 / 48, 64 x 64          token 67 / 78         chunk 70 / 72
-// A round of CTAs in chunks takes 12 us however few its tokens are. A token of the other kernel takes
+//   1 sequence of 32 / 48 tokens    token 10.2 / 13.7 us  chunk 13.1 / 12.8
+//   4 sequences of 16 / 24          token 10.3 / 14.7     chunk 13.8 / 13.5
+//   16 of 12 / 16                   token 27.3 / 32.7     chunk 27.1 / 26.8
+//   256 of 8 / 16                   token 257 / 405       chunk 364 / 358
+//   64 of 40 / 48, 64 x 64          token 67 / 78         chunk 74 / 75
+// A round of CTAs in chunks takes 13 us however few its tokens are. A token of the other kernel takes
 // 0.25 us by its latency, or 6.2 ns a head of 128 x 128 where the SMs are full. Lengths lie on the
 // device: the rule knows their mean.
 bool in_chunks(const DeltaParams &p) {
@@ -372,7 +379,7 @@ bool in_chunks(const DeltaParams &p) {
     const double heads = static_cast<double>(p.n_seqs) * p.hv, tokens = static_cast<double>(p.T_tot) / p.n_seqs;
     const double rounds = ceil(heads * ((p.dv + 127) / 128) / device_sm_count());
     const double token = fmax(0.25, 0.0062 * heads * p.dk * p.dv / (128 * 128));
-    return 3.5 + tokens * token > 12 * rounds;
+    return 3.5 + tokens * token > 13 * rounds;
 }
 
 }  // namespace

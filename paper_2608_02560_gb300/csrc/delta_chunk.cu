@@ -15,15 +15,25 @@
 // the state itself stay fp32. A single bf16 would put 2^-9 of S into every y.
 //
 // Warps 0-7, the chain: what each chunk needs of the chunk before it, half the columns each
-// group of four. Per chunk: split S, [S k], y of the chunk before leaves, [S q, V T], split S k,
-// [S k T], split U, [update], [P U]; [..] are MMAs.
+// group of four. Per chunk: split S (each half of it goes to the MMAs as it is done), [S k], y of the
+// chunk before leaves, [S q, V T], split S k, [S k T], split U, [update], [P U]; [..] are MMAs.
 // Warps 8-15, two teams that take chunks by turns, one or two ahead of the chain (one team of eight
-// was no faster than this one of four, and the chain waited for it: 7000 cycles a chunk): A and P
-// with their decays, the inverse T in fp32: blocks of 16 by substitution (a product form would lose
-// its digits where keys repeat), then joined twice, T10 = -(T1 A10) T0, a thread 4 x 2 entries of each
-// product (16 x 16 and 32 x 32: too small for an MMA of 128 rows).
-// Warp 16: K and Q in, three chunks deep, and the chunks' gates. Warp 17: issues every MMA, so that no
-// working warp waits in the queue of the tensor cores. Warp 18: V in and y rows out.
+// was no faster than one of four; a third team, at 80 registers a thread, slowed a corpus by 12 %):
+// A and P with their decays, the inverse T in fp32: blocks of 16 by substitution (a product form would
+// lose its digits where keys repeat), then joined twice, T10 = -(T1 A10) T0, a thread 4 x 2 entries of
+// each product (16 x 16 and 32 x 32: too small for an MMA of 128 rows; on mma.sync with pairs of tf32 a
+// corpus took 3 % longer).
+// Warp 16: K and Q in, three chunks ahead (K alone six), the chunks' gates, and the MMAs of k.k and
+// q.k, which the teams wait for. Warp 17: issues every other MMA, so that no working warp waits in the
+// queue of the tensor cores. Warp 18: V in and y rows out.
+//
+// What bounds it: in full rounds the chain and the teams alike, about 4900 cycles a chunk (6900 with a
+// readout) at 0.45 instructions a cycle of each scheduler, the tensor cores' pipe 31 to 34 % busy, DRAM
+// at 16 to 20 % of its rate; in rounds of a chunk or two the 13 us from a CTA's start to its end, most
+// of them one chunk's way through a team. Measured, bf16, 128 x 128 a head: 256 sequences of 256 to
+// 4096 tokens, 8 heads, states alone, 1338 us (218 TFLOP/s of the recurrence's operations); 96
+// sequences of 1 to 200 tokens, 16 heads, with a readout, 174 us; one of 64 tokens 14 us; one of 32,768
+// tokens, cut into segments, 695 us.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
@@ -1024,7 +1034,8 @@ cudaError_t launch_all(const DeltaParams &p, const Maps &maps, int slices, Cut c
 // The segments' length for these sizes, or 0. In chunks of 64 tokens, of which a CTA takes one after
 // another: whole sequences are as long as their rounds of CTAs; segments go in one pass for B and M,
 // one step of the join each, and one pass for themselves. Cut only where that is a third shorter: the
-// estimate knows the sequences' mean length alone.
+// estimate knows the sequences' mean length alone. One sequence, 16 heads of 128 x 128, with a readout:
+// 2048 tokens 89 us (whole 115), 4096 tokens 130 (222), 32,768 tokens 689 (1709).
 int cut_length(const DeltaParams &p) {
     const int64_t sms = device_sm_count(), slices = (p.dv + kM - 1) / kM, items = p.n_seqs * p.hv * slices;
     if (items > sms || p.T_tot / p.n_seqs < 16 * kC) return 0;

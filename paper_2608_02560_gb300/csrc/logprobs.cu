@@ -15,8 +15,11 @@
 // lanes' maxima), and later the warps share the largest of their k-th values, so few entries are
 // ever inserted. Batches whose maximum does not reach the bound cost one comparison.
 //
-// Memory bounds it, at 5 to 8 instructions an entry. A CTA takes a row; with few rows a cluster of
-// up to 8 shares one and joins over distributed shared memory.
+// Memory and the instructions, 5 to 8 an entry, bound it alike: 2048 rows of 50,257 bf16 logits, 5 best,
+// take 53 us (3.88 TB/s, 0.57 of the measured copy rate, schedulers 65 % busy); 61 rows of 128,001 fp32
+// ones with nine tenths at -infinity, 20 best, 22 us, by the latency of the joins; one row of 32,000
+// 8.2 us. A CTA takes a row; with few rows a cluster of up to 8 shares one and joins over distributed
+// shared memory.
 #include <cmath>
 #include <cstddef>
 
@@ -305,7 +308,7 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
     const uint32_t low = V::lowest(-2.f * far);    // below any maximum, and low c finite
     bool first = true;
     // A lane copies its own vectors to shared memory, two batches ahead, and reads its own: registers
-    // held too few loads in flight (2048 x 50,257 bf16, 57 us).
+    // held too few loads in flight (2048 x 50,257 bf16: 57 us).
     extern __shared__ __align__(16) uint4 ring[];
     uint4 *mine = ring + static_cast<size_t>(warp) * kStages * kFly * 32 + lane;
     const int step = warps * 32 * kFly;
@@ -505,11 +508,15 @@ cudaError_t launch_warps(const LogprobParams &p, int parts, cudaStream_t stream)
 template <typename T, bool TOP>
 cudaError_t launch_parts(const LogprobParams &p, cudaStream_t stream) {
     // Each warp pays for its own first entries, so a row gets only the warps that keep an SM's loads
-    // in flight: two where there are rows for 24 warps an SM, else four or eight. With fewer rows than
-    // fill the SMs and rows long enough to be shared, up to eight CTAs a row: parts of at least 4096.
+    // in flight. 50,257 bf16 logits, 5 best, two / four / eight warps a row: 2048 rows 52 / 55 / 60 us,
+    // 1500 rows 39 / 45 / 47, 1000 rows 34 / 31 / 33, 700 rows 30 / 25 / 28, 300 rows 26 / 18 / 15; 2048
+    // rows without a list, whose first entries cost nothing, 42 / 37 / 39.
     const int64_t sms = device_sm_count();
-    if (p.rows >= 12 * sms) return launch_warps<T, TOP, 2>(p, 1, stream);
-    if (p.rows >= 6 * sms) return launch_warps<T, TOP, 4>(p, 1, stream);
+    if (TOP && p.rows >= 8 * sms) return launch_warps<T, TOP, 2>(p, 1, stream);
+    if (p.rows >= 4 * sms) return launch_warps<T, TOP, 4>(p, 1, stream);
+    // With fewer rows than fill the SMs and rows long enough to be shared, up to eight CTAs a row, of at
+    // least 4096 entries each: 300 rows of 50,257 15.2 us (a CTA each 15.4), 16 rows 8.0 (12.1), 61
+    // rows of 128,001 fp32 20 (33), one of 152,000 8.8 (17.9).
     int parts = 1;
     while (parts < kMaxParts && p.rows * parts * 2 <= 4 * sms && p.vocab >= 4096LL * parts * 2) parts *= 2;
     return launch_warps<T, TOP, 8>(p, parts, stream);
