@@ -81,6 +81,39 @@ def test_masked_extreme_and_broken_rows(cuda_device, dtype, V):
     _compare(_run(cuda_device, x, tokens, 1.0, 6), ref, 6)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("R,V,k,temp", [(1300, 1001, 5, 1.0), (1217, 2100, 32, 0.7), (1250, 1, 1, 1.0), (700, 1001, 7, 1.0),
+                                        (650, 2309, 0, 1.3), (1300, 515, 0, 1.0)])
+def test_many_rows(cuda_device, dtype, R, V, k, temp):
+    """As many rows as give each few warps, masked, extreme and broken ones among them."""
+    import torch
+    gen = torch.Generator(device=cuda_device).manual_seed(R + V + k)
+    dt = getattr(torch, dtype)
+    x = (3 * torch.randn((R, V), device=cuda_device, generator=gen)).to(dt)
+    x[1::11] = float("-inf")
+    x[2::11] = torch.finfo(dt).min
+    x[3::11, V // 2] = float("nan")
+    x[4::11, V // 3] = float("inf")
+    x[5::11, ::2] = float("-inf")
+    x[6::11] = 1.5
+    x[7::11, 1:] = torch.finfo(dt).min
+    x[8::11, :V - 1] = float("-inf")
+    x[9::11] = torch.arange(V, device=cuda_device).to(dt) * 2.0 ** -6      # every entry enters the list
+    tokens = torch.randint(-1, V, (R,), device=cuda_device, generator=gen)
+    ref = list(oracle.token_logprobs(to_np(x), tokens.tolist(), temp, k))
+    got = [g if g is None else to_np(g) for g in _run(cuda_device, x, tokens, temp, k)]
+    # A difference d of logits is off by d * 2^-23: TOL is that up to 100. The log probabilities of
+    # the seventh kind's masked entries lie far below, and beyond fp32's range are its -infinity.
+    for i in (0, 3) if k else (0,):
+        far = np.isfinite(ref[i]) & (ref[i] < -100)
+        assert set(np.argwhere(far)[:, 0] % 11) <= {7}
+        with np.errstate(over="ignore", invalid="ignore"):
+            near = np.abs(got[i][far] - ref[i][far]) <= np.abs(ref[i][far]) * 2.0 ** -23
+            assert np.all(near | (got[i][far] == ref[i][far].astype(np.float32)))
+        got[i][far] = ref[i][far] = 0.0
+    _compare([g if g is None else torch.from_numpy(g) for g in got], ref, k)
+
+
 def test_sorted_rows_and_ties(cuda_device):
     """Rows in which every entry enters the list of the best, and rows of many equal entries."""
     import torch
