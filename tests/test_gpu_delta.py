@@ -325,6 +325,50 @@ def test_step_matches_the_recurrence(cuda_device, n, hk, hv, dk, dv, dtype, y_dt
     assert pg.precog_device_status()[0] == 0
 
 
+@pytest.mark.parametrize("n,hv,dk,dv,dtype,y_dtype", [
+    (120, 5, 104, 72, "bfloat16", "bfloat16"), (130, 4, 40, 72, "float32", "float32"), (160, 8, 16, 8, "bfloat16", "float32")])
+def test_step_of_large_batches(cuda_device, n, hv, dk, dv, dtype, y_dtype):
+    """Enough rows to fill the SMs, where a thread has two rows of a state."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    table = torch.randn((n + 2, 1, hv, dv, dk), device=cuda_device)
+    before = to_np(table)
+    slots = torch.randperm(n + 2, device=cuda_device)[:n]
+    slots[::17] = -1
+    q, k, v, g, beta, _ = _tensors([n], 1, hv, dk, dv, getattr(torch, dtype), cuda_device, 71, strided=True)
+    y = torch.full((n, hv, dv), float("nan"), dtype=getattr(torch, y_dtype), device=cuda_device)
+    pg.precog_delta_step(pg.delta_inputs(q, k, v, g, beta), table, slots=slots, y_out=y)
+    at = slots.cpu().numpy()
+    S0 = np.where((at >= 0)[:, None, None, None], before[np.maximum(at, 0), 0], 0.0)
+    S, ref_y = _ref(q, k, v, g, beta, torch.arange(n + 1), S0)
+    want = before.copy()
+    want[at[at >= 0], 0] = S[at >= 0]
+    _check(table, want, TOL_F32)
+    _check(y[slots >= 0], ref_y[at >= 0], TOL_F32)
+    assert bool((y[slots < 0] == 0).all()) and pg.precog_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("n,hk,hv,dk,dv,dtype,y_dtype", [
+    (160, 2, 4, 104, 72, "float32", "bfloat16"), (320, 1, 4, 24, 8, "float32", None), (200, 4, 4, 128, 72, "bfloat16", "bfloat16")])
+def test_large_batches_token_by_token(cuda_device, n, hk, hv, dk, dv, dtype, y_dtype):
+    """The same of the scan: fp32 inputs, or bf16 ones of a few tokens each."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    lens = [int(x) for x in np.random.default_rng(n).integers(0, 9, n)]
+    T = sum(lens)
+    q, k, v, g, beta, off = _tensors(lens, hk, hv, dk, dv, getattr(torch, dtype), cuda_device, 81, strided=True)
+    bank = torch.randn((n, 1, hv, dv, dk), device=cuda_device)
+    states = torch.empty_like(bank)
+    y = torch.full((T, hv, dv), float("nan"), dtype=getattr(torch, y_dtype), device=cuda_device) if y_dtype else None
+    pg.precog_delta_scan(pg.delta_inputs(q, k, v, g, beta), off, T, bank=bank, states_out=states, y_out=y)
+    ref_S, ref_y = _ref(q, k, v, g, beta, off, to_np(bank[:, 0]))
+    tol = TOL_F32 if dtype == "float32" else TOL_PAIR
+    _check(states[:, 0], ref_S, tol)
+    if y_dtype:
+        _check(y, ref_y, tol)
+    assert pg.precog_device_status()[0] == 0
+
+
 def test_step_with_slots_outside_the_table(cuda_device):
     import torch
     import paper_2608_02560_gb300 as pg

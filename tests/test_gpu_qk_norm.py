@@ -53,6 +53,29 @@ def test_matches_the_definition(cuda_device, dtype, T, hq, hk, d, rot, norm, int
     assert pg.precog_device_status()[0] == 0
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("hq,hk,d,rot,inter,weight", [(9, 10, 72, 48, False, True), (17, 1, 64, 30, True, False),
+                                                      (3, 12, 200, 200, False, False)])
+def test_many_tokens(cuda_device, dtype, hq, hk, d, rot, inter, weight):
+    """Enough tokens for groups of eight heads, whose last group has fewer."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    T, n_pos, dt = 6001, 300, getattr(torch, dtype)
+    gen = torch.Generator(device=cuda_device).manual_seed(d)
+    proj = torch.randn((T, (hq + hk) * d), device=cuda_device, generator=gen).to(dt)
+    q, k = proj[:, :hq * d].view(T, hq, d), proj[:, hq * d:].view(T, hk, d)
+    wq, wk = (torch.randn((2, d), device=cuda_device, generator=gen) if weight else (None, None))
+    ang = torch.rand((n_pos, rot // 2), device=cuda_device, generator=gen) * 100
+    cos, sin = torch.cos(ang), torch.sin(ang)
+    pos = torch.randint(0, n_pos, (T,), device=cuda_device, generator=gen)
+    qo, ko = (torch.full((T, h, d), float("nan"), dtype=dt, device=cuda_device) for h in (hq, hk))
+    pg.precog_qk_norm_rope(q, k, qo, ko, norm="rms", q_weight=wq, k_weight=wk, cos=cos, sin=sin, positions=pos,
+                           interleaved=inter)
+    n = lambda t: None if t is None else to_np(t)  # noqa: E731
+    for x, w, out in ((q, wq, qo), (k, wk, ko)):
+        _close(out, oracle.qk_norm_rope(n(x), "rms", 1e-6, n(w), n(cos), n(sin), n(pos).astype(int), inter))
+
+
 def test_zero_vectors_extremes_and_default_positions(cuda_device):
     import torch
     import paper_2608_02560_gb300 as pg
