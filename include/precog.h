@@ -457,11 +457,11 @@ typedef struct precog_delta_inputs {
  *   workspace   device scratch of at least precog_delta_scan_workspace_size() bytes, 16-byte
  *               aligned; 0 bytes (and then NULL) unless few long sequences are to be cut
  *               into segments that run at once
- * With BF16 inputs, sequences of more than a few tokens run on the tensor cores in chunks of
- * 64 tokens: state and sums stay fp32 and every intermediate operand is carried as a pair
- * of bf16 numbers (16 significant bits), so results agree with the recurrence to about 1e-5
- * of their norm. F32 inputs and very short sequences run token by token in fp32. Calls of the
- * same shape repeat bit for bit.
+ * With BF16 inputs, batches whose mean length is more than some thirty tokens (12 where the
+ * batch fills the GPU) run on the tensor cores in chunks of 64 tokens: state and sums stay
+ * fp32 and every intermediate operand is carried as a pair of bf16 numbers (16 significant
+ * bits), so results agree with the recurrence to about 1e-5 of their norm. F32 inputs and
+ * shorter sequences run token by token in fp32. Calls of the same shape repeat bit for bit.
  */
 precog_status precog_delta_scan(const precog_delta_inputs *in, const int64_t *d_offsets, int64_t n_seqs,
                                 int64_t T_tot, const void *bank, int32_t bank_dtype, int64_t bank_entries,

@@ -177,39 +177,6 @@ __device__ __forceinline__ void tc_commit(uint64_t *bar) {
                      smem_u32(bar))
                  : "memory");
 }
-// ---- warp-level tensor cores, for products too small for the above ----
-// D (16 x 8) += A (16 x 8) B (8 x 8), tf32 operands (the low 13 bits are not read). Lane 4 g + t
-// holds A[g][t], A[g + 8][t], A[g][t + 4], A[g + 8][t + 4]; B[t][g], B[t + 4][g]; D[g][2 t],
-// D[g][2 t + 1], D[g + 8][2 t], D[g + 8][2 t + 1].
-__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
-}
-// The same of fp32 operands as pairs of tf32 (22 significant bits), without lo * lo; three sums,
-// so that the MMAs do not wait for one another.
-struct Sums3 {
-    float hh[4] = {}, hl[4] = {}, lh[4] = {};
-    __device__ __forceinline__ float operator[](int i) const { return hh[i] + (hl[i] + lh[i]); }
-};
-__device__ __forceinline__ void mma_3tf32(Sums3 &d, const float (&a)[4], const float (&b)[2]) {
-    uint32_t ah[4], al[4], bh[2], bl[2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        ah[i] = __float_as_uint(a[i]) & 0xffffe000u;
-        al[i] = __float_as_uint(a[i] - __uint_as_float(ah[i]));
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        bh[i] = __float_as_uint(b[i]) & 0xffffe000u;
-        bl[i] = __float_as_uint(b[i] - __uint_as_float(bh[i]));
-    }
-    mma_tf32(d.hh, ah, bh);
-    mma_tf32(d.hl, ah, bl);
-    mma_tf32(d.lh, al, bh);
-}
-
 // ---- dependent launches ----
 // Wait until the stream's previous kernel has completed and its writes are visible: the first
 // statement of every thread of a kernel launched with launch_dependent, before any access to
