@@ -409,7 +409,8 @@ precog_status precog_smc_consolidate(float *semantic, int64_t n_slots, int64_t s
  *          be at least one row long (ignored where there is at most one row).
  *   g, beta : fp32 [rows][n_v_heads], dense. g is the logarithm of the decay (usually <= 0;
  *          -infinity forgets the state, and so does anything below -128, which decays by
- *          less than fp32 can hold).
+ *          less than fp32 can hold; growth, g > 0, has to stay within fp32 over the tokens of a call's
+ *          sequence where a workspace is in use).
  * q may be NULL when no readout is requested. Requirements: dk a multiple of 8 in [8, 128],
  * dv a multiple of 8 in [8, 4096], n_v_heads a multiple of n_qk_heads.
  */
@@ -462,6 +463,9 @@ typedef struct precog_delta_inputs {
  * fp32 and every intermediate operand is carried as a pair of bf16 numbers (16 significant
  * bits), so results agree with the recurrence to about 1e-5 of their norm. F32 inputs and
  * shorter sequences run token by token in fp32. Calls of the same shape repeat bit for bit.
+ * NaN and infinity act as in the recurrence, whichever way a sequence runs: tokens before the one that
+ * has them are not touched, and from it on what they reach is not finite (NaN where the recurrence may
+ * have infinity): everything of the head for k, g and beta, the channel for v, the token's y for q.
  */
 precog_status precog_delta_scan(const precog_delta_inputs *in, const int64_t *d_offsets, int64_t n_seqs,
                                 int64_t T_tot, const void *bank, int32_t bank_dtype, int64_t bank_entries,

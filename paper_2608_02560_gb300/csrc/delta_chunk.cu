@@ -38,6 +38,10 @@
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
 // of them enters a sum.
+// NaN and infinity among the inputs of a token reach its whole chunk, 0 * NaN being NaN in the products
+// with T and P, and leave the channel's state not finite, from then on. So the state is looked at once, at
+// the end, and a channel that broke is done again token by token (once_more): sequences that stay finite
+// pay one barrier for it.
 //
 // Few sequences leave SMs idle, and a chain is as long as its sequence. Then each sequence is cut into
 // segments: a state passes through one as S M + B, M a product of e^g (I - beta k k^T) over its tokens.
@@ -76,6 +80,7 @@ constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
 constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = 448;
 
 constexpr int kBarTeam = 1;            // and 2
+constexpr int kBarChain = 3;
 
 // A sum of logs as an unevaluated pair: differences of large sums keep their digits.
 struct Log {
@@ -107,6 +112,20 @@ struct alignas(16) Gates {
     float whole;          // e^{b_C}
 };
 
+// States of one head.
+struct States {
+    void *base;                // nullptr: zeros
+    int dtype;
+    int64_t at;                // elements before row 0
+};
+
+// A CTA's tokens, the state before them and where the one behind them goes (nowhere: nullptr).
+struct Job {
+    int64_t begin, end;
+    States from, to;
+    int head;
+};
+
 template <int NA, bool Y>
 struct Smem {
     // chunks of K and Q on their way, places for k.k in tensor memory: more where no Q and no S q need theirs
@@ -124,6 +143,8 @@ struct Smem {
     uint64_t done_prep[kSlots], free_slot[kSlots], ready[2], done_o[2];
     uint64_t have_s[2], have_k, have_d, have_u;   // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
+    uint32_t broken[kM / 32];         // bit: a value channel whose state is not finite
+    Job job;
     uint32_t tmem_base;
 };
 
@@ -232,10 +253,102 @@ struct Cut {
 };
 __device__ __forceinline__ int64_t segments(int64_t tokens, int len) { return tokens <= len ? 1 : (tokens + len - 1) / len; }
 
+// Tokens begin .. end - 1 once more, one after another as the recurrence is defined, for the value
+// channels whose state the chunks left not finite: there the zeros of T and P met NaN or infinity,
+// 0 * NaN being NaN, and tokens before the broken one lost their readouts with it; or a chunk's whole
+// growth left fp32, which token by token it need not. A warp has 8 rows (`broken`: bits), 4 lanes a row,
+// lane l the four-number groups l, l + 4, ... of its columns. Once nothing of its rows is finite nothing
+// will be again, and what is left of them is NaN. No sequence that stays finite comes here.
+__device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, int first_row, unsigned broken) {
+    constexpr int kGroups = 8;
+    const int64_t begin = job.begin, end = job.end;
+    const int head = job.head;
+    const States from = job.from, to = job.to;
+    const int lane4 = threadIdx.x & 3, row = first_row + (threadIdx.x & 31) / 4, qk = head / (p.hv / p.hk);
+    const bool mine = (broken >> ((threadIdx.x & 31) / 4) & 1u) != 0u;   // (then the row is one of the head's)
+    float4 s[kGroups];
+    auto load4 = [](const __nv_bfloat16 *x) {
+        const uint2 r = *reinterpret_cast<const uint2 *>(x);
+        return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                           __uint_as_float(r.y & 0xffff0000u));
+    };
+    auto dot4 = [](float4 a, float4 b, float sum) { return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, sum)))); };
+    auto row_sum = [](float v) {
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        return v + __shfl_xor_sync(0xffffffffu, v, 1);
+    };
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
+        const int col = 4 * (lane4 + 4 * j);
+        s[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!mine || from.base == nullptr || col >= p.dk) continue;
+        const int64_t at = from.at + static_cast<int64_t>(row) * p.dk + col;
+        s[j] = from.dtype == PRECOG_F32 ? *reinterpret_cast<const float4 *>(static_cast<const float *>(from.base) + at)
+                                        : load4(static_cast<const __nv_bfloat16 *>(from.base) + at);
+    }
+    auto write_y = [&](int64_t t, float v) {
+        if (!mine || lane4 != 0) return;
+        const int64_t at = (t * p.hv + head) * p.dv + row;
+        if (p.y_dtype == PRECOG_F32) static_cast<float *>(p.y)[at] = v;
+        else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+    };
+    int64_t t = begin;
+#pragma unroll 1
+    for (; t < end; ++t) {
+        if ((t - begin) % kC == 0) {
+            bool left = false;
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j)
+                left |= mine && 4 * (lane4 + 4 * j) < p.dk && (isfinite(s[j].x) || isfinite(s[j].y) || isfinite(s[j].z) || isfinite(s[j].w));
+            if (!__any_sync(0xffffffffu, left)) break;
+        }
+        const __nv_bfloat16 *kr = static_cast<const __nv_bfloat16 *>(p.k) + t * p.k_stride + static_cast<int64_t>(qk) * p.dk;
+        const __nv_bfloat16 *qr = p.y ? static_cast<const __nv_bfloat16 *>(p.q) + t * p.q_stride + static_cast<int64_t>(qk) * p.dk : kr;
+        const float g = p.g[t * p.hv + head], beta = p.beta[t * p.hv + head], a = g < kLeastGate ? 0.f : expf(g);
+        const float v = mine ? to_f32(static_cast<const __nv_bfloat16 *>(p.v)[t * p.v_stride + static_cast<int64_t>(head) * p.dv + row]) : 0.f;
+        float sk = 0.f, sq = 0.f, kq = 0.f;
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            const int col = 4 * (lane4 + 4 * j);
+            if (col >= p.dk) continue;
+            const float4 k = load4(kr + col), q = load4(qr + col);
+            s[j] = make_float4(a * s[j].x, a * s[j].y, a * s[j].z, a * s[j].w);
+            sk = dot4(s[j], k, sk);
+            sq = dot4(s[j], q, sq);
+            kq = dot4(k, q, kq);
+        }
+        const float u = beta * (v - row_sum(sk));
+        sq = row_sum(sq), kq = row_sum(kq);
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            const int col = 4 * (lane4 + 4 * j);
+            if (col >= p.dk) continue;
+            const float4 k = load4(kr + col);
+            s[j] = make_float4(fmaf(u, k.x, s[j].x), fmaf(u, k.y, s[j].y), fmaf(u, k.z, s[j].z), fmaf(u, k.w, s[j].w));
+        }
+        if (p.y) write_y(t, p.scale * fmaf(u, kq, sq));
+    }
+    for (; p.y && t < end; ++t) write_y(t, __int_as_float(0x7fffffff));
+    if (!mine || to.base == nullptr) return;
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
+        const int col = 4 * (lane4 + 4 * j);
+        if (col >= p.dk) continue;
+        const int64_t at = to.at + static_cast<int64_t>(row) * p.dk + col;
+        if (to.dtype == PRECOG_F32) {
+            *reinterpret_cast<float4 *>(static_cast<float *>(to.base) + at) = s[j];
+        } else {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(s[j].x, s[j].y), hi = __floats2bfloat162_rn(s[j].z, s[j].w);
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(to.base) + at) =
+                make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+        }
+    }
+}
+
 template <int NA, bool Y, bool CUT>
 __global__ void __launch_bounds__(kThreads, 1)
     delta_chunk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                       const __grid_constant__ CUtensorMap map_v, const DeltaParams p, int slices, const Cut cut) {
+                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ DeltaParams p, int slices, const Cut cut) {
     constexpr int kKeys = NA * 64;               // key coordinates, padded
     // Where K and Q lie in chunk c's stage: the second team has k.k in the tensor memory of its third
     // and fourth warps, so that the teams' work on A falls to all four schedulers.
@@ -324,6 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&sm.done_qs, 1);
         mbar_init(&sm.done_u, 1);
         mbar_init(&sm.done_s, 1);
+        for (int i = 0; i < kM / 32; ++i) sm.broken[i] = 0u;
         fence_barrier_init();
     }
     if (warp == kMmaWarp) {
@@ -704,27 +818,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool live = ident ? row < p.dk : ch < p.dv;
         constexpr int kHalf = kKeys / 2;                 // S's columns of this half of the warps
         const uint32_t col_s = tm + kColS + half * kHalf;
-        const int64_t head_elems = static_cast<int64_t>(p.dv) * p.dk;
         {   // initial state
-            const void *from = nullptr;
-            int dtype = PRECOG_F32;
-            int64_t at = 0;
+            const int64_t head_elems = static_cast<int64_t>(p.dv) * p.dk;
+            Job job = {begin, end, {nullptr, PRECOG_F32, 0}, {nullptr, PRECOG_F32, 0}, head};
             if (CUT && first && !last && cut.joined) {   // (the bank may be where the last segment's state goes)
-                from = cut.begins;
-                at = (seq * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+                job.from = States{cut.begins, PRECOG_F32, (seq * p.hv + head) * head_elems};
             } else if (first && p.bank && !ident) {
-                int64_t entry = p.idx ? p.idx[seq] : seq;
+                const int64_t entry = p.idx ? p.idx[seq] : seq;
                 if (entry < -1 || entry >= p.bank_entries) {
                     if (threadIdx.x == 0) atomicOr(&g_delta_chunk_status, PRECOG_DEV_BAD_INDEX);
-                    entry = -1;
+                } else if (entry >= 0) {
+                    job.from = States{const_cast<void *>(p.bank), p.bank_dtype, ((entry * p.L_total + p.layer) * p.hv + head) * head_elems};
                 }
-                from = entry >= 0 ? p.bank : nullptr;
-                dtype = p.bank_dtype;
-                at = ((entry * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
             } else if (CUT && !first && cut.joined) {
-                from = cut.states;
-                at = ((slot - 1) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+                job.from = States{cut.states, PRECOG_F32, ((slot - 1) * p.hv + head) * head_elems};
             }
+            if (ident) job.to = States{cut.moves, PRECOG_F32, (slot * p.hv + head) * p.dk * p.dk};
+            else if (kept) job.to = States{cut.states, PRECOG_F32, (slot * p.hv + head) * head_elems};
+            else if (last && p.states) job.to = States{p.states, p.state_dtype, ((seq * p.L_total + p.layer) * p.hv + head) * head_elems};
+            if (threadIdx.x == 0) sm.job = job;     // (for the end)
+            const States from = job.from;
+            const int64_t at = from.at + static_cast<int64_t>(ch) * p.dk;
 #pragma unroll
             for (int g = 0; g < kHalf; g += 32) {
                 uint32_t r[32];
@@ -732,13 +846,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 32; e += 8) {
                     const int col = half * kHalf + g + e;
                     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    if (from && live && col < p.dk) delta_load8(from, dtype, at + col, v);
+                    if (from.base && live && col < p.dk) delta_load8(from.base, from.dtype, at + col, v);
                     if (ident && row >= col && row < col + 8) {
 #pragma unroll
                         for (int x = 0; x < 8; ++x) v[x] = row == col + x ? 1.f : 0.f;
                     }
                     if (kept && first && !ident && live && col < p.dk)
-                        delta_store8(cut.begins, PRECOG_F32, (seq * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk + col, v);
+                        delta_store8(cut.begins, PRECOG_F32, ((seq * p.hv + head) * p.dv + ch) * static_cast<int64_t>(p.dk) + col, v);
 #pragma unroll
                     for (int x = 0; x < 8; ++x) r[e + x] = __float_as_uint(v[x]);
                 }
@@ -880,25 +994,32 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait(&sm.done_s, ph, patience);
             tc_fence_after();
         }
-        if (kept || (last && p.states)) {
-            void *to = kept ? (ident ? cut.moves : cut.states) : p.states;
-            const int dtype = kept ? PRECOG_F32 : p.state_dtype;
-            const int64_t at = ident ? (slot * p.hv + head) * p.dk * p.dk + static_cast<int64_t>(row) * p.dk
-                                     : ((kept ? slot : seq * p.L_total + p.layer) * p.hv + head) * head_elems + static_cast<int64_t>(ch) * p.dk;
+        // ---- the state leaves; rows that are not finite are left to once_more ----
+        {
+            uint32_t r[NA][32];
+            f2 zeros = pack2(0.f, 0.f);      // 0 x, summed
 #pragma unroll
-            for (int g = 0; g < kHalf; g += 32) {
-                uint32_t r[32];
-                tmem_ld32_async(col_s + g, r);
-                tmem_ld_wait(r);
+            for (int g = 0; g < NA; ++g) {
+                tmem_ld32_async(col_s + g * 32, r[g]);
+                tmem_ld_wait(r[g]);
 #pragma unroll
-                for (int e = 0; e < 32; e += 8)
-                    if (const int col = half * kHalf + g + e; live && col < p.dk) {
+                for (int e = 0; e < 16; ++e) zeros = fma2(pair_of(r[g], e), pack2(0.f, 0.f), zeros);
+            }
+            float x, y;
+            unpack2(zeros, x, y);
+            if (!kept && live && !(x + y == 0.f)) atomicOr(&sm.broken[quarter], 1u << lane);
+            named_sync(kBarChain, kChain);
+            const States to = sm.job.to;
+            const int64_t at = to.at + static_cast<int64_t>(ident ? row : ch) * p.dk;
+            if (to.base && live && (sm.broken[quarter] >> lane & 1u) == 0u) {
+#pragma unroll
+                for (int e = 0; e < kHalf; e += 8)
+                    if (const int col = half * kHalf + e; col < p.dk) {
                         float v[8];
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) v[x] = __uint_as_float(r[e + x]);
-                        delta_store8(to, dtype, at + col, v);
+                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[e / 32][e % 32 + i]);
+                        delta_store8(to.base, to.dtype, at + col, v);
                     }
-                __syncwarp();
             }
         }
     }
@@ -907,6 +1028,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
+    }
+    if (!kept && warp < kM / 8) {
+        const unsigned rows = sm.broken[warp / 4] >> (warp % 4 * 8) & 0xffu;
+        if (rows) once_more(p, sm.job, slice * kM + warp * 8, rows);
     }
 }
 
