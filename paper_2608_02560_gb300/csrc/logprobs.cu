@@ -6,8 +6,9 @@
 //   log p(token) = d_token - log S,   H = log S - W / S.
 // Every thread keeps (max, S, W) of what it has seen; when its maximum grows by c, S becomes
 // S e^-c and W becomes (W - c S) e^-c, and two threads' sums join the same way. Exponentials below
-// 2^-150 of the largest count as zero, -infinity among them. d is one FMA, x c - max c; the rounding
-// of max c, the same in every term, is taken out of the result. Where max c itself leaves fp32's
+// 2^-150 of the largest count as zero, -infinity among them. d is one FMA, x c - rn(max c), and sums move
+// to another maximum by the difference of the rounded products: so every term carries the rounding of the
+// last maximum's product and no other's, and the result is freed of it. Where max c itself leaves fp32's
 // range (rows of the type's lowest value) the row is summed again with d = (x - max) c.
 //
 // The best entries: each warp keeps its k best in its lanes, sorted, as keys (value, complement of
@@ -52,15 +53,18 @@ __device__ __forceinline__ float clamped(float d) {
     return r;
 }
 
-// The sums seen from the maximum `mx` >= a.mx. c: log2(e) / temperature.
+// The sums seen from the maximum `mx` >= a.mx. c: log2(e) / temperature. (__fmul_rn: never part of an
+// FMA. FAR: without the products, for maxima whose own leave fp32's range.)
+template <bool FAR = false>
 __device__ __forceinline__ Sums moved(const Sums a, float mx, float c) {
     if (mx == a.mx) return a;
-    const float d = clamped((a.mx - mx) * c), f = ex2(d);
+    const float d = clamped(FAR ? (a.mx - mx) * c : __fmul_rn(a.mx, c) - __fmul_rn(mx, c)), f = ex2(d);
     return Sums{mx, a.s * f, fmaf(d, a.s, a.w) * f};
 }
+template <bool FAR = false>
 __device__ __forceinline__ Sums joined(const Sums a, const Sums b, float c) {
     const float mx = fmaxf(a.mx, b.mx);
-    const Sums x = moved(a, mx, c), y = moved(b, mx, c);
+    const Sums x = moved<FAR>(a, mx, c), y = moved<FAR>(b, mx, c);
     return Sums{mx, x.s + y.s, x.w + y.w};
 }
 
@@ -243,7 +247,7 @@ template <bool TOP>
 __device__ __forceinline__ void take_one(float x, uint32_t index, bool in, float c, int k, int lane, Sums &a, Best &b) {
     if (in) {
         if (x > a.mx) a = moved(a, x, c);
-        const float d = clamped(fmaf(x, c, -a.mx * c)), e = ex2(d);
+        const float d = clamped(fmaf(x, c, -__fmul_rn(a.mx, c))), e = ex2(d);
         a.s += e;
         a.w = fmaf(d, e, a.w);
     }
@@ -264,14 +268,14 @@ __device__ __noinline__ Sums sums_far(const T *x, int vocab, float c, int lane) 
     Sums a{kLowest, 0.f, 0.f};
     for (int i = lane; i < vocab; i += 32) {
         const float v = to_f32(x[i]);
-        if (v > a.mx) a = moved(a, v, c);
+        if (v > a.mx) a = moved<true>(a, v, c);
         const float d = clamped((v - a.mx) * c), e = ex2(d);
         a.s += e;
         a.w = fmaf(d, e, a.w);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
-        a = joined(a, Sums{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.w, o)}, c);
+        a = joined<true>(a, Sums{__shfl_xor_sync(0xffffffffu, a.mx, o), __shfl_xor_sync(0xffffffffu, a.s, o), __shfl_xor_sync(0xffffffffu, a.w, o)}, c);
     return a;
 }
 
@@ -297,12 +301,12 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
 
     const float far = kFar * fminf(1.f, 1.f / c);  // a maximum within it: |max c| < kFar
     Sums a{-far, 0.f, 0.f};
-    float nmc = far * c;                           // -max c
+    float nmc = __fmul_rn(far, c);                 // -max c, rounded
     f2 s2 = pack2(0.f, 0.f), w2 = s2;
     Best b;
     if (gw == 0 && head > 0) {
         take_one<TOP>(lane < head ? to_f32(x[lane < head ? lane : 0]) : 0.f, lane, lane < head, c, k, lane, a, b);
-        nmc = -a.mx * c;
+        nmc = -__fmul_rn(a.mx, c);
     }
     const f2 cc = pack2(c, c);
     const uint32_t low = V::lowest(-2.f * far);    // below any maximum, and low c finite
@@ -348,12 +352,12 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
             most = fmaxf(most, top[u]);
         }
         if (most > a.mx) {
-            const float d = clamped((a.mx - most) * c), f = ex2(d);
+            const float next = -__fmul_rn(most, c), d = clamped(next - nmc), f = ex2(d);
             w2 = mul2(fma2(pack2(d, d), s2, w2), pack2(f, f));
             s2 = mul2(s2, pack2(f, f));
             const Sums m = moved(a, most, c);
             a = m;
-            nmc = -most * c;
+            nmc = next;
         }
         const f2 nm = pack2(nmc, nmc);
 #pragma unroll
@@ -461,8 +465,8 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
     const float log_s = log2f(a.s);                        // NaN where the row holds one
     const bool empty = a.s == 0.f;
     auto log_p = [&](float v) {
-        // (the sums' d was off by the rounding of max c, the same in each)
-        const float off = near ? fmaf(a.mx, c, -a.mx * c) : 0.f;
+        // (what the rounding of max c has added to every d)
+        const float off = near ? fmaf(a.mx, c, -__fmul_rn(a.mx, c)) : 0.f;
         return empty ? nan : (v - a.mx) * p.inv_temp - (log_s - off) * kLn2;
     };
     if (lane == 0) {
