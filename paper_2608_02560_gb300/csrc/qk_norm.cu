@@ -115,13 +115,13 @@ __global__ void __launch_bounds__(kThreads, 3) qk_norm_kernel(const QkNormParams
     const bool live = 8 * lane < p.dim;
     const T *in = static_cast<const T *>(p.in[which]) + t * p.in_stride[which];
     T *out = static_cast<T *>(p.out[which]) + t * p.out_stride[which];
-    float cs[4], sn[4];          // of the lane's four pairs; 1 and 0 where nothing turns
+    float cs[4], sn[4];          // of the lane's four pairs
+    bool turn[4];                // (not by 1 and 0: 0 times a partner that is infinite is NaN)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int pair = HALF ? (lane < pairs ? 4 * lane + i : p.rot) : 4 * lane + i;
-        const bool turn = live && pair < p.rot / 2;
-        cs[i] = turn ? p.cos[pos * (p.rot / 2) + pair] : 1.f;
-        sn[i] = turn ? p.sin[pos * (p.rot / 2) + pair] : 0.f;
+        turn[i] = HALF ? lane < pairs : 4 * lane + i < p.rot / 2;
+        cs[i] = turn[i] ? p.cos[pos * (p.rot / 2) + 4 * lane + i] : 1.f;
+        sn[i] = turn[i] ? p.sin[pos * (p.rot / 2) + 4 * lane + i] : 0.f;
     }
     float w[8];
     if constexpr (WEIGHT) {
@@ -167,8 +167,7 @@ __global__ void __launch_bounds__(kThreads, 3) qk_norm_kernel(const QkNormParams
             for (int i = 0; i < 4; ++i) {
                 float &a = x[HALF ? i : 2 * i], &b = x[HALF ? i + 4 : 2 * i + 1];
                 const float a0 = a;
-                a = a0 * cs[i] - b * sn[i];
-                b = b * cs[i] + a0 * sn[i];
+                if (turn[i]) a = a0 * cs[i] - b * sn[i], b = b * cs[i] + a0 * sn[i];
             }
             store8<!HALF>(out + static_cast<int64_t>(h + f) * p.dim, e0, e1, x);
         }
