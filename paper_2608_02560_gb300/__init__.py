@@ -214,6 +214,18 @@ def _stream(stream):
     return _raw_stream()
 
 
+def _workspace(need: int, device, stream):
+    """``need`` bytes of the stream that will work on them: the allocator may hand a freed block to that
+    stream's next tensor at once, and to no other's."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
 def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInputs:
     """Describe x, dt ``[L, T, D]`` (or ``[T, D]``), B, C ``[L, T, N]``, A ``[L, D, N]``.
 
@@ -341,9 +353,7 @@ def precog_retrieve(index, queries, best_idx, best_score=None, workspace=None, s
     M, dim = index.shape
     Q = queries.shape[0]
     if workspace is None:
-        torch = _torch()
-        need = precog_retrieve_workspace_size(M, dim, Q)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=index.device)
+        workspace = _workspace(max(precog_retrieve_workspace_size(M, dim, Q), 16), index.device, stream)
     _check(lib.precog_retrieve(
         _ptr(index), _dtype_code(index), M, dim, _ptr(queries), Q, _ptr(best_idx),
         _ptr(best_score), _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -368,9 +378,7 @@ def precog_retrieve_keys(index_shard, queries, row_offset: int, keys, workspace=
     M, dim = index_shard.shape
     Q = queries.shape[0]
     if workspace is None:
-        torch = _torch()
-        need = precog_retrieve_workspace_size(M, dim, Q)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=queries.device)
+        workspace = _workspace(max(precog_retrieve_workspace_size(M, dim, Q), 16), queries.device, stream)
     _check(lib.precog_retrieve_keys(
         _ptr(index_shard), _dtype_code(index_shard), M, dim, _ptr(queries), Q, int(row_offset), _ptr(keys),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
@@ -405,9 +413,7 @@ def precog_retrieve_topk(index, queries, k, best_idx, best_score=None, workspace
     M, dim = index.shape
     Q = queries.shape[0]
     if workspace is None:
-        torch = _torch()
-        need = int(lib.precog_retrieve_topk_workspace_size(M, dim, Q))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=index.device)
+        workspace = _workspace(max(int(lib.precog_retrieve_topk_workspace_size(M, dim, Q)), 16), index.device, stream)
     _check(lib.precog_retrieve_topk(
         _ptr(index), _dtype_code(index), M, dim, _ptr(queries), Q, k, _ptr(best_idx),
         _ptr(best_score), _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -480,7 +486,7 @@ def precog_delta_scan(inputs: DeltaInputs, offsets, T_tot: int, bank=None, idx=N
     holder = states_out if states_out is not None else bank
     if workspace is None and T_tot >= 1024:   # below, none is needed
         need = int(lib.precog_delta_scan_workspace_size(ctypes.byref(inputs), n, T_tot))
-        workspace = torch.empty(need, dtype=torch.uint8, device=offsets.device) if need else None
+        workspace = _workspace(need, offsets.device, stream) if need else None
     _check(lib.precog_delta_scan(
         ctypes.byref(inputs), _of(offsets, torch.int64, (n + 1,), "offsets"), n, T_tot, _ptr(bank),
         _dtype_code(bank) if bank is not None else PRECOG_F32, bank.shape[0] if bank is not None else 0,
