@@ -228,6 +228,7 @@ __device__ __forceinline__ float merged(float v, float reversed, int lane) {
 
 // The k best entries of a warp. Entries come in the order of their indices: once the warp has k, only
 // ones above the k-th enter; those of a bound that others found may also equal it.
+// (thr and strict are the same in every lane: whole warps branch on them around shuffles.)
 struct Best {
     u64 mine = 0ull;             // entry `lane`, best first
     float thr = -INFINITY;
@@ -383,8 +384,9 @@ __global__ void __launch_bounds__(kWarps * 32) logprobs_kernel(const LogprobPara
 #pragma unroll
                 for (int w = 1; w < kWarps; ++w) v = merged(v, tops[(warp + w) % kWarps][31 - lane], lane);
                 b.bound(__shfl_sync(0xffffffffu, v, k - 1));
-            } else if (const uint32_t others = *reinterpret_cast<volatile uint32_t *>(&shared_bound); others != 0u) {
-                b.bound(value_of(static_cast<u64>(others) << 32));
+            } else {   // one lane's reading for all: others may raise it between two lanes' own
+                const uint32_t others = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t *>(&shared_bound), 0);
+                if (others != 0u) b.bound(value_of(static_cast<u64>(others) << 32));
             }
             if (__any_sync(0xffffffffu, b.enters(most))) {
 #pragma unroll
