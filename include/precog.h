@@ -558,6 +558,7 @@ precog_status precog_qk_norm_rope(const precog_qk_norm_args *args, int64_t T, vo
  *                elements apart (any stride >= vocab; any alignment of the elements)
  *   d_tokens     device int64 [n_rows]; -1: nothing to score, d_logprob[r] = 0. Any other
  *                token outside [0, vocab) gives NaN and flags PRECOG_DEV_BAD_INDEX.
+ *   temperature  above 4.25e-39 (log2(e) / temperature has to be finite) and finite
  *   k            0 .. 32, at most vocab
  * Entries of -infinity have probability 0 (a given one scores -infinity) and rank behind all
  * others. A row that is -infinity throughout has no distribution: its d_logprob, d_entropy and

@@ -738,8 +738,8 @@ precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n
     if (vocab < 1) return fail(PRECOG_ERR_INVALID_ARG, "vocab must be >= 1");
     if (vocab > 0x3fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "vocab must be below 2^30");
     if (row_stride < vocab && n_rows > 1) return fail(PRECOG_ERR_INVALID_ARG, "row_stride must be >= vocab");
-    if (!(temperature > 0.f) || !(1.f / temperature > 0.f) || 1.f / temperature > 3.4e38f)
-        return fail(PRECOG_ERR_INVALID_ARG, "temperature must be positive and finite");
+    if (!(temperature > 0.f) || !(1.f / temperature > 0.f) || !(1.f / temperature * 1.442695f < 3.4e38f))
+        return fail(PRECOG_ERR_INVALID_ARG, "temperature and log2(e) / temperature must be positive and finite");
     if (k < 0 || k > 32) return fail(PRECOG_ERR_UNSUPPORTED, "k must be in [0, 32]");
     if (k > vocab) return fail(PRECOG_ERR_INVALID_ARG, "k must be at most vocab");
     if (n_rows == 0) return ok();
