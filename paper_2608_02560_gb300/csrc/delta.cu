@@ -391,14 +391,6 @@ cudaError_t launch_delta_scan(const DeltaParams &p, cudaStream_t stream) {
     return p.in_dtype == PRECOG_F32 ? scan_cols<float>(p, stream) : scan_cols<__nv_bfloat16>(p, stream);
 }
 
-cudaError_t delta_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0, chunk = 0;
-    cudaError_t e = delta_chunk_status_word_read_clear(&chunk);
-    if (e != cudaSuccess) return e;
-    e = cudaMemcpyFromSymbol(bits, g_delta_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    *bits |= chunk;
-    return cudaMemcpyToSymbol(g_delta_status, &zero, sizeof(uint32_t));
-}
+cudaError_t delta_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_delta_status); }
 
 }  // namespace precog

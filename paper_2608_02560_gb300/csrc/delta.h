@@ -13,7 +13,6 @@ namespace precog {
 // The scan on the tensor cores: bf16 inputs, any lengths.
 cudaError_t launch_delta_chunk(const DeltaParams &p, cudaStream_t stream);
 size_t delta_chunk_workspace_size(const DeltaParams &p);
-cudaError_t delta_chunk_status_word_read_clear(uint32_t *bits);
 
 // Eight neighbouring numbers of a state in its storage type (`at` a multiple of 8).
 __device__ __forceinline__ void delta_load8(const void *base, int dtype, int64_t at, float (&v)[8]) {

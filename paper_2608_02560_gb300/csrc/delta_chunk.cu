@@ -1216,11 +1216,6 @@ cudaError_t launch_delta_chunk(const DeltaParams &p, cudaStream_t stream) {
     return p.dk <= 64 ? launch_all<1>(p, maps, slices, cut, stream) : launch_all<2>(p, maps, slices, cut, stream);
 }
 
-cudaError_t delta_chunk_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_delta_chunk_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_delta_chunk_status, &zero, sizeof(uint32_t));
-}
+cudaError_t delta_chunk_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_delta_chunk_status); }
 
 }  // namespace precog

@@ -55,7 +55,7 @@ struct ScanParams {
 
 // Bounded-wait self-test (selftest.cu).
 cudaError_t launch_wait_timeout(uint32_t limit, cudaStream_t stream);
-cudaError_t selftest_status_word_read_clear(uint32_t *bits);
+cudaError_t selftest_status_word(uint32_t **word);
 
 // SM count of the current device (cached per device; 1 if it cannot be read).
 int device_sm_count();
@@ -102,8 +102,8 @@ cudaError_t launch_scan(const ScanParams &p, cudaStream_t stream);
 // multiple of 64; scan.cu routes launches with fewer work items than SMs to it.
 bool scan_latency_eligible(const ScanParams &p);
 cudaError_t launch_scan_latency(const ScanParams &p, cudaStream_t stream);
-cudaError_t scan_latency_status_word_read_clear(uint32_t *bits);
-cudaError_t scan_status_word_read_clear(uint32_t *bits);
+cudaError_t scan_latency_status_word(uint32_t **word);
+cudaError_t scan_status_word(uint32_t **word);
 
 struct RetrieveParams {
     const void *index;
@@ -130,7 +130,7 @@ cudaError_t launch_decode_keys(const int64_t *keys, int32_t n, int64_t *best_idx
 int retrieve_tc_grid(int64_t M, int sms);
 cudaError_t launch_retrieve_tc(const RetrieveParams &p, int grid, cudaStream_t stream,
                                uint64_t *launches);
-cudaError_t retrieve_tc_status_word_read_clear(uint32_t *bits);
+cudaError_t retrieve_tc_status_word(uint32_t **word);
 
 // Top-k retrieval (k <= 8): partial lists of 8 packed keys per (part, query).
 size_t retrieve_topk_workspace_size(int64_t M, int32_t dim, int32_t n_queries);
@@ -138,12 +138,12 @@ cudaError_t launch_retrieve_topk(const RetrieveParams &p, int k, cudaStream_t st
 cudaError_t launch_retrieve_tc_topk(const RetrieveParams &p, int k, int grid, cudaStream_t stream,
                                     uint64_t *launches);
 cudaError_t launch_retrieve(const RetrieveParams &p, cudaStream_t stream);
-cudaError_t retrieve_status_word_read_clear(uint32_t *bits);
+cudaError_t retrieve_status_word(uint32_t **word);
 
 // Complex diagonal A (scan_complex.cu): A is [L][D][N] (re, im) pairs, states
 // [..][D][N] (re, im) pairs.
 cudaError_t launch_scan_complex(const ScanParams &p, cudaStream_t stream);
-cudaError_t scan_complex_status_word_read_clear(uint32_t *bits);
+cudaError_t scan_complex_status_word(uint32_t **word);
 
 // SMC primitives (smc.cu)
 cudaError_t launch_smc_route(const void *emb, int dtype, int64_t n, int dim, const void *dom, int M,
@@ -152,7 +152,7 @@ cudaError_t launch_smc_route(const void *emb, int dtype, int64_t n, int dim, con
 cudaError_t launch_smc_consolidate(float *sem, int64_t n_slots, int64_t elems, const void *states,
                                    int states_dtype, const int64_t *slots, int64_t n, float alpha,
                                    cudaStream_t stream);
-cudaError_t smc_status_word_read_clear(uint32_t *bits);
+cudaError_t smc_status_word(uint32_t **word);
 
 // One layer of the gated delta rule (delta.cu: token by token; delta_chunk.cu: tensor cores).
 struct DeltaParams {
@@ -179,7 +179,8 @@ struct DeltaParams {
 cudaError_t launch_delta_scan(const DeltaParams &p, cudaStream_t stream);
 cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream);
 size_t delta_scan_workspace_size(const DeltaParams &p);
-cudaError_t delta_status_word_read_clear(uint32_t *bits);
+cudaError_t delta_status_word(uint32_t **word);
+cudaError_t delta_chunk_status_word(uint32_t **word);
 
 // Norms of query and key heads with the rotation (qk_norm.cu).
 struct QkNormParams {
@@ -196,7 +197,7 @@ struct QkNormParams {
     int64_t T;
 };
 cudaError_t launch_qk_norm(const QkNormParams &p, cudaStream_t stream);
-cudaError_t qk_norm_status_word_read_clear(uint32_t *bits);
+cudaError_t qk_norm_status_word(uint32_t **word);
 
 // Log probabilities of given tokens (logprobs.cu).
 struct LogprobParams {
@@ -211,6 +212,6 @@ struct LogprobParams {
     float *top_logprob;
 };
 cudaError_t launch_logprobs(const LogprobParams &p, cudaStream_t stream);
-cudaError_t logprobs_status_word_read_clear(uint32_t *bits);
+cudaError_t logprobs_status_word(uint32_t **word);
 
 }  // namespace precog

@@ -546,11 +546,6 @@ cudaError_t launch_logprobs(const LogprobParams &p, cudaStream_t stream) {
     }
 }
 
-cudaError_t logprobs_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_logprob_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_logprob_status, &zero, sizeof(uint32_t));
-}
+cudaError_t logprobs_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_logprob_status); }
 
 }  // namespace precog

@@ -263,11 +263,6 @@ cudaError_t launch_qk_norm(const QkNormParams &p, cudaStream_t stream) {
     }
 }
 
-cudaError_t qk_norm_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_qk_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_qk_status, &zero, sizeof(uint32_t));
-}
+cudaError_t qk_norm_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_qk_status); }
 
 }  // namespace precog

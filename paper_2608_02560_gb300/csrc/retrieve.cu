@@ -793,15 +793,6 @@ cudaError_t launch_retrieve_topk(const RetrieveParams &p, int k, cudaStream_t st
     return e;
 }
 
-cudaError_t retrieve_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0, tc = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_retrieve_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    e = cudaMemcpyToSymbol(g_retrieve_status, &zero, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    e = retrieve_tc_status_word_read_clear(&tc);
-    *bits |= tc;
-    return e;
-}
+cudaError_t retrieve_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_retrieve_status); }
 
 }  // namespace precog

@@ -683,11 +683,6 @@ cudaError_t launch_retrieve_tc_topk(const RetrieveParams &p, int k, int grid, cu
     return launch_tc<8>(p, grid, stream, launches);
 }
 
-cudaError_t retrieve_tc_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_retrieve_status_tc, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_retrieve_status_tc, &zero, sizeof(uint32_t));
-}
+cudaError_t retrieve_tc_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_retrieve_status_tc); }
 
 }  // namespace precog

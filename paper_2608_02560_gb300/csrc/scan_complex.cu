@@ -870,11 +870,6 @@ cudaError_t launch_scan_complex(const ScanParams &p, cudaStream_t stream) {
     return launch_in<__nv_bfloat16>(p, stream);
 }
 
-cudaError_t scan_complex_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_scan_complex_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_scan_complex_status, &zero, sizeof(uint32_t));
-}
+cudaError_t scan_complex_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_scan_complex_status); }
 
 }  // namespace precog

@@ -328,11 +328,6 @@ cudaError_t launch_scan_latency(const ScanParams &p, cudaStream_t stream) {
     return h0 ? launch_l<__nv_bfloat16, true>(p, stream) : launch_l<__nv_bfloat16, false>(p, stream);
 }
 
-cudaError_t scan_latency_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_scan_latency_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_scan_latency_status, &zero, sizeof(uint32_t));
-}
+cudaError_t scan_latency_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_scan_latency_status); }
 
 }  // namespace precog

@@ -36,11 +36,6 @@ cudaError_t launch_wait_timeout(uint32_t limit, cudaStream_t stream) {
     return e;
 }
 
-cudaError_t selftest_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_selftest_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_selftest_status, &zero, sizeof(uint32_t));
-}
+cudaError_t selftest_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_selftest_status); }
 
 }  // namespace precog

@@ -761,11 +761,6 @@ cudaError_t launch_smc_consolidate(float *sem, int64_t n_slots, int64_t elems, c
     return e;
 }
 
-cudaError_t smc_status_word_read_clear(uint32_t *bits) {
-    uint32_t zero = 0;
-    cudaError_t e = cudaMemcpyFromSymbol(bits, g_smc_status, sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    return cudaMemcpyToSymbol(g_smc_status, &zero, sizeof(uint32_t));
-}
+cudaError_t smc_status_word(uint32_t **word) { return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_smc_status); }
 
 }  // namespace precog
