@@ -103,3 +103,18 @@ def test_a_bank_that_receives_the_states_of_broken_sequences(cuda_device):
         ref_S, _ = _ref(None, k, v, g, beta, off, S0)
     _like(table[:, 0], ref_S, TOL_PAIR)
     assert pg.precog_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("dtype,lens,at", [("bfloat16", [200, 130], 70), ("bfloat16", [5000], 2600), ("float32", [90], 33)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_broken_query_breaks_its_own_readout_alone(cuda_device, dtype, lens, at, value):
+    import torch
+    q, k, v, g, beta, off = _tensors(lens, 1, 2, 64, 64, getattr(torch, dtype), cuda_device, 25, rate=0.2)
+    q[at, 0, 3] = value
+    s, y, alone = _scan(q, k, v, g, beta, off, None, torch.float32, cuda_device)
+    with np.errstate(invalid="ignore", over="ignore"):
+        ref_S, ref_y = _ref(q, k, v, g, beta, off)
+    assert np.isfinite(ref_S).all() and not np.isfinite(ref_y[at]).any()
+    tol = TOL_F32 if dtype == "float32" else TOL_PAIR
+    for got, ref in ((s, ref_S), (alone, ref_S), (y, ref_y)):
+        _like(got, ref, tol)
