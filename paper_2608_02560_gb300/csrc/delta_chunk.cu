@@ -83,7 +83,7 @@ constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
 constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = 448;
 
 constexpr int kBarTeam = 1;            // and 2
-constexpr int kBarChain = 3;
+constexpr int kBarChain = 3, kBarAgain = 4;
 
 // A sum of logs as an unevaluated pair: differences of large sums keep their digits.
 struct Log {
@@ -256,96 +256,192 @@ struct Cut {
 };
 __device__ __forceinline__ int64_t segments(int64_t tokens, int len) { return tokens <= len ? 1 : (tokens + len - 1) / len; }
 
-// Tokens begin .. end - 1 once more, one after another as the recurrence is defined, for the value
-// channels whose state the chunks left not finite: there the zeros of T and P met NaN or infinity,
-// 0 * NaN being NaN, and tokens before the broken one lost their readouts with it; or a chunk's whole
-// growth left fp32, which token by token it need not. A warp has 8 rows (`broken`: bits), 4 lanes a row,
-// lane l the four-number groups l, l + 4, ... of its columns. Once nothing of its rows is finite nothing
-// will be again, and what is left of them is NaN. No sequence that stays finite comes here.
-__device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, int first_row, unsigned broken) {
-    constexpr int kGroups = 8;
-    const int64_t begin = job.begin, end = job.end;
-    const int head = job.head;
-    const States from = job.from, to = job.to;
-    const int lane4 = threadIdx.x & 3, row = first_row + (threadIdx.x & 31) / 4, qk = head / (p.hv / p.hk);
-    const bool mine = (broken >> ((threadIdx.x & 31) / 4) & 1u) != 0u;   // (then the row is one of the head's)
-    float4 s[kGroups];
-    auto load4 = [](const __nv_bfloat16 *x) {
-        const uint2 r = *reinterpret_cast<const uint2 *>(x);
-        return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
-                           __uint_as_float(r.y & 0xffff0000u));
-    };
-    auto dot4 = [](float4 a, float4 b, float sum) { return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, sum)))); };
-    auto row_sum = [](float v) {
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        return v + __shfl_xor_sync(0xffffffffu, v, 1);
-    };
+// A job's tokens once more, one after another as the recurrence is defined, for the value channels whose
+// state the chunks left not finite: there the zeros of T and P met NaN or infinity, 0 * NaN being NaN, and
+// tokens before the broken one lost their readouts with it; or a chunk's whole growth left fp32, which
+// token by token it need not. The first 16 warps, 8 channels each from `first` on (`broken`: bits), 8 lanes
+// two channels: lane l of the 8 has the four-number groups l, l + 8, ... of both ones' keys. Tokens pass
+// through `room`, 64 at a time, as fp32, keys padded with zeros. Once nothing of a warp's states is finite
+// nothing will be again, and the rest of its readouts is NaN. No sequence that stays finite comes here.
+// 152 heads of 128 x 128, 4096 tokens, 244 us: all broken by their first token 535 us, by their last 3.7 ms.
+constexpr int kAgain = 512;
+__host__ __device__ constexpr int again_bytes(int keys) { return 4 * (2 * kC * keys + kC * kM + 3 * kC); }
+template <int NA>
+__device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, float *room, int first, const uint32_t *broken) {
+    constexpr int kKeys = NA * 64, kGroups = kKeys / 32, R = 2;   // four-number groups and channels a lane
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lane8 = lane & 7;
+    const int row = warp * 8 + lane / 8, dk = p.dk, qk = job.head / (p.hv / p.hk);   // and row + 4, counted from `first`
+    const int channels = p.dv - first < kM ? p.dv - first : kM;
+    bool mine[R];                                  // (then the channel is one of the head's)
 #pragma unroll
-    for (int j = 0; j < kGroups; ++j) {
-        const int col = 4 * (lane4 + 4 * j);
-        s[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!mine || from.base == nullptr || col >= p.dk) continue;
-        const int64_t at = from.at + static_cast<int64_t>(row) * p.dk + col;
-        s[j] = from.dtype == PRECOG_F32 ? *reinterpret_cast<const float4 *>(static_cast<const float *>(from.base) + at)
-                                        : load4(static_cast<const __nv_bfloat16 *>(from.base) + at);
-    }
-    auto write_y = [&](int64_t t, float v) {
-        if (!mine || lane4 != 0) return;
-        const int64_t at = (t * p.hv + head) * p.dv + row;
+    for (int r = 0; r < R; ++r) mine[r] = (broken[warp / 4] >> (warp % 4 * 8 + lane / 8 + 4 * r) & 1u) != 0u;
+    const bool want_y = p.y != nullptr;
+    float *ks = room, *qs = ks + kC * kKeys, *vs = qs + kC * kKeys, *as = vs + kC * kM, *bs = as + kC, *kqs = bs + kC;
+    f2 s[R][kGroups][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            const int col = 4 * (lane8 + 8 * j);
+            s[r][j][0] = s[r][j][1] = pack2(0.f, 0.f);
+            if (!mine[r] || job.from.base == nullptr || col >= dk) continue;
+            const int64_t at = job.from.at + static_cast<int64_t>(first + row + 4 * r) * dk + col;
+            if (job.from.dtype == PRECOG_F32) {
+                const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(job.from.base) + at);
+                s[r][j][0] = pack2(v.x, v.y), s[r][j][1] = pack2(v.z, v.w);
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(job.from.base) + at);
+                s[r][j][0] = pack2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
+                s[r][j][1] = pack2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+            }
+        }
+    auto write_y = [&](int64_t t, int r, float v) {
+        const int64_t at = (t * p.hv + job.head) * p.dv + first + row + 4 * r;
         if (p.y_dtype == PRECOG_F32) static_cast<float *>(p.y)[at] = v;
         else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
     };
-    int64_t t = begin;
-#pragma unroll 1
-    for (; t < end; ++t) {
-        if ((t - begin) % kC == 0) {
-            bool left = false;
+    auto no_more = [&](int64_t t, int64_t end) {   // NaN from t on
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            for (int64_t u = t + lane8; want_y && mine[r] && u < end; u += 8) write_y(u, r, __int_as_float(0x7fffffff));
+    };
+    auto open = [&] {                              // anything finite left in the warp
+        bool left = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < kGroups; ++j)
-                left |= mine && 4 * (lane4 + 4 * j) < p.dk && (isfinite(s[j].x) || isfinite(s[j].y) || isfinite(s[j].z) || isfinite(s[j].w));
-            if (!__any_sync(0xffffffffu, left)) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float x, y;
+                    unpack2(s[r][j][i], x, y);
+                    left |= mine[r] && 4 * (lane8 + 8 * j) < dk && (isfinite(x) || isfinite(y));
+                }
+        return __any_sync(0xffffffffu, left);
+    };
+    // 64 rows of `width` numbers from column `col` on, `pitch` apart, zeros beyond the width and the last token
+    auto bring = [&](float *to, int pitch, const void *base, int64_t stride, int64_t col, int width, int64_t t0) {
+        uint4 v[2];                                     // (kC x pitch / 8 pieces: at most two a thread)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = (threadIdx.x + i * kAgain) * 8, t = e / pitch, c = e % pitch;
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (t < kC && t0 + t < job.end && c < width)
+                v[i] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(base) + (t0 + t) * stride + col + c);
         }
-        const __nv_bfloat16 *kr = static_cast<const __nv_bfloat16 *>(p.k) + t * p.k_stride + static_cast<int64_t>(qk) * p.dk;
-        const __nv_bfloat16 *qr = p.y ? static_cast<const __nv_bfloat16 *>(p.q) + t * p.q_stride + static_cast<int64_t>(qk) * p.dk : kr;
-        const float g = p.g[t * p.hv + head], beta = p.beta[t * p.hv + head], a = g < kLeastGate ? 0.f : expf(g);
-        const float v = mine ? to_f32(static_cast<const __nv_bfloat16 *>(p.v)[t * p.v_stride + static_cast<int64_t>(head) * p.dv + row]) : 0.f;
-        float sk = 0.f, sq = 0.f, kq = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = (threadIdx.x + i * kAgain) * 8;
+            if (e >= kC * pitch) continue;
+            float4 lo, hi;
+            lo.x = __uint_as_float(v[i].x << 16), lo.y = __uint_as_float(v[i].x & 0xffff0000u);
+            lo.z = __uint_as_float(v[i].y << 16), lo.w = __uint_as_float(v[i].y & 0xffff0000u);
+            hi.x = __uint_as_float(v[i].z << 16), hi.y = __uint_as_float(v[i].z & 0xffff0000u);
+            hi.z = __uint_as_float(v[i].w << 16), hi.w = __uint_as_float(v[i].w & 0xffff0000u);
+            *reinterpret_cast<float4 *>(to + e) = lo;
+            *reinterpret_cast<float4 *>(to + e + 4) = hi;
+        }
+    };
+    bool going = open();
+    int64_t t0 = job.begin;
+#pragma unroll 1
+    for (; t0 < job.end; t0 += kC) {
+        if (!named_any(kBarAgain, kAgain, going)) break;   // (and the last tokens have been read)
+        bring(ks, kKeys, p.k, p.k_stride, static_cast<int64_t>(qk) * dk, dk, t0);
+        if (want_y) bring(qs, kKeys, p.q, p.q_stride, static_cast<int64_t>(qk) * dk, dk, t0);
+        bring(vs, kM, p.v, p.v_stride, static_cast<int64_t>(job.head) * p.dv + first, channels, t0);
+        if (threadIdx.x < kC && t0 + threadIdx.x < job.end) {
+            const float g = p.g[(t0 + threadIdx.x) * p.hv + job.head];
+            as[threadIdx.x] = g < kLeastGate ? 0.f : expf(g);
+            bs[threadIdx.x] = p.beta[(t0 + threadIdx.x) * p.hv + job.head];
+        }
+        named_sync(kBarAgain, kAgain);
+        if (want_y) {   // k.q of 4 tokens a warp
+            for (int t = warp * 4; t < warp * 4 + 4; ++t) {
+                float sum = 0.f;
+                for (int c = lane; c < kKeys; c += 32) sum = fmaf(ks[t * kKeys + c], qs[t * kKeys + c], sum);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane == 0) kqs[t] = sum;
+            }
+            named_sync(kBarAgain, kAgain);
+        }
+        const int n = job.end - t0 < kC ? static_cast<int>(job.end - t0) : kC;
+        if (!going) {
+            no_more(t0, t0 + n);
+            continue;
+        }
+#pragma unroll 1
+        for (int t = 0; t < n; ++t) {
+            const float4 *k = reinterpret_cast<const float4 *>(ks + t * kKeys) + lane8, *q = reinterpret_cast<const float4 *>(qs + t * kKeys) + lane8;
+            float4 key[kGroups];
+            f2 x[R][2], y[R][2];
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[r][0] = x[r][1] = y[r][0] = y[r][1] = pack2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) {
+                key[j] = k[8 * j];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    x[r][0] = fma2(s[r][j][0], pack2(key[j].x, key[j].y), x[r][0]);
+                    x[r][1] = fma2(s[r][j][1], pack2(key[j].z, key[j].w), x[r][1]);
+                }
+            }
+            if (want_y) {
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) {
+                    const float4 v = q[8 * j];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        y[r][0] = fma2(s[r][j][0], pack2(v.x, v.y), y[r][0]);
+                        y[r][1] = fma2(s[r][j][1], pack2(v.z, v.w), y[r][1]);
+                    }
+                }
+            }
+            auto total = [](const f2 (&v)[2]) {
+                float a, b, c, d;
+                unpack2(v[0], a, b);
+                unpack2(v[1], c, d);
+                return (a + b) + (c + d);
+            };
+            float sk[R], sq[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) sk[r] = total(x[r]), sq[r] = total(y[r]);
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+                for (int r = 0; r < R; ++r) sk[r] += __shfl_xor_sync(0xffffffffu, sk[r], o), sq[r] += __shfl_xor_sync(0xffffffffu, sq[r], o);
+            const float a = as[t], beta = bs[t];
+            const f2 aa = pack2(a, a);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float u = beta * fmaf(-a, sk[r], vs[t * kM + row + 4 * r]);
+                const f2 uu = pack2(u, u);
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) {
+                    s[r][j][0] = fma2(uu, pack2(key[j].x, key[j].y), mul2(aa, s[r][j][0]));
+                    s[r][j][1] = fma2(uu, pack2(key[j].z, key[j].w), mul2(aa, s[r][j][1]));
+                }
+                if (want_y && mine[r] && lane8 == 0) write_y(t0 + t, r, p.scale * fmaf(u, kqs[t], a * sq[r]));
+            }
+        }
+        going = open();
+    }
+    no_more(t0, job.end);
+    if (job.to.base == nullptr) return;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < kGroups; ++j) {
-            const int col = 4 * (lane4 + 4 * j);
-            if (col >= p.dk) continue;
-            const float4 k = load4(kr + col), q = load4(qr + col);
-            s[j] = make_float4(a * s[j].x, a * s[j].y, a * s[j].z, a * s[j].w);
-            sk = dot4(s[j], k, sk);
-            sq = dot4(s[j], q, sq);
-            kq = dot4(k, q, kq);
+            const int col = 4 * (lane8 + 8 * j);
+            if (!mine[r] || col >= dk) continue;
+            const int64_t at = job.to.at + static_cast<int64_t>(first + row + 4 * r) * dk + col;
+            float4 v;
+            unpack2(s[r][j][0], v.x, v.y);
+            unpack2(s[r][j][1], v.z, v.w);
+            if (job.to.dtype == PRECOG_F32) *reinterpret_cast<float4 *>(static_cast<float *>(job.to.base) + at) = v;
+            else *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(job.to.base) + at) = make_uint2(bits2(v.x, v.y), bits2(v.z, v.w));
         }
-        const float u = beta * (v - row_sum(sk));
-        sq = row_sum(sq), kq = row_sum(kq);
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-            const int col = 4 * (lane4 + 4 * j);
-            if (col >= p.dk) continue;
-            const float4 k = load4(kr + col);
-            s[j] = make_float4(fmaf(u, k.x, s[j].x), fmaf(u, k.y, s[j].y), fmaf(u, k.z, s[j].z), fmaf(u, k.w, s[j].w));
-        }
-        if (p.y) write_y(t, p.scale * fmaf(u, kq, sq));
-    }
-    for (; p.y && t < end; ++t) write_y(t, __int_as_float(0x7fffffff));
-    if (!mine || to.base == nullptr) return;
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j) {
-        const int col = 4 * (lane4 + 4 * j);
-        if (col >= p.dk) continue;
-        const int64_t at = to.at + static_cast<int64_t>(row) * p.dk + col;
-        if (to.dtype == PRECOG_F32) {
-            *reinterpret_cast<float4 *>(static_cast<float *>(to.base) + at) = s[j];
-        } else {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(s[j].x, s[j].y), hi = __floats2bfloat162_rn(s[j].z, s[j].w);
-            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(to.base) + at) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-        }
-    }
 }
 
 template <int NA, bool Y, bool CUT>
@@ -1032,10 +1128,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    if (!kept && warp < kM / 8) {
-        const unsigned rows = sm.broken[warp / 4] >> (warp % 4 * 8) & 0xffu;
-        if (rows) once_more(p, sm.job, slice * kM + warp * 8, rows);
-    }
+    static_assert(again_bytes(kKeys) <= static_cast<int>(sizeof(sm.v) + sizeof(sm.kq)), "the tokens' room");
+    if (!kept && warp < kAgain / 32 && (sm.broken[0] | sm.broken[1] | sm.broken[2] | sm.broken[3]) != 0u)
+        once_more<NA>(p, sm.job, reinterpret_cast<float *>(sm.v), slice * kM, sm.broken);
 }
 
 // The segments' initial states: state after segment s = state before it * M + B, in the place of B,

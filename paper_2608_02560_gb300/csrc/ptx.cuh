@@ -361,6 +361,16 @@ __device__ __forceinline__ void named_sync(int id, int threads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// The same, and whether `v` holds in any of the threads.
+__device__ __forceinline__ bool named_any(int id, int threads, bool v) {
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n bar.red.or.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(any)
+                 : "r"(id), "r"(threads), "r"(static_cast<uint32_t>(v))
+                 : "memory");
+    return any != 0;
+}
+
 // 2^x on the SFU (MUFU.EX2), flush-to-zero: the hardware instruction itself.
 __device__ __forceinline__ float ex2(float x) {
     float y;
