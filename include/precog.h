@@ -458,8 +458,8 @@ typedef struct precog_delta_inputs {
  *   workspace   device scratch of at least precog_delta_scan_workspace_size() bytes, 16-byte
  *               aligned; 0 bytes (and then NULL) unless few long sequences are to be cut
  *               into segments that run at once
- * With BF16 inputs, batches whose mean length is more than some thirty tokens (12 where the
- * batch fills the GPU) run on the tensor cores in chunks of 64 tokens: state and sums stay
+ * With BF16 inputs, batches whose mean length T_tot / n_seqs is more than some thirty tokens (12
+ * where the batch fills the GPU) run on the tensor cores in chunks of 64 tokens: state and sums stay
  * fp32 and every intermediate operand is carried as a pair of bf16 numbers (16 significant
  * bits). With keys of norm 1 results agree with the recurrence, in units of the largest entry, to
  * about 1e-5 where keys differ and dk is 64 or more, and to 1e-4 whatever the keys while betas stay

@@ -366,14 +366,16 @@ cudaError_t launch_delta_step(const DeltaParams &p, cudaStream_t stream) {
 namespace {
 
 // Whether the chunk kernel is the faster one, by what both measured (16 heads of 128 x 128 unless said):
-//   1 sequence of 32 / 48 tokens    token 10.2 / 13.7 us  chunk 13.1 / 12.8
-//   4 sequences of 16 / 24          token 10.3 / 14.7     chunk 13.8 / 13.5
-//   16 of 12 / 16                   token 27.3 / 32.7     chunk 27.1 / 26.8
-//   256 of 8 / 16                   token 257 / 405       chunk 364 / 358
-//   64 of 40 / 48, 64 x 64          token 67 / 78         chunk 74 / 75
+//   1 sequence of 32 / 48 tokens    token 10.2 / 13.7 us  chunk 13.0 / 12.8
+//   4 sequences of 16 / 24          token 10.3 / 14.7     chunk 13.8 / 13.7
+//   16 of 12 / 16                   token 27.3 / 32.7     chunk 27.5 / 27.1
+//   256 of 8 / 16                   token 257 / 405       chunk 370 / 365
+//   64 of 40 / 48, 64 x 64          token 67 / 78         chunk 76 / 76
 // A round of CTAs in chunks takes 13 us however few its tokens are. A token of the other kernel takes
 // 0.25 us by its latency, or 6.2 ns a head of 128 x 128 where the SMs are full. Lengths lie on the
-// device: the rule knows their mean.
+// device: the rule knows their mean, T_tot / n_seqs, and a batch whose one long sequence is hidden among
+// short ones goes token by token (400 tokens among fifteen empty sequences, one head: 100 us by these
+// figures, some 30 in chunks).
 bool in_chunks(const DeltaParams &p) {
     if (p.in_dtype != PRECOG_BF16 || p.n_seqs <= 0) return false;
     const double heads = static_cast<double>(p.n_seqs) * p.hv, tokens = static_cast<double>(p.T_tot) / p.n_seqs;

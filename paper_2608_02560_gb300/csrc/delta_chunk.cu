@@ -30,13 +30,13 @@
 // q.k, which the teams wait for. Warp 17: issues every other MMA, so that no working warp waits in the
 // queue of the tensor cores. Warp 18: V in and y rows out.
 //
-// What bounds it: in full rounds the chain and the teams alike, about 4900 cycles a chunk (6900 with a
-// readout) at 0.45 instructions a cycle of each scheduler, the tensor cores' pipe 31 to 34 % busy, DRAM
-// at 16 to 20 % of its rate; in rounds of a chunk or two the 13 us from a CTA's start to its end, most
-// of them one chunk's way through a team. Measured, bf16, 128 x 128 a head: 256 sequences of 256 to
-// 4096 tokens, 8 heads, states alone, 1338 us (218 TFLOP/s of the recurrence's operations); 96
-// sequences of 1 to 200 tokens, 16 heads, with a readout, 174 us; one of 64 tokens 14 us; one of 32,768
-// tokens, cut into segments, 695 us.
+// What bounds it: in full rounds the chain and the teams alike, 2.44 us or some 4700 cycles a chunk (3.6
+// us, 7000 with a readout) at 0.45 instructions a cycle of each scheduler, the tensor cores' pipe 33 to 35 %
+// busy, DRAM at 16 to 21 % of its rate; in rounds of a chunk or two the 13 us from a CTA's start to its
+// end, most of them one chunk's way through a team. Measured, bf16, 128 x 128 a head: 256 sequences of 256
+// to 4096 tokens, 8 heads, states alone, 1343 to 1366 us (215 TFLOP/s of the recurrence's operations); 96
+// sequences of 1 to 200 tokens, 16 heads, with a readout, 174 to 178 us; one of 64 tokens 15 us; one of
+// 32,768 tokens, cut into segments, 634 us.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
@@ -1258,7 +1258,7 @@ cudaError_t launch_all(const DeltaParams &p, const Maps &maps, int slices, Cut c
 // another: whole sequences are as long as their rounds of CTAs; segments go in one pass for B and M,
 // one step of the join each, and one pass for themselves. Cut only where that is a third shorter: the
 // estimate knows the sequences' mean length alone. One sequence, 16 heads of 128 x 128, with a readout:
-// 2048 tokens 89 us (whole 115), 4096 tokens 130 (222), 32,768 tokens 689 (1709).
+// 2048 tokens 85 us (whole 116), 4096 tokens 124 (222), 32,768 tokens 627 (1702).
 int cut_length(const DeltaParams &p) {
     const int64_t sms = device_sm_count(), slices = (p.dv + kM - 1) / kM, items = p.n_seqs * p.hv * slices;
     if (items > sms || p.T_tot / p.n_seqs < 16 * kC) return 0;

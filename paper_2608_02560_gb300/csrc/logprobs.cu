@@ -18,8 +18,8 @@
 // ever inserted. Batches whose maximum does not reach the bound cost one comparison.
 //
 // Memory and the instructions, 5 to 8 an entry, bound it alike: 2048 rows of 50,257 bf16 logits, 5 best,
-// take 53 us (3.88 TB/s, 0.57 of the measured copy rate, schedulers 65 % busy); 61 rows of 128,001 fp32
-// ones with nine tenths at -infinity, 20 best, 22 us, by the latency of the joins; one row of 32,000
+// take 53 us (3.87 TB/s, 0.57 of the measured copy rate, schedulers 66 % busy); 61 rows of 128,001 fp32
+// ones with nine tenths at -infinity, 20 best, 22.5 us, by the latency of the joins; one row of 32,000
 // 8.2 us. A CTA takes a row; with few rows a cluster of up to 8 shares one and joins over distributed
 // shared memory.
 #include <cmath>

@@ -8,8 +8,9 @@
 // pairs are neighbours, else four of the lower half and the same four of the upper one; outputs
 // may therefore be the inputs. A group keeps its token's rotations and the weights in registers
 // and takes kHeads heads, kFly of them in flight. What bounds it is memory: each number is read
-// once and written once (65,521 tokens of 16 + 8 heads of 128 bf16: 145 us, 5.66 TB/s, 0.83 of the
-// measured copy rate; a single token its launch). A group of lanes a head, rather than a warp, keeps
+// once and written once (65,521 tokens of 16 + 8 heads of 128 bf16, slices of a projection, weights, pairs
+// of neighbours: 146 us, 5.64 TB/s, 0.83 of the measured copy rate; the same of whole tensors, no weights,
+// pairs of halves, 134; a single token its launch). A group of lanes a head, rather than a warp, keeps
 // every lane's loads 16 bytes wide: a first kernel of 32 scalar lanes a head took 468 us.
 #include <type_traits>
 
@@ -214,8 +215,9 @@ __global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const QkNormParam
 
 template <typename T, int G, bool HALF, bool WEIGHT>
 cudaError_t launch_lanes(const QkNormParams &p, cudaStream_t stream) {
-    // Eight heads a group reuse its rotations and weights (16 + 8 heads of 128: 65,521 tokens 132 us, one
-    // head a group 380; 1000 tokens 3.6 and 6.8); fewer where that would leave SMs with less than two CTAs.
+    // Eight heads a group reuse its rotations and weights (16 + 8 heads of 128, whole tensors, halves: 65,521
+    // tokens 134 us, one head a group 380; 1000 tokens 3.5 and 6.8); fewer where that would leave SMs with
+    // less than two CTAs.
     int per = kHeads;
     auto parts_of = [&](int heads) { return (heads + per - 1) / per; };
     while (per > 1 && p.T * (parts_of(p.heads[0]) + parts_of(p.heads[1])) * G < 2LL * device_sm_count() * kThreads) per /= 2;
@@ -237,7 +239,7 @@ template <typename T>
 cudaError_t launch_typed(const QkNormParams &p, cudaStream_t stream) {
     cudaError_t e;
     if (p.rot != 0 && !p.interleaved && p.rot % 8 != 0) {
-        // (slower where both could run: 65,521 tokens of 16 + 8 heads of 128 take 415 us, the others 132)
+        // (slower where both could run: the same 65,521 tokens take 415 us, the other kernel 134)
         const int64_t vectors = p.T * (static_cast<int64_t>(p.heads[0]) + p.heads[1]), blocks = (vectors * 16 + kThreads - 1) / kThreads;
         if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
         qk_norm_any_kernel<T, 16><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p, vectors);
