@@ -409,8 +409,8 @@ precog_status precog_smc_consolidate(float *semantic, int64_t n_slots, int64_t s
  *          be at least one row long (ignored where there is at most one row).
  *   g, beta : fp32 [rows][n_v_heads], dense. g is the logarithm of the decay (usually <= 0;
  *          -infinity forgets the state, and so does anything below -128, which decays by
- *          less than fp32 can hold; growth, g > 0, has to stay within fp32 over the tokens of a call's
- *          sequence where a workspace is in use).
+ *          less than fp32 can hold; gates that grow more than e-fold over 64 tokens, or over a part
+ *          of a sequence that is cut, make the scan go token by token there).
  * q may be NULL when no readout is requested. Requirements: dk a multiple of 8 in [8, 128],
  * dv a multiple of 8 in [8, 4096], n_v_heads a multiple of n_qk_heads.
  */

@@ -44,13 +44,16 @@
 // NaN and infinity among the inputs of a token reach its whole chunk, 0 * NaN being NaN in the products
 // with T and P, and leave the channel's state not finite, from then on. So the state is looked at once, at
 // the end, and a channel that broke is done again token by token (once_more): sequences that stay finite
-// pay one barrier for it.
+// pay two barriers for it. So is every channel where gates grow more than e-fold over a chunk: rounding
+// grows with them in the differences that make T (g = 0.1 a token, beta = 1: 3e-3 of the largest entry; g = 0.5:
+// anything), though the correction may hold the state itself back.
 //
 // Few sequences leave SMs idle, and a chain is as long as its sequence. Then each sequence is cut into
 // segments: a state passes through one as S M + B, M a product of e^g (I - beta k k^T) over its tokens.
 // First B (from the zero state, or for the first segment from the initial one) and M (the rows of the
 // identity, with v = 0) of all segments but the last; then the segments' initial states one after
-// another (delta_join_kernel); then the segments themselves, with their readout.
+// another (delta_join_kernel); then the segments themselves, with their readout. Where a segment's gates
+// grow, or B or M is not finite, the join rolls rows over the segment itself.
 //
 // Tensor memory: S [128 columns]; a pair area [128]: S's pair, then U, whose place its decayed pair
 // takes; places [64] by turns: a chunk's k.k and q.k, then its S k, then that one's pair, then U's
@@ -78,6 +81,9 @@ constexpr int kH = kC / 2, kB = kC / 4;    // the inverse: blocks of 16, joined 
 constexpr int kBlock = kH * kH;            // a quarter of A
 constexpr uint32_t kTile = kC * 128;   // bytes of a [64 tokens][64 keys] bf16 tile
 constexpr float kLeastGate = -128.f;   // e^-128 is 0 in fp32
+// Growth (sums of positive gates) up to which chunks and segments keep their digits. The entries of T and of
+// M are differences of e^growth, so what rounding leaves of them is that much larger than their own.
+constexpr float kMostGrowth = 1.f;
 
 // tensor memory columns
 constexpr uint32_t kColS = 0, kColPair = 128, kColK = 256, kColQ = 448;
@@ -122,11 +128,14 @@ struct States {
     int64_t at;                // elements before row 0
 };
 
-// A CTA's tokens, the state before them and where the one behind them goes (nowhere: nullptr).
+// A CTA's tokens, the state before them and where the one behind them goes (nowhere: nullptr); in shared
+// memory for the end, since in registers they made the chunks' own spill (one long sequence: 714 us).
 struct Job {
     int64_t begin, end;
     States from, to;
     int head;
+    bool m;                    // it is M
+    bool again;                // what breaks is done again (else: by the join)
 };
 
 template <int NA, bool Y>
@@ -146,7 +155,8 @@ struct Smem {
     uint64_t done_prep[kSlots], free_slot[kSlots], ready[2], done_o[2];
     uint64_t have_s[2], have_k, have_d, have_u;   // the chain's operands are in tensor memory
     uint64_t done_ks, done_qs, done_u, done_s;
-    uint32_t broken[kM / 32];         // bit: a value channel whose state is not finite
+    uint32_t broken[kM / 32];         // bit: a value channel that the chunks cannot be trusted with
+    uint32_t growing;                 // a gate above 0 was seen
     Job job;
     uint32_t tmem_base;
 };
@@ -256,17 +266,33 @@ struct Cut {
 };
 __device__ __forceinline__ int64_t segments(int64_t tokens, int len) { return tokens <= len ? 1 : (tokens + len - 1) / len; }
 
+// Whether a job's gates grow too far for the chunks, or its whole length's for M; by a warp.
+__device__ __noinline__ bool too_far(const DeltaParams &p, const Job &job) {
+    const int lane = threadIdx.x & 31;
+    float growth = 0.f;
+    for (int64_t t0 = job.begin; t0 < job.end; t0 += kC) {
+        float up = 0.f;
+        for (int64_t t = t0 + lane; t < t0 + kC && t < job.end; t += 32) up += fmaxf(p.g[t * p.hv + job.head], 0.f);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) up += __shfl_xor_sync(0xffffffffu, up, o);
+        growth = job.m ? growth + up : up;
+        if (growth > kMostGrowth) return true;
+    }
+    return false;
+}
+
 // A job's tokens once more, one after another as the recurrence is defined, for the value channels whose
 // state the chunks left not finite: there the zeros of T and P met NaN or infinity, 0 * NaN being NaN, and
-// tokens before the broken one lost their readouts with it; or a chunk's whole growth left fp32, which
-// token by token it need not. The first 16 warps, 8 channels each from `first` on (`broken`: bits), 8 lanes
+// tokens before the broken one lost their readouts with it; and for all of them where gates grow. The first
+// 16 warps, 8 channels each from `first` on (`broken`: bits), 8 lanes
 // two channels: lane l of the 8 has the four-number groups l, l + 8, ... of both ones' keys. Tokens pass
 // through `room`, 64 at a time, as fp32, keys padded with zeros. Once nothing of a warp's states is finite
-// nothing will be again, and the rest of its readouts is NaN. No sequence that stays finite comes here.
+// nothing will be again, and the rest of its readouts is NaN. No sequence comes here that stays finite and
+// whose gates decay.
 // 152 heads of 128 x 128, 4096 tokens, 244 us: all broken by their first token 535 us, by their last 3.7 ms.
 constexpr int kAgain = 512;
 __host__ __device__ constexpr int again_bytes(int keys) { return 4 * (2 * kC * keys + kC * kM + 3 * kC); }
-template <int NA>
+template <int NA, bool Y>
 __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, float *room, int first, const uint32_t *broken) {
     constexpr int kKeys = NA * 64, kGroups = kKeys / 32, R = 2;   // four-number groups and channels a lane
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lane8 = lane & 7;
@@ -275,7 +301,6 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
     bool mine[R];                                  // (then the channel is one of the head's)
 #pragma unroll
     for (int r = 0; r < R; ++r) mine[r] = (broken[warp / 4] >> (warp % 4 * 8 + lane / 8 + 4 * r) & 1u) != 0u;
-    const bool want_y = p.y != nullptr;
     float *ks = room, *qs = ks + kC * kKeys, *vs = qs + kC * kKeys, *as = vs + kC * kM, *bs = as + kC, *kqs = bs + kC;
     f2 s[R][kGroups][2];
 #pragma unroll
@@ -303,7 +328,7 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
     auto no_more = [&](int64_t t, int64_t end) {   // NaN from t on
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            for (int64_t u = t + lane8; want_y && mine[r] && u < end; u += 8) write_y(u, r, __int_as_float(0x7fffffff));
+            for (int64_t u = t + lane8; Y && mine[r] && u < end; u += 8) write_y(u, r, __int_as_float(0x7fffffff));
     };
     auto open = [&] {                              // anything finite left in the warp
         bool left = false;
@@ -348,7 +373,7 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
     for (; t0 < job.end; t0 += kC) {
         if (!named_any(kBarAgain, kAgain, going)) break;   // (and the last tokens have been read)
         bring(ks, kKeys, p.k, p.k_stride, static_cast<int64_t>(qk) * dk, dk, t0);
-        if (want_y) bring(qs, kKeys, p.q, p.q_stride, static_cast<int64_t>(qk) * dk, dk, t0);
+        if (Y) bring(qs, kKeys, p.q, p.q_stride, static_cast<int64_t>(qk) * dk, dk, t0);
         bring(vs, kM, p.v, p.v_stride, static_cast<int64_t>(job.head) * p.dv + first, channels, t0);
         if (threadIdx.x < kC && t0 + threadIdx.x < job.end) {
             const float g = p.g[(t0 + threadIdx.x) * p.hv + job.head];
@@ -356,7 +381,7 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
             bs[threadIdx.x] = p.beta[(t0 + threadIdx.x) * p.hv + job.head];
         }
         named_sync(kBarAgain, kAgain);
-        if (want_y) {   // k.q of 4 tokens a warp
+        if (Y) {   // k.q of 4 tokens a warp
             for (int t = warp * 4; t < warp * 4 + 4; ++t) {
                 float sum = 0.f;
                 for (int c = lane; c < kKeys; c += 32) sum = fmaf(ks[t * kKeys + c], qs[t * kKeys + c], sum);
@@ -387,7 +412,7 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
                     x[r][1] = fma2(s[r][j][1], pack2(key[j].z, key[j].w), x[r][1]);
                 }
             }
-            if (want_y) {
+            if (Y) {
 #pragma unroll
                 for (int j = 0; j < kGroups; ++j) {
                     const float4 v = q[8 * j];
@@ -422,7 +447,7 @@ __device__ __noinline__ void once_more(const DeltaParams &p, const Job &job, flo
                     s[r][j][0] = fma2(uu, pack2(key[j].x, key[j].y), mul2(aa, s[r][j][0]));
                     s[r][j][1] = fma2(uu, pack2(key[j].z, key[j].w), mul2(aa, s[r][j][1]));
                 }
-                if (want_y && mine[r] && lane8 == 0) write_y(t0 + t, r, p.scale * fmaf(u, kqs[t], a * sq[r]));
+                if (Y && mine[r] && lane8 == 0) write_y(t0 + t, r, p.scale * fmaf(u, kqs[t], a * sq[r]));
             }
         }
         going = open();
@@ -537,6 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&sm.done_u, 1);
         mbar_init(&sm.done_s, 1);
         for (int i = 0; i < kM / 32; ++i) sm.broken[i] = 0u;
+        sm.growing = 0u;
         fence_barrier_init();
     }
     if (warp == kMmaWarp) {
@@ -665,6 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto gate = [&](int c) {
             constexpr float kL = 1.44269502f, kLl = 1.92596303e-8f;   // log2 e
             Gates &to = sm.gates[c % kStages];
+            if (g[0] > 0.f || g[1] > 0.f) sm.growing = 1u;
             Log x[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -919,7 +946,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t col_s = tm + kColS + half * kHalf;
         {   // initial state
             const int64_t head_elems = static_cast<int64_t>(p.dv) * p.dk;
-            Job job = {begin, end, {nullptr, PRECOG_F32, 0}, {nullptr, PRECOG_F32, 0}, head};
+            Job job = {begin, end, {nullptr, PRECOG_F32, 0}, {nullptr, PRECOG_F32, 0}, head, ident, !kept || (first && !ident)};
             if (CUT && first && !last && cut.joined) {   // (the bank may be where the last segment's state goes)
                 job.from = States{cut.begins, PRECOG_F32, (seq * p.hv + head) * head_elems};
             } else if (first && p.bank && !ident) {
@@ -1093,8 +1120,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait(&sm.done_s, ph, patience);
             tc_fence_after();
         }
-        // ---- the state leaves; rows that are not finite are left to once_more ----
+        // ---- the state leaves; broken rows are left to once_more ----
         {
+            named_sync(kBarChain, kChain);   // (thread 0 wrote the job, which a sequence without chunks waits for here alone)
+            const bool again = !kept || (first && !ident), grown = sm.growing != 0u && too_far(p, sm.job);
             uint32_t r[NA][32];
             f2 zeros = pack2(0.f, 0.f);      // 0 x, summed
 #pragma unroll
@@ -1106,18 +1135,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             float x, y;
             unpack2(zeros, x, y);
-            if (!kept && live && !(x + y == 0.f)) atomicOr(&sm.broken[quarter], 1u << lane);
+            if (live && (grown || (again && !(x + y == 0.f)))) atomicOr(&sm.broken[quarter], 1u << lane);
             named_sync(kBarChain, kChain);
             const States to = sm.job.to;
             const int64_t at = to.at + static_cast<int64_t>(ident ? row : ch) * p.dk;
-            if (to.base && live && (sm.broken[quarter] >> lane & 1u) == 0u) {
+            const bool broke = (sm.broken[quarter] >> lane & 1u) != 0u;
+            if (to.base && live && !(broke && again)) {
 #pragma unroll
                 for (int e = 0; e < kHalf; e += 8)
                     if (const int col = half * kHalf + e; col < p.dk) {
                         float v[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[e / 32][e % 32 + i]);
-                        delta_store8(to.base, to.dtype, at + col, v);
+                        for (int i = 0; i < 8; ++i) v[i] = ident && broke ? __int_as_float(0x7fffffff) : __uint_as_float(r[e / 32][e % 32 + i]);
+                        delta_store8(to.base, to.dtype, at + col, v);   // (NaN for M: the join goes without it)
                     }
             }
         }
@@ -1129,15 +1159,57 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_dealloc(tmem, 512);
     }
     static_assert(again_bytes(kKeys) <= static_cast<int>(sizeof(sm.v) + sizeof(sm.kq)), "the tokens' room");
-    if (!kept && warp < kAgain / 32 && (sm.broken[0] | sm.broken[1] | sm.broken[2] | sm.broken[3]) != 0u)
-        once_more<NA>(p, sm.job, reinterpret_cast<float *>(sm.v), slice * kM, sm.broken);
+    if (sm.job.again && warp < kAgain / 32 && (sm.broken[0] | sm.broken[1] | sm.broken[2] | sm.broken[3]) != 0u)
+        once_more<NA, Y>(p, sm.job, reinterpret_cast<float *>(sm.v), slice * kM, sm.broken);
 }
 
 // The segments' initial states: state after segment s = state before it * M + B, in the place of B,
 // for 16 value channels a CTA. M comes through shared memory, the next one while this one is used.
 constexpr int kJoinRows = 16, kJoinThreads = 128;
 
-__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaParams p, const Cut cut) {
+// Four rows of a state, a lane 4 columns of each, rolled over tokens t .. end - 1 as the recurrence is
+// defined: where B or M is not finite, or M was given up because the segment's gates grow. Four tokens' loads
+// are in flight at a time.
+__device__ __noinline__ void rolled(const DeltaParams &p, float4 (&s)[4], int head, int row, int64_t t, int64_t end) {
+    const int c = (threadIdx.x & 31) * 4, qk = head / (p.hv / p.hk);
+    const __nv_bfloat16 *kp = static_cast<const __nv_bfloat16 *>(p.k) + static_cast<int64_t>(qk) * p.dk + c;
+    const __nv_bfloat16 *vp = static_cast<const __nv_bfloat16 *>(p.v) + static_cast<int64_t>(head) * p.dv + row;
+#pragma unroll 1
+    for (; t < end; t += 4) {
+        uint2 k[4];
+        float g[4], beta[4], v[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {   // (beyond the end: nothing decays, nothing enters)
+            const bool there = t + u < end;
+            k[u] = there && c < p.dk ? *reinterpret_cast<const uint2 *>(kp + (t + u) * p.k_stride) : make_uint2(0u, 0u);
+            g[u] = there ? p.g[(t + u) * p.hv + head] : 0.f;
+            beta[u] = there ? p.beta[(t + u) * p.hv + head] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] = there && row + i < p.dv ? to_f32(vp[(t + u) * p.v_stride + i]) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (t + u >= end) break;
+            const float x = __uint_as_float(k[u].x << 16), y = __uint_as_float(k[u].x & 0xffff0000u);
+            const float z = __uint_as_float(k[u].y << 16), w = __uint_as_float(k[u].y & 0xffff0000u);
+            const float a = g[u] < kLeastGate ? 0.f : expf(g[u]);
+            float sk[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sk[i] = fmaf(s[i].w, w, fmaf(s[i].z, z, fmaf(s[i].y, y, s[i].x * x)));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sk[i] += __shfl_xor_sync(0xffffffffu, sk[i], o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float n = beta[u] * fmaf(-a, sk[i], v[u][i]);
+                s[i] = make_float4(fmaf(n, x, a * s[i].x), fmaf(n, y, a * s[i].y), fmaf(n, z, a * s[i].z), fmaf(n, w, a * s[i].w));
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const __grid_constant__ DeltaParams p, const Cut cut) {
     extern __shared__ __align__(16) float join_smem[];
     const int dk = p.dk, pitch = dk + 4;
     float *move[2] = {join_smem, join_smem + dk * dk};
@@ -1168,6 +1240,23 @@ __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaPar
     }
     // thread: 4 rows of warp `threadIdx.x / 32`, 4 columns
     const int r = threadIdx.x / 32 * 4, c = threadIdx.x % 32 * 4;
+    // The rows behind segment `seg`, from what they were before it: those that broke in it.
+    auto mend = [&](float4 (&now)[4], int64_t seg) {
+        auto whole = [&](float4 v) { return __all_sync(0xffffffffu, c >= dk || (isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w))); };
+        float4 was[4];
+        bool broke[4], any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            was[i] = c < dk ? *reinterpret_cast<const float4 *>(rows + (r + i) * pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            broke[i] = r0 + r + i < p.dv && !whole(now[i]) && whole(was[i]);
+            any |= broke[i];
+        }
+        if (!any) return;
+        rolled(p, was, head, r0 + r, begin + seg * cut.len, begin + (seg + 1) * cut.len);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (broke[i]) now[i] = was[i];
+    };
     for (int64_t seg = 1; seg + 1 < segs; ++seg) {
         if (seg + 2 < segs) fetch(seg + 1);
         else cp_async_commit();
@@ -1201,14 +1290,18 @@ __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaPar
             }
         }
         __syncthreads();
+        float4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            unpack2(acc[i][0], x[i].x, x[i].y);
+            unpack2(acc[i][1], x[i].z, x[i].w);
+        }
+        mend(x, seg);
         if (c < dk) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float4 x;
-                unpack2(acc[i][0], x.x, x.y);
-                unpack2(acc[i][1], x.z, x.w);
-                *reinterpret_cast<float4 *>(rows + (r + i) * pitch + c) = x;
-                if (r0 + r + i < p.dv) *reinterpret_cast<float4 *>(state(seg, r + i) + c) = x;
+                *reinterpret_cast<float4 *>(rows + (r + i) * pitch + c) = x[i];
+                if (r0 + r + i < p.dv) *reinterpret_cast<float4 *>(state(seg, r + i) + c) = x[i];
             }
         }
         __syncthreads();

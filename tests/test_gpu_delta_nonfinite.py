@@ -73,19 +73,36 @@ def test_what_precedes_a_broken_token_is_untouched(cuda_device, what, dtype, y_d
     _like(y, ref_y, tol)
 
 
-@pytest.mark.parametrize("lens", [[150], [100, 64, 1, 130]])
-def test_growth_that_the_correction_holds_back(cuda_device, lens):
-    """A key that repeats, beta = 1, gates that grow e^1.5-fold a token: each token replaces what the
-    key holds, so the state stays small although the growth over a chunk is beyond fp32."""
+@pytest.mark.parametrize("lens", [[150], [100, 64, 1, 130], [5000], [1500, 2100]])
+@pytest.mark.parametrize("rate", [0.01, 0.1, 0.5, 1.5])
+def test_growth_that_the_correction_holds_back(cuda_device, rate, lens):
+    """Two keys by turns, beta = 1, gates that grow: each token replaces what its key holds, so the state
+    stays small although the growth over a chunk or a segment is anything up to beyond fp32."""
     import torch
     q, k, v, g, beta, off = _tensors(lens, 1, 2, 64, 72, torch.bfloat16, cuda_device, 3)
     k.zero_()
-    k[:, :, 9] = 1.0
-    g.fill_(1.5)
+    k[::2, :, 9] = 1.0
+    k[1::2, :, 30] = 1.0
+    g.fill_(rate)
+    g[:, 1] *= torch.rand(g.shape[0], device=cuda_device).round()
     beta.fill_(1.0)
     s, y, alone = _scan(q, k, v, g, beta, off, None, torch.float32, cuda_device)
     ref_S, ref_y = _ref(q, k, v, g, beta, off)
-    assert np.isfinite(ref_S).all()
+    assert np.abs(ref_S).max() < 1e3
+    for got, ref in ((s, ref_S), (alone, ref_S), (y, ref_y)):
+        _like(got, ref, TOL_PAIR)
+
+
+@pytest.mark.parametrize("lens,rate", [([300], 0.1), ([90, 200], 0.02), ([4000], 0.01), ([1400, 1300], 0.02)])
+def test_growth_of_the_state_itself(cuda_device, lens, rate):
+    """Keys that differ and betas below 1: what the keys do not touch grows with the gates."""
+    import torch
+    q, k, v, g, beta, off = _tensors(lens, 1, 1, 64, 136, torch.bfloat16, cuda_device, 13)
+    g.fill_(rate)
+    beta *= 0.2
+    S0 = torch.randn((len(lens), 1, 1, 136, 64), device=cuda_device)
+    s, y, alone = _scan(q, k, v, g, beta, off, S0, torch.bfloat16, cuda_device)
+    ref_S, ref_y = _ref(q, k, v, g, beta, off, to_np(S0[:, 0]))
     for got, ref in ((s, ref_S), (alone, ref_S), (y, ref_y)):
         _like(got, ref, TOL_PAIR)
 
