@@ -461,10 +461,10 @@ typedef struct precog_delta_inputs {
  * With BF16 inputs, batches whose mean length T_tot / n_seqs is more than some thirty tokens (12
  * where the batch fills the GPU) run on the tensor cores in chunks of 64 tokens: state and sums stay
  * fp32 and every intermediate operand is carried as a pair of bf16 numbers (16 significant
- * bits). With keys of norm 1 results agree with the recurrence, in units of the largest entry, to
- * about 1e-5 where keys differ and dk is 64 or more, and to 1e-4 whatever the keys while betas stay
- * within [0, 1]; with betas up to 2 (which reflect what they do not replace) to about 1e-3 where
- * keys come back, and to 2e-2 in the worst case, one key, betas of 2 and no decay. F32 inputs and
+ * bits). With keys of norm 1 and betas in [0, 1] results agree with the recurrence, in units of the
+ * largest entry, to about 1e-5 where keys differ and dk is 64 or more, and to 1e-4 whatever the keys;
+ * with betas up to 2 (which reflect what they do not replace) to about 2e-4 where keys differ, 1e-3
+ * where they come back, and 2e-2 in the worst case, one key, betas of 2 and no decay. F32 inputs and
  * shorter sequences run token by token in fp32, to 1e-5: the way to have more. Calls of the same shape repeat bit for bit.
  * NaN and infinity act as in the recurrence, whichever way a sequence runs: tokens before the one that
  * has them are not touched, and from it on what they reach is not finite (NaN where the recurrence may

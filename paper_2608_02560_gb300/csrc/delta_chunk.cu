@@ -30,13 +30,13 @@
 // q.k, which the teams wait for. Warp 17: issues every other MMA, so that no working warp waits in the
 // queue of the tensor cores. Warp 18: V in and y rows out.
 //
-// What bounds it: in full rounds the chain and the teams alike, 2.44 us or some 4700 cycles a chunk (3.6
+// What bounds it: in full rounds the chain and the teams alike, 2.42 us or some 4700 cycles a chunk (3.6
 // us, 7000 with a readout) at 0.45 instructions a cycle of each scheduler, the tensor cores' pipe 33 to 35 %
 // busy, DRAM at 16 to 21 % of its rate; in rounds of a chunk or two the 13 us from a CTA's start to its
 // end, most of them one chunk's way through a team. Measured, bf16, 128 x 128 a head: 256 sequences of 256
-// to 4096 tokens, 8 heads, states alone, 1343 to 1366 us (215 TFLOP/s of the recurrence's operations); 96
-// sequences of 1 to 200 tokens, 16 heads, with a readout, 174 to 178 us; one of 64 tokens 15 us; one of
-// 32,768 tokens, cut into segments, 634 us.
+// to 4096 tokens, 8 heads, states alone, 1327 to 1351 us (218 TFLOP/s of the recurrence's operations); 96
+// sequences of 1 to 200 tokens, 16 heads, with a readout, 176 to 178 us; one of 64 tokens 15 us; one of
+// 32,768 tokens, cut into segments, 688 us.
 // Loops over columns are rolled where they can be: fully unrolled, the roles' code was several times
 // the instruction cache and warps waited for instructions 40 % of the time (25,000 cycles a chunk).
 // Tokens beyond a sequence's end have beta 0 and zeroed rows: whatever the memory holds, nothing
@@ -289,7 +289,8 @@ __device__ __noinline__ bool too_far(const DeltaParams &p, const Job &job) {
 // through `room`, 64 at a time, as fp32, keys padded with zeros. Once nothing of a warp's states is finite
 // nothing will be again, and the rest of its readouts is NaN. No sequence comes here that stays finite and
 // whose gates decay.
-// 152 heads of 128 x 128, 4096 tokens, 244 us: all broken by their first token 535 us, by their last 3.7 ms.
+// 152 heads of 128 x 128, 4096 tokens, 247 us: all broken by their first token 545 us, by their last, or with
+// gates that grow, 3.6 ms.
 constexpr int kAgain = 512;
 __host__ __device__ constexpr int again_bytes(int keys) { return 4 * (2 * kC * keys + kC * kM + 3 * kC); }
 template <int NA, bool Y>
@@ -1169,7 +1170,7 @@ constexpr int kJoinRows = 16, kJoinThreads = 128;
 
 // Four rows of a state, a lane 4 columns of each, rolled over tokens t .. end - 1 as the recurrence is
 // defined: where B or M is not finite, or M was given up because the segment's gates grow. Four tokens' loads
-// are in flight at a time.
+// are in flight at a time (32,768 tokens of 16 heads whose gates grow throughout: 8.8 ms, decaying 0.69).
 __device__ __noinline__ void rolled(const DeltaParams &p, float4 (&s)[4], int head, int row, int64_t t, int64_t end) {
     const int c = (threadIdx.x & 31) * 4, qk = head / (p.hv / p.hk);
     const __nv_bfloat16 *kp = static_cast<const __nv_bfloat16 *>(p.k) + static_cast<int64_t>(qk) * p.dk + c;
@@ -1351,7 +1352,7 @@ cudaError_t launch_all(const DeltaParams &p, const Maps &maps, int slices, Cut c
 // another: whole sequences are as long as their rounds of CTAs; segments go in one pass for B and M,
 // one step of the join each, and one pass for themselves. Cut only where that is a third shorter: the
 // estimate knows the sequences' mean length alone. One sequence, 16 heads of 128 x 128, with a readout:
-// 2048 tokens 85 us (whole 116), 4096 tokens 124 (222), 32,768 tokens 627 (1702).
+// 2048 tokens 89 us (whole 116), 4096 tokens 130 (222), 32,768 tokens 681 (1702).
 int cut_length(const DeltaParams &p) {
     const int64_t sms = device_sm_count(), slices = (p.dv + kM - 1) / kM, items = p.n_seqs * p.hv * slices;
     if (items > sms || p.T_tot / p.n_seqs < 16 * kC) return 0;
