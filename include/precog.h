@@ -573,6 +573,191 @@ precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n
                                     float *d_logprob, float *d_entropy, int64_t *d_top_idx,
                                     float *d_top_logprob, void *stream);
 
+/* ------------------------------------------------------------------------------------
+ * Around a selective state space layer: its short causal convolution, single tokens of its
+ * scan, the end of its block; and logits before a token is chosen.
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * Rows and weights of the short causal convolution over each of `dim` channels,
+ *   y[t,d] = act(bias[d] + sum_{j < kernel} weight[d,j] * x[t - kernel + 1 + j, d]),
+ * act = SiLU (a / (1 + e^-a)) or none. The inputs before a sequence's first token are its
+ * window: the kernel - 1 inputs that its past left, oldest first. The window belongs to a
+ * layer's state as the scan's does: an injected chunk without its window is not the chunk.
+ *   x, y     [rows][dim] in `dtype` (F32 or BF16), rows x_stride / y_stride elements apart
+ *            (at least dim; ignored where there is at most one row)
+ *   weight   fp32 [dim][kernel], bias fp32 [dim] or NULL
+ * Sums are fp32. Requirements: dim a multiple of 8, kernel 2, 3 or 4; pointers and row
+ * strides 16-byte aligned.
+ */
+typedef struct precog_conv_args {
+    int32_t dtype;             /* precog_dtype: F32 or BF16 */
+    int32_t dim;
+    int32_t kernel;
+    int32_t silu;              /* 0 or 1 */
+    const void *x;
+    void *y;
+    int64_t x_stride;
+    int64_t y_stride;
+    const float *weight;
+    const float *bias;
+} precog_conv_args;
+
+/*
+ * precog_causal_conv -- the convolution over a ragged batch of sequences: chunks of a corpus
+ * from empty windows, or queries from injected ones (as precog_encode_chunks and
+ * precog_prefill_from_state do for the states).
+ *   d_offsets    device int64 [n_seqs+1]: sequence c owns rows d_offsets[c] ..
+ *                d_offsets[c+1]-1 of x and y. A sequence whose offsets decrease or leave
+ *                [0, T_tot] is skipped and flags PRECOG_DEV_BAD_OFFSETS, and sequences behind
+ *                it may be skipped too. Lengths of zero are allowed: the window is handed on.
+ *   T_tot        rows of x and y (below 2^31); y rows outside every sequence are left untouched
+ *   bank         device [bank_entries][L_total][kernel-1][dim] in `dtype`, or NULL: nothing
+ *                came before any sequence (zeros)
+ *   d_idx        device int64 [n_seqs]: the bank row whose layer `layer` is sequence c's window
+ *                (-1: zeros; outside [-1, bank_entries), where a NULL bank has no entries: zeros,
+ *                and flags PRECOG_DEV_BAD_INDEX); NULL: row c, and bank_entries must be at least
+ *                n_seqs
+ *   windows_out  device [n_seqs][L_total][kernel-1][dim] in `dtype`: layer `layer` of entry c
+ *                receives the window that the token behind sequence c needs (its last inputs,
+ *                the older of them its own window's where it is shorter); or NULL
+ * y, windows_out, x and bank must not share memory (rows of x and y may be slices of one buffer).
+ */
+precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_offsets, int64_t n_seqs,
+                                 int64_t T_tot, const void *bank, int64_t bank_entries, const int64_t *d_idx,
+                                 void *windows_out, int32_t layer, int32_t L_total, void *stream);
+
+/*
+ * precog_conv_step -- one token of the convolution for each of n sequences, on a table of
+ * windows that is updated in place (row i of x is the next input of the sequence whose window
+ * is windows[d_slots[i]][layer]).
+ *   windows   device [n_slots][L_total][kernel-1][dim] in `dtype`; must not share memory with
+ *             x or y (y may be x itself)
+ *   d_slots   as precog_delta_step: each slot at most once (not verified: repeated slots race);
+ *             NULL: row i; -1: an idle row, whose y is zeroed; any other slot outside
+ *             [0, n_slots) likewise, and flags PRECOG_DEV_BAD_INDEX
+ */
+precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *windows, int64_t n_slots,
+                               const int64_t *d_slots, int32_t layer, int32_t L_total, void *stream);
+
+/*
+ * precog_scan_step -- one token of the diagonal scan for each of n sequences through
+ * in->n_layers layers, on a table of fp32 states that is updated in place: the recurrence of
+ * precog_scan_inputs, whose "token rows" are the n sequences (x, dt [L][n][D], B, C [L][n][N]),
+ * and
+ *   y[t,d] = (sum_n C[t,n] h[d,n] + skip[d] x[t,d]) * silu(gate[t,d])
+ * (the sum's real part for PRECOG_A_COMPLEX; PRECOG_A_POWER is taken as any A and not verified).
+ *   states    device fp32 [n_slots][L_total][D][N] (PRECOG_A_COMPLEX: pairs [..][N][2]); layers
+ *             layer0 .. layer0+L-1 of the named slots are read and written, nothing else
+ *   d_slots   as precog_conv_step; all layers use it
+ *   skip      fp32 [L][D], or NULL: none
+ *   gate      [L][n][D] in in->in_dtype, rows gate_stride and layers gate_layer_stride elements
+ *             apart, or NULL: none
+ *   y_out     device [L][n][D] in y_dtype (F32 or BF16)
+ * y_out, states and the inputs must not share memory.
+ */
+precog_status precog_scan_step(const precog_scan_inputs *in, int64_t n, void *states, int64_t n_slots,
+                               const int64_t *d_slots, int32_t layer0, int32_t L_total, const float *skip,
+                               const void *gate, int64_t gate_stride, int64_t gate_layer_stride, void *y_out,
+                               int32_t y_dtype, void *stream);
+
+/*
+ * Arguments of precog_block_norm. Of every row,
+ *   a <- x + skip * skip_input                                      (skip given)
+ *   a <- a * silu(gate)                                             (gate given, gate_first)
+ *   a <- a / sqrt(mean a^2 + eps) * weight, over each of `groups`   (norm == PRECOG_NORM_RMS)
+ *   a <- a * silu(gate)                                             (gate given, not gate_first)
+ * without a residual: out = a; with one:
+ *   h <- residual + scale * scale_weight * a ;  residual_out = h
+ *   out = h / sqrt(mean h^2 + eps) * out_weight                     (out given)
+ *   x, skip_input, gate, out    [T][dim] in `dtype` (F32 or BF16), each with its own row stride
+ *   residual, residual_out      [T][dim] in residual_dtype (F32; or BF16 where dtype is BF16)
+ *   skip, weight, scale_weight, out_weight   fp32 [dim], or NULL: no skip, and 1
+ * Arithmetic is fp32 from end to end: h goes into its norm before it is rounded. Outputs may be
+ * the very rows of an input of the same type; otherwise nothing may share memory with them.
+ * Requirements: dim / groups a multiple of 8, at most 16384; groups == 1 where both residual
+ * and out are given; pointers and row strides 16-byte aligned.
+ */
+typedef struct precog_block_norm_args {
+    int32_t dtype;             /* precog_dtype: F32 or BF16 */
+    int32_t residual_dtype;
+    int32_t dim;
+    int32_t groups;
+    int32_t norm;              /* PRECOG_NORM_NONE or PRECOG_NORM_RMS */
+    int32_t gate_first;        /* 0 or 1 */
+    float scale;
+    float eps;
+    const void *x;
+    const void *skip_input;
+    const void *gate;
+    const void *residual;
+    void *residual_out;
+    void *out;
+    int64_t x_stride;
+    int64_t skip_stride;
+    int64_t gate_stride;
+    int64_t residual_stride;
+    int64_t residual_out_stride;
+    int64_t out_stride;
+    const float *skip;
+    const float *weight;
+    const float *scale_weight;
+    const float *out_weight;
+} precog_block_norm_args;
+
+/* precog_block_norm -- the end of a block over T tokens, one pass. */
+precog_status precog_block_norm(const precog_block_norm_args *args, int64_t T, void *stream);
+
+/*
+ * Arguments of precog_adjust_logits. Entry i of row r, in fp32 and in this order:
+ *   z <- z > 0 ? z / d_repetition[r] : z * d_repetition[r]    where i is in the row's history
+ *   z <- z - times * d_frequency[r] - d_presence[r]           where `times`, how often i is in the
+ *                        counted part of the history (from its entry d_count_from[r] on), is not 0
+ *   z <- z + d_bias[j]                                        where d_bias_idx[j] == i
+ *   z <- -infinity                                            where the row's mask has bit i clear
+ * and out[r][i] is z rounded to `dtype`. Any of them may be NULL.
+ *   logits, out   device [n_rows][vocab] in `dtype` (F32, BF16 or F16), rows `stride` and
+ *                 out_stride elements apart (any alignment of the elements); out may be logits
+ *   d_history     device int64 tokens; row r's are entries d_history_offsets[r] ..
+ *                 d_history_offsets[r+1]-1 (its prompt, then its answer)
+ *   d_count_from  device int64 [n_rows] (e.g. the prompts' lengths), clamped to the history; NULL: 0
+ *   d_bias_idx, d_bias, d_bias_offsets   int64 tokens and fp32 biases, lists as the history's; of a
+ *                 token that a row names twice the last bias counts
+ *   d_mask        device int32 [n_masks][ceil(vocab / 32)]: bit i % 32 of word i / 32 allows token i
+ *   d_mask_rows   device int64 [n_rows]: the row's mask (-1: everything is allowed; other values
+ *                 outside [0, n_masks) likewise, and flag PRECOG_DEV_BAD_INDEX); NULL: mask r
+ * Tokens of -1 in a list are ignored (padding); others outside [0, vocab) are ignored and flag
+ * PRECOG_DEV_BAD_INDEX. A list whose offsets decrease or leave [0, n_history] or [0, n_bias] is
+ * empty and flags PRECOG_DEV_BAD_OFFSETS. Lists are shorter than 2^31 in all.
+ */
+typedef struct precog_adjust_args {
+    int32_t dtype;             /* precog_dtype */
+    int32_t reserved;          /* must be 0 */
+    int64_t vocab;
+    int64_t stride;
+    int64_t out_stride;
+    const void *logits;
+    void *out;
+    const int64_t *d_history;
+    const int64_t *d_history_offsets;
+    const int64_t *d_count_from;
+    int64_t n_history;
+    const float *d_repetition;
+    const float *d_frequency;
+    const float *d_presence;
+    const int64_t *d_bias_idx;
+    const float *d_bias;
+    const int64_t *d_bias_offsets;
+    int64_t n_bias;
+    const int32_t *d_mask;
+    int64_t n_masks;
+    const int64_t *d_mask_rows;
+} precog_adjust_args;
+
+/* precog_adjust_logits -- penalties for repeated tokens, biases and grammar masks on the logits
+ * of n_rows rows, one pass. */
+precog_status precog_adjust_logits(const precog_adjust_args *args, int64_t n_rows, void *stream);
+
 /*
  * precog_selftest_wait_timeout -- diagnostic; the paper has no counterpart.
  * Every kernel here that waits on copies (TMA completion on an mbarrier) gives

@@ -396,3 +396,92 @@ def token_logprobs(logits, tokens, temperature=1.0, k=0):
         idx[r, :len(order)] = order
         best[r, :len(order)] = logp[order]
     return lp, H, idx, best
+
+
+def silu(x):
+    """x / (1 + e^-x); 0 at -infinity's side is reached without overflow."""
+    x = _f64(x)
+    with np.errstate(over="ignore", invalid="ignore"):
+        return x / (1.0 + np.exp(-x))
+
+
+def causal_conv(x, weight, offsets, bias=None, act=True, windows=None):
+    """y[t] = act(bias + sum_j weight[:, j] x[t - K + 1 + j]) of each sequence of ``x [T, D]``, whose
+    window ``windows[c] [K - 1, D]`` (default zeros) comes before it. Returns ``(y, the windows behind)``;
+    rows of y outside every sequence are NaN."""
+    x, weight = _f64(x), _f64(weight)
+    D, K = weight.shape
+    n = len(offsets) - 1
+    y, behind = np.full(x.shape, np.nan), np.zeros((n, K - 1, D))
+    for c in range(n):
+        seq = np.concatenate([np.zeros((K - 1, D)) if windows is None else _f64(windows[c]),
+                              x[int(offsets[c]):int(offsets[c + 1])]])
+        for t in range(len(seq) - K + 1):
+            a = np.zeros(D) if bias is None else _f64(bias).copy()
+            for j in range(K):
+                a += weight[:, j] * seq[t + j]
+            y[int(offsets[c]) + t] = silu(a) if act else a
+        behind[c] = seq[len(seq) - (K - 1):]
+    return y, behind
+
+
+def scan_step(x, dt, A, B, C, h, skip=None, gate=None):
+    """One token of each row through one layer of the diagonal scan: x, dt ``[n, D]``, B, C ``[n, N]``, A
+    ``[D, N]`` (real or complex), h ``[n, D, N]``. Returns ``(h, y)``."""
+    x, dt, B, C = _f64(x), _f64(dt), _f64(B), _f64(C)
+    A, h = np.asarray(A), np.asarray(h)
+    h = np.exp(dt[:, :, None] * A) * h + (x * dt)[:, :, None] * B[:, None, :]
+    y = (h.real * C[:, None, :]).sum(-1)
+    if skip is not None:
+        y = y + _f64(skip) * x
+    return h, y if gate is None else y * silu(gate)
+
+
+def rms(x, eps, groups=1):
+    x = _f64(x)
+    g = x.reshape(x.shape[0], groups, -1)
+    return (g / np.sqrt((g * g).mean(-1, keepdims=True) + eps)).reshape(x.shape)
+
+
+def block_norm(x, skip=None, skip_input=None, gate=None, gate_first=True, norm=True, weight=None, groups=1,
+               residual=None, scale=1.0, out_norm=False, out_weight=None, eps=1e-6):
+    """Skip, gate, norm and residual of rows ``[T, D]``. Returns ``(out, residual_out)``."""
+    a = _f64(x)
+    if skip is not None:
+        a = a + _f64(skip) * _f64(skip_input)
+    if gate is not None and gate_first:
+        a = a * silu(gate)
+    if norm:
+        a = rms(a, eps, groups) * (1.0 if weight is None else _f64(weight))
+    if gate is not None and not gate_first:
+        a = a * silu(gate)
+    if residual is None:
+        return a, None
+    h = _f64(residual) + _f64(scale) * a
+    return (rms(h, eps) * (1.0 if out_weight is None else _f64(out_weight)) if out_norm else None), h
+
+
+def adjust_logits(z, history=None, count_from=None, repetition=None, frequency=None, presence=None, biases=None,
+                  allowed=None):
+    """Row by row, token by token: ``history[r]`` a list of tokens, counted from entry ``count_from[r]`` on,
+    ``biases[r]`` a list of (token, bias) whose last entry of a token counts, ``allowed[r]`` a set or None."""
+    out = _f64(z).copy()
+    R, V = out.shape
+    for r in range(R):
+        text = [] if history is None else list(history[r])
+        start = 0 if count_from is None else min(max(int(count_from[r]), 0), len(text))
+        for i in set(text) - {-1}:
+            if repetition is not None:
+                p = float(repetition[r])
+                out[r, i] = out[r, i] / p if out[r, i] > 0 else out[r, i] * p
+            times = text[start:].count(i)
+            if times:
+                out[r, i] -= (times * float(frequency[r]) if frequency is not None else 0.0)
+                out[r, i] -= (float(presence[r]) if presence is not None else 0.0)
+        for i, b in dict([] if biases is None else biases[r]).items():
+            if i != -1:
+                out[r, i] += b
+        if allowed is not None and allowed[r] is not None:
+            for i in set(range(V)) - set(allowed[r]):
+                out[r, i] = -np.inf
+    return out

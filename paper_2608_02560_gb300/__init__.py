@@ -21,6 +21,11 @@ Functions carry the C names:
   from injected matrix states, and one token of each sequence on a table of states
 * :func:`precog_qk_norm_rope`     -- norms of query and key heads with the position rotation
 * :func:`precog_token_logprobs`   -- log probabilities of given tokens, entropy, best entries
+* :func:`precog_causal_conv`, :func:`precog_conv_step` -- the short causal convolution in front of a
+  scan: chunks or queries from injected windows, and one token of each sequence
+* :func:`precog_scan_step`        -- one token of the diagonal scan of each sequence on a table of states
+* :func:`precog_block_norm`       -- skip, gate, norm and residual at the end of a block, the next one's norm
+* :func:`precog_adjust_logits`    -- penalties for repeated tokens, biases and grammar masks on logits
 * :func:`precog_retrieve_noalloc`  -- top-1 retrieval without a caller workspace
 * :func:`precog_device_status`    -- device-side status word; :func:`precog_status_string`,
   :func:`precog_last_error`, :func:`precog_abi_version`, :func:`precog_launch_count`
@@ -79,6 +84,37 @@ class QkNormArgs(ctypes.Structure):
                 ("d_positions", ctypes.c_void_p)]
 
 
+class ConvArgs(ctypes.Structure):
+    """Mirror of ``precog_conv_args`` (include/precog.h)."""
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("kernel", ctypes.c_int32),
+                ("silu", ctypes.c_int32), ("x", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p)]
+
+
+class BlockNormArgs(ctypes.Structure):
+    """Mirror of ``precog_block_norm_args`` (include/precog.h)."""
+    _fields_ = [("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("norm", ctypes.c_int32), ("gate_first", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("x", ctypes.c_void_p),
+                ("skip_input", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("residual_out", ctypes.c_void_p), ("out", ctypes.c_void_p), ("x_stride", ctypes.c_int64),
+                ("skip_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("residual_out_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("skip", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("scale_weight", ctypes.c_void_p), ("out_weight", ctypes.c_void_p)]
+
+
+class AdjustArgs(ctypes.Structure):
+    """Mirror of ``precog_adjust_args`` (include/precog.h)."""
+    _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32), ("vocab", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("logits", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("d_history", ctypes.c_void_p), ("d_history_offsets", ctypes.c_void_p),
+                ("d_count_from", ctypes.c_void_p), ("n_history", ctypes.c_int64), ("d_repetition", ctypes.c_void_p),
+                ("d_frequency", ctypes.c_void_p), ("d_presence", ctypes.c_void_p), ("d_bias_idx", ctypes.c_void_p),
+                ("d_bias", ctypes.c_void_p), ("d_bias_offsets", ctypes.c_void_p), ("n_bias", ctypes.c_int64),
+                ("d_mask", ctypes.c_void_p), ("n_masks", ctypes.c_int64), ("d_mask_rows", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -134,6 +170,17 @@ def load_library(path: str = LIB_PATH):
     lib.precog_qk_norm_rope.argtypes = [ctypes.POINTER(QkNormArgs), i64, vp]
     lib.precog_token_logprobs.restype = i32
     lib.precog_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, ctypes.c_float, i32, vp, vp, vp, vp, vp]
+    lib.precog_causal_conv.restype = i32
+    lib.precog_causal_conv.argtypes = [ctypes.POINTER(ConvArgs), vp, i64, i64, vp, i64, vp, vp, i32, i32, vp]
+    lib.precog_conv_step.restype = i32
+    lib.precog_conv_step.argtypes = [ctypes.POINTER(ConvArgs), i64, vp, i64, vp, i32, i32, vp]
+    lib.precog_scan_step.restype = i32
+    lib.precog_scan_step.argtypes = [ctypes.POINTER(ScanInputs), i64, vp, i64, vp, i32, i32, vp, vp, i64, i64, vp, i32,
+                                     vp]
+    lib.precog_block_norm.restype = i32
+    lib.precog_block_norm.argtypes = [ctypes.POINTER(BlockNormArgs), i64, vp]
+    lib.precog_adjust_logits.restype = i32
+    lib.precog_adjust_logits.argtypes = [ctypes.POINTER(AdjustArgs), i64, vp]
     lib.precog_selftest_wait_timeout.restype = i32
     lib.precog_selftest_wait_timeout.argtypes = [ctypes.c_uint32, vp]
     lib.precog_device_status.restype = i32
@@ -250,6 +297,7 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     s = ScanInputs(L, D, N, _dtype_code(x), a_kind, 0, _ptr(x), _ptr(dt), _ptr(B), _ptr(C), _ptr(A), T * D, T * N)
     # the struct holds raw device pointers: keep the tensors alive as long as it lives
     s._keepalive = (x, dt, B, C, A)
+    s.rows = T
     return s
 
 
@@ -560,6 +608,191 @@ def precog_token_logprobs(logits, tokens, logprob, entropy=None, top_idx=None, t
         _of(logprob, torch.float32, (R,), "logprob"), _of(entropy, torch.float32, (R,), "entropy"),
         _of(top_idx, torch.int64, (R, k), "top_idx"), _of(top_logprob, torch.float32, (R, k), "top_logprob"),
         _stream(stream)))
+
+
+def _current_device() -> int:
+    torch = _torch()
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return get() if get is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device: tensors of another one are refused."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != device:
+            raise ValueError(f"tensors must live on the current device, cuda:{device}")
+
+
+def _conv_args(x, weight, bias, silu: bool, y_out) -> ConvArgs:
+    torch = _torch()
+    T, D = x.shape
+    if y_out is None or y_out.shape != x.shape:
+        raise ValueError("y_out must have the shape of x")
+    if y_out.dtype is not x.dtype:
+        raise TypeError("x and y_out must have one dtype")
+    K = weight.shape[-1]
+    (xp, xs), (yp, ys) = _rows(x, "x"), _rows(y_out, "y_out")
+    return ConvArgs(_dtype_code(x), D, K, int(silu), xp, yp, xs, ys, _of(weight, torch.float32, (D, K), "weight"),
+                    _of(bias, torch.float32, (D,), "bias"))
+
+
+def _windows(t, x, K: int, what: str):
+    if t is not None and (t.dim() != 4 or t.shape[2:] != (K - 1, x.shape[1])):
+        raise ValueError(f"{what} must be [entries, layers, {K - 1}, {x.shape[1]}], got {tuple(t.shape)}")
+    if t is not None and t.dtype is not x.dtype:
+        raise TypeError(f"{what} and x must have one dtype")
+    return _ptr(t)
+
+
+def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=None, idx=None, layer: int = 0,
+                       windows_out=None, y_out=None, stream=None):
+    """The causal convolution with fp32 ``weight [D, K]`` (K = 2, 3 or 4) and ``bias [D]``, then SiLU, of
+    the sequences (rows ``offsets[c]..offsets[c + 1]``) of x ``[T, D]`` (rows may be strided) into ``y_out``.
+    The inputs before a sequence are ``bank[idx[c], layer]`` (``[entries, layers, K - 1, D]``; -1 or no bank:
+    zeros); ``windows_out[c, layer]`` receives those that its next token needs."""
+    torch = _torch()
+    _on_current_device(x, weight, offsets, bias, bank, idx, windows_out, y_out)
+    if idx is not None and bank is None:
+        raise ValueError("idx is given without bank")
+    args, n = _conv_args(x, weight, bias, silu, y_out), offsets.numel() - 1
+    K = weight.shape[1]
+    bp, wp = _windows(bank, x, K, "bank"), _windows(windows_out, x, K, "windows_out")
+    if windows_out is not None and windows_out.shape[0] != n:
+        raise ValueError("windows_out must have one entry per sequence")
+    if bank is not None and windows_out is not None and bank.shape[1] != windows_out.shape[1]:
+        raise ValueError("bank and windows_out must have the same number of layers")
+    holder = windows_out if windows_out is not None else bank
+    _check(load_library().precog_causal_conv(
+        ctypes.byref(args), _of(offsets, torch.int64, (n + 1,), "offsets"), n, x.shape[0], bp,
+        bank.shape[0] if bank is not None else 0, _of(idx, torch.int64, (n,), "idx"), wp, layer,
+        holder.shape[1] if holder is not None else layer + 1, _stream(stream)))
+
+
+def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = True, layer: int = 0, y_out=None,
+                     stream=None):
+    """One token of :func:`precog_causal_conv` for each row of x ``[n, D]``, on the table ``windows [slots,
+    layers, K - 1, D]`` (updated in place) at the rows' int64 ``slots`` (-1: an idle row), into ``y_out``
+    (which may be x)."""
+    torch = _torch()
+    _on_current_device(x, weight, windows, slots, bias, y_out)
+    args = _conv_args(x, weight, bias, silu, y_out)
+    wp = _windows(windows, x, weight.shape[1], "windows")
+    _check(load_library().precog_conv_step(
+        ctypes.byref(args), x.shape[0], wp, windows.shape[0], _of(slots, torch.int64, (x.shape[0],), "slots"), layer,
+        windows.shape[1], _stream(stream)))
+
+
+def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, skip=None, gate=None, y_out=None,
+                     stream=None):
+    """One token of the diagonal scan for each of the n rows that ``inputs`` (x, dt ``[L, n, D]``) has, on the
+    fp32 (complex A: complex64) table ``states [slots, layers, D, N]``, updated in place, at the rows' int64
+    ``slots`` (-1: an idle row), into ``y_out [L, n, D]``: the readout, plus fp32 ``skip [L, D]`` times x,
+    times SiLU of ``gate [L, n, D]`` (each row contiguous)."""
+    torch = _torch()
+    L, D, N, n = inputs.n_layers, inputs.D, inputs.N, inputs.rows
+    _on_current_device(inputs._keepalive[0], states, slots, skip, gate, y_out)
+    kind = torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32
+    if states.dim() != 4 or states.shape[2:] != (D, N) or states.dtype is not kind:
+        raise ValueError(f"states must be {kind} [slots, layers, {D}, {N}]")
+    if L == 1:   # [n, D] stands for one layer's [1, n, D]
+        y_out, gate = (t.unsqueeze(0) if t is not None and t.dim() == 2 else t for t in (y_out, gate))
+        skip = skip.unsqueeze(0) if skip is not None and skip.dim() == 1 else skip
+    if y_out is None or y_out.shape != (L, n, D):
+        raise ValueError("y_out must be [L, n, D]")
+    gp, gs, gls = None, 0, 0
+    if gate is not None:
+        if gate.shape != (L, n, D):
+            raise ValueError("gate must be [L, n, D]")
+        if gate.dtype is not inputs._keepalive[0].dtype:
+            raise TypeError("gate and x must have one dtype")
+        if not gate.is_cuda:
+            raise ValueError("tensors passed to libprecog must live on the GPU")
+        gls, gs, one = gate.stride()
+        if one != 1 and D > 1:
+            raise ValueError("the rows of gate must be contiguous")
+        gp = gate.data_ptr()
+    _check(load_library().precog_scan_step(
+        ctypes.byref(inputs), n, _ptr(states), states.shape[0], _of(slots, torch.int64, (n,), "slots"), layer0,
+        states.shape[1], _of(skip, torch.float32, (L, D), "skip"), gp, gs, gls, _ptr(y_out), _dtype_code(y_out),
+        _stream(stream)))
+
+
+def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_first: bool = True, weight=None,
+                      groups: int = 1, residual=None, scale=1.0, residual_out=None, out_weight=None, eps: float = 1e-6,
+                      norm: str | None = None, stream=None):
+    """The end of a block over the rows of x ``[T, D]`` (all rows may be strided): ``a = x + skip *
+    skip_input``, times SiLU of ``gate`` (before the norm, or behind it), the RMS norm of each of ``groups``
+    with ``weight`` (``norm``: ``"rms"`` or ``"none"``; default: ``"rms"`` where there is a weight). Without
+    a residual ``out`` is a; with one, ``residual_out = residual + scale * a`` (``scale`` a number or fp32
+    ``[D]``) and ``out``, if given, the RMS norm of that with ``out_weight``. Weights are fp32 ``[D]``; outputs
+    may be inputs of their type."""
+    torch = _torch()
+    _on_current_device(x, out, skip, skip_input, gate, weight, residual, residual_out, out_weight)
+    if norm is None:
+        norm = "none" if weight is None else "rms"
+    if norm not in ("none", "rms"):
+        raise ValueError('norm must be "none" or "rms"')
+    T, D = x.shape
+    for t, what in ((skip_input, "skip_input"), (gate, "gate"), (out, "out"), (residual, "residual"),
+                    (residual_out, "residual_out")):
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"{what} must have the shape of x")
+        if t is not None and t.dtype is not x.dtype and what[:8] != "residual":
+            raise TypeError(f"{what} and x must have one dtype")
+    if residual is not None and residual_out is not None and residual.dtype is not residual_out.dtype:
+        raise TypeError("residual and residual_out must have one dtype")
+    scale_weight = None
+    if isinstance(scale, torch.Tensor):
+        scale, scale_weight = 1.0, scale
+        _on_current_device(scale_weight)
+    (xp, xs), (sp, ss), (gp, gs) = _rows(x, "x"), _rows(skip_input, "skip_input"), _rows(gate, "gate")
+    (rp, rs), (rop, ros), (op, os_) = _rows(residual, "residual"), _rows(residual_out, "residual_out"), _rows(out, "out")
+    f32, vec = torch.float32, (D,)
+    args = BlockNormArgs(_dtype_code(x), _dtype_code(residual) if residual is not None else PRECOG_F32, D, groups,
+                         _NORMS[norm], int(gate_first), scale, eps, xp, sp, gp, rp, rop, op, xs, ss, gs, rs, ros, os_,
+                         _of(skip, f32, vec, "skip"), _of(weight, f32, vec, "weight"),
+                         _of(scale_weight, f32, vec, "scale"), _of(out_weight, f32, vec, "out_weight"))
+    _check(load_library().precog_block_norm(ctypes.byref(args), T, _stream(stream)))
+
+
+def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_from=None, repetition=None,
+                         frequency=None, presence=None, bias_idx=None, bias=None, bias_offsets=None, mask=None,
+                         mask_rows=None, stream=None):
+    """Logits ``[R, V]`` (rows may be strided) before a token is chosen, into ``out`` (which may be logits):
+    fp32 ``repetition``, ``frequency`` and ``presence`` penalties ``[R]`` for the tokens of each row's int64
+    ``history`` (entries ``history_offsets[r]..history_offsets[r + 1]``; counted from entry ``count_from[r]``
+    on), fp32 ``bias`` of the tokens ``bias_idx`` (lists by ``bias_offsets``), and -infinity where row
+    ``mask_rows[r]`` (-1: none) of the int32 bit ``mask [masks, ceil(V / 32)]`` has a token's bit clear."""
+    torch = _torch()
+    _on_current_device(logits, out, history, history_offsets, count_from, repetition, frequency, presence, bias_idx,
+                       bias, bias_offsets, mask, mask_rows)
+    R, V = logits.shape
+    if out.shape != logits.shape:
+        raise ValueError("out must have the shape of logits")
+    if out.dtype is not logits.dtype:
+        raise TypeError("logits and out must have one dtype")
+    if (bias is None) != (bias_idx is None) or (bias is None) != (bias_offsets is None):
+        raise ValueError("bias_idx, bias and bias_offsets must be given together")
+    if history is not None and history_offsets is None:
+        raise ValueError("history needs history_offsets")
+    if history is None and not (repetition is None and frequency is None and presence is None):
+        raise ValueError("penalties need a history")
+    if mask_rows is not None and mask is None:
+        raise ValueError("mask_rows is given without mask")
+    (lp, ls), (op, os_) = _rows(logits, "logits"), _rows(out, "out")
+    i64, f32, row, ends = torch.int64, torch.float32, (R,), (R + 1,)
+    nh = history.numel() if history is not None else 0
+    nb = bias.numel() if bias is not None else 0
+    nm = mask.shape[0] if mask is not None else 0
+    args = AdjustArgs(_dtype_code(logits), 0, V, ls, os_, lp, op, _of(history, i64, (nh,), "history"),
+                      _of(history_offsets, i64, ends, "history_offsets"), _of(count_from, i64, row, "count_from"), nh,
+                      _of(repetition, f32, row, "repetition"), _of(frequency, f32, row, "frequency"),
+                      _of(presence, f32, row, "presence"), _of(bias_idx, i64, (nb,), "bias_idx"),
+                      _of(bias, f32, (nb,), "bias"), _of(bias_offsets, i64, ends, "bias_offsets"), nb,
+                      _of(mask, torch.int32, (nm, (V + 31) // 32), "mask"), nm,
+                      _of(mask_rows, i64, row, "mask_rows"))
+    _check(load_library().precog_adjust_logits(ctypes.byref(args), R, _stream(stream)))
 
 
 def precog_selftest_wait_timeout(iterations: int = 4096, stream=None):

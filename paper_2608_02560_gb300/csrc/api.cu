@@ -149,12 +149,77 @@ precog::DeltaParams delta_params(const precog_delta_inputs *in) {
     return p;
 }
 
+// Rows of `row` bytes, `stride` bytes apart.
+struct RowSpan {
+    const void *at;
+    int64_t stride, row;
+};
+
+// Whether two tensors of n rows share memory. Rows of one stride may lie between one another (slices of one
+// buffer); otherwise their ranges have to be apart. `same_ok`: the very same rows do not count.
+bool overlap(const RowSpan &a, const RowSpan &b, int64_t n, bool same_ok) {
+    if (a.at == nullptr || b.at == nullptr || n == 0 || a.row == 0 || b.row == 0) return false;
+    if (same_ok && a.at == b.at && a.row == b.row && (n == 1 || a.stride == b.stride)) return false;
+    using wide = __int128;   // (strides are the caller's, and may be anything)
+    const wide pa = static_cast<wide>(reinterpret_cast<uintptr_t>(a.at)), pb = static_cast<wide>(reinterpret_cast<uintptr_t>(b.at));
+    if (pa + static_cast<wide>(n - 1) * a.stride + a.row <= pb || pb + static_cast<wide>(n - 1) * b.stride + b.row <= pa) return false;
+    if (n == 1 || a.stride != b.stride || a.stride == 0) return true;
+    wide gap = (pb - pa) % a.stride;
+    if (gap < 0) gap += a.stride;
+    return gap < a.row || gap + b.row > a.stride;
+}
+
+// Bytes of a table [entries][layers][row bytes], as one row; false beyond 2^63.
+bool table_span(const void *at, int64_t entries, int64_t layers, int64_t row, RowSpan *span) {
+    const __int128 bytes = static_cast<__int128>(entries) * layers;
+    if (bytes > INT64_MAX || bytes * row > INT64_MAX) return false;
+    *span = RowSpan{at, 0, at == nullptr ? 0 : static_cast<int64_t>(bytes * row)};
+    return true;
+}
+
+// The range of all of a tensor's rows, as one row.
+RowSpan whole(const RowSpan &a, int64_t n) {
+    if (a.at == nullptr || n == 0) return RowSpan{a.at, 0, 0};
+    const __int128 bytes = static_cast<__int128>(n - 1) * a.stride + a.row;
+    return RowSpan{a.at, 0, bytes > INT64_MAX ? INT64_MAX : static_cast<int64_t>(bytes)};
+}
+
+// Checks shared by the convolution's two calls; fills what they have in common.
+precog_status check_conv(const precog_conv_args *a, int64_t rows, int32_t layer, int32_t L_total, precog::ConvParams *p) {
+    if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
+    if (a->dtype != PRECOG_F32 && a->dtype != PRECOG_BF16)
+        return fail(PRECOG_ERR_UNSUPPORTED, "dtype must be PRECOG_F32 or PRECOG_BF16");
+    const int sz = dtype_size(a->dtype);
+    if (a->dim < 8 || a->dim % 8 != 0) return fail(PRECOG_ERR_UNSUPPORTED, "dim=%d: a positive multiple of 8 is implemented", a->dim);
+    if (a->kernel < 2 || a->kernel > 4) return fail(PRECOG_ERR_UNSUPPORTED, "kernel=%d: 2, 3 and 4 are implemented", a->kernel);
+    if (a->silu != 0 && a->silu != 1) return fail(PRECOG_ERR_INVALID_ARG, "silu must be 0 or 1");
+    if (L_total < 1 || layer < 0 || layer >= L_total) return fail(PRECOG_ERR_INVALID_ARG, "layer must be in [0, L_total)");
+    if (a->weight == nullptr || !aligned16(a->weight) || !aligned16(a->bias))
+        return fail(PRECOG_ERR_INVALID_ARG, "weight must be non-NULL, weight and bias 16-byte aligned");
+    std::memset(p, 0, sizeof(*p));
+    p->x = a->x, p->y = a->y;
+    p->x_stride = rows > 1 ? a->x_stride : 0, p->y_stride = rows > 1 ? a->y_stride : 0;
+    if (rows > 0) {
+        if (a->x == nullptr || a->y == nullptr || !aligned16(a->x) || !aligned16(a->y))
+            return fail(PRECOG_ERR_INVALID_ARG, "x and y must be non-NULL and 16-byte aligned");
+        if (rows > 1 && (a->x_stride < a->dim || a->y_stride < a->dim))
+            return fail(PRECOG_ERR_INVALID_ARG, "row strides smaller than a row");
+        if ((p->x_stride * sz) % 16 != 0 || (p->y_stride * sz) % 16 != 0)
+            return fail(PRECOG_ERR_INVALID_ARG, "row strides must keep 16-byte alignment");
+    }
+    p->weight = a->weight, p->bias = a->bias;
+    p->dim = a->dim, p->kernel = a->kernel, p->dtype = a->dtype, p->silu = a->silu;
+    p->layer = layer, p->L_total = L_total;
+    return PRECOG_OK;
+}
+
 // The kernel files' status words, taken and cleared at once: a copy of each would wait for the device
 // every time (eleven words: 144 us a call, so 22).
 constexpr cudaError_t (*kStatusWord[])(uint32_t **) = {
     precog::scan_status_word,    precog::scan_complex_status_word, precog::scan_latency_status_word, precog::retrieve_status_word,
     precog::retrieve_tc_status_word, precog::smc_status_word,      precog::selftest_status_word,     precog::delta_status_word,
-    precog::delta_chunk_status_word, precog::qk_norm_status_word,  precog::logprobs_status_word};
+    precog::delta_chunk_status_word, precog::qk_norm_status_word,  precog::logprobs_status_word,     precog::conv_status_word,
+    precog::scan_step_status_word, precog::adjust_status_word};
 constexpr int kStatusWords = sizeof(kStatusWord) / sizeof(kStatusWord[0]);
 static_assert(kStatusWords <= 32, "a lane each");
 struct StatusWords {
@@ -787,6 +852,258 @@ precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n
     p.top_logprob = d_top_logprob;
     cudaError_t e = precog::launch_logprobs(p, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "logprobs launch");
+    return ok();
+}
+
+precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_offsets, int64_t n_seqs, int64_t T_tot,
+                                 const void *bank, int64_t bank_entries, const int64_t *d_idx, void *windows_out,
+                                 int32_t layer, int32_t L_total, void *stream) {
+    if (T_tot < 0) return fail(PRECOG_ERR_INVALID_ARG, "T_tot must be >= 0");
+    if (n_seqs < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_seqs must be >= 0");
+    precog::ConvParams p;
+    if (T_tot > 0x7fffffffLL || n_seqs > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "T_tot and n_seqs must be below 2^31");
+    precog_status s = check_conv(args, T_tot, layer, L_total, &p);
+    if (s != PRECOG_OK) return s;
+    if (d_offsets == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "d_offsets is NULL");
+    if (bank) {
+        if (!aligned16(bank)) return fail(PRECOG_ERR_INVALID_ARG, "bank not 16-byte aligned");
+        if (bank_entries < 0) return fail(PRECOG_ERR_INVALID_ARG, "bank_entries must be >= 0");
+        if (d_idx == nullptr && bank_entries < n_seqs)
+            return fail(PRECOG_ERR_INVALID_ARG, "d_idx is NULL but bank has fewer rows than sequences");
+    } else {
+        bank_entries = 0;   // (and what d_idx names has to be -1)
+    }
+    if (!aligned16(windows_out)) return fail(PRECOG_ERR_INVALID_ARG, "windows_out not 16-byte aligned");
+    const int64_t sz = dtype_size(p.dtype), row = p.dim * sz;
+    const RowSpan x{p.x, p.x_stride * sz, row}, y{p.y, p.y_stride * sz, row};
+    RowSpan from, to;
+    if (!table_span(bank, bank ? bank_entries : 0, L_total, row * (p.kernel - 1), &from) ||
+        !table_span(windows_out, n_seqs, L_total, row * (p.kernel - 1), &to))
+        return fail(PRECOG_ERR_UNSUPPORTED, "tables beyond 2^63 bytes");
+    if (overlap(x, y, T_tot, false))
+        return fail(PRECOG_ERR_INVALID_ARG, "y must not share memory with x: tokens read the inputs before them");
+    // a sequence's window is written while other parts of it may still read theirs
+    if (overlap(from, to, 1, false)) return fail(PRECOG_ERR_INVALID_ARG, "windows_out must not share memory with bank");
+    if (overlap(whole(x, T_tot), to, 1, false) || overlap(whole(y, T_tot), to, 1, false) || overlap(whole(y, T_tot), from, 1, false))
+        return fail(PRECOG_ERR_INVALID_ARG, "windows and rows must not share memory");
+    if (n_seqs == 0) return ok();
+    p.offsets = d_offsets;
+    p.n_seqs = n_seqs;
+    p.T_tot = T_tot;
+    p.bank = bank;
+    p.bank_entries = bank_entries;
+    p.idx = d_idx;
+    p.windows = windows_out;
+    cudaError_t e = precog::launch_conv(p, false, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "convolution launch");
+    return ok();
+}
+
+precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *windows, int64_t n_slots,
+                               const int64_t *d_slots, int32_t layer, int32_t L_total, void *stream) {
+    if (n < 0) return fail(PRECOG_ERR_INVALID_ARG, "n must be >= 0");
+    if (n > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    precog::ConvParams p;
+    precog_status s = check_conv(args, n, layer, L_total, &p);
+    if (s != PRECOG_OK) return s;
+    if (windows == nullptr || !aligned16(windows))
+        return fail(PRECOG_ERR_INVALID_ARG, "windows must be non-NULL and 16-byte aligned");
+    if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (d_slots == nullptr && n_slots < n)
+        return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
+    const int64_t sz = dtype_size(p.dtype), row = p.dim * sz;
+    const RowSpan x{p.x, p.x_stride * sz, row}, y{p.y, p.y_stride * sz, row};
+    if (overlap(x, y, n, true)) return fail(PRECOG_ERR_INVALID_ARG, "y must be x itself or share no memory with it");
+    RowSpan table;
+    if (!table_span(windows, n_slots, L_total, row * (p.kernel - 1), &table))
+        return fail(PRECOG_ERR_UNSUPPORTED, "tables beyond 2^63 bytes");
+    if (overlap(whole(x, n), table, 1, false) || overlap(whole(y, n), table, 1, false))
+        return fail(PRECOG_ERR_INVALID_ARG, "windows and rows must not share memory");
+    if (n == 0) return ok();
+    p.n_seqs = n;
+    p.T_tot = n;
+    p.bank_entries = n_slots;
+    p.idx = d_slots;
+    p.windows = windows;
+    cudaError_t e = precog::launch_conv(p, true, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "convolution step launch");
+    return ok();
+}
+
+precog_status precog_scan_step(const precog_scan_inputs *in, int64_t n, void *states, int64_t n_slots,
+                               const int64_t *d_slots, int32_t layer0, int32_t L_total, const float *skip,
+                               const void *gate, int64_t gate_stride, int64_t gate_layer_stride, void *y_out,
+                               int32_t y_dtype, void *stream) {
+    if (n < 0) return fail(PRECOG_ERR_INVALID_ARG, "n must be >= 0");
+    if (n > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    precog_status s = check_scan_inputs(in, n, true);
+    if (s != PRECOG_OK) return s;
+    if (states == nullptr || !aligned16(states))
+        return fail(PRECOG_ERR_INVALID_ARG, "states must be non-NULL and 16-byte aligned");
+    if (layer0 < 0 || L_total < 1 || static_cast<int64_t>(layer0) + in->n_layers > L_total)
+        return fail(PRECOG_ERR_INVALID_ARG, "layers [layer0, layer0+n_layers) exceed L_total");
+    if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (d_slots == nullptr && n_slots < n)
+        return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
+    if (y_out == nullptr || !state_dtype_ok(y_dtype) || !aligned16(y_out))
+        return fail(PRECOG_ERR_INVALID_ARG, "y_out must be 16-byte aligned F32 or BF16");
+    if (!aligned16(skip) || !aligned16(gate)) return fail(PRECOG_ERR_INVALID_ARG, "skip and gate must be 16-byte aligned");
+    if (gate) {
+        const int sz = dtype_size(in->in_dtype);
+        if ((n > 1 && gate_stride < in->D) || (in->n_layers > 1 && gate_layer_stride < in->D))
+            return fail(PRECOG_ERR_INVALID_ARG, "gate strides smaller than a row");
+        if ((n > 1 && (gate_stride * sz) % 16 != 0) || (in->n_layers > 1 && (gate_layer_stride * sz) % 16 != 0))
+            return fail(PRECOG_ERR_INVALID_ARG, "gate strides must keep 16-byte alignment");
+    }
+    if (n == 0) return ok();
+    const int64_t sz = dtype_size(in->in_dtype), parts = in->a_kind == PRECOG_A_COMPLEX ? 2 : 1;
+    const RowSpan y{y_out, 0, in->n_layers * n * in->D * dtype_size(y_dtype)};
+    const RowSpan inputs[6] = {whole(RowSpan{in->x, in->layer_stride_xd * sz, n * in->D * sz}, in->n_layers),
+                               whole(RowSpan{in->dt, in->layer_stride_xd * sz, n * in->D * sz}, in->n_layers),
+                               whole(RowSpan{in->B, in->layer_stride_bc * sz, n * in->N * sz}, in->n_layers),
+                               whole(RowSpan{in->C, in->layer_stride_bc * sz, n * in->N * sz}, in->n_layers),
+                               RowSpan{in->A, 0, 4LL * parts * in->n_layers * in->D * in->N},
+                               whole(RowSpan{gate, gate_layer_stride * sz, whole(RowSpan{gate, gate_stride * sz, in->D * sz}, n).row}, in->n_layers)};
+    RowSpan table;
+    if (!table_span(states, n_slots, L_total, 4LL * parts * in->D * in->N, &table))
+        return fail(PRECOG_ERR_UNSUPPORTED, "tables beyond 2^63 bytes");
+    bool shared = overlap(y, table, 1, false);
+    for (const RowSpan &r : inputs) shared = shared || overlap(r, table, 1, false) || overlap(r, y, 1, false);
+    if (shared) return fail(PRECOG_ERR_INVALID_ARG, "y_out, states and inputs must not share memory");
+    precog::ScanStepParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.x = in->x, p.dt = in->dt, p.B = in->B, p.C = in->C, p.A = in->A;
+    p.ls_xd = in->n_layers > 1 ? in->layer_stride_xd : 0;
+    p.ls_bc = in->n_layers > 1 ? in->layer_stride_bc : 0;
+    p.n_layers = in->n_layers, p.D = in->D, p.in_dtype = in->in_dtype;
+    p.complex = in->a_kind == PRECOG_A_COMPLEX;
+    p.n = n;
+    p.states = static_cast<float *>(states);
+    p.n_slots = n_slots;
+    p.slots = d_slots;
+    p.layer0 = layer0, p.L_total = L_total;
+    p.skip = skip;
+    p.gate = gate;
+    p.gate_stride = n > 1 ? gate_stride : 0;
+    p.gate_layer_stride = in->n_layers > 1 ? gate_layer_stride : 0;
+    p.y = y_out, p.y_dtype = y_dtype;
+    cudaError_t e = precog::launch_scan_step(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "scan step launch");
+    return ok();
+}
+
+precog_status precog_block_norm(const precog_block_norm_args *a, int64_t T, void *stream) {
+    if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
+    if (T < 0) return fail(PRECOG_ERR_INVALID_ARG, "T must be >= 0");
+    if ((a->dtype != PRECOG_F32 && a->dtype != PRECOG_BF16) || (a->residual_dtype != PRECOG_F32 && a->residual_dtype != PRECOG_BF16))
+        return fail(PRECOG_ERR_UNSUPPORTED, "dtype and residual_dtype must be PRECOG_F32 or PRECOG_BF16");
+    if (a->residual && a->dtype == PRECOG_F32 && a->residual_dtype != PRECOG_F32)
+        return fail(PRECOG_ERR_UNSUPPORTED, "a residual of F32 rows must be F32");
+    if (a->groups < 1 || a->dim < 8) return fail(PRECOG_ERR_INVALID_ARG, "groups must be >= 1 and dim >= 8");
+    if (a->dim % a->groups != 0 || a->dim / a->groups % 8 != 0)
+        return fail(PRECOG_ERR_UNSUPPORTED, "dim / groups must be a multiple of 8");
+    if (a->dim / a->groups > 16384) return fail(PRECOG_ERR_UNSUPPORTED, "norms over more than 16384 entries are not implemented");
+    if (a->norm != PRECOG_NORM_NONE && a->norm != PRECOG_NORM_RMS)
+        return fail(PRECOG_ERR_INVALID_ARG, "norm must be PRECOG_NORM_NONE or _RMS");
+    if (a->gate_first != 0 && a->gate_first != 1) return fail(PRECOG_ERR_INVALID_ARG, "gate_first must be 0 or 1");
+    if (!(a->eps >= 0.f)) return fail(PRECOG_ERR_INVALID_ARG, "eps must be >= 0");
+    if ((a->skip == nullptr) != (a->skip_input == nullptr))
+        return fail(PRECOG_ERR_INVALID_ARG, "skip and skip_input must be given together");
+    if ((a->residual == nullptr) != (a->residual_out == nullptr))
+        return fail(PRECOG_ERR_INVALID_ARG, "residual and residual_out must be given together");
+    if (a->residual && a->out && a->groups != 1)
+        return fail(PRECOG_ERR_UNSUPPORTED, "groups are not implemented with a norm of the residual");
+    if (T > 0x7fffffffLL / a->groups) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    if (T == 0) return ok();
+    if (a->x == nullptr || (a->out == nullptr && a->residual_out == nullptr))
+        return fail(PRECOG_ERR_INVALID_ARG, "x and one of out and residual_out must be non-NULL");
+    precog::BlockNormParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.x = a->x, p.skip_input = a->skip_input, p.gate = a->gate, p.residual = a->residual;
+    p.residual_out = a->residual_out, p.out = a->out;
+    const int64_t sz = dtype_size(a->dtype), rsz = dtype_size(a->residual_dtype);
+    struct {
+        const void *at;
+        int64_t stride, size;
+        int64_t *to;
+    } rows[6] = {{a->x, a->x_stride, sz, &p.x_stride},
+                 {a->skip_input, a->skip_stride, sz, &p.skip_stride},
+                 {a->gate, a->gate_stride, sz, &p.gate_stride},
+                 {a->residual, a->residual_stride, rsz, &p.residual_stride},
+                 {a->residual_out, a->residual_out_stride, rsz, &p.residual_out_stride},
+                 {a->out, a->out_stride, sz, &p.out_stride}};
+    RowSpan span[6];
+    for (int i = 0; i < 6; ++i) {
+        *rows[i].to = T > 1 ? rows[i].stride : 0;
+        span[i] = RowSpan{rows[i].at, *rows[i].to * rows[i].size, a->dim * rows[i].size};
+        if (rows[i].at == nullptr) continue;
+        if (!aligned16(rows[i].at)) return fail(PRECOG_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+        if (T > 1 && rows[i].stride < a->dim) return fail(PRECOG_ERR_INVALID_ARG, "row strides smaller than a row");
+        if (span[i].stride % 16 != 0) return fail(PRECOG_ERR_INVALID_ARG, "row strides must keep 16-byte alignment");
+    }
+    // an entry's inputs are read, by the thread that writes its outputs, before those are written
+    for (int i = 0; i < 5; ++i)
+        if (overlap(span[i], span[5], T, i < 4) || (i < 4 && overlap(span[i], span[4], T, true)))
+            return fail(PRECOG_ERR_INVALID_ARG, "outputs must be inputs' very rows or share no memory with them or one another");
+    if (!aligned16(a->skip) || !aligned16(a->weight) || !aligned16(a->scale_weight) || !aligned16(a->out_weight))
+        return fail(PRECOG_ERR_INVALID_ARG, "skip and weights must be 16-byte aligned");
+    p.skip = a->skip, p.weight = a->weight, p.scale_weight = a->scale_weight, p.out_weight = a->out_weight;
+    p.scale = a->scale, p.eps = a->eps;
+    p.dim = a->dim, p.groups = a->groups, p.dtype = a->dtype, p.residual_dtype = a->residual ? a->residual_dtype : PRECOG_F32;
+    p.norm = a->norm, p.gate_first = a->gate_first;
+    p.T = T;
+    cudaError_t e = precog::launch_block_norm(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "block norm launch");
+    return ok();
+}
+
+precog_status precog_adjust_logits(const precog_adjust_args *a, int64_t n_rows, void *stream) {
+    if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
+    const int sz = dtype_size(a->dtype);
+    if (sz == 0) return fail(PRECOG_ERR_UNSUPPORTED, "dtype must be F16, BF16 or F32");
+    if (n_rows < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_rows must be >= 0");
+    if (a->reserved != 0) return fail(PRECOG_ERR_INVALID_ARG, "reserved must be 0");
+    if (a->vocab < 1) return fail(PRECOG_ERR_INVALID_ARG, "vocab must be >= 1");
+    if (a->vocab > 0x3fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "vocab must be below 2^30");
+    if (n_rows > 1 && (a->stride < a->vocab || a->out_stride < a->vocab))
+        return fail(PRECOG_ERR_INVALID_ARG, "row strides must be >= vocab");
+    if (a->n_history < 0 || a->n_bias < 0 || a->n_masks < 0)
+        return fail(PRECOG_ERR_INVALID_ARG, "n_history, n_bias and n_masks must be >= 0");
+    if (a->n_history > 0x7fffffffLL || a->n_bias > 0x7fffffffLL)
+        return fail(PRECOG_ERR_UNSUPPORTED, "lists of 2^31 entries or more are not implemented");
+    if (n_rows > 0x7fffffffLL / ((a->vocab + 1023) / 1024)) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    if (n_rows == 0) return ok();
+    if (a->logits == nullptr || a->out == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "logits and out must be non-NULL");
+    const uintptr_t odd = static_cast<uintptr_t>(sz - 1);
+    if (((reinterpret_cast<uintptr_t>(a->logits) | reinterpret_cast<uintptr_t>(a->out)) & odd) != 0)
+        return fail(PRECOG_ERR_INVALID_ARG, "logits and out must be aligned to their elements");
+    const bool penalised = a->d_repetition || a->d_frequency || a->d_presence;
+    if (a->d_history && a->d_history_offsets == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "d_history needs d_history_offsets");
+    if (a->n_history > 0 && penalised && a->d_history == nullptr)
+        return fail(PRECOG_ERR_INVALID_ARG, "n_history > 0 needs d_history");
+    if (a->n_bias > 0 && (a->d_bias_idx == nullptr || a->d_bias == nullptr || a->d_bias_offsets == nullptr))
+        return fail(PRECOG_ERR_INVALID_ARG, "n_bias > 0 needs d_bias_idx, d_bias and d_bias_offsets");
+    if (a->d_mask_rows && a->d_mask == nullptr && a->n_masks > 0) return fail(PRECOG_ERR_INVALID_ARG, "d_mask_rows is given without d_mask");
+    if (a->d_mask && a->d_mask_rows == nullptr && a->n_masks < n_rows)
+        return fail(PRECOG_ERR_INVALID_ARG, "d_mask_rows is NULL but there are fewer masks than rows");
+    precog::AdjustParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.logits = a->logits, p.out = a->out;
+    p.dtype = a->dtype;
+    p.rows = n_rows, p.vocab = a->vocab;
+    p.stride = n_rows > 1 ? a->stride : 0, p.out_stride = n_rows > 1 ? a->out_stride : 0;
+    if (overlap(RowSpan{p.logits, p.stride * sz, p.vocab * sz}, RowSpan{p.out, p.out_stride * sz, p.vocab * sz}, n_rows, true))
+        return fail(PRECOG_ERR_INVALID_ARG, "out must be logits itself or share no memory with it");
+    if (a->n_history > 0 && penalised) {
+        p.history = a->d_history, p.history_offsets = a->d_history_offsets, p.count_from = a->d_count_from;
+        p.n_history = a->n_history;
+        p.repetition = a->d_repetition, p.frequency = a->d_frequency, p.presence = a->d_presence;
+    }
+    if (a->n_bias > 0) p.bias_idx = a->d_bias_idx, p.bias = a->d_bias, p.bias_offsets = a->d_bias_offsets, p.n_bias = a->n_bias;
+    if (a->d_mask) p.mask = reinterpret_cast<const uint32_t *>(a->d_mask), p.n_masks = a->n_masks;
+    p.mask_rows = a->d_mask_rows;   // (without masks: each has to be -1)
+    cudaError_t e = precog::launch_adjust(p, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e, "logit adjustment launch");
     return ok();
 }
 

@@ -1,0 +1,139 @@
+// The end of a block in one pass over its rows: skip, gate, norm, residual with its scale, the next block's norm.
+//
+//   a = x + skip u ;  a <- a silu(gate) [before the norm] ;  a <- a rsqrt(mean a^2 + eps) weight [of each group]
+//   a <- a silu(gate) [after the norm] ;  without a residual: out = a
+//   h = residual + scale a ;  residual_out = h ;  out = h rsqrt(mean h^2 + eps) out_weight
+//
+// A row (or, where groups are normed, a group of one) belongs to WARPS warps whose lanes hold eight
+// neighbouring entries CH times; what is read is read once and stays in registers as fp32 until it is
+// written. Sums are fp32, in an order that depends on the row's length alone.
+#include "../../include/precog.h"
+#include "internal.h"
+#include "ptx.cuh"
+#include "vec8.cuh"
+
+namespace precog {
+namespace {
+
+// Sum over the row's warps; `slot` says which of the two sums (each has its own shared words).
+template <int WARPS>
+__device__ __forceinline__ float row_sum(float v, float (*part)[WARPS < 2 ? 1 : WARPS], int in_row) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (WARPS > 1) {
+        if ((threadIdx.x & 31) == 0) (*part)[in_row / 32] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) v += (*part)[i];
+    }
+    return v;
+}
+
+template <typename T, typename TR, int WARPS, int CH>
+__global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kernel(const BlockNormParams p, int64_t rows) {
+    grid_dependency_wait();
+    constexpr int kLanes = 32 * WARPS, kBlock = WARPS > 4 ? kLanes : 128, kRows = kBlock / kLanes;
+    __shared__ float part[2][kRows][WARPS < 2 ? 1 : WARPS];
+    const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + mine;
+    const bool live = row < rows;   // (all rows of a CTA meet at its barriers)
+    const int64_t t = live ? row / p.groups : 0;
+    const int size = p.dim / p.groups, first = live ? static_cast<int>(row - t * p.groups) * size : 0;
+    float v[CH][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int e = (c * kLanes + lane) * 8;
+        if (!live || e >= size) continue;
+        unpack8(load8(static_cast<const T *>(p.x) + t * p.x_stride + first + e), v[c]);
+        if (p.skip) {
+            float u[8];
+            unpack8(load8(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e), u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = fmaf(p.skip[first + e + i], u[i], v[c][i]);
+        }
+        if (p.gate && p.gate_first) {
+            float g[8];
+            unpack8(load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e), g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(g[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+    }
+    float scale = 1.f;
+    if (p.norm == PRECOG_NORM_RMS) scale = rsqrtf(row_sum<WARPS>(sum, &part[0][mine], lane) / static_cast<float>(size) + p.eps);
+    sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int e = (c * kLanes + lane) * 8;
+        if (!live || e >= size) continue;
+        if (p.norm == PRECOG_NORM_RMS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= scale * (p.weight ? p.weight[first + e + i] : 1.f);
+        }
+        if (p.gate && !p.gate_first) {
+            float g[8];
+            unpack8(load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e), g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(g[i]);
+        }
+        if (p.residual) {
+            float r[8];
+            unpack8(load8(static_cast<const TR *>(p.residual) + t * p.residual_stride + first + e), r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[c][i] = fmaf(p.scale * (p.scale_weight ? p.scale_weight[first + e + i] : 1.f), v[c][i], r[i]);
+                sum = fmaf(v[c][i], v[c][i], sum);
+            }
+            TR *out = static_cast<TR *>(p.residual_out) + t * p.residual_out_stride + first + e;
+            store8(out, pack8(out, v[c]));
+        }
+    }
+    if (p.out == nullptr) return;   // (for all threads or none)
+    scale = p.residual ? rsqrtf(row_sum<WARPS>(sum, &part[1][mine], lane) / static_cast<float>(size) + p.eps) : 1.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int e = (c * kLanes + lane) * 8;
+        if (!live || e >= size) continue;
+        if (p.residual) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= scale * (p.out_weight ? p.out_weight[first + e + i] : 1.f);
+        }
+        T *out = static_cast<T *>(p.out) + t * p.out_stride + first + e;
+        store8(out, pack8(out, v[c]));
+    }
+}
+
+template <typename T, typename TR, int WARPS, int CH>
+cudaError_t launch_shape(const BlockNormParams &p, cudaStream_t stream) {
+    constexpr int kBlock = WARPS > 4 ? 32 * WARPS : 128, kRows = kBlock / (32 * WARPS);
+    const int64_t rows = p.T * p.groups, blocks = (rows + kRows - 1) / kRows;
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    const cudaError_t e = launch_dependent(block_norm_kernel<T, TR, WARPS, CH>, dim3(static_cast<unsigned>(blocks)), dim3(kBlock), 0, stream, p, rows);
+    if (e == cudaSuccess) count_launches(1);
+    return e;
+}
+
+template <typename T, typename TR>
+cudaError_t launch_typed(const BlockNormParams &p, cudaStream_t stream) {
+    const int size = p.dim / p.groups;
+    if (size <= 256) return launch_shape<T, TR, 1, 1>(p, stream);
+    if (size <= 512) return launch_shape<T, TR, 1, 2>(p, stream);
+    if (size <= 1024) return launch_shape<T, TR, 4, 1>(p, stream);
+    if (size <= 2048) return launch_shape<T, TR, 8, 1>(p, stream);
+    if (size <= 4096) return launch_shape<T, TR, 8, 2>(p, stream);
+    if (size <= 8192) return launch_shape<T, TR, 8, 4>(p, stream);
+    return launch_shape<T, TR, 16, 4>(p, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t stream) {
+    if (p.dtype == PRECOG_F32) return launch_typed<float, float>(p, stream);
+    return p.residual_dtype == PRECOG_F32 ? launch_typed<__nv_bfloat16, float>(p, stream)
+                                          : launch_typed<__nv_bfloat16, __nv_bfloat16>(p, stream);
+}
+
+}  // namespace precog

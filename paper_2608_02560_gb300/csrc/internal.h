@@ -214,4 +214,74 @@ struct LogprobParams {
 cudaError_t launch_logprobs(const LogprobParams &p, cudaStream_t stream);
 cudaError_t logprobs_status_word(uint32_t **word);
 
+// The short causal convolution (conv.cu), over sequences or for one token of each row.
+struct ConvParams {
+    const void *x;
+    void *y;
+    int64_t x_stride, y_stride;             // elements between rows
+    const float *weight, *bias;             // [dim][kernel], [dim] or nullptr
+    int32_t dim, kernel, dtype, silu;
+    const int64_t *offsets;                 // [n_seqs + 1]
+    int64_t n_seqs;                         // step: rows
+    int64_t T_tot;
+    const void *bank;                       // nullptr: nothing before the sequences
+    int64_t bank_entries;                   // step: slots of the table
+    const int64_t *idx;                     // step: slots
+    void *windows;                          // step: the table
+    int32_t layer, L_total;
+};
+cudaError_t launch_conv(const ConvParams &p, bool step, cudaStream_t stream);
+cudaError_t conv_status_word(uint32_t **word);
+
+// One token of the diagonal scan on a table of states (scan_step.cu).
+struct ScanStepParams {
+    const void *x, *dt, *B, *C;
+    const float *A;
+    int64_t ls_xd, ls_bc;                   // layer strides in elements
+    int32_t n_layers, D, in_dtype, complex;
+    int64_t n;
+    float *states;                          // [n_slots][L_total][D][16], complex: pairs
+    int64_t n_slots;
+    const int64_t *slots;
+    int32_t layer0, L_total;
+    const float *skip;                      // [n_layers][D] or nullptr
+    const void *gate;
+    int64_t gate_stride, gate_layer_stride;
+    void *y;
+    int32_t y_dtype;
+};
+cudaError_t launch_scan_step(const ScanStepParams &p, cudaStream_t stream);
+cudaError_t scan_step_status_word(uint32_t **word);
+
+// The end of a block (block_norm.cu).
+struct BlockNormParams {
+    const void *x, *skip_input, *gate, *residual;
+    void *residual_out, *out;
+    int64_t x_stride, skip_stride, gate_stride, residual_stride, residual_out_stride, out_stride;
+    const float *skip, *weight, *scale_weight, *out_weight;
+    float scale, eps;
+    int32_t dim, groups, dtype, residual_dtype, norm, gate_first;
+    int64_t T;
+};
+cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t stream);
+
+// Penalties, biases and masks on logits (adjust.cu).
+struct AdjustParams {
+    const void *logits;
+    void *out;
+    int32_t dtype;
+    int64_t rows, vocab, stride, out_stride;
+    const int64_t *history, *history_offsets, *count_from;
+    int64_t n_history;
+    const float *repetition, *frequency, *presence;
+    const int64_t *bias_idx, *bias_offsets;
+    const float *bias;
+    int64_t n_bias;
+    const uint32_t *mask;
+    int64_t n_masks;
+    const int64_t *mask_rows;
+};
+cudaError_t launch_adjust(const AdjustParams &p, cudaStream_t stream);
+cudaError_t adjust_status_word(uint32_t **word);
+
 }  // namespace precog
