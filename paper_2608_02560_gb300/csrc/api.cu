@@ -1069,8 +1069,8 @@ precog_status precog_adjust_logits(const precog_adjust_args *a, int64_t n_rows, 
         return fail(PRECOG_ERR_INVALID_ARG, "row strides must be >= vocab");
     if (a->n_history < 0 || a->n_bias < 0 || a->n_masks < 0)
         return fail(PRECOG_ERR_INVALID_ARG, "n_history, n_bias and n_masks must be >= 0");
-    if (a->n_history > 0x7fffffffLL || a->n_bias > 0x7fffffffLL)
-        return fail(PRECOG_ERR_UNSUPPORTED, "lists of 2^31 entries or more are not implemented");
+    if (a->n_history > 0x3fffffffLL || a->n_bias > 0x3fffffffLL)
+        return fail(PRECOG_ERR_UNSUPPORTED, "lists of 2^30 entries or more are not implemented");
     if (n_rows > 0x7fffffffLL / ((a->vocab + 1023) / 1024)) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
     if (n_rows == 0) return ok();
     if (a->logits == nullptr || a->out == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "logits and out must be non-NULL");

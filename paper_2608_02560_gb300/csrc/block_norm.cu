@@ -30,6 +30,16 @@ __device__ __forceinline__ float row_sum(float v, float (*part)[WARPS < 2 ? 1 : 
     return v;
 }
 
+// fp32 weights of eight entries, or 1
+__device__ __forceinline__ void weights8(const float *w, int e, float (&v)[8]) {
+    if (w == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.f;
+        return;
+    }
+    unpack8(load8(w + e), v);
+}
+
 template <typename T, typename TR, int WARPS, int CH>
 __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kernel(const BlockNormParams p, int64_t rows) {
     grid_dependency_wait();
@@ -38,26 +48,39 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
     const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + mine;
     const bool live = row < rows;   // (all rows of a CTA meet at its barriers)
-    const int64_t t = live ? row / p.groups : 0;
-    const int size = p.dim / p.groups, first = live ? static_cast<int>(row - t * p.groups) * size : 0;
-    float v[CH][8];
+    const int64_t t = live ? (p.groups == 1 ? row : row / p.groups) : 0;
+    const int size = p.groups == 1 ? p.dim : p.dim / p.groups, first = live ? static_cast<int>(row - t * p.groups) * size : 0;
+    // every load of the row before the first is used
+    Raw8<T> x[CH], u[CH], g[CH];
+    Raw8<TR> res[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int e = (c * kLanes + lane) * 8;
+        if (!live || e >= size) continue;
+        x[c] = load8(static_cast<const T *>(p.x) + t * p.x_stride + first + e);
+        if (p.skip) u[c] = load8(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e);
+        if (p.gate) g[c] = load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e);
+        if (p.residual) res[c] = load8(static_cast<const TR *>(p.residual) + t * p.residual_stride + first + e);
+    }
+    float v[CH][8], w[8];
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int e = (c * kLanes + lane) * 8;
         if (!live || e >= size) continue;
-        unpack8(load8(static_cast<const T *>(p.x) + t * p.x_stride + first + e), v[c]);
+        unpack8(x[c], v[c]);
         if (p.skip) {
-            float u[8];
-            unpack8(load8(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e), u);
+            float s[8];
+            unpack8(u[c], s);
+            weights8(p.skip, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = fmaf(p.skip[first + e + i], u[i], v[c][i]);
+            for (int i = 0; i < 8; ++i) v[c][i] = fmaf(w[i], s[i], v[c][i]);
         }
         if (p.gate && p.gate_first) {
-            float g[8];
-            unpack8(load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e), g);
+            float s[8];
+            unpack8(g[c], s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(g[i]);
+            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(s[i]);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
@@ -70,21 +93,23 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
         const int e = (c * kLanes + lane) * 8;
         if (!live || e >= size) continue;
         if (p.norm == PRECOG_NORM_RMS) {
+            weights8(p.weight, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= scale * (p.weight ? p.weight[first + e + i] : 1.f);
+            for (int i = 0; i < 8; ++i) v[c][i] *= scale * w[i];
         }
         if (p.gate && !p.gate_first) {
-            float g[8];
-            unpack8(load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e), g);
+            float s[8];
+            unpack8(g[c], s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(g[i]);
+            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(s[i]);
         }
         if (p.residual) {
             float r[8];
-            unpack8(load8(static_cast<const TR *>(p.residual) + t * p.residual_stride + first + e), r);
+            unpack8(res[c], r);
+            weights8(p.scale_weight, first + e, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                v[c][i] = fmaf(p.scale * (p.scale_weight ? p.scale_weight[first + e + i] : 1.f), v[c][i], r[i]);
+                v[c][i] = fmaf(p.scale * w[i], v[c][i], r[i]);
                 sum = fmaf(v[c][i], v[c][i], sum);
             }
             TR *out = static_cast<TR *>(p.residual_out) + t * p.residual_out_stride + first + e;
@@ -98,8 +123,9 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
         const int e = (c * kLanes + lane) * 8;
         if (!live || e >= size) continue;
         if (p.residual) {
+            weights8(p.out_weight, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= scale * (p.out_weight ? p.out_weight[first + e + i] : 1.f);
+            for (int i = 0; i < 8; ++i) v[c][i] *= scale * w[i];
         }
         T *out = static_cast<T *>(p.out) + t * p.out_stride + first + e;
         store8(out, pack8(out, v[c]));

@@ -5,7 +5,7 @@
 // Inputs before a sequence's first token come from its window, K - 1 rows [oldest .. newest] that the
 // sequence's past left (a bank's entry, a table's slot), or are zero. A thread has eight channels and rolls
 // over a segment of tokens with the last K - 1 inputs in registers, so a row is read once and, at the start
-// of a segment, K - 1 rows again.
+// of a segment, K - 1 rows again. Loads run four tokens ahead of the arithmetic.
 //
 // Segments of S tokens of ragged sequences need no prefix sums: item i belongs to the sequence c with
 // base(c) <= i < base(c + 1), base(c) = offsets[c] / S + c, because base(c + 1) - base(c) is at least
@@ -21,65 +21,74 @@ namespace {
 __device__ uint32_t g_conv_status;
 
 constexpr int kThreads = 128;
+// Tokens whose loads are in flight together; a multiple of the K inputs that are held.
+constexpr int ahead(int K) { return K == 3 ? 3 : 4; }
 
+// Eight channels' taps and biases, as pairs of neighbouring channels.
 template <typename T, int K>
-struct Lane {
-    float w[K][8], bias[8];
-    __device__ __forceinline__ void weights(const ConvParams &p, int d) {
+struct Taps {
+    f2 w[K][4], bias[4];
+    __device__ __forceinline__ void load(const ConvParams &p, int d) {
+        float flat[8 * K];
+        const float4 *from = reinterpret_cast<const float4 *>(p.weight + static_cast<int64_t>(d) * K);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            bias[i] = p.bias ? p.bias[d + i] : 0.f;
-#pragma unroll
-            for (int j = 0; j < K; ++j) w[j][i] = p.weight[static_cast<int64_t>(d + i) * K + j];
+        for (int i = 0; i < 2 * K; ++i) {
+            const float4 q = __ldg(from + i);
+            flat[4 * i] = q.x, flat[4 * i + 1] = q.y, flat[4 * i + 2] = q.z, flat[4 * i + 3] = q.w;
         }
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[j][i] = pack2(flat[2 * i * K + j], flat[(2 * i + 1) * K + j]);
+        float4 b[2] = {};
+        if (p.bias) {
+            b[0] = __ldg(reinterpret_cast<const float4 *>(p.bias + d));
+            b[1] = __ldg(reinterpret_cast<const float4 *>(p.bias + d) + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) bias[2 * i] = pack2(b[i].x, b[i].y), bias[2 * i + 1] = pack2(b[i].z, b[i].w);
     }
-    // y of the inputs before[0 .. K - 2] and now
-    __device__ __forceinline__ Raw8<T> out(const float (&before)[K - 1][8], const float (&now)[8], bool act) const {
-        float y[8];
+    // y of inputs in[0 .. K - 1], oldest first
+    __device__ __forceinline__ Raw8<T> out(const f2 (*const (&in)[K])[4], bool act) const {
+        f2 y[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float a = bias[i];
+        for (int i = 0; i < 4; ++i) {
+            y[i] = bias[i];
 #pragma unroll
-            for (int j = 0; j < K - 1; ++j) a = fmaf(w[j][i], before[j][i], a);
-            a = fmaf(w[K - 1][i], now[i], a);
-            y[i] = act ? silu<T>(a) : a;
+            for (int j = 0; j < K; ++j) y[i] = fma2(w[j][i], (*in[j])[i], y[i]);
+            if (act) y[i] = silu2<T>(y[i]);
         }
         return pack8(static_cast<const T *>(nullptr), y);
     }
 };
 
 template <typename T, int K>
-__global__ void __launch_bounds__(kThreads) conv_kernel(const ConvParams p, int segment, int64_t items) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) conv_kernel(const ConvParams p, int segment, int64_t items) {
     grid_dependency_wait();
-    const int groups = p.dim / 8;
+    const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t item = at / groups;
+    const int64_t item = at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups);
     if (item >= items) return;
     const int d = static_cast<int>(at - item * groups) * 8;
-    // (in every thread of an item, so that every sequence is looked at whichever way the search goes)
-    if (item < p.n_seqs) {
+    if (item < p.n_seqs && d == 0) {   // every sequence is looked at, whichever way the search goes
         const int64_t a = p.offsets[item], b = p.offsets[item + 1];
-        if (a < 0 || b < a || b > p.T_tot) {
-            if (d == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_OFFSETS);
-        }
+        if (a < 0 || b < a || b > p.T_tot) atomicOr(&g_conv_status, PRECOG_DEV_BAD_OFFSETS);
     }
-    int64_t lo = 0, hi = p.n_seqs;   // base(lo) <= item < base(hi)
+    int lo = 0, hi = static_cast<int>(p.n_seqs);   // base(lo) <= item < base(hi)
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) / 2;
+        const int mid = lo + (hi - lo) / 2;
         if (p.offsets[mid] / segment + mid <= item) lo = mid;
         else hi = mid;
     }
     const int64_t c = lo, a = p.offsets[c], b = p.offsets[c + 1];
     if (a < 0 || b < a || b > p.T_tot) return;
     const int64_t part = item - (a / segment + c);
-    int64_t t = a + part * segment;
-    if (part < 0 || t > b || (t == b && part > 0)) return;   // (an empty sequence leaves its window all the same)
-    const int64_t end = t + segment < b ? t + segment : b;
+    const int64_t begin = a + part * segment;
+    if (part < 0 || begin > b || (begin == b && part > 0)) return;   // (an empty sequence leaves its window all the same)
+    const int n = static_cast<int>(begin + segment < b ? segment : b - begin);
 
-    const T *x = static_cast<const T *>(p.x) + d;
-    float before[K - 1][8];
     const T *window = nullptr;
-    if ((p.bank != nullptr || p.idx != nullptr) && t - (K - 1) < a) {
+    if ((p.bank != nullptr || p.idx != nullptr) && begin - (K - 1) < a) {
         const int64_t row = p.idx ? p.idx[c] : c;
         if (row < -1 || row >= p.bank_entries) {
             if (d == 0 && part == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_INDEX);
@@ -87,72 +96,126 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const ConvParams p, int 
             window = static_cast<const T *>(p.bank) + ((row * p.L_total + p.layer) * (K - 1)) * p.dim + d;
         }
     }
+    const T *x = static_cast<const T *>(p.x) + begin * p.x_stride + d;
+    // where input t of the segment is, which for t < 0 may be the window's (or nowhere: 0)
+    auto place = [&](int t) -> const T * {
+        const T *w = window == nullptr ? nullptr : window + (begin - a + t + K - 1) * p.dim;
+        return begin + t >= a ? x + t * p.x_stride : w;
+    };
+    constexpr int kAhead = ahead(K);
+    Raw8<T> next[kAhead] = {}, past[K - 1] = {};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (u < n) next[u] = load8(x + u * p.x_stride);
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
-        const int64_t s = t - (K - 1) + j;
-        Raw8<T> r = {};
-        if (s >= a) r = load8(x + s * p.x_stride);
-        else if (window != nullptr) r = load8(window + (s - a + K - 1) * p.dim);
-        unpack8(r, before[j]);
+        const T *at_j = place(j - (K - 1));
+        if (at_j != nullptr) past[j] = load8(at_j);
     }
-    Lane<T, K> lane;
-    lane.weights(p, d);
-    T *y = static_cast<T *>(p.y) + d;
-    for (; t < end; ++t) {
-        float now[8];
-        unpack8(load8(x + t * p.x_stride), now);
-        store8(y + t * p.y_stride, lane.out(before, now, p.silu != 0));
+    Taps<T, K> taps;
+    taps.load(p, d);
+    f2 in[K][4];   // input t in place t mod K
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j)
+    for (int j = 1; j < K; ++j) unpack8(past[j - 1], in[j]);
+    T *y = static_cast<T *>(p.y) + begin * p.y_stride + d;
+    const T *from = x + kAhead * p.x_stride;
+    const bool act = p.silu != 0;
+    auto token = [&](int u, bool more) {   // (u: a constant once unrolled)
+        unpack8(next[u], in[u % K]);
+        if (more) next[u] = load8(from + u * p.x_stride);
+        const f2(*of[K])[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) before[j][i] = j + 1 < K - 1 ? before[j + 1 < K - 1 ? j + 1 : 0][i] : now[i];
+        for (int j = 0; j < K; ++j) of[j] = &in[(u + 1 + j) % K];
+        store8(y + u * p.y_stride, taps.out(of, act));
+    };
+    int t = 0;
+    for (; t + 2 * kAhead <= n; t += kAhead, from += kAhead * p.x_stride, y += kAhead * p.y_stride) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) token(u, true);
     }
-    if (end == b && p.windows != nullptr) {
+    for (; t < n; t += kAhead, from += kAhead * p.x_stride, y += kAhead * p.y_stride) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (t + u < n) token(u, t + u + kAhead < n);
+    }
+    if (begin + n == b && p.windows != nullptr) {   // the last inputs, as they are stored
         T *out = static_cast<T *>(p.windows) + ((c * p.L_total + p.layer) * (K - 1)) * p.dim + d;
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) store8(out + static_cast<int64_t>(j) * p.dim, pack8(out, before[j]));
+        for (int j = 0; j < K - 1; ++j) {
+            const T *at_j = place(n - (K - 1) + j);
+            store8(out + static_cast<int64_t>(j) * p.dim, at_j != nullptr ? load8(at_j) : Raw8<T>{});
+        }
     }
 }
 
-template <typename T, int K>
+// R rows a thread, with the taps of one.
+template <typename T, int K, int R>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p) {
     grid_dependency_wait();
-    const int groups = p.dim / 8;
+    const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t row = at / groups;
-    if (row >= p.n_seqs) return;
-    const int d = static_cast<int>(at - row * groups) * 8;
-    const int64_t slot = p.idx ? p.idx[row] : row;
-    T *y = static_cast<T *>(p.y) + row * p.y_stride + d;
-    if (slot < 0 || slot >= p.bank_entries) {
-        if (slot != -1 && d == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_INDEX);
-        store8(y, Raw8<T>{});
-        return;
+    const int64_t first = R * (at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups));
+    if (first >= p.n_seqs) return;
+    const int d = static_cast<int>(at - first / R * groups) * 8;
+    int64_t slot[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        slot[r] = first + r;
+        if (p.idx && first + r < p.n_seqs) slot[r] = p.idx[first + r];
     }
-    T *window = static_cast<T *>(p.windows) + ((slot * p.L_total + p.layer) * (K - 1)) * p.dim + d;
-    Raw8<T> raw[K];
+    T *window[R];
+    Raw8<T> raw[R][K];
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) raw[j] = load8(window + static_cast<int64_t>(j) * p.dim);
-    raw[K - 1] = load8(static_cast<const T *>(p.x) + row * p.x_stride + d);
-    Lane<T, K> lane;
-    lane.weights(p, d);
-    float before[K - 1][8], now[8];
+    for (int r = 0; r < R; ++r) {
+        const bool live = first + r < p.n_seqs, there = slot[r] >= 0 && slot[r] < p.bank_entries;
+        if (live && !there && slot[r] != -1 && d == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_INDEX);
+        window[r] = live && there ? static_cast<T *>(p.windows) + ((slot[r] * p.L_total + p.layer) * (K - 1)) * p.dim + d : nullptr;
+    }
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) unpack8(raw[j], before[j]);
-    unpack8(raw[K - 1], now);
-    store8(y, lane.out(before, now, p.silu != 0));
+    for (int r = 0; r < R; ++r) {
+        if (window[r] == nullptr) continue;
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) store8(window + static_cast<int64_t>(j) * p.dim, raw[j + 1]);
+        for (int j = 0; j < K - 1; ++j) raw[r][j] = load8(window[r] + static_cast<int64_t>(j) * p.dim);
+        raw[r][K - 1] = load8(static_cast<const T *>(p.x) + (first + r) * p.x_stride + d);
+    }
+    Taps<T, K> taps;
+    taps.load(p, d);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (first + r >= p.n_seqs) continue;
+        T *y = static_cast<T *>(p.y) + (first + r) * p.y_stride + d;
+        if (window[r] == nullptr) {
+            store8(y, Raw8<T>{});
+            continue;
+        }
+        f2 in[K][4];
+        const f2(*of[K])[4];
+#pragma unroll
+        for (int j = 0; j < K; ++j) unpack8(raw[r][j], in[j]), of[j] = &in[j];
+        store8(y, taps.out(of, p.silu != 0));
+#pragma unroll
+        for (int j = 0; j < K - 1; ++j) store8(window[r] + static_cast<int64_t>(j) * p.dim, raw[r][j + 1]);
+    }
 }
 
 template <typename T, int K>
 cudaError_t launch_k(const ConvParams &p, bool step, cudaStream_t stream) {
-    const int segment = 32;
-    const int64_t groups = p.dim / 8, items = step ? p.n_seqs : (p.T_tot + segment - 1) / segment + p.n_seqs;
-    const int64_t blocks = (items * groups + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = step ? launch_dependent(conv_step_kernel<T, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, p)
-                               : launch_dependent(conv_kernel<T, K>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, p, segment, items);
+    const int64_t groups = p.dim / 8, fill = static_cast<int64_t>(device_sm_count()) * 4 * kThreads;
+    cudaError_t e;
+    auto go = [&](auto kernel, int64_t threads, auto... more) {
+        const int64_t blocks = (threads + kThreads - 1) / kThreads;
+        if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+        return launch_dependent(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, p, more...);
+    };
+    if (step) {
+        if (p.n_seqs * groups >= 2 * fill) e = go(conv_step_kernel<T, K, 2>, (p.n_seqs + 1) / 2 * groups);
+        else e = go(conv_step_kernel<T, K, 1>, p.n_seqs * groups);
+    } else {
+        int segment = 4;
+        while (segment < 128 && p.T_tot / (2 * segment) * groups >= fill / 3) segment *= 2;
+        const int64_t items = (p.T_tot + segment - 1) / segment + p.n_seqs;
+        e = go(conv_kernel<T, K>, items * groups, segment, items);
+    }
     if (e == cudaSuccess) count_launches(1);
     return e;
 }

@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <cstdint>
 
+#include "ptx.cuh"
+
 namespace precog {
 
 template <typename T> struct Raw8 { uint4 q[1]; };
@@ -56,12 +58,45 @@ __device__ __forceinline__ Raw8<__nv_bfloat16> pack8(const __nv_bfloat16 *, cons
 }
 
 // x / (1 + e^-x); NaN stays, and -infinity gives NaN as the formula does. For rows that are stored in 16 bits
-// the quick exponential and quotient (together within 2^-19 of the value while |x| < 10) are far below the
+// the quick exponential and reciprocal (together within 2^-19 of the value while |x| < 10) are far below the
 // rounding; where e^-x leaves 2^126 they give 0. Rows in fp32 get the exact ones.
+constexpr float kMinusLog2e = -1.4426950408889634f;
+__device__ __forceinline__ float rcp_quick(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 template <typename T>
 __device__ __forceinline__ float silu(float x) {
     if constexpr (sizeof(T) == 4) return x / (1.f + expf(-x));
-    return __fdividef(x, 1.f + __expf(-x));
+    return x * rcp_quick(1.f + ex2(x * kMinusLog2e));
+}
+// two at once
+template <typename T>
+__device__ __forceinline__ f2 silu2(f2 x) {
+    float a, b;
+    if constexpr (sizeof(T) == 4) {
+        unpack2(x, a, b);
+        return pack2(silu<T>(a), silu<T>(b));
+    }
+    unpack2(mul2(x, pack2(kMinusLog2e, kMinusLog2e)), a, b);
+    return mul2(x, pack2(rcp_quick(1.f + ex2(a)), rcp_quick(1.f + ex2(b))));
+}
+
+// the same eight as four pairs
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T> &r, f2 (&v)[4]) {
+    float e[8];
+    unpack8(r, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> pack8(const T *, const f2 (&v)[4]) {
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], e[2 * i], e[2 * i + 1]);
+    return pack8(static_cast<const T *>(nullptr), e);
 }
 
 }  // namespace precog

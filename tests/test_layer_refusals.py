@@ -141,7 +141,7 @@ def _adjust_args(**kw):
 @pytest.mark.parametrize("change,expect", [
     ({"dtype": 3}, 2), ({"reserved": 1}, 1), ({"vocab": 0}, 1), ({"vocab": 1 << 30, "stride": 1 << 30, "out_stride": 1 << 30}, 2),
     ({"stride": 99}, 1), ({"out_stride": -1}, 1), ({"n_history": -1}, 1), ({"n_bias": -1}, 1), ({"n_masks": -1}, 1),
-    ({"n_history": 1 << 31}, 2), ({"n_bias": 1 << 31}, 2), ({"logits": 0}, 1), ({"out": 0}, 1), ({"logits": X + 1}, 1),
+    ({"n_history": 1 << 30}, 2), ({"n_bias": 1 << 30}, 2), ({"logits": 0}, 1), ({"out": 0}, 1), ({"logits": X + 1}, 1),
     ({"out": Y + 1}, 1), ({"out": X + 2}, 1), ({"d_history": 0}, 1), ({"d_history_offsets": 0}, 1), ({"d_bias": 0}, 1),
     ({"d_bias_idx": 0}, 1), ({"d_bias_offsets": 0}, 1), ({"n_masks": 3}, 1), ({"d_mask": 0, "d_mask_rows": W}, 1)])
 def test_adjust_logits_rejects_bad_arguments(lib, change, expect):
