@@ -5,7 +5,7 @@
 // Inputs before a sequence's first token come from its window, K - 1 rows [oldest .. newest] that the
 // sequence's past left (a bank's entry, a table's slot), or are zero. A thread has eight channels and rolls
 // over a segment of tokens with the last K - 1 inputs in registers, so a row is read once and, at the start
-// of a segment, K - 1 rows again. Loads run four tokens ahead of the arithmetic.
+// of a segment, K - 1 rows again. Copies run eight tokens ahead of the arithmetic.
 //
 // Segments of S tokens of ragged sequences need no prefix sums: item i belongs to the sequence c with
 // base(c) <= i < base(c + 1), base(c) = offsets[c] / S + c, because base(c + 1) - base(c) is at least
@@ -21,8 +21,7 @@ namespace {
 __device__ uint32_t g_conv_status;
 
 constexpr int kThreads = 128;
-// Tokens whose loads are in flight together; a multiple of the K inputs that are held.
-constexpr int ahead(int K) { return K == 3 ? 3 : 4; }
+constexpr int kAhead = 8;   // tokens whose loads are in flight together
 
 // Eight channels' taps and biases, as pairs of neighbouring channels.
 template <typename T, int K>
@@ -63,7 +62,7 @@ struct Taps {
 };
 
 template <typename T, int K>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) conv_kernel(const ConvParams p, int segment, int64_t items) {
+__global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, int segment, int64_t items) {
     grid_dependency_wait();
     const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
@@ -102,11 +101,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) conv_kernel(
         const T *w = window == nullptr ? nullptr : window + (begin - a + t + K - 1) * p.dim;
         return begin + t >= a ? x + t * p.x_stride : w;
     };
-    constexpr int kAhead = ahead(K);
-    Raw8<T> next[kAhead] = {}, past[K - 1] = {};
+    // A thread's next kAhead inputs are on their way to its own places in shared memory (registers for them would
+    // cost the warps that hide their latency).
+    constexpr int kPieces = sizeof(T) / 2;
+    __shared__ uint4 ring[kAhead][kPieces][kThreads];
+    auto fetch = [&](int place, const T *from, bool there) {
+        if (there) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-        if (u < n) next[u] = load8(x + u * p.x_stride);
+            for (int i = 0; i < kPieces; ++i) cp_async16_exact(&ring[place][i][threadIdx.x], reinterpret_cast<const uint4 *>(from) + i);
+        }
+        cp_async_commit();
+    };
+    Raw8<T> past[K - 1] = {};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) fetch(u, x + u * p.x_stride, u < n);
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
         const T *at_j = place(j - (K - 1));
@@ -120,23 +128,26 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) conv_kernel(
     T *y = static_cast<T *>(p.y) + begin * p.y_stride + d;
     const T *from = x + kAhead * p.x_stride;
     const bool act = p.silu != 0;
-    auto token = [&](int u, bool more) {   // (u: a constant once unrolled)
-        unpack8(next[u], in[u % K]);
-        if (more) next[u] = load8(from + u * p.x_stride);
-        const f2(*of[K])[4];
+    constexpr int kRound = K == 3 ? 3 : 4;   // tokens after which the inputs' places repeat
+    int slot = 0;
+    for (int t = 0; t < n; t += kRound) {
 #pragma unroll
-        for (int j = 0; j < K; ++j) of[j] = &in[(u + 1 + j) % K];
-        store8(y + u * p.y_stride, taps.out(of, act));
-    };
-    int t = 0;
-    for (; t + 2 * kAhead <= n; t += kAhead, from += kAhead * p.x_stride, y += kAhead * p.y_stride) {
+        for (int u = 0; u < kRound; ++u) {
+            if (t + u >= n) break;
+            cp_async_wait<kAhead - 1>();
+            Raw8<T> raw;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) token(u, true);
-    }
-    for (; t < n; t += kAhead, from += kAhead * p.x_stride, y += kAhead * p.y_stride) {
+            for (int i = 0; i < kPieces; ++i) raw.q[i] = ring[slot][i][threadIdx.x];
+            fetch(slot, from, t + u + kAhead < n);
+            slot = (slot + 1) % kAhead;
+            from += p.x_stride;
+            unpack8(raw, in[u % K]);
+            const f2(*of[K])[4];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (t + u < n) token(u, t + u + kAhead < n);
+            for (int j = 0; j < K; ++j) of[j] = &in[(u + 1 + j) % K];
+            store8(y, taps.out(of, act));
+            y += p.y_stride;
+        }
     }
     if (begin + n == b && p.windows != nullptr) {   // the last inputs, as they are stored
         T *out = static_cast<T *>(p.windows) + ((c * p.L_total + p.layer) * (K - 1)) * p.dim + d;
