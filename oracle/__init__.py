@@ -30,6 +30,7 @@ module compiles it with gcc and marshals numpy arrays into it.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 import subprocess
@@ -470,11 +471,12 @@ def adjust_logits(z, history=None, count_from=None, repetition=None, frequency=N
     for r in range(R):
         text = [] if history is None else list(history[r])
         start = 0 if count_from is None else min(max(int(count_from[r]), 0), len(text))
+        counted = collections.Counter(text[start:])
         for i in set(text) - {-1}:
             if repetition is not None:
                 p = float(repetition[r])
                 out[r, i] = out[r, i] / p if out[r, i] > 0 else out[r, i] * p
-            times = text[start:].count(i)
+            times = counted[i]
             if times:
                 out[r, i] -= (times * float(frequency[r]) if frequency is not None else 0.0)
                 out[r, i] -= (float(presence[r]) if presence is not None else 0.0)

@@ -34,6 +34,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libprecog.so")
@@ -115,6 +116,15 @@ class AdjustArgs(ctypes.Structure):
                 ("d_mask", ctypes.c_void_p), ("n_masks", ctypes.c_int64), ("d_mask_rows", ctypes.c_void_p)]
 
 
+def _packer(cls) -> struct.Struct:
+    """Packs what a Structure of ``cls`` would hold (pointers as numbers, 0 for NULL)."""
+    codes = {ctypes.c_int32: "i", ctypes.c_float: "f", ctypes.c_int64: "q", ctypes.c_void_p: "P"}
+    return struct.Struct("@" + "".join(codes[kind] for _, kind in cls._fields_))
+
+
+# A Structure of 24 fields takes 1.0 us to fill on the Arm cores beside a GB300 and 0.5 to pass, a packed one 0.2
+# and 0.3; the launches that follow are of 2 to 3 us.
+_packed_calls = {}
 _lib = None
 
 
@@ -195,6 +205,11 @@ def load_library(path: str = LIB_PATH):
     lib.precog_retrieve_noalloc.argtypes = [vp, i32, i64, i32, vp, i32, vp, vp, vp]
     lib.precog_launch_count.restype = ctypes.c_uint64
     lib.precog_launch_count.argtypes = []
+    for name, cls in (("precog_causal_conv", ConvArgs), ("precog_conv_step", ConvArgs),
+                      ("precog_block_norm", BlockNormArgs), ("precog_adjust_logits", AdjustArgs)):
+        call = lib[name]        # the same function, with its arguments' struct as packed bytes
+        call.restype, call.argtypes = i32, [ctypes.c_char_p] + getattr(lib, name).argtypes[1:]
+        _packed_calls[name] = (call, _packer(cls).pack)
     _lib = lib
     return lib
 
@@ -610,39 +625,65 @@ def precog_token_logprobs(logits, tokens, logprob, entropy=None, top_idx=None, t
         _stream(stream)))
 
 
+_device_getter = None
+
+
 def _current_device() -> int:
-    torch = _torch()
-    get = getattr(torch._C, "_cuda_getDevice", None)
-    return get() if get is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+    global _device_getter
+    if _device_getter is None:
+        torch = _torch()
+        get = getattr(torch._C, "_cuda_getDevice", None)
+        if get is None or not torch.cuda.is_initialized():
+            return torch.cuda.current_device()
+        _device_getter = get
+    return _device_getter()
 
 
-def _on_current_device(*tensors):
-    """The library launches on the current device: tensors of another one are refused."""
-    device = _current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != device:
-            raise ValueError(f"tensors must live on the current device, cuda:{device}")
+def _elsewhere(t, what: str, device: int):
+    if not t.is_cuda:
+        raise ValueError("tensors passed to libprecog must live on the GPU")
+    raise ValueError(f"{what} must live on the current device, cuda:{device}, where the library launches")
 
 
-def _conv_args(x, weight, bias, silu: bool, y_out) -> ConvArgs:
-    torch = _torch()
-    T, D = x.shape
-    if y_out is None or y_out.shape != x.shape:
-        raise ValueError("y_out must have the shape of x")
-    if y_out.dtype is not x.dtype:
-        raise TypeError("x and y_out must have one dtype")
-    K = weight.shape[-1]
-    (xp, xs), (yp, ys) = _rows(x, "x"), _rows(y_out, "y_out")
-    return ConvArgs(_dtype_code(x), D, K, int(silu), xp, yp, xs, ys, _of(weight, torch.float32, (D, K), "weight"),
-                    _of(bias, torch.float32, (D,), "bias"))
+def _matrix(t, shape, dtype, device: int, what: str):
+    """(pointer, elements between rows) of a tensor ``[rows, n]`` whose rows are contiguous; None: (0, 0)."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        _elsewhere(t, what, device)
+    between, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return t.data_ptr(), between
 
 
-def _windows(t, x, K: int, what: str):
-    if t is not None and (t.dim() != 4 or t.shape[2:] != (K - 1, x.shape[1])):
-        raise ValueError(f"{what} must be [entries, layers, {K - 1}, {x.shape[1]}], got {tuple(t.shape)}")
-    if t is not None and t.dtype is not x.dtype:
-        raise TypeError(f"{what} and x must have one dtype")
-    return _ptr(t)
+def _dense(t, shape, dtype, device: int, what: str) -> int:
+    """The pointer of a contiguous tensor of this shape and dtype; None: 0."""
+    if t is None:
+        return 0
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        _elsewhere(t, what, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _windows(t, K: int, D: int, dtype, device: int, what: str):
+    """(pointer, entries, layers) of a table of windows ``[entries, layers, K - 1, D]``."""
+    if t is None:
+        return 0, 0, 0
+    if t.dim() != 4:
+        raise ValueError(f"{what} must be [entries, layers, {K - 1}, {D}], got {tuple(t.shape)}")
+    entries, layers = t.shape[:2]
+    return _dense(t, (entries, layers, K - 1, D), dtype, device, what), entries, layers
 
 
 def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=None, idx=None, layer: int = 0,
@@ -651,22 +692,28 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
     the sequences (rows ``offsets[c]..offsets[c + 1]``) of x ``[T, D]`` (rows may be strided) into ``y_out``.
     The inputs before a sequence are ``bank[idx[c], layer]`` (``[entries, layers, K - 1, D]``; -1 or no bank:
     zeros); ``windows_out[c, layer]`` receives those that its next token needs."""
-    torch = _torch()
-    _on_current_device(x, weight, offsets, bias, bank, idx, windows_out, y_out)
+    if y_out is None:
+        raise ValueError("y_out is required")
     if idx is not None and bank is None:
         raise ValueError("idx is given without bank")
-    args, n = _conv_args(x, weight, bias, silu, y_out), offsets.numel() - 1
-    K = weight.shape[1]
-    bp, wp = _windows(bank, x, K, "bank"), _windows(windows_out, x, K, "windows_out")
-    if windows_out is not None and windows_out.shape[0] != n:
+    load_library()
+    torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
+    (T, D), K, n = shape, weight.shape[-1], offsets.numel() - 1
+    xp, xs = _matrix(x, shape, dtype, device, "x")
+    yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
+    bp, entries, layers = _windows(bank, K, D, dtype, device, "bank")
+    wp, outs, out_layers = _windows(windows_out, K, D, dtype, device, "windows_out")
+    if windows_out is not None and outs != n:
         raise ValueError("windows_out must have one entry per sequence")
-    if bank is not None and windows_out is not None and bank.shape[1] != windows_out.shape[1]:
+    if bank is not None and windows_out is not None and layers != out_layers:
         raise ValueError("bank and windows_out must have the same number of layers")
-    holder = windows_out if windows_out is not None else bank
-    _check(load_library().precog_causal_conv(
-        ctypes.byref(args), _of(offsets, torch.int64, (n + 1,), "offsets"), n, x.shape[0], bp,
-        bank.shape[0] if bank is not None else 0, _of(idx, torch.int64, (n,), "idx"), wp, layer,
-        holder.shape[1] if holder is not None else layer + 1, _stream(stream)))
+    call, pack = _packed_calls["precog_causal_conv"]
+    _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
+                     _dense(weight, (D, K), torch.float32, device, "weight"),
+                     _dense(bias, (D,), torch.float32, device, "bias")),
+                _dense(offsets, (n + 1,), torch.int64, device, "offsets"), n, T, bp, entries,
+                _dense(idx, (n,), torch.int64, device, "idx"), wp, layer, out_layers or layers or layer + 1,
+                _stream(stream)))
 
 
 def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = True, layer: int = 0, y_out=None,
@@ -674,13 +721,19 @@ def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = Tru
     """One token of :func:`precog_causal_conv` for each row of x ``[n, D]``, on the table ``windows [slots,
     layers, K - 1, D]`` (updated in place) at the rows' int64 ``slots`` (-1: an idle row), into ``y_out``
     (which may be x)."""
-    torch = _torch()
-    _on_current_device(x, weight, windows, slots, bias, y_out)
-    args = _conv_args(x, weight, bias, silu, y_out)
-    wp = _windows(windows, x, weight.shape[1], "windows")
-    _check(load_library().precog_conv_step(
-        ctypes.byref(args), x.shape[0], wp, windows.shape[0], _of(slots, torch.int64, (x.shape[0],), "slots"), layer,
-        windows.shape[1], _stream(stream)))
+    if y_out is None:
+        raise ValueError("y_out is required")
+    load_library()
+    torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
+    (n, D), K = shape, weight.shape[-1]
+    xp, xs = _matrix(x, shape, dtype, device, "x")
+    yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
+    wp, n_slots, layers = _windows(windows, K, D, dtype, device, "windows")
+    call, pack = _packed_calls["precog_conv_step"]
+    _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
+                     _dense(weight, (D, K), torch.float32, device, "weight"),
+                     _dense(bias, (D,), torch.float32, device, "bias")),
+                n, wp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer, layers, _stream(stream)))
 
 
 def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, skip=None, gate=None, y_out=None,
@@ -689,33 +742,37 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
     fp32 (complex A: complex64) table ``states [slots, layers, D, N]``, updated in place, at the rows' int64
     ``slots`` (-1: an idle row), into ``y_out [L, n, D]``: the readout, plus fp32 ``skip [L, D]`` times x,
     times SiLU of ``gate [L, n, D]`` (each row contiguous)."""
-    torch = _torch()
+    torch, device = _torch(), _current_device()
     L, D, N, n = inputs.n_layers, inputs.D, inputs.N, inputs.rows
-    _on_current_device(inputs._keepalive[0], states, slots, skip, gate, y_out)
-    kind = torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32
-    if states.dim() != 4 or states.shape[2:] != (D, N) or states.dtype is not kind:
-        raise ValueError(f"states must be {kind} [slots, layers, {D}, {N}]")
+    for t in inputs._keepalive:
+        if t is not None and t.get_device() != device:
+            _elsewhere(t, "the inputs", device)
     if L == 1:   # [n, D] stands for one layer's [1, n, D]
         y_out, gate = (t.unsqueeze(0) if t is not None and t.dim() == 2 else t for t in (y_out, gate))
         skip = skip.unsqueeze(0) if skip is not None and skip.dim() == 1 else skip
-    if y_out is None or y_out.shape != (L, n, D):
-        raise ValueError("y_out must be [L, n, D]")
-    gp, gs, gls = None, 0, 0
+    if states.dim() != 4:
+        raise ValueError(f"states must be [slots, layers, {D}, {N}], got {tuple(states.shape)}")
+    n_slots, layers = states.shape[:2]
+    if y_out is None:
+        raise ValueError("y_out is required")
+    gp = gs = gls = 0
     if gate is not None:
         if gate.shape != (L, n, D):
             raise ValueError("gate must be [L, n, D]")
         if gate.dtype is not inputs._keepalive[0].dtype:
             raise TypeError("gate and x must have one dtype")
-        if not gate.is_cuda:
-            raise ValueError("tensors passed to libprecog must live on the GPU")
+        if gate.get_device() != device:
+            _elsewhere(gate, "gate", device)
         gls, gs, one = gate.stride()
         if one != 1 and D > 1:
             raise ValueError("the rows of gate must be contiguous")
         gp = gate.data_ptr()
     _check(load_library().precog_scan_step(
-        ctypes.byref(inputs), n, _ptr(states), states.shape[0], _of(slots, torch.int64, (n,), "slots"), layer0,
-        states.shape[1], _of(skip, torch.float32, (L, D), "skip"), gp, gs, gls, _ptr(y_out), _dtype_code(y_out),
-        _stream(stream)))
+        ctypes.byref(inputs), n,
+        _dense(states, (n_slots, layers, D, N), torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
+               device, "states"), n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
+        _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
+        _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), _stream(stream)))
 
 
 def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_first: bool = True, weight=None,
@@ -727,33 +784,32 @@ def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_f
     a residual ``out`` is a; with one, ``residual_out = residual + scale * a`` (``scale`` a number or fp32
     ``[D]``) and ``out``, if given, the RMS norm of that with ``out_weight``. Weights are fp32 ``[D]``; outputs
     may be inputs of their type."""
-    torch = _torch()
-    _on_current_device(x, out, skip, skip_input, gate, weight, residual, residual_out, out_weight)
+    load_library()
+    torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
     if norm is None:
-        norm = "none" if weight is None else "rms"
-    if norm not in ("none", "rms"):
+        kind = PRECOG_NORM_NONE if weight is None else PRECOG_NORM_RMS
+    elif norm == "none" or norm == "rms":
+        kind = _NORMS[norm]
+    else:
         raise ValueError('norm must be "none" or "rms"')
-    T, D = x.shape
-    for t, what in ((skip_input, "skip_input"), (gate, "gate"), (out, "out"), (residual, "residual"),
-                    (residual_out, "residual_out")):
-        if t is not None and t.shape != x.shape:
-            raise ValueError(f"{what} must have the shape of x")
-        if t is not None and t.dtype is not x.dtype and what[:8] != "residual":
-            raise TypeError(f"{what} and x must have one dtype")
-    if residual is not None and residual_out is not None and residual.dtype is not residual_out.dtype:
-        raise TypeError("residual and residual_out must have one dtype")
-    scale_weight = None
+    T, D = shape
+    f32, vec, scale_weight = torch.float32, (D,), 0
     if isinstance(scale, torch.Tensor):
-        scale, scale_weight = 1.0, scale
-        _on_current_device(scale_weight)
-    (xp, xs), (sp, ss), (gp, gs) = _rows(x, "x"), _rows(skip_input, "skip_input"), _rows(gate, "gate")
-    (rp, rs), (rop, ros), (op, os_) = _rows(residual, "residual"), _rows(residual_out, "residual_out"), _rows(out, "out")
-    f32, vec = torch.float32, (D,)
-    args = BlockNormArgs(_dtype_code(x), _dtype_code(residual) if residual is not None else PRECOG_F32, D, groups,
-                         _NORMS[norm], int(gate_first), scale, eps, xp, sp, gp, rp, rop, op, xs, ss, gs, rs, ros, os_,
-                         _of(skip, f32, vec, "skip"), _of(weight, f32, vec, "weight"),
-                         _of(scale_weight, f32, vec, "scale"), _of(out_weight, f32, vec, "out_weight"))
-    _check(load_library().precog_block_norm(ctypes.byref(args), T, _stream(stream)))
+        scale, scale_weight = 1.0, _dense(scale, vec, f32, device, "scale")
+    xp, xs = _matrix(x, shape, dtype, device, "x")
+    sp, ss = _matrix(skip_input, shape, dtype, device, "skip_input")
+    gp, gs = _matrix(gate, shape, dtype, device, "gate")
+    res_dtype, res_code = f32, PRECOG_F32
+    if residual is not None:
+        res_dtype, res_code = residual.dtype, _dtype_code(residual)
+    rp, rs = _matrix(residual, shape, res_dtype, device, "residual")
+    rop, ros = _matrix(residual_out, shape, res_dtype, device, "residual_out")
+    op, os_ = _matrix(out, shape, dtype, device, "out")
+    call, pack = _packed_calls["precog_block_norm"]
+    _check(call(pack(_dtype_code(x), res_code, D, groups, kind, 1 if gate_first else 0, scale, eps, xp, sp, gp, rp, rop,
+                     op, xs, ss, gs, rs, ros, os_, _dense(skip, vec, f32, device, "skip"),
+                     _dense(weight, vec, f32, device, "weight"), scale_weight,
+                     _dense(out_weight, vec, f32, device, "out_weight")), T, _stream(stream)))
 
 
 def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_from=None, repetition=None,
@@ -764,14 +820,6 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
     ``history`` (entries ``history_offsets[r]..history_offsets[r + 1]``; counted from entry ``count_from[r]``
     on), fp32 ``bias`` of the tokens ``bias_idx`` (lists by ``bias_offsets``), and -infinity where row
     ``mask_rows[r]`` (-1: none) of the int32 bit ``mask [masks, ceil(V / 32)]`` has a token's bit clear."""
-    torch = _torch()
-    _on_current_device(logits, out, history, history_offsets, count_from, repetition, frequency, presence, bias_idx,
-                       bias, bias_offsets, mask, mask_rows)
-    R, V = logits.shape
-    if out.shape != logits.shape:
-        raise ValueError("out must have the shape of logits")
-    if out.dtype is not logits.dtype:
-        raise TypeError("logits and out must have one dtype")
     if (bias is None) != (bias_idx is None) or (bias is None) != (bias_offsets is None):
         raise ValueError("bias_idx, bias and bias_offsets must be given together")
     if history is not None and history_offsets is None:
@@ -780,19 +828,25 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
         raise ValueError("penalties need a history")
     if mask_rows is not None and mask is None:
         raise ValueError("mask_rows is given without mask")
-    (lp, ls), (op, os_) = _rows(logits, "logits"), _rows(out, "out")
+    load_library()
+    torch, device, dtype, shape = _torch(), _current_device(), logits.dtype, logits.shape
+    R, V = shape
+    lp, ls = _matrix(logits, shape, dtype, device, "logits")
+    op, os_ = _matrix(out, shape, dtype, device, "out")
     i64, f32, row, ends = torch.int64, torch.float32, (R,), (R + 1,)
     nh = history.numel() if history is not None else 0
     nb = bias.numel() if bias is not None else 0
     nm = mask.shape[0] if mask is not None else 0
-    args = AdjustArgs(_dtype_code(logits), 0, V, ls, os_, lp, op, _of(history, i64, (nh,), "history"),
-                      _of(history_offsets, i64, ends, "history_offsets"), _of(count_from, i64, row, "count_from"), nh,
-                      _of(repetition, f32, row, "repetition"), _of(frequency, f32, row, "frequency"),
-                      _of(presence, f32, row, "presence"), _of(bias_idx, i64, (nb,), "bias_idx"),
-                      _of(bias, f32, (nb,), "bias"), _of(bias_offsets, i64, ends, "bias_offsets"), nb,
-                      _of(mask, torch.int32, (nm, (V + 31) // 32), "mask"), nm,
-                      _of(mask_rows, i64, row, "mask_rows"))
-    _check(load_library().precog_adjust_logits(ctypes.byref(args), R, _stream(stream)))
+    call, pack = _packed_calls["precog_adjust_logits"]
+    _check(call(pack(_dtype_code(logits), 0, V, ls, os_, lp, op, _dense(history, (nh,), i64, device, "history"),
+                     _dense(history_offsets, ends, i64, device, "history_offsets"),
+                     _dense(count_from, row, i64, device, "count_from"), nh,
+                     _dense(repetition, row, f32, device, "repetition"),
+                     _dense(frequency, row, f32, device, "frequency"), _dense(presence, row, f32, device, "presence"),
+                     _dense(bias_idx, (nb,), i64, device, "bias_idx"), _dense(bias, (nb,), f32, device, "bias"),
+                     _dense(bias_offsets, ends, i64, device, "bias_offsets"), nb,
+                     _dense(mask, (nm, (V + 31) // 32), torch.int32, device, "mask"), nm,
+                     _dense(mask_rows, row, i64, device, "mask_rows")), R, _stream(stream)))
 
 
 def precog_selftest_wait_timeout(iterations: int = 4096, stream=None):

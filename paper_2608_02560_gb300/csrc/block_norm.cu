@@ -147,10 +147,10 @@ cudaError_t launch_typed(const BlockNormParams &p, cudaStream_t stream) {
     const int size = p.dim / p.groups;
     if (size <= 256) return launch_shape<T, TR, 1, 1>(p, stream);
     if (size <= 512) return launch_shape<T, TR, 1, 2>(p, stream);
-    if (size <= 1024) return launch_shape<T, TR, 4, 1>(p, stream);
-    if (size <= 2048) return launch_shape<T, TR, 8, 1>(p, stream);
+    if (size <= 1024) return launch_shape<T, TR, 2, 2>(p, stream);
+    if (size <= 2048) return launch_shape<T, TR, 4, 2>(p, stream);
     if (size <= 4096) return launch_shape<T, TR, 8, 2>(p, stream);
-    if (size <= 8192) return launch_shape<T, TR, 8, 4>(p, stream);
+    if (size <= 8192) return launch_shape<T, TR, 16, 2>(p, stream);
     return launch_shape<T, TR, 16, 4>(p, stream);
 }
 

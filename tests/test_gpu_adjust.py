@@ -101,6 +101,15 @@ def test_rows_match_the_definition(cuda_device, dtype, R, V, pad):
         assert bool((again["x"].as_strided((R, pad), (V + pad, 1), 0) == 5.0).all())
 
 
+@pytest.mark.parametrize("V", [2048, 2049, 6000])
+def test_few_rows_with_long_lists(cuda_device, V):
+    c = _case(cuda_device, 4, V, "float32", V)
+    r = np.random.default_rng(V)
+    c["history"][1] = list(r.integers(0, V, 20_000))
+    c["biases"][2] = [(int(i), float(np.float32(b))) for i, b in zip(r.integers(0, V, 5000), r.standard_normal(5000))]
+    _check(c, _run(cuda_device, c), to_np(c["x"]))
+
+
 @pytest.mark.parametrize("on", ["rep", "freq", "pres", "bias", "masks", "nothing"])
 def test_each_alone(cuda_device, on):
     c = _case(cuda_device, 6, 500, "float32", 3, rep=on == "rep", freq=on == "freq", pres=on == "pres",
@@ -169,6 +178,29 @@ def test_bad_tokens_lists_and_masks_are_ignored_and_flagged(cuda_device):
     plain(mask=torch.zeros((0, 2), dtype=torch.int32, device=d), mask_rows=i64(-1, -1, -1), history=empty,
           history_offsets=i64(0, 0, 0, 0), repetition=rep, bias_idx=empty, bias=rep.new_ones(0), bias_offsets=i64(0, 0, 0, 0))
     assert pg.precog_device_status()[0] == 0 and torch.equal(out, x)
+
+
+@pytest.mark.parametrize("dtype,V,pad", [("bfloat16", 30_011, 5), ("float32", 30_020, 0), ("float16", 30_008, 8), ("bfloat16", 131_075, 1)])
+def test_a_batch_of_many_logits(cuda_device, dtype, V, pad):
+    """More than 152 * 2 * 16,384 logits go through a copy and a launch behind it. Rows among them whose tokens do not fit
+    in its table (20,000 different ones), with one token 30,000 times, and with 9000 biases, some of them twice."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    R = 170 if V < 100_000 else 45
+    c = _case(cuda_device, R, V, dtype, V + pad, longest=200, pad=pad)
+    r = np.random.default_rng(3)
+    c["history"][3] = list(r.permutation(V)[:20_000])
+    c["history"][7] = [V - 1] * 30_000 + [0, -1]
+    c["history"][11] = list(r.integers(0, V, 9000))
+    c["start"][[3, 7, 11]] = 5000
+    c["biases"][5] = [(int(i), float(np.float32(b))) for i, b in zip(r.integers(0, V, 9000), r.standard_normal(9000))]
+    c["biases"][3] = c["biases"][5][:500]
+    out = _run(cuda_device, c)
+    assert pg.precog_device_status()[0] == 0
+    _check(c, out, to_np(c["x"]))
+    again = dict(c, x=c["x"].clone())
+    _run(cuda_device, again, out=again["x"])
+    assert torch.equal(again["x"], out)
 
 
 def test_calls_of_one_input_repeat_bit_for_bit(cuda_device):

@@ -163,29 +163,36 @@ def test_the_binding_checks_shapes_dtypes_and_devices(lib, monkeypatch):
     """Host tensors stand in where the check comes before the pointer is taken."""
     import torch
     import paper_2608_02560_gb300 as pg
-    monkeypatch.setattr(pg, "_on_current_device", lambda *t: None)
+    monkeypatch.setattr(pg, "_current_device", lambda: -1)     # (a host tensor's)
     x, w, off = torch.zeros(6, 8), torch.zeros(8, 4), torch.zeros(3, dtype=torch.int64)
-    win = torch.zeros(2, 1, 3, 8)
-    with pytest.raises(ValueError, match="GPU"):
-        pg.precog_causal_conv(x, w, off, y_out=torch.zeros_like(x))
-    with pytest.raises(ValueError, match="shape of x"):
-        pg.precog_causal_conv(x, w, off, y_out=x[:3])
-    with pytest.raises(ValueError, match="shape of x"):
+    win, g = torch.zeros(2, 1, 3, 8), torch.zeros(6, 8)
+    with pytest.raises(ValueError, match="y_out"):
         pg.precog_causal_conv(x, w, off)
+    with pytest.raises(ValueError, match="y_out"):
+        pg.precog_causal_conv(x, w, off, y_out=x[:3])
     with pytest.raises(ValueError, match="without bank"):
-        pg.precog_causal_conv(x, w, off, idx=off, y_out=torch.zeros_like(x))
-    with pytest.raises(TypeError, match="one dtype"):
+        pg.precog_causal_conv(x, w, off, idx=off, y_out=g)
+    with pytest.raises(ValueError, match="bank must be"):
+        pg.precog_causal_conv(x, w, off, bank=win[:, :, :2], y_out=g)
+    with pytest.raises(ValueError, match="one entry per sequence"):
+        pg.precog_causal_conv(x, w, off, windows_out=win[:1], y_out=g)
+    with pytest.raises(ValueError, match="number of layers"):
+        pg.precog_causal_conv(x, w, off, bank=win.repeat(1, 2, 1, 1), windows_out=win, y_out=g)
+    with pytest.raises(ValueError, match="rows of x"):
+        pg.precog_causal_conv(torch.zeros(8, 6).t(), w, off, y_out=g)
+    with pytest.raises(TypeError, match="y_out"):
         pg.precog_conv_step(x, w, win, y_out=x.half())
-    with pytest.raises(ValueError, match="windows must be"):
-        pg._windows(win[:, :, :2], x, 4, "windows")
-    with pytest.raises(TypeError, match="one dtype"):
-        pg._windows(win.half(), x, 4, "windows")
-    g = torch.zeros(6, 8)
-    with pytest.raises(ValueError, match="shape of x"):
+    with pytest.raises(TypeError, match="windows"):
+        pg.precog_conv_step(x, w, win.half(), y_out=g)
+    with pytest.raises(ValueError, match="windows must be contiguous"):
+        pg.precog_conv_step(x, w, torch.zeros(2, 1, 8, 3).transpose(2, 3), y_out=g)
+    with pytest.raises(ValueError, match="weight"):
+        pg.precog_conv_step(x, torch.zeros(9, 4), win, y_out=g)
+    with pytest.raises(ValueError, match="out must be"):
         pg.precog_block_norm(x, out=x[:, :4])
-    with pytest.raises(TypeError, match="one dtype"):
+    with pytest.raises(TypeError, match="out"):
         pg.precog_block_norm(x, out=x.half())
-    with pytest.raises(TypeError, match="one dtype"):
+    with pytest.raises(TypeError, match="residual_out"):
         pg.precog_block_norm(x, residual=g, residual_out=g.bfloat16())
     with pytest.raises(ValueError, match="norm"):
         pg.precog_block_norm(x, out=x, norm="l2")
@@ -197,7 +204,22 @@ def test_the_binding_checks_shapes_dtypes_and_devices(lib, monkeypatch):
         pg.precog_adjust_logits(x, x, repetition=g)
     with pytest.raises(ValueError, match="without mask"):
         pg.precog_adjust_logits(x, x, mask_rows=off)
-    with pytest.raises(TypeError, match="one dtype"):
+    with pytest.raises(TypeError, match="out"):
         pg.precog_adjust_logits(x, x.half())
+    with pytest.raises(ValueError, match="mask must be"):
+        pg.precog_adjust_logits(x, g, mask=torch.zeros(1, 2, dtype=torch.int32))
+    monkeypatch.setattr(pg, "_current_device", lambda: 0)
     with pytest.raises(ValueError, match="GPU"):
-        pg.precog_adjust_logits(x, x)
+        pg.precog_causal_conv(x, w, off, y_out=g)
+    with pytest.raises(ValueError, match="GPU"):
+        pg.precog_block_norm(x, out=g)
+    with pytest.raises(ValueError, match="GPU"):
+        pg.precog_adjust_logits(x, g)
+
+
+def test_packed_arguments_are_the_structures_bytes(lib):
+    """The binding packs its arguments instead of filling a Structure: the same bytes, field by field."""
+    import paper_2608_02560_gb300 as pg
+    for cls in (pg.ConvArgs, pg.BlockNormArgs, pg.AdjustArgs):
+        values = [1.5 if kind is ctypes.c_float else i + 3 for i, (_, kind) in enumerate(cls._fields_)]
+        assert bytes(cls(*values)) == pg._packer(cls).pack(*values)
