@@ -315,7 +315,7 @@ template <typename T>
 cudaError_t launch_typed(const AdjustParams &p, cudaStream_t stream) {
     const int64_t tokens = p.rows * p.vocab, sms = device_sm_count();
     const auto slices_of = [&](int slice) { return static_cast<unsigned>((p.vocab + slice - 1) / slice); };
-    const bool many = tokens >= sms * 2 * 16384, biases = p.bias != nullptr;
+    const bool many = tokens >= sms * 8192, biases = p.bias != nullptr;
     if (!p.history && !biases) {
         const int slice = many ? 16384 : 2048;
         return launch_slices(copy_kernel<T>, p, slice, kThreads, 0, stream, slice, slices_of(slice), false);

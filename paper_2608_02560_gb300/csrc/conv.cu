@@ -128,25 +128,34 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
     T *y = static_cast<T *>(p.y) + begin * p.y_stride + d;
     const T *from = x + kAhead * p.x_stride;
     const bool act = p.silu != 0;
-    constexpr int kRound = K == 3 ? 3 : 4;   // tokens after which the inputs' places repeat
+    constexpr int kRound = K == 3 ? 6 : 4;   // tokens after which the inputs' places repeat, two at a time
     int slot = 0;
     for (int t = 0; t < n; t += kRound) {
 #pragma unroll
-        for (int u = 0; u < kRound; ++u) {
+        for (int u = 0; u < kRound; u += 2) {
             if (t + u >= n) break;
-            cp_async_wait<kAhead - 1>();
-            Raw8<T> raw;
+            cp_async_wait<kAhead - 2>();
+            Raw8<T> raw[2];
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) raw.q[i] = ring[slot][i][threadIdx.x];
-            fetch(slot, from, t + u + kAhead < n);
-            slot = (slot + 1) % kAhead;
-            from += p.x_stride;
-            unpack8(raw, in[u % K]);
-            const f2(*of[K])[4];
+            for (int v = 0; v < 2; ++v) {
 #pragma unroll
-            for (int j = 0; j < K; ++j) of[j] = &in[(u + 1 + j) % K];
-            store8(y, taps.out(of, act));
-            y += p.y_stride;
+                for (int i = 0; i < kPieces; ++i) raw[v].q[i] = ring[slot + v][i][threadIdx.x];
+                fetch(slot + v, from + v * p.x_stride, t + u + v + kAhead < n);
+            }
+            slot = (slot + 2) % kAhead;
+            from += 2 * p.x_stride;
+            Raw8<T> r[2];
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                unpack8(raw[v], in[(u + v) % K]);
+                const f2(*of[K])[4];
+#pragma unroll
+                for (int j = 0; j < K; ++j) of[j] = &in[(u + v + 1 + j) % K];
+                r[v] = taps.out(of, act);
+            }
+            store8(y, r[0]);
+            if (t + u + 1 < n) store8(y + p.y_stride, r[1]);
+            y += 2 * p.y_stride;
         }
     }
     if (begin + n == b && p.windows != nullptr) {   // the last inputs, as they are stored
