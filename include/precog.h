@@ -641,7 +641,7 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
                                const int64_t *d_slots, int32_t layer, int32_t L_total, void *stream);
 
 /*
- * precog_scan_step -- one token of the diagonal scan for each of n sequences through
+ * Arguments of precog_scan_step: one token of the diagonal scan for each of n sequences through
  * in->n_layers layers, on a table of fp32 states that is updated in place: the recurrence of
  * precog_scan_inputs, whose "token rows" are the n sequences (x, dt [L][n][D], B, C [L][n][N]),
  * and
@@ -656,10 +656,23 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
  *   y_out     device [L][n][D] in y_dtype (F32 or BF16)
  * y_out, states and the inputs must not share memory.
  */
-precog_status precog_scan_step(const precog_scan_inputs *in, int64_t n, void *states, int64_t n_slots,
-                               const int64_t *d_slots, int32_t layer0, int32_t L_total, const float *skip,
-                               const void *gate, int64_t gate_stride, int64_t gate_layer_stride, void *y_out,
-                               int32_t y_dtype, void *stream);
+typedef struct precog_scan_step_args {
+    void *states;
+    int64_t n_slots;
+    const int64_t *d_slots;
+    int32_t layer0;
+    int32_t L_total;
+    const float *skip;
+    const void *gate;
+    int64_t gate_stride;
+    int64_t gate_layer_stride;
+    void *y_out;
+    int32_t y_dtype;           /* precog_dtype: F32 or BF16 */
+    int32_t reserved;          /* must be 0 */
+} precog_scan_step_args;
+
+/* precog_scan_step -- the next token of n sequences. */
+precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_step_args *args, int64_t n, void *stream);
 
 /*
  * Arguments of precog_block_norm. Of every row,

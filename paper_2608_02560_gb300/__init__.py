@@ -93,6 +93,14 @@ class ConvArgs(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+class ScanStepArgs(ctypes.Structure):
+    """Mirror of ``precog_scan_step_args`` (include/precog.h)."""
+    _fields_ = [("states", ctypes.c_void_p), ("n_slots", ctypes.c_int64), ("d_slots", ctypes.c_void_p),
+                ("layer0", ctypes.c_int32), ("L_total", ctypes.c_int32), ("skip", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("gate_layer_stride", ctypes.c_int64),
+                ("y_out", ctypes.c_void_p), ("y_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class BlockNormArgs(ctypes.Structure):
     """Mirror of ``precog_block_norm_args`` (include/precog.h)."""
     _fields_ = [("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("dim", ctypes.c_int32),
@@ -185,8 +193,7 @@ def load_library(path: str = LIB_PATH):
     lib.precog_conv_step.restype = i32
     lib.precog_conv_step.argtypes = [ctypes.POINTER(ConvArgs), i64, vp, i64, vp, i32, i32, vp]
     lib.precog_scan_step.restype = i32
-    lib.precog_scan_step.argtypes = [ctypes.POINTER(ScanInputs), i64, vp, i64, vp, i32, i32, vp, vp, i64, i64, vp, i32,
-                                     vp]
+    lib.precog_scan_step.argtypes = [ctypes.POINTER(ScanInputs), ctypes.POINTER(ScanStepArgs), i64, vp]
     lib.precog_block_norm.restype = i32
     lib.precog_block_norm.argtypes = [ctypes.POINTER(BlockNormArgs), i64, vp]
     lib.precog_adjust_logits.restype = i32
@@ -205,10 +212,11 @@ def load_library(path: str = LIB_PATH):
     lib.precog_retrieve_noalloc.argtypes = [vp, i32, i64, i32, vp, i32, vp, vp, vp]
     lib.precog_launch_count.restype = ctypes.c_uint64
     lib.precog_launch_count.argtypes = []
-    for name, cls in (("precog_causal_conv", ConvArgs), ("precog_conv_step", ConvArgs),
+    for name, cls in (("precog_causal_conv", ConvArgs), ("precog_conv_step", ConvArgs), ("precog_scan_step", ScanStepArgs),
                       ("precog_block_norm", BlockNormArgs), ("precog_adjust_logits", AdjustArgs)):
         call = lib[name]        # the same function, with its arguments' struct as packed bytes
-        call.restype, call.argtypes = i32, [ctypes.c_char_p] + getattr(lib, name).argtypes[1:]
+        call.restype = i32
+        call.argtypes = [ctypes.c_char_p if t is ctypes.POINTER(cls) else t for t in getattr(lib, name).argtypes]
         _packed_calls[name] = (call, _packer(cls).pack)
     _lib = lib
     return lib
@@ -303,7 +311,7 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     N = B.shape[-1]
     if dt.shape != x.shape or B.shape != (L, T, N) or (C is not None and C.shape != B.shape):
         raise ValueError("x/dt/B/C shapes disagree")
-    torch = _torch()
+    torch = _torch_module or _torch()
     if a_kind == PRECOG_A_COMPLEX:
         if A.shape != (L, D, N) or A.dtype != torch.complex64:
             raise ValueError("complex A must be complex64 [L, D, N]")
@@ -767,12 +775,14 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
         if one != 1 and D > 1:
             raise ValueError("the rows of gate must be contiguous")
         gp = gate.data_ptr()
-    _check(load_library().precog_scan_step(
-        ctypes.byref(inputs), n,
-        _dense(states, (n_slots, layers, D, N), torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
-               device, "states"), n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
-        _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
-        _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), _stream(stream)))
+    load_library()
+    call, pack = _packed_calls["precog_scan_step"]
+    _check(call(
+        ctypes.byref(inputs),
+        pack(_dense(states, (n_slots, layers, D, N), torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
+                    device, "states"), n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
+             _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
+             _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), 0), n, _stream(stream)))
 
 
 def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_first: bool = True, weight=None,

@@ -930,10 +930,14 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
     return ok();
 }
 
-precog_status precog_scan_step(const precog_scan_inputs *in, int64_t n, void *states, int64_t n_slots,
-                               const int64_t *d_slots, int32_t layer0, int32_t L_total, const float *skip,
-                               const void *gate, int64_t gate_stride, int64_t gate_layer_stride, void *y_out,
-                               int32_t y_dtype, void *stream) {
+precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_step_args *a, int64_t n, void *stream) {
+    if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
+    if (a->reserved != 0) return fail(PRECOG_ERR_INVALID_ARG, "reserved must be 0");
+    void *const states = a->states, *const y_out = a->y_out;
+    const int64_t n_slots = a->n_slots, *const d_slots = a->d_slots, gate_stride = a->gate_stride, gate_layer_stride = a->gate_layer_stride;
+    const int32_t layer0 = a->layer0, L_total = a->L_total, y_dtype = a->y_dtype;
+    const float *const skip = a->skip;
+    const void *const gate = a->gate;
     if (n < 0) return fail(PRECOG_ERR_INVALID_ARG, "n must be >= 0");
     if (n > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
     precog_status s = check_scan_inputs(in, n, true);

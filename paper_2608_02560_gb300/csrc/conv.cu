@@ -61,24 +61,41 @@ struct Taps {
     }
 };
 
+// The sequence with base(c) <= item < base(c + 1), by all lanes of a warp: 32 places are looked at together where they
+// have one item (two loads one behind the other for 1000 sequences, not ten). Within [0, n_seqs) whatever the offsets.
+__device__ __forceinline__ int sequence_of(const ConvParams &p, int64_t item, int segment) {
+    int lo = 0, hi = static_cast<int>(p.n_seqs);
+    auto begins = [&](int c) { return p.offsets[c] / segment + c <= item; };
+    if (__all_sync(0xffffffffu, item == __shfl_sync(0xffffffffu, item, 0))) {
+        const int lane = threadIdx.x % 32;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32, mid = lo + step * (lane + 1);
+            lo += step * __popc(__ballot_sync(0xffffffffu, mid < hi && begins(mid)));
+            hi = min(hi, lo + step);
+        }
+        return lo;
+    }
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (begins(mid)) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
 template <typename T, int K>
 __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, int segment, int64_t items) {
     grid_dependency_wait();
     const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t item = at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups);
-    if (item >= items) return;
     const int d = static_cast<int>(at - item * groups) * 8;
     if (item < p.n_seqs && d == 0) {   // every sequence is looked at, whichever way the search goes
         const int64_t a = p.offsets[item], b = p.offsets[item + 1];
         if (a < 0 || b < a || b > p.T_tot) atomicOr(&g_conv_status, PRECOG_DEV_BAD_OFFSETS);
     }
-    int lo = 0, hi = static_cast<int>(p.n_seqs);   // base(lo) <= item < base(hi)
-    while (hi - lo > 1) {
-        const int mid = lo + (hi - lo) / 2;
-        if (p.offsets[mid] / segment + mid <= item) lo = mid;
-        else hi = mid;
-    }
+    const int lo = sequence_of(p, item, segment);
+    if (item >= items) return;
     const int64_t c = lo, a = p.offsets[c], b = p.offsets[c + 1];
     if (a < 0 || b < a || b > p.T_tot) return;
     const int64_t part = item - (a / segment + c);
@@ -231,8 +248,12 @@ cudaError_t launch_k(const ConvParams &p, bool step, cudaStream_t stream) {
         if (p.n_seqs * groups >= 2 * fill) e = go(conv_step_kernel<T, K, 2>, (p.n_seqs + 1) / 2 * groups);
         else e = go(conv_step_kernel<T, K, 1>, p.n_seqs * groups);
     } else {
-        int segment = 4;
-        while (segment < 128 && p.T_tot / (2 * segment) * groups >= fill / 3) segment *= 2;
+        // As long as the segments fit the GPU at once, with half of one left over a sequence; at most 64 tokens, from
+        // where on what a segment's start costs no longer counts (us for 557,000 tokens of 256 sequences, 2048 channels,
+        // segments of 16, 32, 64, 128: 933, 727, 672, 674).
+        const int64_t at_once = fill / groups - p.n_seqs / 2;
+        const int64_t tokens = at_once > 0 ? (p.T_tot + at_once - 1) / at_once : 64;
+        const int segment = tokens >= 64 ? 64 : tokens < 4 ? 4 : static_cast<int>((tokens + 3) / 4 * 4);
         const int64_t items = (p.T_tot + segment - 1) / segment + p.n_seqs;
         e = go(conv_kernel<T, K>, items * groups, segment, items);
     }

@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(kThreads) scan_step_complex_kernel(const ScanS
 template <typename Kernel>
 cudaError_t launch_kernel(Kernel kernel, const ScanStepParams &p, int channels, int warps, cudaStream_t stream) {
     const int64_t channel_warps = (p.D + channels - 1) / channels, columns = channel_warps * p.n_layers;
-    int64_t row_blocks = (static_cast<int64_t>(device_sm_count()) * warps + columns - 1) / columns;
-    if (row_blocks > p.n) row_blocks = p.n;
+    int64_t row_blocks = static_cast<int64_t>(device_sm_count()) * warps / columns;
+    row_blocks = row_blocks < 1 ? 1 : row_blocks > p.n ? p.n : row_blocks;
     const int64_t blocks = (columns * row_blocks * 32 + kThreads - 1) / kThreads;
     if (columns > 0x7fffffffLL || blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     return launch_dependent(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, p,
@@ -254,7 +254,7 @@ cudaError_t launch_scan_step(const ScanStepParams &p, cudaStream_t stream) {
     cudaError_t e;
     if (p.complex) e = f32 ? launch_kernel(scan_step_complex_kernel<float>, p, 8, 128, stream)
                            : launch_kernel(scan_step_complex_kernel<__nv_bfloat16>, p, 8, 128, stream);
-    else e = f32 ? launch_kernel(scan_step_kernel<float>, p, 32, 32, stream) : launch_kernel(scan_step_kernel<__nv_bfloat16>, p, 32, 32, stream);
+    else e = f32 ? launch_kernel(scan_step_kernel<float>, p, 32, 12, stream) : launch_kernel(scan_step_kernel<__nv_bfloat16>, p, 32, 12, stream);
     if (e == cudaSuccess) count_launches(1);
     return e;
 }

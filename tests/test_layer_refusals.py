@@ -78,15 +78,16 @@ def test_conv_step_rejects_bad_arguments(lib, kw, expect):
 
 
 def _scan_step(lib, n=3, states=T1, n_slots=3, slots=None, layer0=0, L=2, skip=None, gate=None, gs=64, gls=192, y=Y, ydt=0,
-               **change):
+               reserved=0, **change):
     import paper_2608_02560_gb300 as pg
     s = _set(pg.ScanInputs(2, 64, 16, pg.PRECOG_BF16, pg.PRECOG_A_GENERAL, 0, X, X + 0x10000, X + 0x20000, X + 0x30000,
                            X + 0x40000, 192, 48), change)
-    return lib.precog_scan_step(ctypes.byref(s), n, states, n_slots, slots, layer0, L, skip, gate, gs, gls, y, ydt, None)
+    a = pg.ScanStepArgs(states, n_slots, slots, layer0, L, skip, gate, gs, gls, y, ydt, reserved)
+    return lib.precog_scan_step(ctypes.byref(s), ctypes.byref(a), n, None)
 
 
 @pytest.mark.parametrize("kw,expect", [
-    (dict(N=8), 2), (dict(D=12), 2), (dict(in_dtype=2), 2), (dict(a_kind=3), 1), (dict(x=0), 1), (dict(C=0), 1), (dict(A=0), 1),
+    (dict(reserved=1), 1), (dict(N=8), 2), (dict(D=12), 2), (dict(in_dtype=2), 2), (dict(a_kind=3), 1), (dict(x=0), 1), (dict(C=0), 1), (dict(A=0), 1),
     (dict(layer_stride_xd=128), 1), (dict(n=-1), 1), (dict(n=1 << 31), 2), (dict(states=None), 1), (dict(states=T1 + 8), 1),
     (dict(n_slots=2), 1), (dict(n_slots=-1, slots=W), 1), (dict(layer0=1), 1), (dict(layer0=-1), 1), (dict(L=1), 1),
     (dict(y=None), 1), (dict(y=Y + 8), 1), (dict(ydt=2), 1), (dict(skip=W + 4), 1), (dict(gate=W + 8), 1), (dict(gate=W, gs=56), 1),
@@ -97,7 +98,9 @@ def test_scan_step_rejects_bad_arguments(lib, kw, expect):
     before = lib.precog_launch_count()
     assert _scan_step(lib, **kw) == expect
     assert lib.precog_launch_count() == before
-    assert lib.precog_scan_step(None, 1, T1, 1, None, 0, 1, None, None, 0, 0, Y, 0, None) == 1
+    import paper_2608_02560_gb300 as pg
+    assert lib.precog_scan_step(None, ctypes.byref(pg.ScanStepArgs(T1, 1, None, 0, 1, None, None, 0, 0, Y, 0, 0)), 1, None) == 1
+    assert lib.precog_scan_step(ctypes.byref(pg.ScanInputs()), None, 1, None) == 1
 
 
 def _norm_args(**kw):
@@ -220,6 +223,6 @@ def test_the_binding_checks_shapes_dtypes_and_devices(lib, monkeypatch):
 def test_packed_arguments_are_the_structures_bytes(lib):
     """The binding packs its arguments instead of filling a Structure: the same bytes, field by field."""
     import paper_2608_02560_gb300 as pg
-    for cls in (pg.ConvArgs, pg.BlockNormArgs, pg.AdjustArgs):
+    for cls in (pg.ConvArgs, pg.ScanStepArgs, pg.BlockNormArgs, pg.AdjustArgs):
         values = [1.5 if kind is ctypes.c_float else i + 3 for i, (_, kind) in enumerate(cls._fields_)]
         assert bytes(cls(*values)) == pg._packer(cls).pack(*values)
