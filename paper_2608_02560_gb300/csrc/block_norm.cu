@@ -4,8 +4,8 @@
 //   a <- a silu(gate) [after the norm] ;  without a residual: out = a
 //   h = residual + scale a ;  residual_out = h ;  out = h rsqrt(mean h^2 + eps) out_weight
 //
-// A row (or, where groups are normed, a group of one) belongs to WARPS warps whose lanes hold eight
-// neighbouring entries CH times; what is read is read once and stays in registers as fp32 until it is
+// A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold eight neighbouring
+// entries CH times each; what is read is read once and stays in registers as fp32 until it is
 // written. Sums are fp32, in an order that depends on the row's length alone.
 #include "../../include/precog.h"
 #include "internal.h"
@@ -15,17 +15,17 @@
 namespace precog {
 namespace {
 
-// Sum over the row's warps; `slot` says which of the two sums (each has its own shared words).
-template <int WARPS>
-__device__ __forceinline__ float row_sum(float v, float (*part)[WARPS < 2 ? 1 : WARPS], int in_row) {
+// Sum over the row's lanes (each use has its own shared words).
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, float *part, int in_row) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (WARPS > 1) {
-        if ((threadIdx.x & 31) == 0) (*part)[in_row / 32] = v;
+    for (int o = (LANES < 32 ? LANES : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (LANES > 32) {
+        if ((threadIdx.x & 31) == 0) part[in_row / 32] = v;
         __syncthreads();
         v = 0.f;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) v += (*part)[i];
+        for (int i = 0; i < LANES / 32; ++i) v += part[i];
     }
     return v;
 }
@@ -40,22 +40,22 @@ __device__ __forceinline__ void weights8(const float *w, int e, float (&v)[8]) {
     unpack8(load8(w + e), v);
 }
 
-template <typename T, typename TR, int WARPS, int CH>
-__global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kernel(const BlockNormParams p, int64_t rows) {
+template <typename T, typename TR, int LANES, int CH>
+__global__ void __launch_bounds__(LANES > 128 ? LANES : 128) block_norm_kernel(const BlockNormParams p, int64_t rows) {
     grid_dependency_wait();
-    constexpr int kLanes = 32 * WARPS, kBlock = WARPS > 4 ? kLanes : 128, kRows = kBlock / kLanes;
-    __shared__ float part[2][kRows][WARPS < 2 ? 1 : WARPS];
-    const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    constexpr int kBlock = LANES > 128 ? LANES : 128, kRows = kBlock / LANES;
+    __shared__ float part[2][kRows][LANES > 32 ? LANES / 32 : 1];
+    const int mine = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + mine;
     const bool live = row < rows;   // (all rows of a CTA meet at its barriers)
-    const int64_t t = live ? (p.groups == 1 ? row : row / p.groups) : 0;
+    const int64_t t = live ? (p.groups == 1 ? row : static_cast<unsigned>(row) / static_cast<unsigned>(p.groups)) : 0;   // (rows < 2^31)
     const int size = p.groups == 1 ? p.dim : p.dim / p.groups, first = live ? static_cast<int>(row - t * p.groups) * size : 0;
     // every load of the row before the first is used
     Raw8<T> x[CH], u[CH], g[CH];
     Raw8<TR> res[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * kLanes + lane) * 8;
+        const int e = (c * LANES + lane) * 8;
         if (!live || e >= size) continue;
         x[c] = load8(static_cast<const T *>(p.x) + t * p.x_stride + first + e);
         if (p.skip) u[c] = load8(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e);
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * kLanes + lane) * 8;
+        const int e = (c * LANES + lane) * 8;
         if (!live || e >= size) continue;
         unpack8(x[c], v[c]);
         if (p.skip) {
@@ -86,11 +86,11 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
         for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
     }
     float scale = 1.f;
-    if (p.norm == PRECOG_NORM_RMS) scale = rsqrtf(row_sum<WARPS>(sum, &part[0][mine], lane) / static_cast<float>(size) + p.eps);
+    if (p.norm == PRECOG_NORM_RMS) scale = rsqrtf(row_sum<LANES>(sum, part[0][mine], lane) / static_cast<float>(size) + p.eps);
     sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * kLanes + lane) * 8;
+        const int e = (c * LANES + lane) * 8;
         if (!live || e >= size) continue;
         if (p.norm == PRECOG_NORM_RMS) {
             weights8(p.weight, first + e, w);
@@ -117,10 +117,10 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
         }
     }
     if (p.out == nullptr) return;   // (for all threads or none)
-    scale = p.residual ? rsqrtf(row_sum<WARPS>(sum, &part[1][mine], lane) / static_cast<float>(size) + p.eps) : 1.f;
+    scale = p.residual ? rsqrtf(row_sum<LANES>(sum, part[1][mine], lane) / static_cast<float>(size) + p.eps) : 1.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * kLanes + lane) * 8;
+        const int e = (c * LANES + lane) * 8;
         if (!live || e >= size) continue;
         if (p.residual) {
             weights8(p.out_weight, first + e, w);
@@ -132,12 +132,12 @@ __global__ void __launch_bounds__(WARPS > 4 ? 32 * WARPS : 128) block_norm_kerne
     }
 }
 
-template <typename T, typename TR, int WARPS, int CH>
+template <typename T, typename TR, int LANES, int CH>
 cudaError_t launch_shape(const BlockNormParams &p, cudaStream_t stream) {
-    constexpr int kBlock = WARPS > 4 ? 32 * WARPS : 128, kRows = kBlock / (32 * WARPS);
+    constexpr int kBlock = LANES > 128 ? LANES : 128, kRows = kBlock / LANES;
     const int64_t rows = p.T * p.groups, blocks = (rows + kRows - 1) / kRows;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = launch_dependent(block_norm_kernel<T, TR, WARPS, CH>, dim3(static_cast<unsigned>(blocks)), dim3(kBlock), 0, stream, p, rows);
+    const cudaError_t e = launch_dependent(block_norm_kernel<T, TR, LANES, CH>, dim3(static_cast<unsigned>(blocks)), dim3(kBlock), 0, stream, p, rows);
     if (e == cudaSuccess) count_launches(1);
     return e;
 }
@@ -145,13 +145,16 @@ cudaError_t launch_shape(const BlockNormParams &p, cudaStream_t stream) {
 template <typename T, typename TR>
 cudaError_t launch_typed(const BlockNormParams &p, cudaStream_t stream) {
     const int size = p.dim / p.groups;
-    if (size <= 256) return launch_shape<T, TR, 1, 1>(p, stream);
-    if (size <= 512) return launch_shape<T, TR, 1, 2>(p, stream);
-    if (size <= 1024) return launch_shape<T, TR, 2, 2>(p, stream);
-    if (size <= 2048) return launch_shape<T, TR, 4, 2>(p, stream);
-    if (size <= 4096) return launch_shape<T, TR, 8, 2>(p, stream);
-    if (size <= 8192) return launch_shape<T, TR, 16, 2>(p, stream);
-    return launch_shape<T, TR, 16, 4>(p, stream);
+    if (size <= 32) return launch_shape<T, TR, 4, 1>(p, stream);
+    if (size <= 64) return launch_shape<T, TR, 8, 1>(p, stream);
+    if (size <= 128) return launch_shape<T, TR, 16, 1>(p, stream);
+    if (size <= 256) return launch_shape<T, TR, 32, 1>(p, stream);
+    if (size <= 512) return launch_shape<T, TR, 32, 2>(p, stream);
+    if (size <= 1024) return launch_shape<T, TR, 64, 2>(p, stream);
+    if (size <= 2048) return launch_shape<T, TR, 128, 2>(p, stream);
+    if (size <= 4096) return launch_shape<T, TR, 256, 2>(p, stream);
+    if (size <= 8192) return launch_shape<T, TR, 512, 2>(p, stream);
+    return launch_shape<T, TR, 512, 4>(p, stream);
 }
 
 }  // namespace

@@ -185,53 +185,62 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
     }
 }
 
-// R rows a thread, with the taps of one.
-template <typename T, int K, int R>
-__global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p) {
+// One token of each row: a thread has eight channels of the rows first, first + stride, ..., whose taps it keeps. Two
+// rows are on their way while one is worked on, their slots a round before.
+template <typename T, int K>
+struct StepRow {
+    T *window;   // nullptr: idle
+    Raw8<T> in[K];
+};
+template <typename T, int K, int AHEAD>
+__global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p, int stride) {
     grid_dependency_wait();
     const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t first = R * (at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups));
-    if (first >= p.n_seqs) return;
-    const int d = static_cast<int>(at - first / R * groups) * 8;
-    int64_t slot[R];
+    const int64_t first = at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups);
+    if (first >= stride) return;
+    const int d = static_cast<int>(at - first * groups) * 8;
+    auto slot_of = [&](int64_t row) -> int64_t { return row >= p.n_seqs ? -1 : p.idx ? p.idx[row] : row; };
+    auto load = [&](StepRow<T, K> &r, int64_t row, int64_t slot) {
+        r.window = nullptr;
+        if (slot < 0 || slot >= p.bank_entries) {
+            if (slot != -1 && d == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_INDEX);
+            return;
+        }
+        r.window = static_cast<T *>(p.windows) + ((slot * p.L_total + p.layer) * (K - 1)) * p.dim + d;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        slot[r] = first + r;
-        if (p.idx && first + r < p.n_seqs) slot[r] = p.idx[first + r];
-    }
-    T *window[R];
-    Raw8<T> raw[R][K];
+        for (int j = 0; j < K - 1; ++j) r.in[j] = load8(r.window + static_cast<int64_t>(j) * p.dim);
+        r.in[K - 1] = load8(static_cast<const T *>(p.x) + row * p.x_stride + d);
+    };
+    StepRow<T, K> rows[AHEAD];
+    int64_t slot[AHEAD];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const bool live = first + r < p.n_seqs, there = slot[r] >= 0 && slot[r] < p.bank_entries;
-        if (live && !there && slot[r] != -1 && d == 0) atomicOr(&g_conv_status, PRECOG_DEV_BAD_INDEX);
-        window[r] = live && there ? static_cast<T *>(p.windows) + ((slot[r] * p.L_total + p.layer) * (K - 1)) * p.dim + d : nullptr;
-    }
+    for (int r = 0; r < AHEAD; ++r) slot[r] = slot_of(first + static_cast<int64_t>(r) * stride);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (window[r] == nullptr) continue;
+    for (int r = 0; r < AHEAD; ++r) load(rows[r], first + static_cast<int64_t>(r) * stride, slot[r]);
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) raw[r][j] = load8(window[r] + static_cast<int64_t>(j) * p.dim);
-        raw[r][K - 1] = load8(static_cast<const T *>(p.x) + (first + r) * p.x_stride + d);
-    }
+    for (int r = 0; r < AHEAD; ++r) slot[r] = slot_of(first + static_cast<int64_t>(AHEAD + r) * stride);
     Taps<T, K> taps;
     taps.load(p, d);
+    for (int64_t row0 = first; row0 < p.n_seqs; row0 += static_cast<int64_t>(AHEAD) * stride) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (first + r >= p.n_seqs) continue;
-        T *y = static_cast<T *>(p.y) + (first + r) * p.y_stride + d;
-        if (window[r] == nullptr) {
-            store8(y, Raw8<T>{});
-            continue;
+        for (int r = 0; r < AHEAD; ++r) {
+            const int64_t row = row0 + static_cast<int64_t>(r) * stride;
+            if (row >= p.n_seqs) break;
+            Raw8<T> y = {};
+            if (rows[r].window != nullptr) {
+                f2 in[K][4];
+                const f2(*of[K])[4];
+#pragma unroll
+                for (int j = 0; j < K; ++j) unpack8(rows[r].in[j], in[j]), of[j] = &in[j];
+                y = taps.out(of, p.silu != 0);
+#pragma unroll
+                for (int j = 0; j < K - 1; ++j) store8(rows[r].window + static_cast<int64_t>(j) * p.dim, rows[r].in[j + 1]);
+            }
+            store8(static_cast<T *>(p.y) + row * p.y_stride + d, y);
+            load(rows[r], row + static_cast<int64_t>(AHEAD) * stride, slot[r]);
+            slot[r] = slot_of(row + static_cast<int64_t>(2 * AHEAD) * stride);
         }
-        f2 in[K][4];
-        const f2(*of[K])[4];
-#pragma unroll
-        for (int j = 0; j < K; ++j) unpack8(raw[r][j], in[j]), of[j] = &in[j];
-        store8(y, taps.out(of, p.silu != 0));
-#pragma unroll
-        for (int j = 0; j < K - 1; ++j) store8(window[r] + static_cast<int64_t>(j) * p.dim, raw[r][j + 1]);
     }
 }
 
@@ -245,8 +254,10 @@ cudaError_t launch_k(const ConvParams &p, bool step, cudaStream_t stream) {
         return launch_dependent(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, p, more...);
     };
     if (step) {
-        if (p.n_seqs * groups >= 2 * fill) e = go(conv_step_kernel<T, K, 2>, (p.n_seqs + 1) / 2 * groups);
-        else e = go(conv_step_kernel<T, K, 1>, p.n_seqs * groups);
+        // A row a thread where that fits the GPU at once; otherwise as many threads as do.
+        const int64_t at_once = fill / groups < 1 ? 1 : fill / groups;
+        if (p.n_seqs <= at_once) e = go(conv_step_kernel<T, K, 1>, p.n_seqs * groups, static_cast<int>(p.n_seqs));
+        else e = go(conv_step_kernel<T, K, 2>, at_once * groups, static_cast<int>(at_once));
     } else {
         // As long as the segments fit the GPU at once, with half of one left over a sequence; at most 64 tokens, from
         // where on what a segment's start costs no longer counts (us for 557,000 tokens of 256 sequences, 2048 channels,
