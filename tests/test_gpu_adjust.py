@@ -203,6 +203,19 @@ def test_a_batch_of_many_logits(cuda_device, dtype, V, pad):
     assert torch.equal(again["x"], out)
 
 
+@pytest.mark.parametrize("dtype,pad", [("bfloat16", 0), ("bfloat16", 3), ("float32", 2), ("float16", 8)])
+def test_masks_alone_on_many_logits(cuda_device, dtype, pad):
+    import paper_2608_02560_gb300 as pg
+    c = _case(cuda_device, 45, 131_075, dtype, 2, longest=0, rep=False, freq=False, pres=False, bias=0, counts=False, pad=pad)
+    out = _run(cuda_device, c)
+    assert pg.precog_device_status()[0] == 0
+    want = to_np(c["x"]).copy()
+    for r, m in enumerate(c["rows"]):
+        if m >= 0:
+            want[r, ~c["bits"][m]] = -np.inf
+    assert np.array_equal(to_np(out), want)
+
+
 def test_calls_of_one_input_repeat_bit_for_bit(cuda_device):
     import torch
     c = _case(cuda_device, 40, 9001, "bfloat16", 8, longest=3000)

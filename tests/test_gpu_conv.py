@@ -144,9 +144,34 @@ def test_a_cut_sequence_and_single_tokens_give_the_same_bits(cuda_device, dtype,
     assert torch.equal(y, whole) and torch.equal(win, last)
 
 
+@pytest.mark.parametrize("dtype,K", [("bfloat16", 4), ("float32", 4), ("bfloat16", 3), ("float32", 2)])
+def test_long_segments_give_the_bits_of_short_calls(cuda_device, dtype, K):
+    """Enough tokens for the longest segments, against calls of 500 tokens that hand the window on."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    d, dt, D, lens = cuda_device, getattr(torch, dtype), 1032, [39_001, 0, 63, 64, 65, 2500]
+    rn = _rn(d, 12)
+    T = sum(lens)
+    x, w, b = rn(T, D).to(dt), rn(D, K), rn(D)
+    first = rn(len(lens), 1, K - 1, D).to(dt)
+    y, behind = torch.empty_like(x), torch.empty_like(first)
+    pg.precog_causal_conv(x, w, _offsets(lens, d), bias=b, bank=first, windows_out=behind, y_out=y)
+    at, got = 0, torch.empty_like(x)
+    for c, n in enumerate(lens):
+        win = first[c:c + 1].clone()
+        for t in range(at, at + n, 500):
+            m, out = min(500, at + n - t), torch.empty_like(win)
+            pg.precog_causal_conv(x[t:t + m], w, _offsets([m], d), bias=b, bank=win, windows_out=out, y_out=got[t:t + m])
+            win = out
+        assert torch.equal(win[0], behind[c])
+        at += n
+    assert torch.equal(got, y) and pg.precog_device_status()[0] == 0
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("n,dim,K,silu", [(1, 8, 4, True), (1, 2048, 4, True), (5, 264, 3, False), (67, 1032, 4, True),
-                                          (300, 136, 2, True), (256, 4104, 4, True)])
+                                          (300, 136, 2, True), (256, 4104, 4, True), (300, 2056, 3, True),
+                                          (200, 6152, 2, False)])
 def test_steps_match_the_definition(cuda_device, dtype, n, dim, K, silu):
     import torch
     import paper_2608_02560_gb300 as pg
