@@ -307,9 +307,11 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
         C = None if C is None else C.unsqueeze(0)
     if A.dim() == 2:
         A = A.unsqueeze(0)
-    L, T, D = x.shape
-    N = B.shape[-1]
-    if dt.shape != x.shape or B.shape != (L, T, N) or (C is not None and C.shape != B.shape):
+    shape = x.shape
+    L, T, D = shape
+    rows = B.shape
+    N = rows[-1]
+    if dt.shape != shape or rows != (L, T, N) or (C is not None and C.shape != rows):
         raise ValueError("x/dt/B/C shapes disagree")
     torch = _torch_module or _torch()
     if a_kind == PRECOG_A_COMPLEX:
