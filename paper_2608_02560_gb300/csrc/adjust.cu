@@ -10,8 +10,15 @@
 // of its last bias; integer atomics, so their order does not matter), and then the table's tokens are adjusted and put
 // over the copy. In place that is the same: the copy leaves an allowed logit as it was, and a banned one needs none.
 // Few logits: one launch; a CTA has 2048 tokens of a row and a word for each. Many: a copy, and a launch behind it whose
-// CTAs count whole rows (while the copy's last CTAs run) in a hash table, instead of every slice's going through the
-// row's history. Where that table is too small, its tokens are taken 8192 at a time, with a word for each.
+// CTAs count whole rows in a hash table, instead of every slice's going through the row's history. Where that table is
+// too small, its tokens are taken 8192 at a time, with a word for each.
+//
+// Memory bounds the copy, latency the rest. 256 rows of 128,001 bf16 logits, up to 4096 tokens of history, 16 biases,
+// masks that allow a tenth (136 MB, 20.0 us at the measured copy rate): 36.7 us; the copy alone 24.4, without masks
+// 22.1. Before: a CTA a slice with a word a token, 240 us (logits one by one), 66 (16 bytes, eight at once looked up
+// where one had a word), 55 (with the listed ones apart, whether in the same warps or in others: every slice pays for
+// the way from offsets through history and table to scattered logits). A copy by resident CTAs, to make room for the
+// second launch's beside it, took 47; with the shared memory for both set aside it loses the L1 that it cuts from.
 #include <cstddef>
 #include <type_traits>
 
@@ -210,14 +217,14 @@ __device__ __forceinline__ void adjust_range(const AdjustParams &p, Tables<SLOTS
                 const int64_t tok = token[0];
 #pragma unroll
                 for (int i = 0; i + 1 < kAtOnce; ++i) token[i] = token[i + 1];
-                const uint64_t i = static_cast<uint64_t>(tok - begin);
+                const uint64_t i = static_cast<uint64_t>(tok) - static_cast<uint64_t>(begin);
                 if (i < static_cast<unsigned>(size)) touch(static_cast<unsigned>(i), j0 + k * THREADS < row.from ? kSeen : 1u, 0u);
                 else check(tok);
             }
         }
         for (int64_t j = threadIdx.x; j < row.n; j += THREADS) {
             const int64_t tok = p.bias_idx[row.first + j];
-            const uint64_t i = static_cast<uint64_t>(tok - begin);
+            const uint64_t i = static_cast<uint64_t>(tok) - static_cast<uint64_t>(begin);
             if (i < static_cast<unsigned>(size)) touch(static_cast<unsigned>(i), kBiased, static_cast<uint32_t>(j) + 1u);
             else check(tok);
         }
@@ -268,7 +275,7 @@ __device__ __forceinline__ void adjust_range(const AdjustParams &p, Tables<SLOTS
 }
 
 // A copy with the mask, a CTA `slice` tokens of a row. Of a pair of launches it lets the other in early, whose CTAs read
-// no logits and write nothing before the copy has ended.
+// no logits and write nothing before the copy has ended (what they do read was there before the copy began).
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 3) copy_kernel(const AdjustParams p, int slice, unsigned slices, bool pair) {
     grid_dependency_wait();
@@ -315,6 +322,9 @@ template <typename T>
 cudaError_t launch_typed(const AdjustParams &p, cudaStream_t stream) {
     const int64_t tokens = p.rows * p.vocab, sms = device_sm_count();
     const auto slices_of = [&](int slice) { return static_cast<unsigned>((p.vocab + slice - 1) / slice); };
+    // One launch or two: 4 rows of 128,001 logits 6.6 against 9.2 us, 16 of 32,000 7.1 against 9.8; 64 of 32,000 16.4
+    // against 12.7, 16 of 128,001 14.1 against 10.3, 64 of 128,001 51.7 against 19.4. (Slices of 8192 and 32,768: 39.5 and
+    // 37.0 us for the 256 rows above; parts of 65,536: 43.6, rows being few enough to fit the GPU whole.)
     const bool many = tokens >= sms * 8192, biases = p.bias != nullptr;
     if (!p.history && !biases) {
         const int slice = many ? 16384 : 2048;

@@ -4,9 +4,17 @@
 //   a <- a silu(gate) [after the norm] ;  without a residual: out = a
 //   h = residual + scale a ;  residual_out = h ;  out = h rsqrt(mean h^2 + eps) out_weight
 //
-// A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold eight neighbouring
-// entries CH times each; what is read is read once and stays in registers as fp32 until it is
+// A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold eight neighbouring entries CH
+// times each; what is read is read once, all of it before the first is used, and stays in registers as fp32 until it is
 // written. Sums are fp32, in an order that depends on the row's length alone.
+//
+// Memory bounds it: 65,521 rows of 2048, norm, scaled fp32 residual, next norm (1.61 GB, 237 us at the measured copy
+// rate): 235.5 us; rows of 4096 with skip and gate (2.15 GB, 316 us): 338. Two eights a lane are best at every length (rows
+// of 2048, us: 128 lanes 237, 256 lanes with one eight 280, 64 with four 281; of 4096, gated: 256 lanes 340, 128 with four
+// 386, 512 with one 392): more bytes a thread in flight, fewer warps at a barrier. Beyond 4096 a row's barriers leave
+// the CTA waiting (8192: 1.2 to 1.4 of the copy's time in bf16, 1.6 in fp32). Two rows a CTA for one load of the weights
+// took more registers than that saves (278 and 412 us); rows in turn with the next one's copies in shared memory took the
+// L1 that the weights live in (1.4 to 2 times as long).
 #include "../../include/precog.h"
 #include "internal.h"
 #include "ptx.cuh"

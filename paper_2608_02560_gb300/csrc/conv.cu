@@ -7,6 +7,11 @@
 // over a segment of tokens with the last K - 1 inputs in registers, so a row is read once and, at the start
 // of a segment, K - 1 rows again. Copies run eight tokens ahead of the arithmetic.
 //
+// Memory bounds it where there is enough: 557,000 tokens of 256 sequences, 2048 bf16 channels, K = 4 with SiLU (4.57 GB,
+// 673 us at the measured copy rate): 670 us. (1999 us with one token at a time, 798 with four ahead in registers, which
+// left room for 16 warps an SM and 32 KB on the way; eight ahead in shared memory are 64 KB.) 96 sequences of up to 200
+// tokens (13.2 us): 20.0 us, one round of CTAs with 4 warps a scheduler. 64 tokens: 3.3 us.
+//
 // Segments of S tokens of ragged sequences need no prefix sums: item i belongs to the sequence c with
 // base(c) <= i < base(c + 1), base(c) = offsets[c] / S + c, because base(c + 1) - base(c) is at least
 // ceil(len / S) and at least 1. Items without tokens end at once.
@@ -186,7 +191,9 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
 }
 
 // One token of each row: a thread has eight channels of the rows first, first + stride, ..., whose taps it keeps. Two
-// rows are on their way while one is worked on, their slots a round before.
+// rows are on their way while one is worked on, their slots a round before. 256 rows of 8448 bf16 channels, K = 4 (34.8
+// MB, 5.1 us at the measured copy rate): 8.6 us (39 with a row a thread, whose taps are as many bytes as the row's own;
+// 9.5 with two rows a thread in 1.7 rounds of CTAs).
 template <typename T, int K>
 struct StepRow {
     T *window;   // nullptr: idle
