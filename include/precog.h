@@ -741,7 +741,8 @@ precog_status precog_block_norm(const precog_block_norm_args *args, int64_t T, v
  *                 outside [0, n_masks) likewise, and flag PRECOG_DEV_BAD_INDEX); NULL: mask r
  * Tokens of -1 in a list are ignored (padding); others outside [0, vocab) are ignored and flag
  * PRECOG_DEV_BAD_INDEX. A list whose offsets decrease or leave [0, n_history] or [0, n_bias] is
- * empty and flags PRECOG_DEV_BAD_OFFSETS. Lists are shorter than 2^30 in all.
+ * empty and flags PRECOG_DEV_BAD_OFFSETS. Lists are shorter than 2^30 in all; they and the vectors
+ * [n_rows] may have any alignment of their entries.
  */
 typedef struct precog_adjust_args {
     int32_t dtype;             /* precog_dtype */

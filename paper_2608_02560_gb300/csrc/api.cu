@@ -2,6 +2,7 @@
 // kernels, status codes. Nothing here allocates device memory.
 #include <atomic>
 #include <cstdarg>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <utility>
@@ -147,6 +148,13 @@ precog::DeltaParams delta_params(const precog_delta_inputs *in) {
     p.in_dtype = in->in_dtype;
     p.scale = in->scale;
     return p;
+}
+
+// Whether lists of 4- or 8-byte entries are aligned to them.
+bool aligned_to(unsigned bytes, std::initializer_list<const void *> lists) {
+    for (const void *p : lists)
+        if (reinterpret_cast<uintptr_t>(p) % bytes != 0) return false;
+    return true;
 }
 
 // Rows of `row` bytes, `stride` bytes apart.
@@ -864,7 +872,8 @@ precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_
     if (T_tot > 0x7fffffffLL || n_seqs > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "T_tot and n_seqs must be below 2^31");
     precog_status s = check_conv(args, T_tot, layer, L_total, &p);
     if (s != PRECOG_OK) return s;
-    if (d_offsets == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "d_offsets is NULL");
+    if (d_offsets == nullptr || !aligned_to(8, {d_offsets, d_idx}))
+        return fail(PRECOG_ERR_INVALID_ARG, "d_offsets must be non-NULL, d_offsets and d_idx 8-byte aligned");
     if (bank) {
         if (!aligned16(bank)) return fail(PRECOG_ERR_INVALID_ARG, "bank not 16-byte aligned");
         if (bank_entries < 0) return fail(PRECOG_ERR_INVALID_ARG, "bank_entries must be >= 0");
@@ -909,6 +918,7 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
     if (windows == nullptr || !aligned16(windows))
         return fail(PRECOG_ERR_INVALID_ARG, "windows must be non-NULL and 16-byte aligned");
     if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (!aligned_to(8, {d_slots})) return fail(PRECOG_ERR_INVALID_ARG, "d_slots not 8-byte aligned");
     if (d_slots == nullptr && n_slots < n)
         return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
     const int64_t sz = dtype_size(p.dtype), row = p.dim * sz;
@@ -947,6 +957,7 @@ precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_s
     if (layer0 < 0 || L_total < 1 || static_cast<int64_t>(layer0) + in->n_layers > L_total)
         return fail(PRECOG_ERR_INVALID_ARG, "layers [layer0, layer0+n_layers) exceed L_total");
     if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (!aligned_to(8, {d_slots})) return fail(PRECOG_ERR_INVALID_ARG, "d_slots not 8-byte aligned");
     if (d_slots == nullptr && n_slots < n)
         return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
     if (y_out == nullptr || !state_dtype_ok(y_dtype) || !aligned16(y_out))
@@ -1045,6 +1056,10 @@ precog_status precog_block_norm(const precog_block_norm_args *a, int64_t T, void
         if (T > 1 && rows[i].stride < a->dim) return fail(PRECOG_ERR_INVALID_ARG, "row strides smaller than a row");
         if (span[i].stride % 16 != 0) return fail(PRECOG_ERR_INVALID_ARG, "row strides must keep 16-byte alignment");
     }
+    for (const float *w : {a->skip, a->weight, a->scale_weight, a->out_weight})
+        for (int i = 4; i < 6; ++i)
+            if (overlap(whole(span[i], T), RowSpan{w, 0, 4LL * a->dim}, 1, false))
+                return fail(PRECOG_ERR_INVALID_ARG, "outputs and weights must not share memory");
     // an entry's inputs are read, by the thread that writes its outputs, before those are written
     for (int i = 0; i < 5; ++i)
         if (overlap(span[i], span[5], T, i < 4) || (i < 4 && overlap(span[i], span[4], T, true)))
@@ -1081,6 +1096,9 @@ precog_status precog_adjust_logits(const precog_adjust_args *a, int64_t n_rows, 
     const uintptr_t odd = static_cast<uintptr_t>(sz - 1);
     if (((reinterpret_cast<uintptr_t>(a->logits) | reinterpret_cast<uintptr_t>(a->out)) & odd) != 0)
         return fail(PRECOG_ERR_INVALID_ARG, "logits and out must be aligned to their elements");
+    if (!aligned_to(8, {a->d_history, a->d_history_offsets, a->d_count_from, a->d_bias_idx, a->d_bias_offsets, a->d_mask_rows}) ||
+        !aligned_to(4, {a->d_repetition, a->d_frequency, a->d_presence, a->d_bias, a->d_mask}))
+        return fail(PRECOG_ERR_INVALID_ARG, "lists must be aligned to their entries");
     const bool penalised = a->d_repetition || a->d_frequency || a->d_presence;
     if (a->d_history && a->d_history_offsets == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "d_history needs d_history_offsets");
     if (a->n_history > 0 && penalised && a->d_history == nullptr)

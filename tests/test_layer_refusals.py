@@ -50,6 +50,7 @@ def test_convolutions_reject_bad_rows(lib, change, expect):
 
 @pytest.mark.parametrize("kw,expect", [
     (dict(T=-1), 1), (dict(T=1 << 31), 2), (dict(n=-1), 1), (dict(n=1 << 31, out=None), 2), (dict(offsets=None), 1),
+    (dict(offsets=W + 4), 1), (dict(bank=T2, entries=3, idx=W + 4), 1),
     (dict(layer=1), 1), (dict(layer=-1), 1), (dict(L=0), 1), (dict(out=T1 + 8), 1), (dict(bank=T2 + 8, entries=3), 1),
     (dict(bank=T2, entries=2), 1), (dict(bank=T2, entries=-1, idx=W), 1), (dict(bank=T1, entries=3), 1),
     (dict(bank=T1 + 384, entries=3), 1), (dict(out=X), 1), (dict(out=Y + 64), 1), (dict(bank=Y, entries=3), 1),
@@ -69,7 +70,7 @@ def test_causal_conv_does_not_run_in_place_and_takes_slices(lib):
 
 
 @pytest.mark.parametrize("kw,expect", [
-    (dict(n=-1), 1), (dict(windows=None), 1), (dict(windows=T1 + 8), 1), (dict(n_slots=2), 1), (dict(n_slots=-1, slots=W), 1),
+    (dict(n=-1), 1), (dict(slots=W + 4), 1), (dict(windows=None), 1), (dict(windows=T1 + 8), 1), (dict(n_slots=2), 1), (dict(n_slots=-1, slots=W), 1),
     (dict(layer=1), 1), (dict(L=0), 1), (dict(windows=X), 1), (dict(windows=Y + 128), 1), (dict(n=1 << 31, slots=W, L=1), 2),
     (dict(n_slots=1 << 62, slots=W), 2), (dict(n=0, n_slots=0), 0)])
 def test_conv_step_rejects_bad_arguments(lib, kw, expect):
@@ -89,7 +90,7 @@ def _scan_step(lib, n=3, states=T1, n_slots=3, slots=None, layer0=0, L=2, skip=N
 @pytest.mark.parametrize("kw,expect", [
     (dict(reserved=1), 1), (dict(N=8), 2), (dict(D=12), 2), (dict(in_dtype=2), 2), (dict(a_kind=3), 1), (dict(x=0), 1), (dict(C=0), 1), (dict(A=0), 1),
     (dict(layer_stride_xd=128), 1), (dict(n=-1), 1), (dict(n=1 << 31), 2), (dict(states=None), 1), (dict(states=T1 + 8), 1),
-    (dict(n_slots=2), 1), (dict(n_slots=-1, slots=W), 1), (dict(layer0=1), 1), (dict(layer0=-1), 1), (dict(L=1), 1),
+    (dict(n_slots=2), 1), (dict(slots=W + 4), 1), (dict(n_slots=-1, slots=W), 1), (dict(layer0=1), 1), (dict(layer0=-1), 1), (dict(L=1), 1),
     (dict(y=None), 1), (dict(y=Y + 8), 1), (dict(ydt=2), 1), (dict(skip=W + 4), 1), (dict(gate=W + 8), 1), (dict(gate=W, gs=56), 1),
     (dict(gate=W, gs=68), 1), (dict(gate=W, gls=60), 1), (dict(gate=W, gls=196), 1), (dict(y=X), 1), (dict(y=T1 + 512), 1),
     (dict(states=X), 1), (dict(gate=Y), 1), (dict(gate=T1), 1), (dict(gate=Y - 256, gs=64, gls=192), 1),
@@ -117,7 +118,8 @@ def _norm_args(**kw):
     ({"residual": 0, "residual_out": 0, "out": 0}, 1), ({"x": X + 8}, 1), ({"out": Y + 4}, 1), ({"x_stride": 56}, 1),
     ({"gate": W, "gate_stride": 68}, 1), ({"weight": W + 4}, 1), ({"out_weight": W + 8}, 1), ({"scale_weight": W + 2}, 1),
     ({"out": X + 128}, 1), ({"out": T1}, 1), ({"residual_out": X}, 1), ({"residual_out": T1 + 256}, 1),
-    ({"residual_dtype": 1, "residual_out": Y}, 1), ({"gate": Y + 16}, 1)])
+    ({"residual_dtype": 1, "residual_out": Y}, 1), ({"gate": Y + 16}, 1), ({"weight": Y + 256}, 1), ({"out_weight": T1 + 64}, 1),
+    ({"scale_weight": Y}, 1)])
 def test_block_norm_rejects_bad_arguments(lib, change, expect):
     assert lib.precog_block_norm(ctypes.byref(_norm_args(**change)), 10, None) == expect
     assert lib.precog_last_error() != b""
@@ -146,7 +148,10 @@ def _adjust_args(**kw):
     ({"stride": 99}, 1), ({"out_stride": -1}, 1), ({"n_history": -1}, 1), ({"n_bias": -1}, 1), ({"n_masks": -1}, 1),
     ({"n_history": 1 << 30}, 2), ({"n_bias": 1 << 30}, 2), ({"logits": 0}, 1), ({"out": 0}, 1), ({"logits": X + 1}, 1),
     ({"out": Y + 1}, 1), ({"out": X + 2}, 1), ({"d_history": 0}, 1), ({"d_history_offsets": 0}, 1), ({"d_bias": 0}, 1),
-    ({"d_bias_idx": 0}, 1), ({"d_bias_offsets": 0}, 1), ({"n_masks": 3}, 1), ({"d_mask": 0, "d_mask_rows": W}, 1)])
+    ({"d_bias_idx": 0}, 1), ({"d_bias_offsets": 0}, 1), ({"n_masks": 3}, 1), ({"d_mask": 0, "d_mask_rows": W}, 1),
+    ({"d_history": W + 4}, 1), ({"d_history_offsets": W + 4}, 1), ({"d_count_from": W + 4}, 1), ({"d_bias_idx": W + 4}, 1),
+    ({"d_bias_offsets": W + 4}, 1), ({"d_mask_rows": W + 4}, 1), ({"d_repetition": W + 2}, 1), ({"d_frequency": W + 1}, 1),
+    ({"d_presence": W + 2}, 1), ({"d_bias": W + 2}, 1), ({"d_mask": W + 2}, 1)])
 def test_adjust_logits_rejects_bad_arguments(lib, change, expect):
     assert lib.precog_adjust_logits(ctypes.byref(_adjust_args(**change)), 4, None) == expect
     assert lib.precog_last_error() != b""
