@@ -216,6 +216,54 @@ def test_masks_alone_on_many_logits(cuda_device, dtype, pad):
     assert np.array_equal(to_np(out), want)
 
 
+def test_pairs_of_launches_in_order_captured_and_at_once(cuda_device):
+    """Many logits: call upon call without a wait between them, each on what the last one left; the same captured and
+    replayed; and two streams at once. All give the bits of calls that are waited for."""
+    import torch
+    import paper_2608_02560_gb300 as pg
+    d, R, V = cuda_device, 60, 30_011
+    gen = torch.Generator(device=d).manual_seed(8)
+    x = torch.randn((R, V), device=d, generator=gen).bfloat16()
+    history = torch.randint(0, V, (R * 500,), device=d, generator=gen)
+    args = dict(history=history, history_offsets=500 * torch.arange(R + 1, device=d), bias_idx=history[::50].contiguous(),
+                bias=torch.randn(R * 10, device=d, generator=gen), bias_offsets=10 * torch.arange(R + 1, device=d),
+                repetition=1 + torch.rand(R, device=d, generator=gen), frequency=torch.rand(R, device=d, generator=gen),
+                presence=torch.rand(R, device=d, generator=gen))
+
+    def chain(buf, wait):
+        a, b, lp = buf
+        for i in range(6):      # in place, over to the other buffer, back, and read out
+            pg.precog_adjust_logits(a, a, **args)
+            pg.precog_adjust_logits(a, b, **args)
+            pg.precog_adjust_logits(b, a, **args)
+            pg.precog_token_logprobs(a, history[:R], lp[i])
+            if wait:
+                torch.cuda.synchronize()
+
+    buffers = lambda: (x.clone(), torch.zeros_like(x), torch.zeros((6, R), device=d))  # noqa: E731
+    want, got = buffers(), buffers()
+    chain(want, True)
+    chain(got, False)
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    captured, g = buffers(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        chain(captured, False)
+    for _ in range(3):
+        captured[0].copy_(x)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, captured))
+    sides, streams = [buffers(), buffers()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for side, stream in zip(sides, streams):
+        with torch.cuda.stream(stream):
+            chain(side, False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for side in sides for p, q in zip(want, side))
+    assert pg.precog_device_status()[0] == 0
+
+
 def test_calls_of_one_input_repeat_bit_for_bit(cuda_device):
     import torch
     c = _case(cuda_device, 40, 9001, "bfloat16", 8, longest=3000)
