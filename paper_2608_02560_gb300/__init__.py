@@ -223,7 +223,7 @@ def load_library(path: str = LIB_PATH):
 
 
 def _check(status: int):
-    if status != PRECOG_OK:
+    if status:
         raise PrecogError(status, load_library().precog_last_error().decode())
 
 
@@ -263,6 +263,17 @@ def _ptr(t):
         return None
     if not t.is_cuda:
         raise ValueError("tensors passed to libprecog must live on the GPU")
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to libprecog must be contiguous")
+    return t.data_ptr()
+
+
+def _ptr_on(t, device: int):
+    """:func:`_ptr` of a tensor that has to be on GPU ``device``."""
+    if t is None:
+        return None
+    if t.get_device() != device or device < 0:
+        raise ValueError("tensors passed to libprecog must live on the GPU, and on the same one")
     if not t.is_contiguous():
         raise ValueError("tensors passed to libprecog must be contiguous")
     return t.data_ptr()
@@ -319,10 +330,14 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
             raise ValueError("complex A must be complex64 [L, D, N]")
     elif A.shape != (L, D, N) or A.dtype != torch.float32:
         raise ValueError("A must be float32 [L, D, N]")
-    s = ScanInputs(L, D, N, _dtype_code(x), a_kind, 0, _ptr(x), _ptr(dt), _ptr(B), _ptr(C), _ptr(A), T * D, T * N)
+    kind, device = x.dtype, x.get_device()
+    if dt.dtype is not kind or B.dtype is not kind or (C is not None and C.dtype is not kind):
+        raise TypeError("x, dt, B and C must have one dtype")
+    s = ScanInputs(L, D, N, _dtype_code(x), a_kind, 0, _ptr_on(x, device), _ptr_on(dt, device), _ptr_on(B, device),
+                   _ptr_on(C, device), _ptr_on(A, device), T * D, T * N)
     # the struct holds raw device pointers: keep the tensors alive as long as it lives
     s._keepalive = (x, dt, B, C, A)
-    s.rows = T
+    s.rows, s.device = T, device
     return s
 
 
@@ -635,18 +650,25 @@ def precog_token_logprobs(logits, tokens, logprob, entropy=None, top_idx=None, t
         _stream(stream)))
 
 
-_device_getter = None
+# The current device and its stream, once CUDA has begun (each call asks for both: 0.2 us of 7).
+_device_getter = _stream_getter = None
 
 
 def _current_device() -> int:
-    global _device_getter
+    global _device_getter, _stream_getter
     if _device_getter is None:
         torch = _torch()
-        get = getattr(torch._C, "_cuda_getDevice", None)
-        if get is None or not torch.cuda.is_initialized():
+        get, raw = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
+        if get is None or raw is None or not torch.cuda.is_initialized():
             return torch.cuda.current_device()
-        _device_getter = get
+        _device_getter, _stream_getter = get, raw
     return _device_getter()
+
+
+def _stream_on(device: int, stream):
+    if stream is None and _stream_getter is not None:
+        return _stream_getter(device)
+    return _stream(stream)
 
 
 def _elsewhere(t, what: str, device: int):
@@ -663,6 +685,11 @@ def _matrix(t, shape, dtype, device: int, what: str):
         raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    return _first_matrix(t, shape, device, what)
+
+
+def _first_matrix(t, shape, device: int, what: str):
+    """The same of the tensor that the others' shape and dtype come from."""
     if t.get_device() != device:
         _elsewhere(t, what, device)
     between, one = t.stride()
@@ -709,7 +736,7 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
     load_library()
     torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
     (T, D), K, n = shape, weight.shape[-1], offsets.numel() - 1
-    xp, xs = _matrix(x, shape, dtype, device, "x")
+    xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
     bp, entries, layers = _windows(bank, K, D, dtype, device, "bank")
     wp, outs, out_layers = _windows(windows_out, K, D, dtype, device, "windows_out")
@@ -723,7 +750,7 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
                      _dense(bias, (D,), torch.float32, device, "bias")),
                 _dense(offsets, (n + 1,), torch.int64, device, "offsets"), n, T, bp, entries,
                 _dense(idx, (n,), torch.int64, device, "idx"), wp, layer, out_layers or layers or layer + 1,
-                _stream(stream)))
+                _stream_on(device, stream)))
 
 
 def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = True, layer: int = 0, y_out=None,
@@ -736,14 +763,14 @@ def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = Tru
     load_library()
     torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
     (n, D), K = shape, weight.shape[-1]
-    xp, xs = _matrix(x, shape, dtype, device, "x")
+    xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
     wp, n_slots, layers = _windows(windows, K, D, dtype, device, "windows")
     call, pack = _packed_calls["precog_conv_step"]
     _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
                      _dense(weight, (D, K), torch.float32, device, "weight"),
                      _dense(bias, (D,), torch.float32, device, "bias")),
-                n, wp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer, layers, _stream(stream)))
+                n, wp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer, layers, _stream_on(device, stream)))
 
 
 def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, skip=None, gate=None, y_out=None,
@@ -754,11 +781,11 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
     times SiLU of ``gate [L, n, D]`` (each row contiguous)."""
     torch, device = _torch(), _current_device()
     L, D, N, n = inputs.n_layers, inputs.D, inputs.N, inputs.rows
-    for t in inputs._keepalive:
-        if t is not None and t.get_device() != device:
-            _elsewhere(t, "the inputs", device)
+    if inputs.device != device:
+        _elsewhere(inputs._keepalive[0], "the inputs", device)
     if L == 1:   # [n, D] stands for one layer's [1, n, D]
-        y_out, gate = (t.unsqueeze(0) if t is not None and t.dim() == 2 else t for t in (y_out, gate))
+        y_out = y_out.unsqueeze(0) if y_out is not None and y_out.dim() == 2 else y_out
+        gate = gate.unsqueeze(0) if gate is not None and gate.dim() == 2 else gate
         skip = skip.unsqueeze(0) if skip is not None and skip.dim() == 1 else skip
     if states.dim() != 4:
         raise ValueError(f"states must be [slots, layers, {D}, {N}], got {tuple(states.shape)}")
@@ -784,7 +811,7 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
         pack(_dense(states, (n_slots, layers, D, N), torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
                     device, "states"), n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
              _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
-             _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), 0), n, _stream(stream)))
+             _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), 0), n, _stream_on(device, stream)))
 
 
 def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_first: bool = True, weight=None,
@@ -808,20 +835,25 @@ def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_f
     f32, vec, scale_weight = torch.float32, (D,), 0
     if isinstance(scale, torch.Tensor):
         scale, scale_weight = 1.0, _dense(scale, vec, f32, device, "scale")
-    xp, xs = _matrix(x, shape, dtype, device, "x")
-    sp, ss = _matrix(skip_input, shape, dtype, device, "skip_input")
-    gp, gs = _matrix(gate, shape, dtype, device, "gate")
+    xp, xs = _first_matrix(x, shape, device, "x")
+    sp = ss = gp = gs = rp = rs = rop = ros = op = os_ = 0
+    if skip_input is not None:
+        sp, ss = _matrix(skip_input, shape, dtype, device, "skip_input")
+    if gate is not None:
+        gp, gs = _matrix(gate, shape, dtype, device, "gate")
     res_dtype, res_code = f32, PRECOG_F32
     if residual is not None:
         res_dtype, res_code = residual.dtype, _dtype_code(residual)
-    rp, rs = _matrix(residual, shape, res_dtype, device, "residual")
-    rop, ros = _matrix(residual_out, shape, res_dtype, device, "residual_out")
-    op, os_ = _matrix(out, shape, dtype, device, "out")
+        rp, rs = _matrix(residual, shape, res_dtype, device, "residual")
+    if residual_out is not None:
+        rop, ros = _matrix(residual_out, shape, res_dtype, device, "residual_out")
+    if out is not None:
+        op, os_ = _matrix(out, shape, dtype, device, "out")
     call, pack = _packed_calls["precog_block_norm"]
     _check(call(pack(_dtype_code(x), res_code, D, groups, kind, 1 if gate_first else 0, scale, eps, xp, sp, gp, rp, rop,
                      op, xs, ss, gs, rs, ros, os_, _dense(skip, vec, f32, device, "skip"),
                      _dense(weight, vec, f32, device, "weight"), scale_weight,
-                     _dense(out_weight, vec, f32, device, "out_weight")), T, _stream(stream)))
+                     _dense(out_weight, vec, f32, device, "out_weight")), T, _stream_on(device, stream)))
 
 
 def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_from=None, repetition=None,
@@ -843,7 +875,7 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
     load_library()
     torch, device, dtype, shape = _torch(), _current_device(), logits.dtype, logits.shape
     R, V = shape
-    lp, ls = _matrix(logits, shape, dtype, device, "logits")
+    lp, ls = _first_matrix(logits, shape, device, "logits")
     op, os_ = _matrix(out, shape, dtype, device, "out")
     i64, f32, row, ends = torch.int64, torch.float32, (R,), (R + 1,)
     nh = history.numel() if history is not None else 0
@@ -858,7 +890,7 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
                      _dense(bias_idx, (nb,), i64, device, "bias_idx"), _dense(bias, (nb,), f32, device, "bias"),
                      _dense(bias_offsets, ends, i64, device, "bias_offsets"), nb,
                      _dense(mask, (nm, (V + 31) // 32), torch.int32, device, "mask"), nm,
-                     _dense(mask_rows, row, i64, device, "mask_rows")), R, _stream(stream)))
+                     _dense(mask_rows, row, i64, device, "mask_rows")), R, _stream_on(device, stream)))
 
 
 def precog_selftest_wait_timeout(iterations: int = 4096, stream=None):

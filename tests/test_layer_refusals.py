@@ -216,6 +216,12 @@ def test_the_binding_checks_shapes_dtypes_and_devices(lib, monkeypatch):
         pg.precog_adjust_logits(x, x.half())
     with pytest.raises(ValueError, match="mask must be"):
         pg.precog_adjust_logits(x, g, mask=torch.zeros(1, 2, dtype=torch.int32))
+    with pytest.raises(TypeError, match="one dtype"):
+        pg.scan_inputs(x, x.bfloat16(), torch.zeros(6, 16), torch.zeros(8, 16))
+    with pytest.raises(TypeError, match="one dtype"):
+        pg.scan_inputs(x, x, torch.zeros(6, 16), torch.zeros(8, 16), torch.zeros(6, 16).half())
+    with pytest.raises(ValueError, match="GPU"):
+        pg.scan_inputs(x, x, torch.zeros(6, 16), torch.zeros(8, 16))
     monkeypatch.setattr(pg, "_current_device", lambda: 0)
     with pytest.raises(ValueError, match="GPU"):
         pg.precog_causal_conv(x, w, off, y_out=g)
