@@ -38,19 +38,21 @@ __device__ __forceinline__ float row_sum(float v, float *part, int in_row) {
     return v;
 }
 
-// fp32 weights of eight entries, or 1
-__device__ __forceinline__ void weights8(const float *w, int e, float (&v)[8]) {
+// fp32 weights of V entries, or 1
+template <int V>
+__device__ __forceinline__ void weights(const float *w, int e, float (&v)[V]) {
     if (w == nullptr) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 1.f;
+        for (int i = 0; i < V; ++i) v[i] = 1.f;
         return;
     }
-    unpack8(load8(w + e), v);
+    unpack(load_piece<V>(w + e), v);
 }
 
 template <typename T, typename TR, int LANES, int CH>
 __global__ void __launch_bounds__(LANES > 128 ? LANES : 128) block_norm_kernel(const BlockNormParams p, int64_t rows) {
     grid_dependency_wait();
+    constexpr int V = 16 / static_cast<int>(sizeof(T));   // entries of 16 bytes of a row
     constexpr int kBlock = LANES > 128 ? LANES : 128, kRows = kBlock / LANES;
     __shared__ float part[2][kRows][LANES > 32 ? LANES / 32 : 1];
     const int mine = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -59,84 +61,84 @@ __global__ void __launch_bounds__(LANES > 128 ? LANES : 128) block_norm_kernel(c
     const int64_t t = live ? (p.groups == 1 ? row : static_cast<unsigned>(row) / static_cast<unsigned>(p.groups)) : 0;   // (rows < 2^31)
     const int size = p.groups == 1 ? p.dim : p.dim / p.groups, first = live ? static_cast<int>(row - t * p.groups) * size : 0;
     // every load of the row before the first is used
-    Raw8<T> x[CH], u[CH], g[CH];
-    Raw8<TR> res[CH];
+    Piece<T, V> x[CH], u[CH], g[CH];
+    Piece<TR, V> res[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * LANES + lane) * 8;
+        const int e = (c * LANES + lane) * V;
         if (!live || e >= size) continue;
-        x[c] = load8(static_cast<const T *>(p.x) + t * p.x_stride + first + e);
-        if (p.skip) u[c] = load8(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e);
-        if (p.gate) g[c] = load8(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e);
-        if (p.residual) res[c] = load8(static_cast<const TR *>(p.residual) + t * p.residual_stride + first + e);
+        x[c] = load_piece<V>(static_cast<const T *>(p.x) + t * p.x_stride + first + e);
+        if (p.skip) u[c] = load_piece<V>(static_cast<const T *>(p.skip_input) + t * p.skip_stride + first + e);
+        if (p.gate) g[c] = load_piece<V>(static_cast<const T *>(p.gate) + t * p.gate_stride + first + e);
+        if (p.residual) res[c] = load_piece<V>(static_cast<const TR *>(p.residual) + t * p.residual_stride + first + e);
     }
-    float v[CH][8], w[8];
+    float v[CH][V], w[V];
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * LANES + lane) * 8;
+        const int e = (c * LANES + lane) * V;
         if (!live || e >= size) continue;
-        unpack8(x[c], v[c]);
+        unpack(x[c], v[c]);
         if (p.skip) {
-            float s[8];
-            unpack8(u[c], s);
-            weights8(p.skip, first + e, w);
+            float s[V];
+            unpack(u[c], s);
+            weights(p.skip, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = fmaf(w[i], s[i], v[c][i]);
+            for (int i = 0; i < V; ++i) v[c][i] = fmaf(w[i], s[i], v[c][i]);
         }
         if (p.gate && p.gate_first) {
-            float s[8];
-            unpack8(g[c], s);
+            float s[V];
+            unpack(g[c], s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(s[i]);
+            for (int i = 0; i < V; ++i) v[c][i] *= silu<T>(s[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+        for (int i = 0; i < V; ++i) sum = fmaf(v[c][i], v[c][i], sum);
     }
     float scale = 1.f;
     if (p.norm == PRECOG_NORM_RMS) scale = rsqrtf(row_sum<LANES>(sum, part[0][mine], lane) / static_cast<float>(size) + p.eps);
     sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * LANES + lane) * 8;
+        const int e = (c * LANES + lane) * V;
         if (!live || e >= size) continue;
         if (p.norm == PRECOG_NORM_RMS) {
-            weights8(p.weight, first + e, w);
+            weights(p.weight, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= scale * w[i];
+            for (int i = 0; i < V; ++i) v[c][i] *= scale * w[i];
         }
         if (p.gate && !p.gate_first) {
-            float s[8];
-            unpack8(g[c], s);
+            float s[V];
+            unpack(g[c], s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= silu<T>(s[i]);
+            for (int i = 0; i < V; ++i) v[c][i] *= silu<T>(s[i]);
         }
         if (p.residual) {
-            float r[8];
-            unpack8(res[c], r);
-            weights8(p.scale_weight, first + e, w);
+            float r[V];
+            unpack(res[c], r);
+            weights(p.scale_weight, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < V; ++i) {
                 v[c][i] = fmaf(p.scale * w[i], v[c][i], r[i]);
                 sum = fmaf(v[c][i], v[c][i], sum);
             }
             TR *out = static_cast<TR *>(p.residual_out) + t * p.residual_out_stride + first + e;
-            store8(out, pack8(out, v[c]));
+            store_piece(out, v[c]);
         }
     }
     if (p.out == nullptr) return;   // (for all threads or none)
     scale = p.residual ? rsqrtf(row_sum<LANES>(sum, part[1][mine], lane) / static_cast<float>(size) + p.eps) : 1.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int e = (c * LANES + lane) * 8;
+        const int e = (c * LANES + lane) * V;
         if (!live || e >= size) continue;
         if (p.residual) {
-            weights8(p.out_weight, first + e, w);
+            weights(p.out_weight, first + e, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= scale * w[i];
+            for (int i = 0; i < V; ++i) v[c][i] *= scale * w[i];
         }
         T *out = static_cast<T *>(p.out) + t * p.out_stride + first + e;
-        store8(out, pack8(out, v[c]));
+        store_piece(out, v[c]);
     }
 }
 
@@ -153,16 +155,17 @@ cudaError_t launch_shape(const BlockNormParams &p, cudaStream_t stream) {
 template <typename T, typename TR>
 cudaError_t launch_typed(const BlockNormParams &p, cudaStream_t stream) {
     const int size = p.dim / p.groups;
-    if (size <= 32) return launch_shape<T, TR, 4, 1>(p, stream);
-    if (size <= 64) return launch_shape<T, TR, 8, 1>(p, stream);
-    if (size <= 128) return launch_shape<T, TR, 16, 1>(p, stream);
-    if (size <= 256) return launch_shape<T, TR, 32, 1>(p, stream);
-    if (size <= 512) return launch_shape<T, TR, 32, 2>(p, stream);
-    if (size <= 1024) return launch_shape<T, TR, 64, 2>(p, stream);
-    if (size <= 2048) return launch_shape<T, TR, 128, 2>(p, stream);
-    if (size <= 4096) return launch_shape<T, TR, 256, 2>(p, stream);
-    if (size <= 8192) return launch_shape<T, TR, 512, 2>(p, stream);
-    return launch_shape<T, TR, 512, 4>(p, stream);
+    constexpr bool kHalf = sizeof(T) == 2;
+    if (size <= 32) return launch_shape<T, TR, 4, kHalf ? 1 : 2>(p, stream);
+    if (size <= 64) return launch_shape<T, TR, 8, kHalf ? 1 : 2>(p, stream);
+    if (size <= 128) return launch_shape<T, TR, 16, kHalf ? 1 : 2>(p, stream);
+    if (size <= 256) return launch_shape<T, TR, 32, kHalf ? 1 : 2>(p, stream);
+    if (size <= 512) return launch_shape<T, TR, kHalf ? 32 : 64, 2>(p, stream);
+    if (size <= 1024) return launch_shape<T, TR, kHalf ? 64 : 128, 2>(p, stream);
+    if (size <= 2048) return launch_shape<T, TR, kHalf ? 128 : 256, 2>(p, stream);
+    if (size <= 4096) return launch_shape<T, TR, kHalf ? 256 : 512, 2>(p, stream);
+    if (size <= 8192) return launch_shape<T, TR, 512, kHalf ? 2 : 4>(p, stream);
+    return launch_shape<T, TR, 1024, kHalf ? 2 : 4>(p, stream);
 }
 
 }  // namespace

@@ -3,7 +3,7 @@
 //   y[t, d] = act(bias[d] + sum_{j < K} w[d, j] x[t - K + 1 + j, d]),   act = SiLU or none
 //
 // Inputs before a sequence's first token come from its window, K - 1 rows [oldest .. newest] that the
-// sequence's past left (a bank's entry, a table's slot), or are zero. A thread has eight channels and rolls
+// sequence's past left (a bank's entry, a table's slot), or are zero. A thread has 16 bytes of channels and rolls
 // over a segment of tokens with the last K - 1 inputs in registers, so a row is read once and, at the start
 // of a segment, K - 1 rows again. Copies run eight tokens ahead of the arithmetic.
 //
@@ -27,42 +27,65 @@ __device__ uint32_t g_conv_status;
 
 constexpr int kThreads = 128;
 constexpr int kAhead = 8;   // tokens whose loads are in flight together
+template <typename T> constexpr int kResident = sizeof(T) == 2 ? 4 : 5;   // CTAs an SM, by their registers
 
-// Eight channels' taps and biases, as pairs of neighbouring channels.
+// A thread has the channels of 16 bytes of a row, eight of bf16 or four of fp32, as pairs.
+template <typename T> constexpr int kChannels = 16 / static_cast<int>(sizeof(T));
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T *p) { return *reinterpret_cast<const uint4 *>(p); }
+template <typename T>
+__device__ __forceinline__ void store16(T *p, const uint4 &q) { *reinterpret_cast<uint4 *>(p) = q; }
+template <typename T>
+__device__ __forceinline__ void unpack16(const uint4 &q, f2 (&v)[kChannels<T> / 2]) {
+    if constexpr (sizeof(T) == 4) {
+        v[0] = pack2(__uint_as_float(q.x), __uint_as_float(q.y)), v[1] = pack2(__uint_as_float(q.z), __uint_as_float(q.w));
+    } else {
+        float e[8];
+        unpack(Piece<T, 8>{{q}}, e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const f2 (&v)[kChannels<T> / 2]) {
+    float e[kChannels<T>];
+#pragma unroll
+    for (int i = 0; i < kChannels<T> / 2; ++i) unpack2(v[i], e[2 * i], e[2 * i + 1]);
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
+    else return pack(e);
+}
+
 template <typename T, int K>
 struct Taps {
-    f2 w[K][4], bias[4];
+    static constexpr int C = kChannels<T>, P = C / 2;
+    f2 w[K][P], bias[P];
     __device__ __forceinline__ void load(const ConvParams &p, int d) {
-        float flat[8 * K];
+        __align__(16) float flat[C * K], b[C] = {};
         const float4 *from = reinterpret_cast<const float4 *>(p.weight + static_cast<int64_t>(d) * K);
 #pragma unroll
-        for (int i = 0; i < 2 * K; ++i) {
-            const float4 q = __ldg(from + i);
-            flat[4 * i] = q.x, flat[4 * i + 1] = q.y, flat[4 * i + 2] = q.z, flat[4 * i + 3] = q.w;
-        }
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[j][i] = pack2(flat[2 * i * K + j], flat[(2 * i + 1) * K + j]);
-        float4 b[2] = {};
+        for (int i = 0; i < C * K / 4; ++i) *reinterpret_cast<float4 *>(flat + 4 * i) = __ldg(from + i);
         if (p.bias) {
-            b[0] = __ldg(reinterpret_cast<const float4 *>(p.bias + d));
-            b[1] = __ldg(reinterpret_cast<const float4 *>(p.bias + d) + 1);
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i) *reinterpret_cast<float4 *>(b + 4 * i) = __ldg(reinterpret_cast<const float4 *>(p.bias + d) + i);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) bias[2 * i] = pack2(b[i].x, b[i].y), bias[2 * i + 1] = pack2(b[i].z, b[i].w);
+        for (int i = 0; i < P; ++i) {
+            bias[i] = pack2(b[2 * i], b[2 * i + 1]);
+#pragma unroll
+            for (int j = 0; j < K; ++j) w[j][i] = pack2(flat[2 * i * K + j], flat[(2 * i + 1) * K + j]);
+        }
     }
     // y of inputs in[0 .. K - 1], oldest first
-    __device__ __forceinline__ Raw8<T> out(const f2 (*const (&in)[K])[4], bool act) const {
-        f2 y[4];
+    __device__ __forceinline__ uint4 out(const f2 (*const (&in)[K])[P], bool act) const {
+        f2 y[P];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < P; ++i) {
             y[i] = bias[i];
 #pragma unroll
             for (int j = 0; j < K; ++j) y[i] = fma2(w[j][i], (*in[j])[i], y[i]);
             if (act) y[i] = silu2<T>(y[i]);
         }
-        return pack8(static_cast<const T *>(nullptr), y);
+        return pack16<T>(y);
     }
 };
 
@@ -89,12 +112,13 @@ __device__ __forceinline__ int sequence_of(const ConvParams &p, int64_t item, in
 }
 
 template <typename T, int K>
-__global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, int segment, int64_t items) {
+__global__ void __launch_bounds__(kThreads, kResident<T>) conv_kernel(const ConvParams p, int segment, int64_t items) {
     grid_dependency_wait();
-    const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
+    constexpr int C = kChannels<T>;
+    const unsigned groups = static_cast<unsigned>(p.dim) / C;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t item = at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups);
-    const int d = static_cast<int>(at - item * groups) * 8;
+    const int d = static_cast<int>(at - item * groups) * C;
     if (item < p.n_seqs && d == 0) {   // every sequence is looked at, whichever way the search goes
         const int64_t a = p.offsets[item], b = p.offsets[item + 1];
         if (a < 0 || b < a || b > p.T_tot) atomicOr(&g_conv_status, PRECOG_DEV_BAD_OFFSETS);
@@ -125,28 +149,24 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
     };
     // A thread's next kAhead inputs are on their way to its own places in shared memory (registers for them would
     // cost the warps that hide their latency).
-    constexpr int kPieces = sizeof(T) / 2;
-    __shared__ uint4 ring[kAhead][kPieces][kThreads];
+    __shared__ uint4 ring[kAhead][kThreads];
     auto fetch = [&](int place, const T *from, bool there) {
-        if (there) {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) cp_async16_exact(&ring[place][i][threadIdx.x], reinterpret_cast<const uint4 *>(from) + i);
-        }
+        if (there) cp_async16_exact(&ring[place][threadIdx.x], from);
         cp_async_commit();
     };
-    Raw8<T> past[K - 1] = {};
+    uint4 past[K - 1] = {};
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) fetch(u, x + u * p.x_stride, u < n);
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
         const T *at_j = place(j - (K - 1));
-        if (at_j != nullptr) past[j] = load8(at_j);
+        if (at_j != nullptr) past[j] = load16(at_j);
     }
     Taps<T, K> taps;
     taps.load(p, d);
-    f2 in[K][4];   // input t in place t mod K
+    f2 in[K][C / 2];   // input t in place t mod K
 #pragma unroll
-    for (int j = 1; j < K; ++j) unpack8(past[j - 1], in[j]);
+    for (int j = 1; j < K; ++j) unpack16<T>(past[j - 1], in[j]);
     T *y = static_cast<T *>(p.y) + begin * p.y_stride + d;
     const T *from = x + kAhead * p.x_stride;
     const bool act = p.silu != 0;
@@ -157,26 +177,25 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
         for (int u = 0; u < kRound; u += 2) {
             if (t + u >= n) break;
             cp_async_wait<kAhead - 2>();
-            Raw8<T> raw[2];
+            uint4 raw[2];
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) raw[v].q[i] = ring[slot + v][i][threadIdx.x];
+                raw[v] = ring[slot + v][threadIdx.x];
                 fetch(slot + v, from + v * p.x_stride, t + u + v + kAhead < n);
             }
             slot = (slot + 2) % kAhead;
             from += 2 * p.x_stride;
-            Raw8<T> r[2];
+            uint4 r[2];
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                unpack8(raw[v], in[(u + v) % K]);
-                const f2(*of[K])[4];
+                unpack16<T>(raw[v], in[(u + v) % K]);
+                const f2(*of[K])[C / 2];
 #pragma unroll
                 for (int j = 0; j < K; ++j) of[j] = &in[(u + v + 1 + j) % K];
                 r[v] = taps.out(of, act);
             }
-            store8(y, r[0]);
-            if (t + u + 1 < n) store8(y + p.y_stride, r[1]);
+            store16(y, r[0]);
+            if (t + u + 1 < n) store16(y + p.y_stride, r[1]);
             y += 2 * p.y_stride;
         }
     }
@@ -185,28 +204,29 @@ __global__ void __launch_bounds__(kThreads, 4) conv_kernel(const ConvParams p, i
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) {
             const T *at_j = place(n - (K - 1) + j);
-            store8(out + static_cast<int64_t>(j) * p.dim, at_j != nullptr ? load8(at_j) : Raw8<T>{});
+            store16(out + static_cast<int64_t>(j) * p.dim, at_j != nullptr ? load16(at_j) : uint4{});
         }
     }
 }
 
-// One token of each row: a thread has eight channels of the rows first, first + stride, ..., whose taps it keeps. Two
+// One token of each row: a thread has 16 bytes of the rows first, first + stride, ..., whose taps it keeps. Two
 // rows are on their way while one is worked on, their slots a round before. 256 rows of 8448 bf16 channels, K = 4 (34.8
 // MB, 5.1 us at the measured copy rate): 8.6 us (39 with a row a thread, whose taps are as many bytes as the row's own;
 // 9.5 with two rows a thread in 1.7 rounds of CTAs).
 template <typename T, int K>
 struct StepRow {
     T *window;   // nullptr: idle
-    Raw8<T> in[K];
+    uint4 in[K];
 };
 template <typename T, int K, int AHEAD>
-__global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p, int stride) {
+__global__ void __launch_bounds__(kThreads, kResident<T>) conv_step_kernel(const ConvParams p, int stride) {
     grid_dependency_wait();
-    const unsigned groups = static_cast<unsigned>(p.dim) / 8u;
+    constexpr int C = kChannels<T>;
+    const unsigned groups = static_cast<unsigned>(p.dim) / C;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t first = at >> 32 ? at / groups : static_cast<int64_t>(static_cast<unsigned>(at) / groups);
     if (first >= stride) return;
-    const int d = static_cast<int>(at - first * groups) * 8;
+    const int d = static_cast<int>(at - first * groups) * C;
     auto slot_of = [&](int64_t row) -> int64_t { return row >= p.n_seqs ? -1 : p.idx ? p.idx[row] : row; };
     auto load = [&](StepRow<T, K> &r, int64_t row, int64_t slot) {
         r.window = nullptr;
@@ -216,8 +236,8 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p,
         }
         r.window = static_cast<T *>(p.windows) + ((slot * p.L_total + p.layer) * (K - 1)) * p.dim + d;
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) r.in[j] = load8(r.window + static_cast<int64_t>(j) * p.dim);
-        r.in[K - 1] = load8(static_cast<const T *>(p.x) + row * p.x_stride + d);
+        for (int j = 0; j < K - 1; ++j) r.in[j] = load16(r.window + static_cast<int64_t>(j) * p.dim);
+        r.in[K - 1] = load16(static_cast<const T *>(p.x) + row * p.x_stride + d);
     };
     StepRow<T, K> rows[AHEAD];
     int64_t slot[AHEAD];
@@ -234,17 +254,17 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p,
         for (int r = 0; r < AHEAD; ++r) {
             const int64_t row = row0 + static_cast<int64_t>(r) * stride;
             if (row >= p.n_seqs) break;
-            Raw8<T> y = {};
+            uint4 y = {};
             if (rows[r].window != nullptr) {
-                f2 in[K][4];
-                const f2(*of[K])[4];
+                f2 in[K][C / 2];
+                const f2(*of[K])[C / 2];
 #pragma unroll
-                for (int j = 0; j < K; ++j) unpack8(rows[r].in[j], in[j]), of[j] = &in[j];
+                for (int j = 0; j < K; ++j) unpack16<T>(rows[r].in[j], in[j]), of[j] = &in[j];
                 y = taps.out(of, p.silu != 0);
 #pragma unroll
-                for (int j = 0; j < K - 1; ++j) store8(rows[r].window + static_cast<int64_t>(j) * p.dim, rows[r].in[j + 1]);
+                for (int j = 0; j < K - 1; ++j) store16(rows[r].window + static_cast<int64_t>(j) * p.dim, rows[r].in[j + 1]);
             }
-            store8(static_cast<T *>(p.y) + row * p.y_stride + d, y);
+            store16(static_cast<T *>(p.y) + row * p.y_stride + d, y);
             load(rows[r], row + static_cast<int64_t>(AHEAD) * stride, slot[r]);
             slot[r] = slot_of(row + static_cast<int64_t>(2 * AHEAD) * stride);
         }
@@ -253,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvParams p,
 
 template <typename T, int K>
 cudaError_t launch_k(const ConvParams &p, bool step, cudaStream_t stream) {
-    const int64_t groups = p.dim / 8, fill = static_cast<int64_t>(device_sm_count()) * 4 * kThreads;
+    const int64_t groups = p.dim / kChannels<T>, fill = static_cast<int64_t>(device_sm_count()) * kResident<T> * kThreads;
     cudaError_t e;
     auto go = [&](auto kernel, int64_t threads, auto... more) {
         const int64_t blocks = (threads + kThreads - 1) / kThreads;

@@ -19,20 +19,8 @@ constexpr int kThreads = 128;
 constexpr int kN = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <typename T> struct Raw4;
-template <> struct Raw4<float> { using type = uint4; };
-template <> struct Raw4<__nv_bfloat16> { using type = uint2; };
-__device__ __forceinline__ void unpack4(const uint4 &q, float (&v)[4]) {
-    v[0] = __uint_as_float(q.x), v[1] = __uint_as_float(q.y), v[2] = __uint_as_float(q.z), v[3] = __uint_as_float(q.w);
-}
-__device__ __forceinline__ void unpack4(const uint2 &q, float (&v)[4]) {
-    v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xffff0000u);
-    v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xffff0000u);
-}
 template <typename T>
-__device__ __forceinline__ typename Raw4<T>::type raw4(const void *p, int64_t at) {
-    return *reinterpret_cast<const typename Raw4<T>::type *>(static_cast<const T *>(p) + at);
-}
+__device__ __forceinline__ typename Raw4<T>::type raw4(const void *p, int64_t at) { return load4(static_cast<const T *>(p) + at); }
 
 // The part of a launch that a warp works on: 32 channels of one layer, and every row_blocks-th row.
 struct Share {

@@ -1,4 +1,4 @@
-// Eight neighbouring elements of a row, as they are stored (16 bytes, fp32: 32) and as fp32.
+// Neighbouring elements of a row, as they are stored and as fp32; and SiLU.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -9,53 +9,57 @@
 
 namespace precog {
 
-template <typename T> struct Raw8 { uint4 q[1]; };
-template <> struct Raw8<float> { uint4 q[2]; };
-
+// Four neighbouring elements, as they are stored (8 bytes, fp32: 16) and as fp32.
+template <typename T> struct Raw4 { using type = uint2; };
+template <> struct Raw4<float> { using type = uint4; };
 template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T *p) {
-    Raw8<T> r;
+__device__ __forceinline__ typename Raw4<T>::type load4(const T *p) { return *reinterpret_cast<const typename Raw4<T>::type *>(p); }
+__device__ __forceinline__ void unpack4(const uint4 &q, float (&v)[4]) {
+    v[0] = __uint_as_float(q.x), v[1] = __uint_as_float(q.y), v[2] = __uint_as_float(q.z), v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack4(const uint2 &q, float (&v)[4]) {   // bf16
+    v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xffff0000u);
+    v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xffff0000u);
+}
+
+// V of them in pieces of 16 bytes.
+template <typename T, int V> struct Piece { uint4 q[V * static_cast<int>(sizeof(T)) / 16]; };
+
+template <int V, typename T>
+__device__ __forceinline__ Piece<T, V> load_piece(const T *p) {
+    Piece<T, V> r;
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) r.q[i] = reinterpret_cast<const uint4 *>(p)[i];
+    for (int i = 0; i < static_cast<int>(sizeof(r) / 16); ++i) r.q[i] = reinterpret_cast<const uint4 *>(p)[i];
     return r;
 }
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const Raw8<T> &r) {
+template <int V>
+__device__ __forceinline__ void unpack(const Piece<float, V> &r, float (&v)[V]) {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = r.q[i];
-}
-
-__device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < V / 4; ++i) {
         v[4 * i] = __uint_as_float(r.q[i].x), v[4 * i + 1] = __uint_as_float(r.q[i].y);
         v[4 * i + 2] = __uint_as_float(r.q[i].z), v[4 * i + 3] = __uint_as_float(r.q[i].w);
     }
 }
-__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&v)[8]) {
+__device__ __forceinline__ void unpack(const Piece<__nv_bfloat16, 8> &r, float (&v)[8]) {
     const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
-__device__ __forceinline__ Raw8<float> pack8(const float *, const float (&v)[8]) {
-    Raw8<float> r;
+template <int V>
+__device__ __forceinline__ void store_piece(float *p, const float (&v)[V]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        r.q[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
-                            __float_as_uint(v[4 * i + 3]));
-    return r;
+    for (int i = 0; i < V / 4; ++i) reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
-__device__ __forceinline__ Raw8<__nv_bfloat16> pack8(const __nv_bfloat16 *, const float (&v)[8]) {
+__device__ __forceinline__ uint4 pack(const float (&v)[8]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
         w[i] = *reinterpret_cast<const uint32_t *>(&p);
     }
-    Raw8<__nv_bfloat16> r;
-    r.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    return r;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&v)[8]) { *reinterpret_cast<uint4 *>(p) = pack(v); }
 
 // x / (1 + e^-x); NaN stays, and -infinity gives NaN as the formula does. For rows that are stored in 16 bits
 // the quick exponential and reciprocal (together within 2^-19 of the value while |x| < 10) are far below the
@@ -81,22 +85,6 @@ __device__ __forceinline__ f2 silu2(f2 x) {
     }
     unpack2(mul2(x, pack2(kMinusLog2e, kMinusLog2e)), a, b);
     return mul2(x, pack2(rcp_quick(1.f + ex2(a)), rcp_quick(1.f + ex2(b))));
-}
-
-// the same eight as four pairs
-template <typename T>
-__device__ __forceinline__ void unpack8(const Raw8<T> &r, f2 (&v)[4]) {
-    float e[8];
-    unpack8(r, e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pack2(e[2 * i], e[2 * i + 1]);
-}
-template <typename T>
-__device__ __forceinline__ Raw8<T> pack8(const T *, const f2 (&v)[4]) {
-    float e[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpack2(v[i], e[2 * i], e[2 * i + 1]);
-    return pack8(static_cast<const T *>(nullptr), e);
 }
 
 }  // namespace precog
