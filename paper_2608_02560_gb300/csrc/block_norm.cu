@@ -4,17 +4,19 @@
 //   a <- a silu(gate) [after the norm] ;  without a residual: out = a
 //   h = residual + scale a ;  residual_out = h ;  out = h rsqrt(mean h^2 + eps) out_weight
 //
-// A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold eight neighbouring entries CH
-// times each; what is read is read once, all of it before the first is used, and stays in registers as fp32 until it is
-// written. Sums are fp32, in an order that depends on the row's length alone.
+// A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold 16 bytes of neighbouring entries
+// CH times each; what is read is read once, all of it before the first is used, and stays in registers as fp32 until it
+// is written. Sums are fp32, in an order that depends on the row's length and type alone.
 //
-// Memory bounds it: 65,521 rows of 2048, norm, scaled fp32 residual, next norm (1.61 GB, 237 us at the measured copy
-// rate): 235.5 us; rows of 4096 with skip and gate (2.15 GB, 316 us): 338. Two eights a lane are best at every length (rows
-// of 2048, us: 128 lanes 237, 256 lanes with one eight 280, 64 with four 281; of 4096, gated: 256 lanes 340, 128 with four
-// 386, 512 with one 392): more bytes a thread in flight, fewer warps at a barrier. Beyond 4096 a row's barriers leave
-// the CTA waiting (8192: 1.2 to 1.4 of the copy's time in bf16, 1.6 in fp32). Two rows a CTA for one load of the weights
-// took more registers than that saves (278 and 412 us); rows in turn with the next one's copies in shared memory took the
-// L1 that the weights live in (1.4 to 2 times as long); a cluster of two CTAs of 128 threads for a row of 4096 took 491.
+// Memory bounds it: 65,521 bf16 rows of 2048, norm, scaled fp32 residual, next norm (1.61 GB, 237 us at the measured copy
+// rate): 235.5 us; rows of 4096 with skip and gate (2.15 GB, 316 us): 338, in groups of 64 to 512 332 to 344. Twice 16
+// bytes a lane are best at every length (us, rows of 2048: 128 lanes 237, 256 lanes with one piece 280, 64 with four 281;
+// of 4096, gated: 256 lanes 340, 128 with four 386, 512 with one 392; groups of 64 to 256 with one 390): more bytes a
+// thread on the way, fewer warps at a barrier. Four entries a lane in bf16, which would read the fp32 weights in whole
+// lines, took 231 and 364; fp32 rows have them so (32 bytes a lane: 123 us where 16 take 113 for 23,437 rows of 2048).
+// Beyond 4096 a row's barriers leave the CTA waiting (8192: 1.3 to 1.6 of the copy's time). Two rows a CTA for one load of
+// the weights took more registers than that saves (278 and 412 us); rows in turn with the next one's copies in shared
+// memory took the L1 that the weights live in (1.4 to 2 times as long); a cluster of two CTAs for a row of 4096 took 491.
 #include "../../include/precog.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -156,10 +158,10 @@ template <typename T, typename TR>
 cudaError_t launch_typed(const BlockNormParams &p, cudaStream_t stream) {
     const int size = p.dim / p.groups;
     constexpr bool kHalf = sizeof(T) == 2;
-    if (size <= 32) return launch_shape<T, TR, 4, kHalf ? 1 : 2>(p, stream);
-    if (size <= 64) return launch_shape<T, TR, 8, kHalf ? 1 : 2>(p, stream);
-    if (size <= 128) return launch_shape<T, TR, 16, kHalf ? 1 : 2>(p, stream);
-    if (size <= 256) return launch_shape<T, TR, 32, kHalf ? 1 : 2>(p, stream);
+    if (size <= 32) return launch_shape<T, TR, kHalf ? 2 : 4, 2>(p, stream);
+    if (size <= 64) return launch_shape<T, TR, kHalf ? 4 : 8, 2>(p, stream);
+    if (size <= 128) return launch_shape<T, TR, kHalf ? 8 : 16, 2>(p, stream);
+    if (size <= 256) return launch_shape<T, TR, kHalf ? 16 : 32, 2>(p, stream);
     if (size <= 512) return launch_shape<T, TR, kHalf ? 32 : 64, 2>(p, stream);
     if (size <= 1024) return launch_shape<T, TR, kHalf ? 64 : 128, 2>(p, stream);
     if (size <= 2048) return launch_shape<T, TR, kHalf ? 128 : 256, 2>(p, stream);
