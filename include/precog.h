@@ -611,7 +611,8 @@ typedef struct precog_conv_args {
  *                d_offsets[c+1]-1 of x and y. A sequence whose offsets decrease or leave
  *                [0, T_tot] is skipped and flags PRECOG_DEV_BAD_OFFSETS, and sequences behind
  *                it may be skipped too. Lengths of zero are allowed: the window is handed on.
- *   T_tot        rows of x and y (below 2^31); y rows outside every sequence are left untouched
+ *   T_tot        rows of x and y (below 2^31; sequences below 2^30); y rows outside every sequence
+ *                are left untouched
  *   bank         device [bank_entries][L_total][kernel-1][dim] in `dtype`, or NULL: nothing
  *                came before any sequence (zeros)
  *   d_idx        device int64 [n_seqs]: the bank row whose layer `layer` is sequence c's window

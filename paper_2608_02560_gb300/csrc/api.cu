@@ -869,7 +869,8 @@ precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_
     if (T_tot < 0) return fail(PRECOG_ERR_INVALID_ARG, "T_tot must be >= 0");
     if (n_seqs < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_seqs must be >= 0");
     precog::ConvParams p;
-    if (T_tot > 0x7fffffffLL || n_seqs > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "T_tot and n_seqs must be below 2^31");
+    if (T_tot > 0x7fffffffLL || n_seqs > 0x3fffffffLL)
+        return fail(PRECOG_ERR_UNSUPPORTED, "T_tot must be below 2^31, n_seqs below 2^30");
     precog_status s = check_conv(args, T_tot, layer, L_total, &p);
     if (s != PRECOG_OK) return s;
     if (d_offsets == nullptr || !aligned_to(8, {d_offsets, d_idx}))

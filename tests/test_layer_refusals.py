@@ -49,7 +49,7 @@ def test_convolutions_reject_bad_rows(lib, change, expect):
 
 
 @pytest.mark.parametrize("kw,expect", [
-    (dict(T=-1), 1), (dict(T=1 << 31), 2), (dict(n=-1), 1), (dict(n=1 << 31, out=None), 2), (dict(offsets=None), 1),
+    (dict(T=-1), 1), (dict(T=1 << 31), 2), (dict(n=-1), 1), (dict(n=1 << 30, out=None), 2), (dict(offsets=None), 1),
     (dict(offsets=W + 4), 1), (dict(bank=T2, entries=3, idx=W + 4), 1),
     (dict(layer=1), 1), (dict(layer=-1), 1), (dict(L=0), 1), (dict(out=T1 + 8), 1), (dict(bank=T2 + 8, entries=3), 1),
     (dict(bank=T2, entries=2), 1), (dict(bank=T2, entries=-1, idx=W), 1), (dict(bank=T1, entries=3), 1),
