@@ -313,12 +313,13 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     ``a_kind=PRECOG_A_POWER`` states that A[d, n] == (n + 1) * A[d, 0] <= 0 (verified on
     the device); it selects the one-exponential update forms. ``a_kind=PRECOG_A_COMPLEX``
     takes a complex64 A (Eq. 1's complex diagonal) and complex states."""
-    if x.dim() == 2:
+    shape = x.shape
+    if len(shape) == 2:
         x, dt, B = x.unsqueeze(0), dt.unsqueeze(0), B.unsqueeze(0)
         C = None if C is None else C.unsqueeze(0)
+        shape = x.shape
     if A.dim() == 2:
         A = A.unsqueeze(0)
-    shape = x.shape
     L, T, D = shape
     rows = B.shape
     N = rows[-1]
@@ -713,14 +714,20 @@ def _dense(t, shape, dtype, device: int, what: str) -> int:
     return t.data_ptr()
 
 
-def _windows(t, K: int, D: int, dtype, device: int, what: str):
-    """(pointer, entries, layers) of a table of windows ``[entries, layers, K - 1, D]``."""
+def _table(t, rows: int, n: int, dtype, device: int, what: str):
+    """(pointer, entries, layers) of a contiguous table ``[entries, layers, rows, n]``; None: zeros."""
     if t is None:
         return 0, 0, 0
-    if t.dim() != 4:
-        raise ValueError(f"{what} must be [entries, layers, {K - 1}, {D}], got {tuple(t.shape)}")
-    entries, layers = t.shape[:2]
-    return _dense(t, (entries, layers, K - 1, D), dtype, device, what), entries, layers
+    shape = t.shape
+    if len(shape) != 4 or shape[2] != rows or shape[3] != n:
+        raise ValueError(f"{what} must be [entries, layers, {rows}, {n}], got {tuple(shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        _elsewhere(t, what, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr(), shape[0], shape[1]
 
 
 def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=None, idx=None, layer: int = 0,
@@ -738,8 +745,8 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
     (T, D), K, n = shape, weight.shape[-1], offsets.numel() - 1
     xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
-    bp, entries, layers = _windows(bank, K, D, dtype, device, "bank")
-    wp, outs, out_layers = _windows(windows_out, K, D, dtype, device, "windows_out")
+    bp, entries, layers = _table(bank, K - 1, D, dtype, device, "bank")
+    wp, outs, out_layers = _table(windows_out, K - 1, D, dtype, device, "windows_out")
     if windows_out is not None and outs != n:
         raise ValueError("windows_out must have one entry per sequence")
     if bank is not None and windows_out is not None and layers != out_layers:
@@ -765,7 +772,7 @@ def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = Tru
     (n, D), K = shape, weight.shape[-1]
     xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
-    wp, n_slots, layers = _windows(windows, K, D, dtype, device, "windows")
+    wp, n_slots, layers = _table(windows, K - 1, D, dtype, device, "windows")
     call, pack = _packed_calls["precog_conv_step"]
     _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
                      _dense(weight, (D, K), torch.float32, device, "weight"),
@@ -787,9 +794,8 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
         y_out = y_out.unsqueeze(0) if y_out is not None and y_out.dim() == 2 else y_out
         gate = gate.unsqueeze(0) if gate is not None and gate.dim() == 2 else gate
         skip = skip.unsqueeze(0) if skip is not None and skip.dim() == 1 else skip
-    if states.dim() != 4:
-        raise ValueError(f"states must be [slots, layers, {D}, {N}], got {tuple(states.shape)}")
-    n_slots, layers = states.shape[:2]
+    sp, n_slots, layers = _table(states, D, N, torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
+                                 device, "states")
     if y_out is None:
         raise ValueError("y_out is required")
     gp = gs = gls = 0
@@ -808,8 +814,7 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
     call, pack = _packed_calls["precog_scan_step"]
     _check(call(
         ctypes.byref(inputs),
-        pack(_dense(states, (n_slots, layers, D, N), torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
-                    device, "states"), n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
+        pack(sp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
              _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
              _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), 0), n, _stream_on(device, stream)))
 
