@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cstdint>
+#include <type_traits>
 
 #include "ptx.cuh"
 
@@ -22,14 +23,16 @@ __device__ __forceinline__ void unpack4(const uint2 &q, float (&v)[4]) {   // bf
     v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xffff0000u);
 }
 
-// V of them in pieces of 16 bytes.
+// V of them, in pieces of 16 bytes (four of bf16: 8).
 template <typename T, int V> struct Piece { uint4 q[V * static_cast<int>(sizeof(T)) / 16]; };
+template <> struct Piece<__nv_bfloat16, 4> { uint2 q[1]; };
 
 template <int V, typename T>
 __device__ __forceinline__ Piece<T, V> load_piece(const T *p) {
     Piece<T, V> r;
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(r) / 16); ++i) r.q[i] = reinterpret_cast<const uint4 *>(p)[i];
+    for (int i = 0; i < static_cast<int>(sizeof(r.q) / sizeof(r.q[0])); ++i)
+        r.q[i] = reinterpret_cast<const std::remove_extent_t<decltype(r.q)> *>(p)[i];
     return r;
 }
 template <int V>
@@ -40,6 +43,7 @@ __device__ __forceinline__ void unpack(const Piece<float, V> &r, float (&v)[V]) 
         v[4 * i + 2] = __uint_as_float(r.q[i].z), v[4 * i + 3] = __uint_as_float(r.q[i].w);
     }
 }
+__device__ __forceinline__ void unpack(const Piece<__nv_bfloat16, 4> &r, float (&v)[4]) { unpack4(r.q[0], v); }
 __device__ __forceinline__ void unpack(const Piece<__nv_bfloat16, 8> &r, float (&v)[8]) {
     const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
 #pragma unroll
@@ -50,16 +54,17 @@ __device__ __forceinline__ void store_piece(float *p, const float (&v)[V]) {
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
 __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t *>(&p);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
 }
 __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&v)[8]) { *reinterpret_cast<uint4 *>(p) = pack(v); }
+__device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&v)[4]) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+}
 
 // x / (1 + e^-x); NaN stays, and -infinity gives NaN as the formula does. For rows that are stored in 16 bits
 // the quick exponential and reciprocal (together within 2^-19 of the value while |x| < 10) are far below the
