@@ -10,7 +10,8 @@
 // Memory bounds it where there is enough: 557,000 tokens of 256 sequences, 2048 bf16 channels, K = 4 with SiLU (4.57 GB,
 // 673 us at the measured copy rate): 670 to 673 us. (1999 us with one token at a time, 798 with four ahead in registers, which
 // left room for 16 warps an SM and 32 KB on the way; eight ahead in shared memory are 64 KB.) 96 sequences of up to 200
-// tokens (13.2 us): 19.2 us, one round of CTAs with 4 warps a scheduler. 64 tokens: 3.3 us.
+// tokens (13.2 us): 19.2 us, one round of CTAs with 4 warps a scheduler (20.5 with half the channels a thread and six).
+// 64 tokens: 3.3 us.
 //
 // Segments of S tokens of ragged sequences need no prefix sums: item i belongs to the sequence c with
 // base(c) <= i < base(c + 1), base(c) = offsets[c] / S + c, because base(c + 1) - base(c) is at least
