@@ -249,13 +249,22 @@ def _dtype_code(t) -> int:
     global _dtype_codes
     if _dtype_codes is None:
         torch = _torch()
-        # complex64 state/bank buffers are (re, im) fp32 pairs: the F32 storage code
-        _dtype_codes = {torch.float32: PRECOG_F32, torch.bfloat16: PRECOG_BF16, torch.float16: PRECOG_F16,
-                        torch.complex64: PRECOG_F32}
+        _dtype_codes = {torch.float32: PRECOG_F32, torch.bfloat16: PRECOG_BF16, torch.float16: PRECOG_F16}
     code = _dtype_codes.get(t.dtype)
     if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype}")
+        if t.dtype is not _torch().complex64:
+            raise TypeError(f"unsupported dtype {t.dtype}")
+        # complex64 state/bank buffers are (re, im) fp32 pairs: the F32 storage code
+        _resolved(t)
+        code = PRECOG_F32
     return code
+
+
+def _resolved(t):
+    """Refuses a complex tensor whose memory does not hold its values: ``t.conj()`` is contiguous and has t's pointer."""
+    if t.is_conj() or t.is_neg():
+        raise ValueError("tensors passed to libprecog must hold their values: call resolve_conj() and resolve_neg() "
+                         "on a lazily conjugated or negated one")
 
 
 def _ptr(t):
@@ -329,6 +338,7 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     if a_kind == PRECOG_A_COMPLEX:
         if A.shape != (L, D, N) or A.dtype != torch.complex64:
             raise ValueError("complex A must be complex64 [L, D, N]")
+        _resolved(A)
     elif A.shape != (L, D, N) or A.dtype != torch.float32:
         raise ValueError("A must be float32 [L, D, N]")
     kind, device = x.dtype, x.get_device()
@@ -723,6 +733,8 @@ def _table(t, rows: int, n: int, dtype, device: int, what: str):
         raise ValueError(f"{what} must be [entries, layers, {rows}, {n}], got {tuple(shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if dtype.is_complex:
+        _resolved(t)
     if t.get_device() != device:
         _elsewhere(t, what, device)
     if not t.is_contiguous():
