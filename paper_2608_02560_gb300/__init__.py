@@ -245,19 +245,24 @@ def _torch():
     return _torch_module
 
 
-def _dtype_code(t) -> int:
+def _row_code(t) -> int:
+    """The code of real rows."""
     global _dtype_codes
     if _dtype_codes is None:
         torch = _torch()
         _dtype_codes = {torch.float32: PRECOG_F32, torch.bfloat16: PRECOG_BF16, torch.float16: PRECOG_F16}
     code = _dtype_codes.get(t.dtype)
     if code is None:
-        if t.dtype is not _torch().complex64:
-            raise TypeError(f"unsupported dtype {t.dtype}")
-        # complex64 state/bank buffers are (re, im) fp32 pairs: the F32 storage code
-        _resolved(t)
-        code = PRECOG_F32
+        raise TypeError(f"unsupported dtype {t.dtype}")
     return code
+
+
+def _dtype_code(t) -> int:
+    """The code of a buffer or bank of the scans' states: complex64 ones are (re, im) fp32 pairs, F32 as stored."""
+    if t.dtype is _torch().complex64:
+        _resolved(t)
+        return PRECOG_F32
+    return _row_code(t)
 
 
 def _resolved(t):
@@ -344,7 +349,7 @@ def scan_inputs(x, dt, B, A, C=None, a_kind: int = PRECOG_A_GENERAL) -> ScanInpu
     kind, device = x.dtype, x.get_device()
     if dt.dtype is not kind or B.dtype is not kind or (C is not None and C.dtype is not kind):
         raise TypeError("x, dt, B and C must have one dtype")
-    s = ScanInputs(L, D, N, _dtype_code(x), a_kind, 0, _ptr_on(x, device), _ptr_on(dt, device), _ptr_on(B, device),
+    s = ScanInputs(L, D, N, _row_code(x), a_kind, 0, _ptr_on(x, device), _ptr_on(dt, device), _ptr_on(B, device),
                    _ptr_on(C, device), _ptr_on(A, device), T * D, T * N)
     # the struct holds raw device pointers: keep the tensors alive as long as it lives
     s._keepalive = (x, dt, B, C, A)
@@ -388,7 +393,7 @@ def delta_inputs(q, k, v, g, beta, scale: float | None = None) -> DeltaInputs:
     if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
         raise TypeError("q, k and v must have one dtype")
     (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
-    s = DeltaInputs(hk, hv, dk, dv, _dtype_code(k), dk ** -0.5 if scale is None else scale, qp, kp, vp,
+    s = DeltaInputs(hk, hv, dk, dv, _row_code(k), dk ** -0.5 if scale is None else scale, qp, kp, vp,
                     _of(g, torch.float32, (T, hv), "g"), _of(beta, torch.float32, (T, hv), "beta"), qs, ks, vs)
     # the struct holds raw device pointers: keep the tensors alive as long as it lives
     s._keepalive = (q, k, v, g, beta)
@@ -410,7 +415,7 @@ def precog_encode_chunks(inputs: ScanInputs, offsets, T_tot: int, states_out=Non
     _check(lib.precog_encode_chunks(
         ctypes.byref(inputs), _ptr(offsets), n_chunks, T_tot, _ptr(states_out),
         _dtype_code(states_out) if states_out is not None else PRECOG_F32, layer0, L_total,
-        _ptr(y_out), _dtype_code(y_out) if y_out is not None else PRECOG_F32, _stream(stream)))
+        _ptr(y_out), _row_code(y_out) if y_out is not None else PRECOG_F32, _stream(stream)))
 
 
 def precog_encode_chunks_ordered(inputs: ScanInputs, offsets, T_tot: int, order, states_out=None,
@@ -426,7 +431,7 @@ def precog_encode_chunks_ordered(inputs: ScanInputs, offsets, T_tot: int, order,
     _check(lib.precog_encode_chunks_ordered(
         ctypes.byref(inputs), _ptr(offsets), n_chunks, T_tot, _ptr(order), _ptr(states_out),
         _dtype_code(states_out) if states_out is not None else PRECOG_F32, layer0, L_total,
-        _ptr(y_out), _dtype_code(y_out) if y_out is not None else PRECOG_F32, _stream(stream)))
+        _ptr(y_out), _row_code(y_out) if y_out is not None else PRECOG_F32, _stream(stream)))
 
 
 def precog_encode_trajectory(inputs: ScanInputs, offsets, T_tot: int, stride: int, entry_offsets,
@@ -454,7 +459,7 @@ def precog_retrieve(index, queries, best_idx, best_score=None, workspace=None, s
     if workspace is None:
         workspace = _workspace(max(precog_retrieve_workspace_size(M, dim, Q), 16), index.device, stream)
     _check(lib.precog_retrieve(
-        _ptr(index), _dtype_code(index), M, dim, _ptr(queries), Q, _ptr(best_idx),
+        _ptr(index), _row_code(index), M, dim, _ptr(queries), Q, _ptr(best_idx),
         _ptr(best_score), _ptr(workspace), workspace.numel() * workspace.element_size(),
         _stream(stream)))
 
@@ -465,7 +470,7 @@ def precog_retrieve_noalloc(index, queries, best_idx, best_score=None, stream=No
     lib = load_library()
     M, dim = index.shape
     _check(lib.precog_retrieve_noalloc(
-        _ptr(index), _dtype_code(index), M, dim, _ptr(queries), queries.shape[0], _ptr(best_idx),
+        _ptr(index), _row_code(index), M, dim, _ptr(queries), queries.shape[0], _ptr(best_idx),
         _ptr(best_score), _stream(stream)))
 
 
@@ -479,7 +484,7 @@ def precog_retrieve_keys(index_shard, queries, row_offset: int, keys, workspace=
     if workspace is None:
         workspace = _workspace(max(precog_retrieve_workspace_size(M, dim, Q), 16), queries.device, stream)
     _check(lib.precog_retrieve_keys(
-        _ptr(index_shard), _dtype_code(index_shard), M, dim, _ptr(queries), Q, int(row_offset), _ptr(keys),
+        _ptr(index_shard), _row_code(index_shard), M, dim, _ptr(queries), Q, int(row_offset), _ptr(keys),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
@@ -497,7 +502,7 @@ def precog_prefill_from_state(inputs: ScanInputs, n_queries: int, T_q: int, bank
     entries, L_bank = bank.shape[0], bank.shape[1]
     _check(lib.precog_prefill_from_state(
         ctypes.byref(inputs), n_queries, T_q, _ptr(bank), _dtype_code(bank), entries, L_bank,
-        layer0, _ptr(idx), _ptr(y_out), _dtype_code(y_out) if y_out is not None else PRECOG_F32,
+        layer0, _ptr(idx), _ptr(y_out), _row_code(y_out) if y_out is not None else PRECOG_F32,
         _ptr(state_out), _dtype_code(state_out) if state_out is not None else PRECOG_F32,
         _stream(stream)))
 
@@ -514,7 +519,7 @@ def precog_retrieve_topk(index, queries, k, best_idx, best_score=None, workspace
     if workspace is None:
         workspace = _workspace(max(int(lib.precog_retrieve_topk_workspace_size(M, dim, Q)), 16), index.device, stream)
     _check(lib.precog_retrieve_topk(
-        _ptr(index), _dtype_code(index), M, dim, _ptr(queries), Q, k, _ptr(best_idx),
+        _ptr(index), _row_code(index), M, dim, _ptr(queries), Q, k, _ptr(best_idx),
         _ptr(best_score), _ptr(workspace), workspace.numel() * workspace.element_size(),
         _stream(stream)))
 
@@ -528,7 +533,7 @@ def precog_prefill_composed(inputs: ScanInputs, n_queries: int, T_q: int, bank, 
     _check(lib.precog_prefill_composed(
         ctypes.byref(inputs), n_queries, T_q, _ptr(bank), _dtype_code(bank), entries, L_bank, layer0,
         k, _ptr(idx), _ptr(scores), temperature, _ptr(y_out),
-        _dtype_code(y_out) if y_out is not None else PRECOG_F32, _ptr(state_out),
+        _row_code(y_out) if y_out is not None else PRECOG_F32, _ptr(state_out),
         _dtype_code(state_out) if state_out is not None else PRECOG_F32, _stream(stream)))
 
 
@@ -539,7 +544,7 @@ def precog_smc_route(embeddings, domain_protos, sub_protos, J, out_domain, out_s
     n, dim = embeddings.shape
     M, J_max = sub_protos.shape[0], sub_protos.shape[1]
     _check(lib.precog_smc_route(
-        _ptr(embeddings), _dtype_code(embeddings), n, dim, _ptr(domain_protos), M, _ptr(sub_protos),
+        _ptr(embeddings), _row_code(embeddings), n, dim, _ptr(domain_protos), M, _ptr(sub_protos),
         J_max, _ptr(J), _ptr(out_domain), _ptr(out_sub), _ptr(out_slot), _stream(stream)))
 
 
@@ -549,7 +554,7 @@ def precog_smc_consolidate(semantic, states, slots, alpha: float, stream=None):
     n_slots = semantic.shape[0]
     elems = semantic[0].numel() if n_slots else 0
     _check(lib.precog_smc_consolidate(
-        _ptr(semantic), n_slots, elems, _ptr(states), _dtype_code(states), _ptr(slots),
+        _ptr(semantic), n_slots, elems, _ptr(states), _row_code(states), _ptr(slots),
         states.shape[0], alpha, _stream(stream)))
 
 
@@ -588,11 +593,11 @@ def precog_delta_scan(inputs: DeltaInputs, offsets, T_tot: int, bank=None, idx=N
         workspace = _workspace(need, offsets.device, stream) if need else None
     _check(lib.precog_delta_scan(
         ctypes.byref(inputs), _of(offsets, torch.int64, (n + 1,), "offsets"), n, T_tot, _ptr(bank),
-        _dtype_code(bank) if bank is not None else PRECOG_F32, bank.shape[0] if bank is not None else 0,
+        _row_code(bank) if bank is not None else PRECOG_F32, bank.shape[0] if bank is not None else 0,
         _of(idx, torch.int64, (n,), "idx"), _ptr(states_out),
-        _dtype_code(states_out) if states_out is not None else PRECOG_F32, layer,
+        _row_code(states_out) if states_out is not None else PRECOG_F32, layer,
         holder.shape[1] if holder is not None else 1, _ptr(y_out),
-        _dtype_code(y_out) if y_out is not None else PRECOG_F32, _ptr(workspace),
+        _row_code(y_out) if y_out is not None else PRECOG_F32, _ptr(workspace),
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream)))
 
 
@@ -609,7 +614,7 @@ def precog_delta_step(inputs: DeltaInputs, states, slots=None, y_out=None, layer
         raise ValueError("y_out must be [n, Hv, dv]")
     _check(load_library().precog_delta_step(
         ctypes.byref(inputs), n, _ptr(states), states.shape[0], _of(slots, torch.int64, (n,), "slots"), layer,
-        states.shape[1], _ptr(y_out), _dtype_code(y_out), _stream(stream)))
+        states.shape[1], _ptr(y_out), _row_code(y_out), _stream(stream)))
 
 
 _NORMS = {"none": PRECOG_NORM_NONE, "l2": PRECOG_NORM_L2, "rms": PRECOG_NORM_RMS}
@@ -635,7 +640,7 @@ def precog_qk_norm_rope(q, k, q_out, k_out, norm: str = "l2", q_weight=None, k_w
     (qp, qs), (kp, ks) = _rows(q, "q"), _rows(k, "k")
     (qo, qos), (ko, kos) = _rows(q_out, "q_out"), _rows(k_out, "k_out")
     n_pos, half = cos.shape if cos is not None else (0, 0)
-    args = QkNormArgs(hq, hk, d, 2 * half, _dtype_code(q), _NORMS[norm], int(interleaved), eps, qp, kp, qo, ko, qs,
+    args = QkNormArgs(hq, hk, d, 2 * half, _row_code(q), _NORMS[norm], int(interleaved), eps, qp, kp, qo, ko, qs,
                       ks, qos, kos, _of(q_weight, torch.float32, (d,), "q_weight"),
                       _of(k_weight, torch.float32, (d,), "k_weight"), _of(cos, torch.float32, (n_pos, half), "cos"),
                       _of(sin, torch.float32, (n_pos, half), "sin"), n_pos,
@@ -655,7 +660,7 @@ def precog_token_logprobs(logits, tokens, logprob, entropy=None, top_idx=None, t
     k = top_idx.shape[1] if top_idx is not None else 0
     lp, stride = _rows(logits, "logits")
     _check(load_library().precog_token_logprobs(
-        lp, _dtype_code(logits), R, V, stride, _of(tokens, torch.int64, (R,), "tokens"), temperature, k,
+        lp, _row_code(logits), R, V, stride, _of(tokens, torch.int64, (R,), "tokens"), temperature, k,
         _of(logprob, torch.float32, (R,), "logprob"), _of(entropy, torch.float32, (R,), "entropy"),
         _of(top_idx, torch.int64, (R, k), "top_idx"), _of(top_logprob, torch.float32, (R, k), "top_logprob"),
         _stream(stream)))
@@ -764,7 +769,7 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
     if bank is not None and windows_out is not None and layers != out_layers:
         raise ValueError("bank and windows_out must have the same number of layers")
     call, pack = _packed_calls["precog_causal_conv"]
-    _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
+    _check(call(pack(_row_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
                      _dense(weight, (D, K), torch.float32, device, "weight"),
                      _dense(bias, (D,), torch.float32, device, "bias")),
                 _dense(offsets, (n + 1,), torch.int64, device, "offsets"), n, T, bp, entries,
@@ -786,7 +791,7 @@ def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = Tru
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
     wp, n_slots, layers = _table(windows, K - 1, D, dtype, device, "windows")
     call, pack = _packed_calls["precog_conv_step"]
-    _check(call(pack(_dtype_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
+    _check(call(pack(_row_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
                      _dense(weight, (D, K), torch.float32, device, "weight"),
                      _dense(bias, (D,), torch.float32, device, "bias")),
                 n, wp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer, layers, _stream_on(device, stream)))
@@ -828,7 +833,7 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
         ctypes.byref(inputs),
         pack(sp, n_slots, _dense(slots, (n,), torch.int64, device, "slots"), layer0, layers,
              _dense(skip, (L, D), torch.float32, device, "skip"), gp, gs, gls,
-             _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _dtype_code(y_out), 0), n, _stream_on(device, stream)))
+             _dense(y_out, (L, n, D), y_out.dtype, device, "y_out"), _row_code(y_out), 0), n, _stream_on(device, stream)))
 
 
 def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_first: bool = True, weight=None,
@@ -860,14 +865,14 @@ def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_f
         gp, gs = _matrix(gate, shape, dtype, device, "gate")
     res_dtype, res_code = f32, PRECOG_F32
     if residual is not None:
-        res_dtype, res_code = residual.dtype, _dtype_code(residual)
+        res_dtype, res_code = residual.dtype, _row_code(residual)
         rp, rs = _matrix(residual, shape, res_dtype, device, "residual")
     if residual_out is not None:
         rop, ros = _matrix(residual_out, shape, res_dtype, device, "residual_out")
     if out is not None:
         op, os_ = _matrix(out, shape, dtype, device, "out")
     call, pack = _packed_calls["precog_block_norm"]
-    _check(call(pack(_dtype_code(x), res_code, D, groups, kind, 1 if gate_first else 0, scale, eps, xp, sp, gp, rp, rop,
+    _check(call(pack(_row_code(x), res_code, D, groups, kind, 1 if gate_first else 0, scale, eps, xp, sp, gp, rp, rop,
                      op, xs, ss, gs, rs, ros, os_, _dense(skip, vec, f32, device, "skip"),
                      _dense(weight, vec, f32, device, "weight"), scale_weight,
                      _dense(out_weight, vec, f32, device, "out_weight")), T, _stream_on(device, stream)))
@@ -899,7 +904,7 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
     nb = bias.numel() if bias is not None else 0
     nm = mask.shape[0] if mask is not None else 0
     call, pack = _packed_calls["precog_adjust_logits"]
-    _check(call(pack(_dtype_code(logits), 0, V, ls, os_, lp, op, _dense(history, (nh,), i64, device, "history"),
+    _check(call(pack(_row_code(logits), 0, V, ls, os_, lp, op, _dense(history, (nh,), i64, device, "history"),
                      _dense(history_offsets, ends, i64, device, "history_offsets"),
                      _dense(count_from, row, i64, device, "count_from"), nh,
                      _dense(repetition, row, f32, device, "repetition"),
