@@ -739,7 +739,8 @@ precog_status precog_block_norm(const precog_block_norm_args *args, int64_t T, v
  *                 token that a row names twice the last bias counts
  *   d_mask        device int32 [n_masks][ceil(vocab / 32)]: bit i % 32 of word i / 32 allows token i
  *   d_mask_rows   device int64 [n_rows]: the row's mask (-1: everything is allowed; other values
- *                 outside [0, n_masks) likewise, and flag PRECOG_DEV_BAD_INDEX); NULL: mask r
+ *                 outside [0, n_masks) likewise, and flag PRECOG_DEV_BAD_INDEX); NULL: mask r, and
+ *                 n_masks must be at least n_rows where there is a d_mask
  * Tokens of -1 in a list are ignored (padding); others outside [0, vocab) are ignored and flag
  * PRECOG_DEV_BAD_INDEX. A list whose offsets decrease or leave [0, n_history] or [0, n_bias] is
  * empty and flags PRECOG_DEV_BAD_OFFSETS. Lists are shorter than 2^30 in all; they and the vectors

@@ -903,6 +903,8 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
     nh = history.numel() if history is not None else 0
     nb = bias.numel() if bias is not None else 0
     nm = mask.shape[0] if mask is not None else 0
+    if mask is not None and mask_rows is None and nm < R:   # (an empty mask has no address: the C call would see none)
+        raise ValueError("mask_rows is None but there are fewer masks than rows")
     call, pack = _packed_calls["precog_adjust_logits"]
     _check(call(pack(_row_code(logits), 0, V, ls, os_, lp, op, _dense(history, (nh,), i64, device, "history"),
                      _dense(history_offsets, ends, i64, device, "history_offsets"),

@@ -1106,7 +1106,7 @@ precog_status precog_adjust_logits(const precog_adjust_args *a, int64_t n_rows, 
         return fail(PRECOG_ERR_INVALID_ARG, "n_history > 0 needs d_history");
     if (a->n_bias > 0 && (a->d_bias_idx == nullptr || a->d_bias == nullptr || a->d_bias_offsets == nullptr))
         return fail(PRECOG_ERR_INVALID_ARG, "n_bias > 0 needs d_bias_idx, d_bias and d_bias_offsets");
-    if (a->d_mask_rows && a->d_mask == nullptr && a->n_masks > 0) return fail(PRECOG_ERR_INVALID_ARG, "d_mask_rows is given without d_mask");
+    if (a->n_masks > 0 && a->d_mask == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "n_masks > 0 needs d_mask");
     if (a->d_mask && a->d_mask_rows == nullptr && a->n_masks < n_rows)
         return fail(PRECOG_ERR_INVALID_ARG, "d_mask_rows is NULL but there are fewer masks than rows");
     precog::AdjustParams p;
