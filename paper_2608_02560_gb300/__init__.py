@@ -903,6 +903,7 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
     nh = history.numel() if history is not None else 0
     nb = bias.numel() if bias is not None else 0
     nm = mask.shape[0] if mask is not None else 0
+    mp = _dense(mask, (nm, (V + 31) // 32), torch.int32, device, "mask")
     if mask is not None and mask_rows is None and nm < R:   # (an empty mask has no address: the C call would see none)
         raise ValueError("mask_rows is None but there are fewer masks than rows")
     call, pack = _packed_calls["precog_adjust_logits"]
@@ -913,8 +914,7 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
                      _dense(frequency, row, f32, device, "frequency"), _dense(presence, row, f32, device, "presence"),
                      _dense(bias_idx, (nb,), i64, device, "bias_idx"), _dense(bias, (nb,), f32, device, "bias"),
                      _dense(bias_offsets, ends, i64, device, "bias_offsets"), nb,
-                     _dense(mask, (nm, (V + 31) // 32), torch.int32, device, "mask"), nm,
-                     _dense(mask_rows, row, i64, device, "mask_rows")), R, _stream_on(device, stream)))
+                     mp, nm, _dense(mask_rows, row, i64, device, "mask_rows")), R, _stream_on(device, stream)))
 
 
 def precog_selftest_wait_timeout(iterations: int = 4096, stream=None):
