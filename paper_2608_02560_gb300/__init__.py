@@ -768,12 +768,15 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
         raise ValueError("windows_out must have one entry per sequence")
     if bank is not None and windows_out is not None and layers != out_layers:
         raise ValueError("bank and windows_out must have the same number of layers")
+    if bank is not None and idx is None and entries < n:   # (an empty bank has no address: the C call would see none)
+        raise ValueError("idx is None but bank has fewer rows than sequences")
+    L_total = out_layers if windows_out is not None else layers if bank is not None else layer + 1
     call, pack = _packed_calls["precog_causal_conv"]
     _check(call(pack(_row_code(x), D, K, 1 if silu else 0, xp, yp, xs, ys,
                      _dense(weight, (D, K), torch.float32, device, "weight"),
                      _dense(bias, (D,), torch.float32, device, "bias")),
                 _dense(offsets, (n + 1,), torch.int64, device, "offsets"), n, T, bp, entries,
-                _dense(idx, (n,), torch.int64, device, "idx"), wp, layer, out_layers or layers or layer + 1,
+                _dense(idx, (n,), torch.int64, device, "idx"), wp, layer, L_total,
                 _stream_on(device, stream)))
 
 
