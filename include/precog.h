@@ -587,7 +587,8 @@ precog_status precog_token_logprobs(const void *logits, int32_t dtype, int64_t n
  *   x, y     [rows][dim] in `dtype` (F32 or BF16), rows x_stride / y_stride elements apart
  *            (at least dim; ignored where there is at most one row)
  *   weight   fp32 [dim][kernel], bias fp32 [dim] or NULL
- * Sums are fp32. Requirements: dim a multiple of 8, kernel 2, 3 or 4; pointers and row
+ * Sums are fp32; SiLU is within 2^-21 of its value, and where it goes into BF16 within
+ * (5 + 1.2 |a|) 2^-23. Requirements: dim a multiple of 8, kernel 2, 3 or 4; pointers and row
  * strides 16-byte aligned.
  */
 typedef struct precog_conv_args {
@@ -655,6 +656,7 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
  *   gate      [L][n][D] in in->in_dtype, rows gate_stride and layers gate_layer_stride elements
  *             apart, or NULL: none
  *   y_out     device [L][n][D] in y_dtype (F32 or BF16)
+ * SiLU is as the convolution's: within 2^-21, and from BF16 inputs into a BF16 y_out the other.
  * y_out, states and the inputs must not share memory.
  */
 typedef struct precog_scan_step_args {
@@ -687,8 +689,9 @@ precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_s
  *   x, skip_input, gate, out    [T][dim] in `dtype` (F32 or BF16), each with its own row stride
  *   residual, residual_out      [T][dim] in residual_dtype (F32; or BF16 where dtype is BF16)
  *   skip, weight, scale_weight, out_weight   fp32 [dim], or NULL: no skip, and 1
- * Arithmetic is fp32 from end to end: h goes into its norm before it is rounded. Outputs may be
- * the very rows of an input of the same type; otherwise nothing may share memory with them.
+ * Arithmetic is fp32 from end to end: h goes into its norm before it is rounded, and SiLU is as the
+ * convolution's (within 2^-21 where there is an F32 output). Outputs may be the very rows of an
+ * input of the same type; otherwise nothing may share memory with them.
  * Requirements: dim / groups a multiple of 8, at most 16384; groups == 1 where both residual
  * and out are given; pointers and row strides 16-byte aligned.
  */

@@ -55,20 +55,22 @@ __device__ __forceinline__ void weights(const float *w, int e, float (&v)[V]) {
 enum Form { kAll, kInside, kBetween };   // (inside a block: no residual; between two: no skip, no gate)
 // CTAs an SM that the registers have to be enough for: 48 warps of kInside (rows of 4096 above: 32 warps 329 us, 40 304,
 // 48 300; several rows a CTA spill there, 379 in groups of 256 where 40 take 304). Between blocks 40 warps would spill.
-template <typename T, Form FORM, int LANES, int ENTRIES>
+template <typename T, typename TR, Form FORM, int LANES, int ENTRIES>
 constexpr int min_ctas() {
     constexpr int block = LANES > 128 ? LANES : 128;
     if (LANES > 512) return 1;
     if (sizeof(T) == 4 && LANES == 512 && ENTRIES == 16) return 2;   // (8192: 165 us with one, 113 with two, 178 with three)
     if (FORM == kInside) return (LANES <= 64 ? 1280 : 1536) / block;
     if (sizeof(T) == 4 && LANES == 512 && FORM == kBetween) return 3;
+    if (sizeof(T) < sizeof(TR) && FORM == kAll && LANES <= 128) return 7;   // (72 registers, gate to fp32: 65,521 rows of 2048 276 us, with 80 289)
     return 1;
 }
 
 template <typename T, typename TR, Form FORM, int LANES, int ENTRIES>
-__global__ void __launch_bounds__(LANES > 128 ? LANES : 128, min_ctas<T, FORM, LANES, ENTRIES>()) block_norm_kernel(const BlockNormParams p, int64_t rows) {
+__global__ void __launch_bounds__(LANES > 128 ? LANES : 128, min_ctas<T, TR, FORM, LANES, ENTRIES>()) block_norm_kernel(const BlockNormParams p, int64_t rows) {
     grid_dependency_wait();
     constexpr bool kRes = FORM != kInside, kSkipGate = FORM != kBetween;
+    using Widest = std::conditional_t<kRes, TR, T>;   // of the outputs: what the gate has to be exact for
     // Entries in one piece: 16 bytes of a row. Of long bf16 rows beside an fp32 residual 8, so that a warp reads that and the
     // weights in whole lines (rows of 4096: 89 us where 16 bytes take 97, of 8192 102 and 115; of 2048 they are equal, a
     // single row 2.5 and 2.1).
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(LANES > 128 ? LANES : 128, min_ctas<T, FORM, L
             float s[V];
             unpack(g[c], s);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[c][i] *= silu<T>(s[i]);
+            for (int i = 0; i < V; ++i) v[c][i] *= silu<T, Widest>(s[i]);
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) sum = fmaf(v[c][i], v[c][i], sum);
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(LANES > 128 ? LANES : 128, min_ctas<T, FORM, L
             float s[V];
             unpack(g[c], s);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[c][i] *= silu<T>(s[i]);
+            for (int i = 0; i < V; ++i) v[c][i] *= silu<T, Widest>(s[i]);
         }
         if (kRes && p.residual) {
             float r[V];

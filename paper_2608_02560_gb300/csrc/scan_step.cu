@@ -43,6 +43,11 @@ __device__ __forceinline__ bool usable(const ScanStepParams &p, int64_t slot, bo
     if (slot != -1 && flag) atomicOr(&g_scan_step_status, PRECOG_DEV_BAD_INDEX);
     return false;
 }
+// y times SiLU of a gate of type T, as exact as y is stored.
+template <typename T>
+__device__ __forceinline__ float gated(const ScanStepParams &p, float y, float gate) {
+    return y * (p.y_dtype == PRECOG_F32 ? silu<T, float>(gate) : silu<T>(gate));
+}
 __device__ __forceinline__ void store_y(const ScanStepParams &p, int64_t at, float y) {
     if (p.y_dtype == PRECOG_F32) static_cast<float *>(p.y)[at] = y;
     else static_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(y);
@@ -160,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanStepParam
             if (!inside) continue;
             if (state != nullptr) {
                 if (p.skip) y = fmaf(skip, high ? (odd ? x[3] : x[2]) : (odd ? x[1] : x[0]), y);
-                if (p.gate) y *= silu<T>(gate);
+                if (p.gate) y = gated<T>(p, y, gate);
             }
             store_y(p, (l * p.n + i) * p.D + d + part, y);
         }
@@ -220,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) scan_step_complex_kernel(const ScanS
         if (!inside || part != 0) continue;
         if (live) {
             if (p.skip) sum = fmaf(skip, x, sum);
-            if (p.gate) sum *= silu<T>(gate);
+            if (p.gate) sum = gated<T>(p, sum, gate);
         }
         store_y(p, (l * p.n + i) * p.D + d, sum);
     }
