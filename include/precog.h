@@ -623,7 +623,8 @@ typedef struct precog_conv_args {
  *   windows_out  device [n_seqs][L_total][kernel-1][dim] in `dtype`: layer `layer` of entry c
  *                receives the window that the token behind sequence c needs (its last inputs,
  *                the older of them its own window's where it is shorter); or NULL
- * y, windows_out, x and bank must not share memory (rows of x and y may be slices of one buffer).
+ * y, windows_out, x and bank must not share memory (rows of x and y may be slices of one buffer), nor
+ * may y and windows_out with weight, bias, d_offsets and d_idx.
  */
 precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_offsets, int64_t n_seqs,
                                  int64_t T_tot, const void *bank, int64_t bank_entries, const int64_t *d_idx,
@@ -634,7 +635,7 @@ precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_
  * windows that is updated in place (row i of x is the next input of the sequence whose window
  * is windows[d_slots[i]][layer]).
  *   windows   device [n_slots][L_total][kernel-1][dim] in `dtype`; must not share memory with
- *             x or y (y may be x itself)
+ *             x or y (y may be x itself); neither may windows and y with weight, bias and d_slots
  *   d_slots   as precog_delta_step: each slot at most once (not verified: repeated slots race);
  *             NULL: row i; -1: an idle row, whose y is zeroed; any other slot outside
  *             [0, n_slots) likewise, and flags PRECOG_DEV_BAD_INDEX
@@ -657,7 +658,7 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
  *             apart, or NULL: none
  *   y_out     device [L][n][D] in y_dtype (F32 or BF16)
  * SiLU is as the convolution's: within 2^-21, and from BF16 inputs into a BF16 y_out the other.
- * y_out, states and the inputs must not share memory.
+ * y_out, states and the inputs (skip and d_slots among them) must not share memory.
  */
 typedef struct precog_scan_step_args {
     void *states;
@@ -734,7 +735,8 @@ precog_status precog_block_norm(const precog_block_norm_args *args, int64_t T, v
  *   z <- -infinity                                            where the row's mask has bit i clear
  * and out[r][i] is z rounded to `dtype`. Any of them may be NULL.
  *   logits, out   device [n_rows][vocab] in `dtype` (F32, BF16 or F16), rows `stride` and
- *                 out_stride elements apart (any alignment of the elements); out may be logits
+ *                 out_stride elements apart (any alignment of the elements); out may be logits,
+ *                 and its rows share no memory with anything else
  *   d_history     device int64 tokens; row r's are entries d_history_offsets[r] ..
  *                 d_history_offsets[r+1]-1 (its prompt, then its answer)
  *   d_count_from  device int64 [n_rows] (e.g. the prompts' lengths), clamped to the history; NULL: 0

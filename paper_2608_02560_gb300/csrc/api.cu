@@ -192,6 +192,27 @@ RowSpan whole(const RowSpan &a, int64_t n) {
     return RowSpan{a.at, 0, bytes > INT64_MAX ? INT64_MAX : static_cast<int64_t>(bytes)};
 }
 
+// Whether one of n rows shares memory with `bytes` at `at`. What lies between strided rows is nobody's.
+bool touches(const RowSpan &a, int64_t n, const void *at, __int128 bytes) {
+    if (a.at == nullptr || at == nullptr || n == 0 || a.row == 0 || bytes <= 0) return false;
+    using wide = __int128;
+    const wide pa = static_cast<wide>(reinterpret_cast<uintptr_t>(a.at)), pb = static_cast<wide>(reinterpret_cast<uintptr_t>(at));
+    wide i = 0;   // the first row that ends behind `at`
+    if (n > 1 && a.stride > 0 && pb - pa >= a.row) i = (pb - pa - a.row) / a.stride + 1;
+    return i < n && pa + i * a.stride + a.row > pb && pa + i * a.stride < pb + bytes;
+}
+
+// The same of several lists (what is not given is nullptr).
+struct List {
+    const void *at;
+    __int128 bytes;
+};
+bool touches_any(const RowSpan &a, int64_t n, std::initializer_list<List> lists) {
+    for (const List &list : lists)
+        if (touches(a, n, list.at, list.bytes)) return true;
+    return false;
+}
+
 // Checks shared by the convolution's two calls; fills what they have in common.
 precog_status check_conv(const precog_conv_args *a, int64_t rows, int32_t layer, int32_t L_total, precog::ConvParams *p) {
     if (a == nullptr) return fail(PRECOG_ERR_INVALID_ARG, "arguments pointer is NULL");
@@ -896,6 +917,9 @@ precog_status precog_causal_conv(const precog_conv_args *args, const int64_t *d_
     if (overlap(from, to, 1, false)) return fail(PRECOG_ERR_INVALID_ARG, "windows_out must not share memory with bank");
     if (overlap(whole(x, T_tot), to, 1, false) || overlap(whole(y, T_tot), to, 1, false) || overlap(whole(y, T_tot), from, 1, false))
         return fail(PRECOG_ERR_INVALID_ARG, "windows and rows must not share memory");
+    for (const auto &[out, n] : {std::pair(y, T_tot), std::pair(to, static_cast<int64_t>(1))})
+        if (touches_any(out, n, {{p.weight, 4LL * p.dim * p.kernel}, {p.bias, 4LL * p.dim}, {d_offsets, 8 * (n_seqs + 1)}, {d_idx, 8 * n_seqs}}))
+            return fail(PRECOG_ERR_INVALID_ARG, "y and windows_out must not share memory with weight, bias, d_offsets or d_idx");
     if (n_seqs == 0) return ok();
     p.offsets = d_offsets;
     p.n_seqs = n_seqs;
@@ -930,6 +954,9 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
         return fail(PRECOG_ERR_UNSUPPORTED, "tables beyond 2^63 bytes");
     if (overlap(whole(x, n), table, 1, false) || overlap(whole(y, n), table, 1, false))
         return fail(PRECOG_ERR_INVALID_ARG, "windows and rows must not share memory");
+    for (const auto &[out, rows] : {std::pair(y, n), std::pair(table, static_cast<int64_t>(1))})
+        if (touches_any(out, rows, {{p.weight, 4LL * p.dim * p.kernel}, {p.bias, 4LL * p.dim}, {d_slots, 8 * n}}))
+            return fail(PRECOG_ERR_INVALID_ARG, "y and windows must not share memory with weight, bias or d_slots");
     if (n == 0) return ok();
     p.n_seqs = n;
     p.T_tot = n;
@@ -983,7 +1010,9 @@ precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_s
     RowSpan table;
     if (!table_span(states, n_slots, L_total, 4LL * parts * in->D * in->N, &table))
         return fail(PRECOG_ERR_UNSUPPORTED, "tables beyond 2^63 bytes");
-    bool shared = overlap(y, table, 1, false);
+    const int64_t skip_bytes = 4LL * in->n_layers * in->D;
+    bool shared = overlap(y, table, 1, false) || touches_any(y, 1, {{skip, skip_bytes}, {d_slots, 8 * n}}) ||
+                  touches_any(table, 1, {{skip, skip_bytes}, {d_slots, 8 * n}});
     for (const RowSpan &r : inputs) shared = shared || overlap(r, table, 1, false) || overlap(r, y, 1, false);
     if (shared) return fail(PRECOG_ERR_INVALID_ARG, "y_out, states and inputs must not share memory");
     precog::ScanStepParams p;
@@ -1125,6 +1154,12 @@ precog_status precog_adjust_logits(const precog_adjust_args *a, int64_t n_rows, 
     if (a->n_bias > 0) p.bias_idx = a->d_bias_idx, p.bias = a->d_bias, p.bias_offsets = a->d_bias_offsets, p.n_bias = a->n_bias;
     if (a->d_mask) p.mask = reinterpret_cast<const uint32_t *>(a->d_mask), p.n_masks = a->n_masks;
     p.mask_rows = a->d_mask_rows;   // (without masks: each has to be -1)
+    const int64_t per_row = 8 * n_rows, words = (p.vocab + 31) / 32;
+    if (touches_any(RowSpan{p.out, p.out_stride * sz, p.vocab * sz}, n_rows,
+                    {{p.history, 8 * p.n_history}, {p.history_offsets, per_row + 8}, {p.count_from, per_row}, {p.repetition, per_row / 2},
+                     {p.frequency, per_row / 2}, {p.presence, per_row / 2}, {p.bias_idx, 8 * p.n_bias}, {p.bias, 4 * p.n_bias},
+                     {p.bias_offsets, per_row + 8}, {p.mask, static_cast<__int128>(4 * words) * p.n_masks}, {p.mask_rows, per_row}}))
+        return fail(PRECOG_ERR_INVALID_ARG, "out must not share memory with lists, vectors or masks");
     cudaError_t e = precog::launch_adjust(p, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "logit adjustment launch");
     return ok();

@@ -71,8 +71,8 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&v)[4
 //   into 16 bits: the quick exponential and reciprocal, together within (5 + 1.2 |x|) 2^-23 of the value (2^-19 while
 //   |x| < 10), far below the rounding; where e^-x leaves 2^126 they give 0;
 //   into fp32: the same two with their errors taken back, within 7 * 2^-24 of the value. What -x log2(e) loses is an fma's
-//   difference, and enters as 2^low = 1 + low ln 2 (|low| < 2^-17); the quotient is q + (x - d q) r. 4 for the
-//   exponential, and one each for its product with 1 + low ln 2, for d, and for the quotient. (65,521 rows of 2048, gate,
+//   difference (Dekker's product in two parts), and enters as 2^low = 1 + low ln 2 (|low| < 2^-17); the quotient is
+//   q + (x - d q) r (Markstein's correction by the residual). 4 for the exponential, and one each for its product with 1 + low ln 2, for d, and for the quotient. (65,521 rows of 2048, gate,
 //   norm, fp32 residual, next norm: 276 us; with the 16-bit form 267, with expf and a quotient 292.)
 constexpr float kMinusLog2e = -1.4426950408889634f;
 constexpr float kMinusLog2eLow = -1.9259629911266175e-8f;   // what the constant above lacks
