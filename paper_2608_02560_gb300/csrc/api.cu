@@ -940,7 +940,7 @@ precog_status precog_conv_step(const precog_conv_args *args, int64_t n, void *wi
     precog::ConvParams p;
     precog_status s = check_conv(args, n, layer, L_total, &p);
     if (s != PRECOG_OK) return s;
-    if (windows == nullptr || !aligned16(windows))
+    if ((n > 0 && windows == nullptr) || !aligned16(windows))
         return fail(PRECOG_ERR_INVALID_ARG, "windows must be non-NULL and 16-byte aligned");
     if (n_slots < 0) return fail(PRECOG_ERR_INVALID_ARG, "n_slots must be >= 0");
     if (!aligned_to(8, {d_slots})) return fail(PRECOG_ERR_INVALID_ARG, "d_slots not 8-byte aligned");
@@ -980,7 +980,7 @@ precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_s
     if (n > 0x7fffffffLL) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
     precog_status s = check_scan_inputs(in, n, true);
     if (s != PRECOG_OK) return s;
-    if (states == nullptr || !aligned16(states))
+    if ((n > 0 && states == nullptr) || !aligned16(states))
         return fail(PRECOG_ERR_INVALID_ARG, "states must be non-NULL and 16-byte aligned");
     if (layer0 < 0 || L_total < 1 || static_cast<int64_t>(layer0) + in->n_layers > L_total)
         return fail(PRECOG_ERR_INVALID_ARG, "layers [layer0, layer0+n_layers) exceed L_total");
@@ -988,7 +988,7 @@ precog_status precog_scan_step(const precog_scan_inputs *in, const precog_scan_s
     if (!aligned_to(8, {d_slots})) return fail(PRECOG_ERR_INVALID_ARG, "d_slots not 8-byte aligned");
     if (d_slots == nullptr && n_slots < n)
         return fail(PRECOG_ERR_INVALID_ARG, "d_slots is NULL but the table has fewer slots than rows");
-    if (y_out == nullptr || !state_dtype_ok(y_dtype) || !aligned16(y_out))
+    if ((n > 0 && y_out == nullptr) || !state_dtype_ok(y_dtype) || !aligned16(y_out))
         return fail(PRECOG_ERR_INVALID_ARG, "y_out must be 16-byte aligned F32 or BF16");
     if (!aligned16(skip) || !aligned16(gate)) return fail(PRECOG_ERR_INVALID_ARG, "skip and gate must be 16-byte aligned");
     if (gate) {
@@ -1052,14 +1052,14 @@ precog_status precog_block_norm(const precog_block_norm_args *a, int64_t T, void
         return fail(PRECOG_ERR_INVALID_ARG, "norm must be PRECOG_NORM_NONE or _RMS");
     if (a->gate_first != 0 && a->gate_first != 1) return fail(PRECOG_ERR_INVALID_ARG, "gate_first must be 0 or 1");
     if (!(a->eps >= 0.f)) return fail(PRECOG_ERR_INVALID_ARG, "eps must be >= 0");
+    if (a->residual && a->out && a->groups != 1)
+        return fail(PRECOG_ERR_UNSUPPORTED, "groups are not implemented with a norm of the residual");
+    if (T > 0x7fffffffLL / a->groups) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
+    if (T == 0) return ok();   // (rows of which there are none need no address)
     if ((a->skip == nullptr) != (a->skip_input == nullptr))
         return fail(PRECOG_ERR_INVALID_ARG, "skip and skip_input must be given together");
     if ((a->residual == nullptr) != (a->residual_out == nullptr))
         return fail(PRECOG_ERR_INVALID_ARG, "residual and residual_out must be given together");
-    if (a->residual && a->out && a->groups != 1)
-        return fail(PRECOG_ERR_UNSUPPORTED, "groups are not implemented with a norm of the residual");
-    if (T > 0x7fffffffLL / a->groups) return fail(PRECOG_ERR_UNSUPPORTED, "too many rows for one call");
-    if (T == 0) return ok();
     if (a->x == nullptr || (a->out == nullptr && a->residual_out == nullptr))
         return fail(PRECOG_ERR_INVALID_ARG, "x and one of out and residual_out must be non-NULL");
     precog::BlockNormParams p;
