@@ -62,6 +62,7 @@ class ScanInputs(ctypes.Structure):
                 ("x", ctypes.c_void_p), ("dt", ctypes.c_void_p),
                 ("B", ctypes.c_void_p), ("C", ctypes.c_void_p), ("A", ctypes.c_void_p),
                 ("layer_stride_xd", ctypes.c_int64), ("layer_stride_bc", ctypes.c_int64)]
+    rows = device = None     # of the tensors behind it, where scan_inputs made it
 
 
 class DeltaInputs(ctypes.Structure):
@@ -805,24 +806,29 @@ def precog_scan_step(inputs: ScanInputs, states, slots=None, layer0: int = 0, sk
     """One token of the diagonal scan for each of the n rows that ``inputs`` (x, dt ``[L, n, D]``) has, on the
     fp32 (complex A: complex64) table ``states [slots, layers, D, N]``, updated in place, at the rows' int64
     ``slots`` (-1: an idle row), into ``y_out [L, n, D]``: the readout, plus fp32 ``skip [L, D]`` times x,
-    times SiLU of ``gate [L, n, D]`` (each row contiguous)."""
+    times SiLU of ``gate [L, n, D]`` (each row contiguous). Inputs that were filled field by field do not know
+    their rows; ``y_out`` says how many there are."""
+    if y_out is None:
+        raise ValueError("y_out is required")
     torch, device = _torch(), _current_device()
     L, D, N, n = inputs.n_layers, inputs.D, inputs.N, inputs.rows
-    if inputs.device != device:
-        _elsewhere(inputs._keepalive[0], "the inputs", device)
     if L == 1:   # [n, D] stands for one layer's [1, n, D]
-        y_out = y_out.unsqueeze(0) if y_out is not None and y_out.dim() == 2 else y_out
+        y_out = y_out.unsqueeze(0) if y_out.dim() == 2 else y_out
         gate = gate.unsqueeze(0) if gate is not None and gate.dim() == 2 else gate
         skip = skip.unsqueeze(0) if skip is not None and skip.dim() == 1 else skip
     sp, n_slots, layers = _table(states, D, N, torch.complex64 if inputs.a_kind == PRECOG_A_COMPLEX else torch.float32,
                                  device, "states")
-    if y_out is None:
-        raise ValueError("y_out is required")
+    if n is None:
+        if y_out.dim() != 3:
+            raise ValueError(f"y_out must be [L, n, D], got {tuple(y_out.shape)}")
+        n = y_out.shape[1]
+    elif inputs.device != device:
+        _elsewhere(inputs._keepalive[0], "the inputs", device)
     gp = gs = gls = 0
     if gate is not None:
         if gate.shape != (L, n, D):
             raise ValueError("gate must be [L, n, D]")
-        if gate.dtype is not inputs._keepalive[0].dtype:
+        if _row_code(gate) != inputs.in_dtype:
             raise TypeError("gate and x must have one dtype")
         if gate.get_device() != device:
             _elsewhere(gate, "gate", device)
