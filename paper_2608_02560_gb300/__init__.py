@@ -694,6 +694,10 @@ def _elsewhere(t, what: str, device: int):
     raise ValueError(f"{what} must live on the current device, cuda:{device}, where the library launches")
 
 
+def _no_matrix(t, what: str):
+    raise ValueError(f"{what} must be a matrix, got {tuple(t.shape)}")
+
+
 def _matrix(t, shape, dtype, device: int, what: str):
     """(pointer, elements between rows) of a tensor ``[rows, n]`` whose rows are contiguous; None: (0, 0)."""
     if t is None:
@@ -759,8 +763,10 @@ def precog_causal_conv(x, weight, offsets, bias=None, silu: bool = True, bank=No
     if idx is not None and bank is None:
         raise ValueError("idx is given without bank")
     load_library()
-    torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
-    (T, D), K, n = shape, weight.shape[-1], offsets.numel() - 1
+    torch, device, dtype, shape, taps = _torch(), _current_device(), x.dtype, x.shape, weight.shape
+    if len(shape) != 2 or len(taps) != 2:
+        _no_matrix(*((x, "x") if len(shape) != 2 else (weight, "weight")))
+    (T, D), K, n = shape, taps[1], offsets.numel() - 1
     xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
     bp, entries, layers = _table(bank, K - 1, D, dtype, device, "bank")
@@ -789,8 +795,10 @@ def precog_conv_step(x, weight, windows, slots=None, bias=None, silu: bool = Tru
     if y_out is None:
         raise ValueError("y_out is required")
     load_library()
-    torch, device, dtype, shape = _torch(), _current_device(), x.dtype, x.shape
-    (n, D), K = shape, weight.shape[-1]
+    torch, device, dtype, shape, taps = _torch(), _current_device(), x.dtype, x.shape, weight.shape
+    if len(shape) != 2 or len(taps) != 2:
+        _no_matrix(*((x, "x") if len(shape) != 2 else (weight, "weight")))
+    (n, D), K = shape, taps[1]
     xp, xs = _first_matrix(x, shape, device, "x")
     yp, ys = _matrix(y_out, shape, dtype, device, "y_out")
     wp, n_slots, layers = _table(windows, K - 1, D, dtype, device, "windows")
@@ -862,6 +870,8 @@ def precog_block_norm(x, out=None, skip=None, skip_input=None, gate=None, gate_f
         kind = _NORMS[norm]
     else:
         raise ValueError('norm must be "none" or "rms"')
+    if len(shape) != 2:
+        _no_matrix(x, "x")
     T, D = shape
     f32, vec, scale_weight = torch.float32, (D,), 0
     if isinstance(scale, torch.Tensor):
@@ -905,12 +915,16 @@ def precog_adjust_logits(logits, out, history=None, history_offsets=None, count_
         raise ValueError("mask_rows is given without mask")
     load_library()
     torch, device, dtype, shape = _torch(), _current_device(), logits.dtype, logits.shape
+    if len(shape) != 2:
+        _no_matrix(logits, "logits")
     R, V = shape
     lp, ls = _first_matrix(logits, shape, device, "logits")
     op, os_ = _matrix(out, shape, dtype, device, "out")
     i64, f32, row, ends = torch.int64, torch.float32, (R,), (R + 1,)
     nh = history.numel() if history is not None else 0
     nb = bias.numel() if bias is not None else 0
+    if mask is not None and mask.dim() != 2:
+        _no_matrix(mask, "mask")
     nm = mask.shape[0] if mask is not None else 0
     mp = _dense(mask, (nm, (V + 31) // 32), torch.int32, device, "mask")
     if mask is not None and mask_rows is None and nm < R:   # (an empty mask has no address: the C call would see none)
