@@ -588,6 +588,9 @@ def precog_delta_scan(inputs: DeltaInputs, offsets, T_tot: int, bank=None, idx=N
         raise ValueError("bank and states_out must have the same number of layers")
     if y_out is not None and tuple(y_out.shape) != (T_tot, inputs.n_v_heads, inputs.dv):
         raise ValueError("y_out must be [T_tot, Hv, dv]")
+    # (an empty bank has no address: the C call would see none)
+    if bank is not None and ((idx is None and bank.shape[0] < n) or not 0 <= layer < bank.shape[1]):
+        raise ValueError("bank has no entry for every sequence, or no such layer")
     holder = states_out if states_out is not None else bank
     if workspace is None and T_tot >= 1024:   # below, none is needed
         need = int(lib.precog_delta_scan_workspace_size(ctypes.byref(inputs), n, T_tot))
