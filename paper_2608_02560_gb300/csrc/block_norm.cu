@@ -6,14 +6,17 @@
 //
 // A row (or, where groups are normed, a group of one) belongs to LANES lanes that hold ENTRIES entries each, in pieces of
 // 16 bytes; what is read is read once, all of it before the first is used, and stays in registers as fp32 until it is
-// written. Sums are fp32, in an order that depends on the row's length and the types alone.
+// written. Sums are fp32, in an order that depends on the row's length, the types and, for long bf16 rows beside an fp32
+// residual, on whether the call has a skip or gate.
 //
 // Memory bounds it: 65,521 bf16 rows of 2048, norm, scaled fp32 residual, next norm (1.61 GB, 237 us at the measured copy
 // rate): 232 us; rows of 4096 with skip and gate (2.15 GB, 316 us): 300, in groups of 64 to 512 304 to 315. What carries it
 // is warps: the first kernel, one load after the other, took 461 and 577, all loads ahead 280 and 342, CTAs of four warps
 // for 2048 (two pieces a lane instead of one) 237, registers for what a call has 300. Two pieces a lane are best at every
 // length: one, or four, took 280 for 2048, and one 390 for groups. fp32 rows: 23,437 of 2048 112 us (32 bytes a lane in one
-// piece 123), 5859 of 8192 113 to 125. Beyond that, and with all of skip, gate and residual, 1.4 to 1.8 of the copy's time.
+// piece 123), 5859 of 8192 113 to 125. Rows of 16,384 take 1.6 of the copy's time; with all of skip,
+// gate and fp32 residual rows of 2048 1.05, of 4096 1.24, of 8192 and 16,384 1.7 and 1.6 (fp32 rows of 8192 1.4). Lanes go to the next power of two, which
+// other widths pay for: bf16 rows of 1536, 2560, 5120 and 6144 take 1.1, 1.2, 1.3 and 1.2 of it.
 // Two rows a CTA for one load of the weights took more registers than that saves; rows in turn with the next one's copies
 // in shared memory took the L1 that the weights live in (1.4 to 2 times as long); a cluster of two CTAs a row took 491
 // for the rows of 4096.
