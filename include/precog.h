@@ -743,6 +743,7 @@ precog_status precog_block_norm(const precog_block_norm_args *args, int64_t T, v
  *   d_bias_idx, d_bias, d_bias_offsets   int64 tokens and fp32 biases, lists as the history's; of a
  *                 token that a row names twice the last bias counts
  *   d_mask        device int32 [n_masks][ceil(vocab / 32)]: bit i % 32 of word i / 32 allows token i
+ *                 (NULL: n_masks must be 0)
  *   d_mask_rows   device int64 [n_rows]: the row's mask (-1: everything is allowed; other values
  *                 outside [0, n_masks) likewise, and flag PRECOG_DEV_BAD_INDEX); NULL: mask r, and
  *                 n_masks must be at least n_rows where there is a d_mask

@@ -554,8 +554,11 @@ def precog_smc_consolidate(semantic, states, slots, alpha: float, stream=None):
     lib = load_library()
     n_slots = semantic.shape[0]
     elems = semantic[0].numel() if n_slots else 0
+    if semantic.is_complex():   # pairs
+        _resolved(semantic)
+        elems *= 2
     _check(lib.precog_smc_consolidate(
-        _ptr(semantic), n_slots, elems, _ptr(states), _row_code(states), _ptr(slots),
+        _ptr(semantic), n_slots, elems, _ptr(states), _dtype_code(states), _ptr(slots),
         states.shape[0], alpha, _stream(stream)))
 
 
