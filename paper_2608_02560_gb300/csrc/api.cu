@@ -197,6 +197,7 @@ bool touches(const RowSpan &a, int64_t n, const void *at, __int128 bytes) {
     if (a.at == nullptr || at == nullptr || n == 0 || a.row == 0 || bytes <= 0) return false;
     using wide = __int128;
     const wide pa = static_cast<wide>(reinterpret_cast<uintptr_t>(a.at)), pb = static_cast<wide>(reinterpret_cast<uintptr_t>(at));
+    if (pb + bytes <= pa || pb >= pa + static_cast<wide>(n - 1) * a.stride + a.row) return false;   // (as a rule)
     wide i = 0;   // the first row that ends behind `at`
     if (n > 1 && a.stride > 0 && pb - pa >= a.row) i = (pb - pa - a.row) / a.stride + 1;
     return i < n && pa + i * a.stride + a.row > pb && pa + i * a.stride < pb + bytes;
